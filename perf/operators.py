@@ -268,11 +268,9 @@ def _gemm_plan(case):
 
 def _bias_grad_plan(case):
     from paper_2606_11718_b200 import binding as ccl
-    m = ccl.Mat(case["M"], case["N"], 2)
-    need = ccl.ccl_bias_act_grad_workspace(m)
-    return {"ccl": ccl, "m": m, "act": getattr(ccl, "ACT_" + case["act"].upper()),
+    return {"ccl": ccl, "m": ccl.Mat(case["M"], case["N"], 2), "act": getattr(ccl, "ACT_" + case["act"].upper()),
             "dz": torch.empty(case["M"], case["N"], dtype=BF16, device="cuda") if case["act"] != "none" else None,
-            "dbias": _empty(case["N"]), "ws": torch.empty(need, dtype=torch.uint8, device="cuda") if need else None}
+            "dbias": _empty(case["N"])}
 
 
 def _moe_plan(case):
@@ -299,7 +297,7 @@ def _own(s):
         ccl.ccl_gemm_act_grad(plan["d"], s["a"], s["w"], s["z"], plan["out"], plan["ws"], act=plan["act"], dbias=plan["dbias"])
         return {"dz": plan["out"], "dbias": plan["dbias"]} if case["dbias"] else {"dz": plan["out"]}
     if case["op"] == "bias_grad":
-        ccl.ccl_bias_act_grad(plan["m"], s["dy"], s["z"], plan["dz"], plan["dbias"], plan["ws"], act=plan["act"])
+        ccl.ccl_bias_act_grad(plan["m"], s["dy"], s["z"], plan["dz"], plan["dbias"], act=plan["act"])
         return {"dbias": plan["dbias"]} if plan["dz"] is None else {"dz": plan["dz"], "dbias": plan["dbias"]}
     ccl.ccl_moe_tokens(plan["d"], s["x"], s["router"], s["w_gu"], s["w_down"], plan["y"], plan["ws"], residual=s["residual"])
     return {"y": plan["y"]}

@@ -322,6 +322,103 @@ ccl_status ccl_gemm_status(void* cuda_stream, int32_t* detail);
 ccl_status ccl_gemm_static_ws(const ccl_gemm_desc* d, const void* A_dev, const void* B_dev, void* C_dev,
                               void* cuda_stream);
 
+/* ---- feed-forward operators around the GEMM --------------------------------------------
+ *
+ * What a feed-forward block does between its GEMMs, in their epilogues, and its gradients.  The paper has no counterpart:
+ * like ccl_gemm_swiglu these keep activations in the layout the next GEMM reads (Sec. 3.3).  bf16 storage, fp32 arithmetic,
+ * every output rounded once, to nearest even.
+ */
+
+typedef enum {
+    CCL_ACT_NONE = 0,
+    CCL_ACT_RELU = 1,
+    CCL_ACT_GELU_TANH = 2, /* z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
+    CCL_ACT_GELU_ERF = 3,  /* z/2 (1 + erf(z / sqrt 2))                     */
+    CCL_ACT_SILU = 4       /* z / (1 + exp(-z))                             */
+} ccl_act;
+
+/*
+ * C = bf16( act(Z) + residual ),  Z = A*B + bias  (fp32 throughout).
+ *   act           a ccl_act
+ *   bias_dev      bf16 [N], or NULL: none
+ *   residual_dev  bf16 [M x N] in the layout d->C describes, or NULL: none.  It may be C_dev itself (the residual stream
+ *                 updated in place): every element is read before it is written
+ *   preact_dev    receives bf16(Z) in the layout d->C describes (what the gradient needs), or NULL: not wanted
+ */
+typedef struct ccl_epilogue {
+    int32_t act;
+    const void* bias_dev;
+    const void* residual_dev;
+    void* preact_dev;
+} ccl_epilogue;
+
+/*
+ * d, A_dev, B_dev, C_dev, requirements, errors, bounded waits and asynchrony as for ccl_gemm; bias, residual and pre-activation
+ * 16-byte aligned as well.  Workspace: ccl_gemm_epilogue_workspace bytes (its plan is not always ccl_gemm's); without it
+ * CCL_ERR_WORKSPACE.  Calls that can overlap on the GPU must not share a workspace.
+ */
+ccl_status ccl_gemm_epilogue_workspace(const ccl_gemm_desc* d, size_t* bytes);
+ccl_status ccl_gemm_epilogue(const ccl_gemm_desc* d, const ccl_epilogue* e, const void* A_dev, const void* B_dev, void* C_dev,
+                             void* ws_dev, size_t ws_bytes, void* cuda_stream);
+
+/*
+ * The gradient on its way back through act(): the product that brings it (dH = dY * W^T of the layer behind) with the
+ * activation's slope in its epilogue,
+ *   dZ = bf16( (A*B) .* act'(Z) ),   dbias[n] = bf16( sum over m of (A*B)[m][n] * act'(Z[m][n]) )
+ * (the sum is of the unrounded fp32 values, in a fixed order: the same bits on every run).  With ccl_gemm_epilogue's Z:
+ * act'(Z) is the slope at the rounded pre-activation.  relu'(0) = 0.
+ *   Z_dev      bf16 [M x N] in the layout d->C describes; may be dZ_dev itself; NULL only with CCL_ACT_NONE
+ *   dbias_dev  bf16 [N], or NULL: not wanted
+ * The rest of the gradient of ccl_gemm_epilogue is plain calls: d residual = dC, dA = dZ * B^T and dB = A^T * dZ by ccl_gemm.
+ * Requirements, errors and waits as for ccl_gemm; workspace: ccl_gemm_act_grad_workspace bytes (with dbias_dev = NULL only
+ * what a K split needs of them).
+ */
+ccl_status ccl_gemm_act_grad_workspace(const ccl_gemm_desc* d, size_t* bytes);
+ccl_status ccl_gemm_act_grad(const ccl_gemm_desc* d, int32_t act, const void* A_dev, const void* B_dev, const void* Z_dev,
+                             void* dZ_dev, void* dbias_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream);
+
+/*
+ * The same where no product comes in front (an output layer, a bias without an activation):
+ *   dZ = bf16( dY .* act'(Z) ),   dbias[n] = bf16( sum over m of dY[m][n] * act'(Z[m][n]) )
+ * dY, Z and dZ are all stored as `m` describes (2-byte elements, any layout the map accepts; padding is not touched); dZ_dev may
+ * be dY_dev or Z_dev.  Z_dev is not read with CCL_ACT_NONE; dZ_dev or dbias_dev may be NULL: not wanted.  Any shape; bases
+ * 2-byte aligned.  Column groups of 8 that are aligned 16-byte pieces of the buffer take the fast path.  No workspace.
+ */
+ccl_status ccl_bias_act_grad(const ccl_mat* m, int32_t act, const void* dY_dev, const void* Z_dev, void* dZ_dev,
+                             void* dbias_dev, void* cuda_stream);
+
+/*
+ * A mixture-of-experts feed-forward layer for a few tokens (a decode step), router to output, in one launch:
+ *   logits = X * Wr^T (fp32),  p = softmax(logits) over the E experts,  the topk largest p of each token (equal ones: the
+ *   lowest expert first),  weight w = p, divided by the sum of the token's topk p when norm_topk is set,
+ *   Y[t] = bf16( residual[t] + sum over the chosen experts e of w_te * Wd_e * bf16( silu(Wg_e x_t) .* (Wu_e x_t) ) )
+ *   X [T x H], residual [T x H] (or NULL; may be Y itself), Y [T x H]: bf16 row-major
+ *   Wr        bf16 [E x H]
+ *   Wgu       per expert bf16 [2I x H] (K along the rows): I gate rows, then I up rows; with gu_strips = S > 1 the rows form S
+ *             strips of 2I/S, each with its gate rows first and its up rows behind them (the operand ccl_gemm_grouped_swiglu takes
+ *             as an N-split CCL B with b_trans = 1); expert e at Wgu_dev + e * gu_stride_bytes (0: densely packed)
+ *   Wd        per expert bf16 [H x I] (K along the rows), expert e at Wd_dev + e * d_stride_bytes (0: densely packed)
+ *   ids_dev   int32 [T x topk], weights_dev fp32 [T x topk]: the choice, best first; NULL: not wanted
+ * Requirements: 1 <= T <= 64, 1 <= E <= 512, 1 <= topk <= min(E, 16), H in [8, 8192] and I in [8, 32768] multiples of 8, gu_strips a divisor of
+ * I / 8 (else CCL_ERR_SHAPE / CCL_ERR_UNSUPPORTED); X, residual, Y, Wr, Wgu, Wd and the workspace 16-byte aligned, strides multiples of
+ * 16 bytes (else CCL_ERR_ALIGN).
+ * One cooperative launch of one CTA per SM, which meet at two grid-wide barriers; the waits are bounded and reported by
+ * ccl_gemm_status (code 8).  A logit that is NaN is never chosen before a number; NaN inputs give NaN outputs for their token.
+ * Workspace: ccl_moe_tokens_workspace bytes, whatever they hold; calls that can overlap on the GPU must not share it.  The result does
+ * not depend on the order in which CTAs run.
+ */
+typedef struct ccl_moe_desc {
+    int64_t T, H, I;
+    int32_t E, topk;
+    int32_t norm_topk;
+    int32_t gu_strips;
+    int64_t gu_stride_bytes, d_stride_bytes;
+} ccl_moe_desc;
+ccl_status ccl_moe_tokens_workspace(const ccl_moe_desc* d, size_t* bytes);
+ccl_status ccl_moe_tokens(const ccl_moe_desc* d, const void* X_dev, const void* Wr_dev, const void* Wgu_dev, const void* Wd_dev,
+                          const void* residual_dev, void* Y_dev, int32_t* ids_dev, float* weights_dev, void* ws_dev,
+                          size_t ws_bytes, void* cuda_stream);
+
 /* ---- remote-traffic counter (Sec. 4.1 metric, every touched byte counted: no L2 filter) */
 
 typedef enum { CCL_PLACE_RR = 0, CCL_PLACE_BLOCK = 1, CCL_PLACE_BEST = 2 } ccl_place;

@@ -17,10 +17,12 @@ OK, ERR_INVALID_ARG, ERR_SHAPE, ERR_ALIGN, ERR_UNSUPPORTED, ERR_CUDA, ERR_WORKSP
 ROWMAJOR, CCL, CCL_INTERLEAVED = 0, 1, 2
 PART_NONE, PART_ROWS, PART_COLS, PART_2D = 0, 1, 2, 3
 PLACE_RR, PLACE_BLOCK, PLACE_BEST = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU_TANH, ACT_GELU_ERF, ACT_SILU = 0, 1, 2, 3, 4
 ASSIGN_N_STRIPS, ASSIGN_M_STRIPS, ASSIGN_EXPLICIT, ASSIGN_2D = 0, 1, 2, 3
 
 EXPORTS = ["ccl_map_offset", "ccl_map_inverse", "ccl_buffer_bytes", "ccl_strip_stride", "ccl_repack", "ccl_repack_batched", "ccl_repack_transpose", "ccl_gemm_workspace",
-           "ccl_gemm", "ccl_gemm_batched_workspace", "ccl_gemm_batched", "ccl_gemm_grouped", "ccl_gemm_grouped_swiglu", "ccl_gemm_grouped_k", "ccl_gemm_axpby", "ccl_gemm_swiglu", "ccl_gemm_static_ws", "ccl_gemm_status", "ccl_selftest_wait_timeout", "ccl_traffic_sizes", "ccl_traffic", "ccl_traffic_l2", "ccl_traffic_lru", "ccl_probe_l2_latency", "ccl_last_error", "ccl_launch_count", "ccl_version"]
+           "ccl_gemm", "ccl_gemm_batched_workspace", "ccl_gemm_batched", "ccl_gemm_grouped", "ccl_gemm_grouped_swiglu", "ccl_gemm_grouped_k", "ccl_gemm_axpby", "ccl_gemm_swiglu", "ccl_gemm_static_ws", "ccl_gemm_status", "ccl_selftest_wait_timeout", "ccl_gemm_epilogue_workspace", "ccl_gemm_epilogue",
+           "ccl_gemm_act_grad_workspace", "ccl_gemm_act_grad", "ccl_bias_act_grad", "ccl_moe_tokens_workspace", "ccl_moe_tokens", "ccl_traffic_sizes", "ccl_traffic", "ccl_traffic_l2", "ccl_traffic_lru", "ccl_probe_l2_latency", "ccl_last_error", "ccl_launch_count", "ccl_version"]
 
 
 class CclError(RuntimeError):
@@ -43,6 +45,20 @@ class GemmDesc(C.Structure):
     _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("A", Mat), ("B", Mat), ("C", Mat),
                 ("a_trans", C.c_int32), ("b_trans", C.c_int32), ("out_part", C.c_int32), ("P", C.c_int32),
                 ("grouped_raster", C.c_int32), ("part_m", C.c_int32)]
+
+
+class Epilogue(C.Structure):
+    """ccl_epilogue"""
+    _fields_ = [("act", C.c_int32), ("bias_dev", C.c_void_p), ("residual_dev", C.c_void_p), ("preact_dev", C.c_void_p)]
+
+
+class MoeDesc(C.Structure):
+    """ccl_moe_desc"""
+    _fields_ = [("T", C.c_int64), ("H", C.c_int64), ("I", C.c_int64), ("E", C.c_int32), ("topk", C.c_int32), ("norm_topk", C.c_int32),
+                ("gu_strips", C.c_int32), ("gu_stride_bytes", C.c_int64), ("d_stride_bytes", C.c_int64)]
+
+    def __init__(self, T=0, E=0, topk=0, H=0, I=0, norm_topk=1, gu_strips=1, gu_stride_bytes=0, d_stride_bytes=0):
+        super().__init__(T, H, I, E, topk, norm_topk, gu_strips, gu_stride_bytes, d_stride_bytes)
 
 
 class TrafficDesc(C.Structure):
@@ -97,6 +113,13 @@ def lib():
         l.ccl_gemm_static_ws.argtypes = [C.POINTER(GemmDesc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         l.ccl_gemm_status.argtypes = [C.c_void_p, C.POINTER(C.c_int32)]
         l.ccl_selftest_wait_timeout.argtypes = [C.c_int32, C.c_uint32, C.c_void_p, C.c_void_p]
+        l.ccl_gemm_epilogue_workspace.argtypes = [C.POINTER(GemmDesc), C.POINTER(C.c_size_t)]
+        l.ccl_gemm_epilogue.argtypes = [C.POINTER(GemmDesc), C.POINTER(Epilogue), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        l.ccl_gemm_act_grad_workspace.argtypes = [C.POINTER(GemmDesc), C.POINTER(C.c_size_t)]
+        l.ccl_gemm_act_grad.argtypes = [C.POINTER(GemmDesc), C.c_int32] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
+        l.ccl_bias_act_grad.argtypes = [C.POINTER(Mat), C.c_int32] + [C.c_void_p] * 5
+        l.ccl_moe_tokens_workspace.argtypes = [C.POINTER(MoeDesc), C.POINTER(C.c_size_t)]
+        l.ccl_moe_tokens.argtypes = [C.POINTER(MoeDesc)] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]
         l.ccl_traffic_sizes.argtypes = [C.POINTER(TrafficDesc), C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
         l.ccl_traffic.argtypes = [C.POINTER(TrafficDesc), C.c_void_p, C.c_void_p, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                   C.c_void_p, C.c_void_p]
@@ -260,6 +283,79 @@ def ccl_gemm_swiglu(d, A, B, Cout):
         if t.numel() * t.element_size() < ccl_buffer_bytes(m):
             raise ValueError("ccl_gemm_swiglu: operand buffer too small")
     _check(lib().ccl_gemm_swiglu(C.byref(d), _ptr(A), _ptr(B), _ptr(Cout), _stream()))
+
+
+def _holds(t, nbytes):
+    return t.is_cuda and t.is_contiguous() and t.numel() * t.element_size() >= nbytes
+
+
+def _vector(t, n, what):
+    if t is not None and not (t.dtype == torch.bfloat16 and _holds(t, 2 * n)):
+        raise ValueError(f"{what} must be a contiguous bfloat16 CUDA tensor with at least {n} entries")
+
+
+def _operands(what, *pairs):
+    for t, nbytes in pairs:
+        if t is not None and not _holds(t, nbytes):
+            raise ValueError(f"{what}: an operand must be a contiguous CUDA tensor that holds what the descriptor says")
+
+
+def _size(fn, d):
+    n = C.c_size_t()
+    _check(fn(C.byref(d), C.byref(n)))
+    return n.value
+
+
+def ccl_gemm_epilogue_workspace(d):
+    return _size(lib().ccl_gemm_epilogue_workspace, d)
+
+
+def ccl_gemm_epilogue(d, A, B, Cout, ws=None, act=ACT_NONE, bias=None, residual=None, preact=None):
+    """C = act(A*B + bias) + residual; preact receives A*B + bias.  bias: [N] bfloat16; residual (may be Cout) and preact in C's layout."""
+    c_bytes = ccl_buffer_bytes(d.C)
+    _operands("ccl_gemm_epilogue", (A, ccl_buffer_bytes(d.A)), (B, ccl_buffer_bytes(d.B)), (Cout, c_bytes), (residual, c_bytes), (preact, c_bytes))
+    _vector(bias, d.N, "ccl_gemm_epilogue: bias")
+    e = Epilogue(act, _ptr(bias), _ptr(residual), _ptr(preact))
+    ws_bytes = ws.numel() * ws.element_size() if ws is not None else 0
+    _check(lib().ccl_gemm_epilogue(C.byref(d), C.byref(e), _ptr(A), _ptr(B), _ptr(Cout), _ptr(ws), ws_bytes, _stream()))
+
+
+def ccl_gemm_act_grad_workspace(d):
+    return _size(lib().ccl_gemm_act_grad_workspace, d)
+
+
+def ccl_gemm_act_grad(d, A, B, preact, dz, ws=None, act=ACT_NONE, dbias=None):
+    """dz = (A*B) * act'(preact), dbias = its column sums.  preact and dz in C's layout; dbias: [N] bfloat16."""
+    c_bytes = ccl_buffer_bytes(d.C)
+    _operands("ccl_gemm_act_grad", (A, ccl_buffer_bytes(d.A)), (B, ccl_buffer_bytes(d.B)), (preact, c_bytes), (dz, c_bytes))
+    _vector(dbias, d.N, "ccl_gemm_act_grad: dbias")
+    ws_bytes = ws.numel() * ws.element_size() if ws is not None else 0
+    _check(lib().ccl_gemm_act_grad(C.byref(d), act, _ptr(A), _ptr(B), _ptr(preact), _ptr(dz), _ptr(dbias), _ptr(ws), ws_bytes, _stream()))
+
+
+def ccl_bias_act_grad(m, dy, preact, dz, dbias=None, act=ACT_NONE):
+    """dz = dy * act'(preact) (None: not wanted), dbias = its column sums; dy, preact and dz as `m` describes, dbias: [cols] bfloat16."""
+    nbytes = ccl_buffer_bytes(m)
+    _operands("ccl_bias_act_grad", (dy, nbytes), (preact, nbytes), (dz, nbytes))
+    _vector(dbias, m.cols, "ccl_bias_act_grad: dbias")
+    _check(lib().ccl_bias_act_grad(C.byref(m), act, _ptr(dy), _ptr(preact), _ptr(dz), _ptr(dbias), _stream()))
+
+
+def ccl_moe_tokens_workspace(d):
+    return _size(lib().ccl_moe_tokens_workspace, d)
+
+
+def ccl_moe_tokens(d, X, Wr, Wgu, Wd, Y, ws, residual=None, ids=None, weights=None):
+    """A mixture-of-experts layer for d.T tokens: Y = residual + sum over each token's topk experts.  Wr [E x H], Wgu per expert
+    [2I x H], Wd per expert [H x I]; ids int32 / weights float32 [T x topk] receive the choice if wanted."""
+    th, gu, dn = 2 * d.T * d.H, 4 * d.I * d.H, 2 * d.I * d.H
+    _operands("ccl_moe_tokens", (X, th), (Y, th), (residual, th), (Wr, 2 * d.E * d.H), (Wgu, (d.E - 1) * (d.gu_stride_bytes or gu) + gu),
+              (Wd, (d.E - 1) * (d.d_stride_bytes or dn) + dn), (ids, 4 * d.T * d.topk), (weights, 4 * d.T * d.topk))
+    if (ids is not None and ids.dtype != torch.int32) or (weights is not None and weights.dtype != torch.float32):
+        raise ValueError("ccl_moe_tokens: ids must be int32 and weights float32")
+    ws_bytes = ws.numel() * ws.element_size() if ws is not None else 0
+    _check(lib().ccl_moe_tokens(C.byref(d), _ptr(X), _ptr(Wr), _ptr(Wgu), _ptr(Wd), _ptr(residual), _ptr(Y), _ptr(ids), _ptr(weights), _ptr(ws), ws_bytes,
+                                _stream()))
 
 
 GEMM_STATIC_WS_BYTES = 8 * 1024 * 1024

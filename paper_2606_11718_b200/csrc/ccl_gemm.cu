@@ -30,6 +30,9 @@
 
 namespace ccl {
 
+constexpr int kWaveSlots = 64;
+static __device__ unsigned int g_wave_ctr[kWaveSlots];
+
 template <int BN, int CTAS, bool SWIGLU = false, int RAG = 0, bool FULL = true, int KS = 0>
 static ccl_status configure(uint32_t smem_bytes) {
     static uint32_t configured_for = 0;
@@ -69,7 +72,7 @@ static ccl_status launch(const GemmPlan& plan, const CUtensorMap& ma, const CUte
 }
 
 // CTA pairs of the 2-CTA kernel that can be resident at once (0 if clusters cannot be launched)
-static int resident_pairs() {
+int resident_pairs() {
     static int pairs = -1;
     if (pairs >= 0) return pairs;
     uint32_t smem = kSmemBudget + kEpiBytes + 2048;
@@ -101,13 +104,61 @@ static int query_clusters() {
     if (cudaOccupancyMaxActiveClusters(&n, ccl_gemm_kernel<256, 1, false, 0, false, KS>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); n = 0; }
     return n;
 }
-static int resident_clusters(int ks, bool have_device) {
+int resident_clusters(int ks, bool have_device) {
     static int cached[9] = {-1, -1, -1, -1, -1, -1, -1, -1, -1};
     if (!have_device) return ks == 2 ? 64 : (ks == 4 ? 32 : 16);
     if (cached[ks] < 0) cached[ks] = ks == 2 ? query_clusters<2>() : (ks == 4 ? query_clusters<4>() : query_clusters<8>());
     return cached[ks];
 }
 
+// SM count and resident CTA pairs of the current device; the figures of a B200 when no device is usable
+// (the planner then still validates and sizes the workspace the same way a B200 would).
+bool device_units(int* sms, int* pairs) {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0) {
+        *sms = n; *pairs = resident_pairs();
+        return true;
+    }
+    (void)cudaGetLastError();
+    *sms = 148; *pairs = 74;
+    return false;
+}
+
+// Soft wave barrier for problems of three or more full rounds of tiles (CCL_GEMM_WAVESYNC=0 turns it off, =n syncs
+// every n-th round): without it the CTAs that share an A panel or B
+// columns drift apart by more than the L2 holds and fetch the same lines from DRAM 2-3 times.
+ccl_status wave_barrier(GemmPlan& plan, bool plain, cudaStream_t st) {
+    plan.p.wave_ctr = nullptr;
+    static const int wave_sync = []() { const char* f = std::getenv("CCL_GEMM_WAVESYNC"); return f ? atoi(f) : 1; }();
+    plan.p.wave_period = wave_sync > 0 ? wave_sync : 1; plan.p.wave_wait_ns = 20000;        // one wait gives up after 20 us
+    // (long tiles only: with K below 4096, or a batch of small problems, the CTAs share little and the waits only cost --
+    // measured -9 % on 128 batched expert GEMMs and on a 16384 x 1536 x 2048 fused gate/up GEMM)
+    const bool any_rag = plan.p.a.rag || plan.p.b.rag || plan.p.c.rag;      // (CTAs that skip the empty places of a short last strip would miss the meeting)
+    if (!(wave_sync > 0 && plan.p.sch_rounds >= 3 && plan.p.kb_per_split >= 64 && plain && !any_rag)) return CCL_OK;
+    // One of kWaveSlots counters in the library image, handed out round-robin: a launch recorded into a CUDA graph
+    // keeps its slot for good while eager calls rotate through all of them, so two GEMMs that overlap on the GPU
+    // can land on one counter -- the barrier is soft (a wait just ends early or runs into its 20 us bound), results
+    // never depend on it.  A device ordinal beyond the table runs without the barrier.
+    static std::atomic<unsigned int> next{0};
+    static std::mutex base_mutex;
+    static unsigned int* base[64] = {};                  // address of the counters, per device
+    int dev = 0;
+    CCL_CUDA_TRY(cudaGetDevice(&dev));
+    unsigned int* ctr0 = nullptr;
+    if (dev >= 0 && dev < 64) {
+        std::lock_guard<std::mutex> lock(base_mutex);
+        if (!base[dev]) CCL_CUDA_TRY(cudaGetSymbolAddress(reinterpret_cast<void**>(&base[dev]), g_wave_ctr));
+        ctr0 = base[dev];
+    }
+    if (ctr0) {
+        plan.p.wave_ctr = ctr0 + next.fetch_add(1) % kWaveSlots;
+        CCL_CUDA_TRY(cudaMemsetAsync(plan.p.wave_ctr, 0, sizeof(unsigned int), st));
+    }
+    return CCL_OK;
+}
+
+ccl_status epi_status_take(int* code);      // ccl_gemm_epi.cu
+ccl_status moe_status_take(int* code);      // ccl_moe.cu
 ccl_status repack_status_take(int* code);   // ccl_repack.cu
 ccl_status repack_selftest_launch(const void* src_dev, uint64_t limit_ns, cudaStream_t st);   // ccl_repack.cu
 
@@ -174,19 +225,6 @@ static void make_key(const ccl_gemm_desc* d, const int64_t* batch4, const void* 
         for (const char* c = v ? v : ""; *c && pos + 2 < sizeof(k->env); ++c) k->env[pos++] = *c;
         if (pos + 1 < sizeof(k->env)) k->env[pos++] = ';';
     }
-}
-
-// SM count and resident CTA pairs of the current device; the figures of a B200 when no device is usable
-// (the planner then still validates and sizes the workspace the same way a B200 would).
-static bool device_units(int* sms, int* pairs) {
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0) {
-        *sms = n; *pairs = resident_pairs();
-        return true;
-    }
-    (void)cudaGetLastError();
-    *sms = 148; *pairs = 74;
-    return false;
 }
 
 constexpr int64_t kMaxBatch = 65536;
@@ -341,38 +379,7 @@ static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
         plan.p.bal_mark = 1ull;
         CCL_CUDA_TRY(cudaMemsetAsync(plan.p.bal_flags, 0, (size_t)plan.grid * 2 * 32, st));
     }
-    // Soft wave barrier for problems of three or more full rounds of tiles (CCL_GEMM_WAVESYNC=0 turns it off, =n syncs
-    // every n-th round): without it the CTAs that share an A panel or B
-    // columns drift apart by more than the L2 holds and fetch the same lines from DRAM 2-3 times.
-    plan.p.wave_ctr = nullptr;
-    {
-        static const int wave_sync = []() { const char* f = std::getenv("CCL_GEMM_WAVESYNC"); return f ? atoi(f) : 1; }();
-        plan.p.wave_period = wave_sync > 0 ? wave_sync : 1; plan.p.wave_wait_ns = 20000;        // one wait gives up after 20 us
-        // (long tiles only: with K below 4096, or a batch of small problems, the CTAs share little and the waits only cost --
-        // measured -9 % on 128 batched expert GEMMs and on a 16384 x 1536 x 2048 fused gate/up GEMM)
-        const bool any_rag = plan.p.a.rag || plan.p.b.rag || plan.p.c.rag;      // (CTAs that skip the empty places of a short last strip would miss the meeting)
-        if (wave_sync > 0 && plan.p.sch_rounds >= 3 && plan.p.kb_per_split >= 64 && batch == 1 && !m_offs && !k_offs && !any_rag) {
-            // One of kWaveSlots counters in the library image, handed out round-robin: a launch recorded into a CUDA graph
-            // keeps its slot for good while eager calls rotate through all of them, so two GEMMs that overlap on the GPU
-            // can land on one counter -- the barrier is soft (a wait just ends early or runs into its 20 us bound), results
-            // never depend on it.  A device ordinal beyond the table runs without the barrier.
-            static std::atomic<unsigned int> next{0};
-            static std::mutex base_mutex;
-            static unsigned int* base[64] = {};                  // address of the counters, per device
-            int dev = 0;
-            CCL_CUDA_TRY(cudaGetDevice(&dev));
-            unsigned int* ctr0 = nullptr;
-            if (dev >= 0 && dev < 64) {
-                std::lock_guard<std::mutex> lock(base_mutex);
-                if (!base[dev]) CCL_CUDA_TRY(cudaGetSymbolAddress(reinterpret_cast<void**>(&base[dev]), g_wave_ctr));
-                ctr0 = base[dev];
-            }
-            if (ctr0) {
-                plan.p.wave_ctr = ctr0 + next.fetch_add(1) % kWaveSlots;
-                CCL_CUDA_TRY(cudaMemsetAsync(plan.p.wave_ctr, 0, sizeof(unsigned int), st));
-            }
-        }
-    }
+    if ((s = wave_barrier(plan, batch == 1 && !m_offs && !k_offs, st))) return s;
     if (k_offs) {                                        // ragged K: one CTA per tile (make_plan)
         if (plan.bn == 256) s = launch<256, 1, false, 2>(plan, ma, mb, mc, st);
         else if (plan.bn == 192) s = launch<192, 1, false, 2>(plan, ma, mb, mc, st);
@@ -491,6 +498,9 @@ extern "C" ccl_status ccl_gemm_status(void* cuda_stream, int32_t* detail) {
     if (v) CCL_CUDA_TRY(cudaMemcpyToSymbol(g_gemm_status, &z, sizeof(int)));
     ccl_status s = repack_status_take(&rv);
     if (s) return s;
+    int ev = 0, mv = 0;
+    if ((s = epi_status_take(&ev)) || (s = moe_status_take(&mv))) return s;
+    if (!v) v = ev ? ev : mv;
     if (detail) *detail = v ? v : (rv ? 100 + rv : 0);
     if (v == 5) return fail(CCL_ERR_SHAPE, "ccl_gemm_grouped: row offsets outside [0, M] or a problem with more rows than max_rows (such problems were not computed)");
     if (v || rv) return fail(CCL_ERR_TIMEOUT, "a bounded device-side wait expired (code %d)", v ? v : 100 + rv);

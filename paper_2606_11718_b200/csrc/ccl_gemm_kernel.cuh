@@ -1,6 +1,6 @@
 // The GEMM kernel and what it shares with the host code that plans and launches it: tile constants, the parameter block,
 // PTX wrappers (tcgen05, TMA, mbarrier, cluster), the tile walk, the kernel template and the split-K reduction.
-// Included by ccl_gemm.cu only.
+// Included by ccl_gemm.cu and ccl_gemm_epi.cu, which instantiate different kernels and have a status word each.
 #ifndef CCL_GEMM_KERNEL_CUH_
 #define CCL_GEMM_KERNEL_CUH_
 
@@ -13,6 +13,7 @@
 
 #include <cuda_bf16.h>
 
+#include "ccl_act.cuh"
 #include "ccl_common.h"
 #include "ccl_tma.h"
 
@@ -31,9 +32,7 @@ constexpr uint32_t kSmemBudget = 192 * 1024;    // ring of operand stages
 constexpr int64_t kRaggedDense = 4096;         // problems of a ragged batch whose tile prefix is kept in shared memory
 constexpr uint32_t kEpiBytes = 4 * 2 * 32 * 128; // epilogue staging: per warp two buffers of 32 rows x 128 B
 
-__device__ int g_gemm_status = 0;
-constexpr int kWaveSlots = 64;
-__device__ unsigned int g_wave_ctr[kWaveSlots];
+static __device__ int g_gemm_status = 0;
 
 // Division of a non-negative int by a launch constant as a multiply-high and a shift (an integer division costs a few
 // hundred cycles, and the tile walk of a short GEMM is nothing but divisions).  For d >= 2: l = ceil(log2 d),
@@ -140,6 +139,13 @@ struct GemmParams {
     // memset node in front of the launch (so a replayed CUDA graph clears them as well) and set to bal_mark by the kernel
     unsigned long long bal_mark;
     unsigned long long* bal_flags;
+    // epilogue of ccl_gemm_epilogue (EPI = 1) and ccl_gemm_act_grad (EPI = 2); all matrices are laid out like C
+    int32_t act;                    // ccl_act
+    FastDiv fd_wm;
+    const uint16_t* bias;           // EPI 1: [N] bf16 or NULL
+    const uint16_t* addend;         // EPI 1: the residual or NULL; EPI 2: the pre-activation Z
+    uint16_t* preact;               // EPI 1: receives the pre-activation, or NULL
+    float* colsum;                  // EPI 2: partial column sums [row blocks][N] fp32, or NULL
 };
 
 // ---- PTX wrappers ---------------------------------------------------------------------------
@@ -345,6 +351,38 @@ __device__ __forceinline__ int64_t c_offset(const GemmParams& p, int64_t m, int6
     return (int64_t)g * p.c_stride + (int64_t)rr * p.c_row + xx;
 }
 
+// One row's 8 columns from column n on, whose element offset in C's layout is `off`: fp32 accumulators -> what C gets (fp32,
+// before the rounding).  EPI 1: act(v + bias) + residual, the pre-activation stored on the way.  EPI 2: v * act'(z).
+// `ok` off: nothing is stored and, for EPI 2, v becomes zero (it goes into column sums).
+template <int EPI>
+__device__ __forceinline__ void epilogue8(const GemmParams& p, float (&v)[8], int64_t off, int n, bool ok) {
+    float x[8];
+    if (EPI == 1) {
+        if (p.bias) {
+            bf16x8_unpack(ld_global_v4_if(p.bias + n, ok), x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += x[i];
+        }
+        if (p.preact) st_global_v4_if(p.preact + off, bf16x8_pack(v), ok);
+        act8(p.act, v);
+        if (p.addend) {
+            bf16x8_unpack(ld_global_v4_if(p.addend + off, ok), x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += x[i];
+        }
+    }
+    if (EPI == 2) {
+        if (p.act != CCL_ACT_NONE) {
+            bf16x8_unpack(ld_global_v4_if(p.addend + off, ok), x);
+            slope8(p.act, v, x);
+        }
+        if (!ok) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        }
+    }
+}
+
 // Ragged K: first row, k blocks and rows of the last block of problem e (an empty or out-of-range problem: one block of
 // zero rows, so that its output is written as zeros).
 __device__ __forceinline__ unsigned int ld_acquire_u32(const unsigned int* p) {
@@ -508,7 +546,9 @@ struct Scheduler {
 // RAG: 1 = ragged M (ccl_gemm_grouped), 2 = ragged K (ccl_gemm_grouped_k) -- instantiations of their own, so that the tile
 // walk and the k loops of all other calls stay as they are (the extra branches cost 1-1.5 us on a 15-30 us GEMM)
 // KS > 0: cluster split along K (CTAS = 1): the KS CTAs of a cluster share one tile
-template <int BN, int CTAS, bool SWIGLU = false, int RAG = 0, bool FULL = true, int KS = 0>
+// EPI: 1 = bias, activation and residual in the epilogue (ccl_gemm_epilogue), 2 = activation slope and column sums
+// (ccl_gemm_act_grad)
+template <int BN, int CTAS, bool SWIGLU = false, int RAG = 0, bool FULL = true, int KS = 0, int EPI = 0>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                 const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_a2,
@@ -535,6 +575,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     constexpr int SUBN1 = NSUB == 1 ? 0 : BN - 256;   // width of the second
     constexpr int ACC_COLS = 256;                     // TMEM columns between accumulators
     constexpr int NACC = 2;                           // accumulator barriers in use
+    static_assert(EPI == 0 || (!SWIGLU && RAG == 0), "the epilogue operators are plain calls");
     static_assert(!SWIGLU || BN == 512, "the gated activation pairs the two accumulators of a wide tile");
     constexpr int TILE_N = SWIGLU ? SUBN : BN;        // tile width in the columns the tile walk counts (output columns)
     constexpr int SUBH = SUBN / CTAS;                // B columns of the first sub-tile this CTA stages
@@ -934,8 +975,36 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     }
                 }
             };
+            // EPI: this lane's 64 accumulators through the epilogue, 8 columns at a time, and the piece's column sums into
+            // the row block's line of the partial sums (block = the 32 rows of this warp in this tile)
+            auto epilogue_piece = [&](uint32_t (&r)[64], int c) {
+                const int n64 = nb + c * 64;
+                const bool row_ok = m < t.m1;
+                const int64_t off = c_offset<FULL>(p, min(m, t.m1 - 1), n64);
+                float v[64];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float (&v8)[8] = *reinterpret_cast<float(*)[8]>(&v[8 * j]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v8[i] = __uint_as_float(r[8 * j + i]);
+                    epilogue8<EPI>(p, v8, off + 8 * j, n64 + 8 * j, row_ok && n64 + 8 * j < t.n1);
+                }
+                uint32_t pk[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) pk[i] = bf16_pack(v[2 * i], v[2 * i + 1]);
+                store_packed(pk, c);
+                if (EPI == 2 && p.colsum) {
+                    column_sums64(v, lane);
+                    int sm, jm;
+                    p.fd_wm.divmod(t.m0, sm, jm);
+                    const int64_t blk = ((int64_t)sm * p.tps_m + jm / (BM * CTAS)) * (4 * CTAS) + rank * 4 + quad;
+                    if (n64 + 2 * lane < t.n1)           // (n1 - n64 is a multiple of 8)
+                        *reinterpret_cast<float2*>(p.colsum + blk * p.N + n64 + 2 * lane) = make_float2(v[0], v[1]);
+                }
+            };
             auto store_piece = [&](uint32_t (&r)[64], int c) {
                 if (p.splits > 1) { store_partial(r, c); return; }
+                if (EPI != 0) { epilogue_piece(r, c); return; }
                 if (FULL && p.axpby) axpby_piece(r, c);
                 uint32_t pk[32];
                 pack(r, pk);
@@ -999,7 +1068,8 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 cluster_sync();
                 // (a tile lies inside one strip of C: the columns of a row follow each other from the tile's first column on)
                 const int row = t.m0 + quad * 32 + lane;
-                unsigned short* crow = p.C + c_offset<FULL>(p, min(row, t.m1 - 1), nb) + (int)krank * JS * 4;
+                const int64_t coff = c_offset<FULL>(p, min(row, t.m1 - 1), nb) + (int)krank * JS * 4;
+                unsigned short* crow = p.C + coff;
 #pragma unroll 1
                 for (int c = 0; c < npieces; ++c)
 #pragma unroll
@@ -1013,6 +1083,20 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                             a1.x += v1.x; a1.y += v1.y; a1.z += v1.z; a1.w += v1.w;
                         }
                         const int col = nb + c * 64 + ((int)krank * JS + js) * 4;
+                        if (EPI != 0) {
+                            float v[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
+                            const bool ok8 = row < t.m1 && col < t.n1;
+                            epilogue8<EPI>(p, v, coff + c * 64 + js * 4, col, ok8);
+                            st_global_v4_if(crow + c * 64 + js * 4, bf16x8_pack(v), ok8);
+                            if (EPI == 2 && p.colsum) {
+                                const float sum = column_sums8(v, lane);
+                                int sm, jm;
+                                p.fd_wm.divmod(t.m0, sm, jm);
+                                const int64_t blk = ((int64_t)sm * p.tps_m + jm / BM) * 4 + quad;
+                                if ((lane & 3) == 0 && col < t.n1) p.colsum[blk * p.N + col + (lane >> 2)] = sum;
+                            }
+                            continue;
+                        }
                         if (p.axpby) {                             // C <- alpha * sum + beta * C (C read through its own layout)
                             const uint4 cv = ld_global_v4_if(crow + c * 64 + js * 4, p.beta != 0.0f && row < t.m1 && col < t.n1);
                             const float al = p.alpha, be = p.beta;
@@ -1172,7 +1256,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 
 // Split-K epilogue: C = bf16( ws[0] + ws[1] + ... + ws[splits-1] ), the sum taken in that fixed order so
 // the result is the same on every run.  One thread per 8 consecutive columns of a row.
-__global__ void __launch_bounds__(256) splitk_reduce_kernel(const GemmParams p) {
+static __global__ void __launch_bounds__(256) splitk_reduce_kernel(const GemmParams p) {
     const int64_t n8 = p.N / 8, per_problem = (int64_t)p.M * n8, total = per_problem * p.batch;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t e = i / per_problem, r = i - e * per_problem;

@@ -1,6 +1,6 @@
 // Host-side planning of a GEMM call: operand checks, the choice of kernel variant (tile shape, CTA pairing, K splits, cluster
 // split, balanced split) from a cost model built on measured per-block figures, the parameter block and the tensor maps.
-// Included by ccl_gemm.cu only, after ccl_gemm_kernel.cuh.
+// Included by ccl_gemm.cu and ccl_gemm_epi.cu, after ccl_gemm_kernel.cuh.
 #ifndef CCL_GEMM_PLAN_CUH_
 #define CCL_GEMM_PLAN_CUH_
 
@@ -93,7 +93,10 @@ static ccl_status merge_width(int64_t* cur, int64_t w, const char* dim) {
 // units = schedulable CTAs (1-CTA kernel) or CTA pairs (2-CTA kernel) the device can hold at once
 // cap > 0: a ragged batch -- the tile grid of one problem covers `cap` rows, d->M is the total row count of A and C
 // ragk: a batch with ragged K -- d->K is the total row count of the concatenated A [K x M] and B [K x N]
-static int resident_clusters(int ks, bool have_device);
+int resident_clusters(int ks, bool have_device);     // ccl_gemm.cu, like the next three
+int resident_pairs();
+bool device_units(int* sms, int* pairs);
+ccl_status wave_barrier(GemmPlan& plan, bool plain, cudaStream_t st);
 
 // Modelled cycles of one k block (64 of K) of a tile `b` columns wide on `c` CTAs: the tensor pipe needs 2 cycles per tile
 // column (128 rows per SM, UMMA_K = 16, four steps); the SM pulls its share of the operands (its 128 rows of A and its
@@ -108,8 +111,9 @@ static double kblock_cycles(int b, int c, bool b_kmajor, int64_t active) {
 }
 
 // have_device: the unit counts come from the current device (else the figures of a B200)
+// epi: 1 / 2 = a plan for ccl_gemm_epilogue / ccl_gemm_act_grad
 static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, const void* A, const void* B, const void* C, int sms, int pairs, GemmPlan* plan,
-                            int64_t cap = 0, bool ragk = false, size_t max_ws = ~(size_t)0, bool have_device = false) {
+                            int64_t cap = 0, bool ragk = false, size_t max_ws = ~(size_t)0, bool have_device = false, int epi = 0) {
     if (!d) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: NULL descriptor");
     if (d->M <= 0 || d->N <= 0 || d->K <= 0) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: M, N, K must be positive");
     if (d->M >= (INT64_C(1) << 31) || d->N >= (INT64_C(1) << 31) || d->K >= (INT64_C(1) << 31)) return fail(CCL_ERR_UNSUPPORTED, "ccl_gemm: dimension too large");
@@ -210,6 +214,8 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     if (strips_m > 1 && at && Wm % 8) return fail(CCL_ERR_UNSUPPORTED, "ccl_gemm: strips of %lld columns of an A stored [K x M] are not a multiple of 8", (long long)Wm);
     int ctas = 1, bn = 256, splits = 1;
     double best = -1.0;
+    // (the epilogue operators have the 256- and 128-column kernels only where an optional feature of the layouts is in use)
+    const bool epi_full = epi && (il_a || il_b || il_c || ka || kb || any_rag || d->out_part == CCL_PART_2D);
     // Test overrides (environment): CCL_GEMM_CTAS = 1|2, CCL_GEMM_BN = 128|192|256|384|512, CCL_GEMM_SPLITK = number of K splits.
     const char* force_ctas = std::getenv("CCL_GEMM_CTAS");
     const char* force_bn = std::getenv("CCL_GEMM_BN");
@@ -222,6 +228,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
             if (c == 1 && b > 256) continue;
             if (c == 2 && b == 192 && !bt && il_b) continue;    // 96 columns per CTA of an N-contiguous B: a box and a half (see the kernel), not across chunks
             if (b == 192 && (c == 2 ? no_192_pair : no_192)) continue;
+            if (epi_full && b != 256 && b != 128) continue;
             if (b == 384 && (cap > 0 || ragk)) continue;            // (no ragged-batch instantiation of the 256 + 128 tile)
             if (force_bn && atoi(force_bn) != b) continue;
             if (swiglu && !(c == 2 && b == 512)) continue;          // the gated activation pairs the two accumulators of the wide tile
@@ -268,7 +275,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     {
         const char* force_bal = std::getenv("CCL_GEMM_BALANCED");   // 0: never, 1: whenever the call qualifies
         const int want = force_bal ? atoi(force_bal) : -1;
-        const bool can = want != 0 && batch == 1 && !swiglu && cap == 0 && !ragk && !any_rag && num_kb >= 2 && !(force_split && atoi(force_split) > 1);
+        const bool can = want != 0 && !epi && batch == 1 && !swiglu && cap == 0 && !ragk && !any_rag && num_kb >= 2 && !(force_split && atoi(force_split) > 1);
         double best_bal = -1.0;
         int bc = 0, bb = 0;
         int64_t bal_rounds = 0;
@@ -357,7 +364,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     p.M = (int32_t)d->M; p.N = (int32_t)Nc; p.K = (int32_t)d->K;
     const int bn_walk = swiglu ? 256 : bn;              // tile width in C columns
     p.pair_dist = swiglu ? (int32_t)Wn : 0; p.fd_wn = make_fastdiv(Wn);
-    p.Wm = (int32_t)Wm; p.Wn = (int32_t)Wn;
+    p.Wm = (int32_t)Wm; p.Wn = (int32_t)Wn; p.fd_wm = make_fastdiv(Wm);
     p.tps_m = (int32_t)((Wm + bm - 1) / bm); p.tps_n = (int32_t)((Wn + bn_walk - 1) / bn_walk);
     p.tiles_m = (int32_t)((Mt + Wm - 1) / Wm) * p.tps_m; p.tiles_n = (int32_t)((Nc + Wn - 1) / Wn) * p.tps_n;
     p.num_kb = (int32_t)num_kb;

@@ -391,7 +391,7 @@ ccl_status ccl_bias_act_grad(const ccl_mat* m, int32_t act, const void* dY_dev, 
  * A mixture-of-experts feed-forward layer for a few tokens (a decode step), router to output, in one launch:
  *   logits = X * Wr^T (fp32),  p = softmax(logits) over the E experts,  the topk largest p of each token (equal ones: the
  *   lowest expert first),  weight w = p, divided by the sum of the token's topk p when norm_topk is set,
- *   Y[t] = bf16( residual[t] + sum over the chosen experts e of w_te * Wd_e * bf16( silu(Wg_e x_t) .* (Wu_e x_t) ) )
+ *   Y[t] = bf16( residual[t] + sum over the chosen experts e of w_te * Wd_e * ( silu(Wg_e x_t) .* (Wu_e x_t) ) )
  *   X [T x H], residual [T x H] (or NULL; may be Y itself), Y [T x H]: bf16 row-major
  *   Wr        bf16 [E x H]
  *   Wgu       per expert bf16 [2I x H] (K along the rows): I gate rows, then I up rows; with gu_strips = S > 1 the rows form S

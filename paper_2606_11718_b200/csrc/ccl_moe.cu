@@ -3,93 +3,160 @@
 //
 // Bound by memory: every chosen expert's weights are read once (3 H I elements each) and nothing else is of that order; with
 // m tokens an expert the arithmetic is 2 m flops per 2-byte weight, far below what the tensor cores take.  So the kernel is a
-// stream of weight rows through a shared-memory ring, filled by bulk copies that never wait for anything but a free slot:
+// stream of weights through shared memory that stops for nothing it can avoid:
 //   1. router: the CTAs share the E x T dot products; first meeting of the grid; every CTA then works out the same top-k and the
 //      same lists of tokens per expert by itself
-//   2. gate and up: the (expert, 8 features) units are shared out evenly.  A unit is 16 weight rows -- 8 gate, 8 up -- times
-//      its expert's tokens (n = 8 columns): one m16n8k16 accumulator then holds the gate and the up value of a
+//   2. gate and up: the (expert, 16 features) units are shared out evenly.  A unit is 32 weight rows -- 16 gate, 16 up -- times
+//      its expert's tokens (n = 8 columns): two m16n8k16 accumulators then hold the gate and the up value of a
 //      feature in the same lane, and silu(gate) * up needs no exchange.  h goes to the workspace; second meeting
-//   3. down: a CTA owns a few rows of Wd (H / #SMs of them, at most 16) and takes every chosen expert's: the sum over a token's
-//      experts stays inside the CTA, in a fixed order, and Y is written once.  The ring is filled with phase 3's
-//      weights while phase 2's last units and the meeting are still going on: the stream does not stop there.
-// Warp roles: 8 consumer warps split every slot's k range between them; warp 8 fills the weight ring; warp 9 waits for the
-// second meeting and fills the (small) ring of h rows.
+//   3. down: a pair of CTAs (a cluster) owns a few rows of Wd (2 H / #SMs of them, at most 32) and takes every chosen expert's:
+//      the sum over a token's experts stays inside the pair, in a fixed order, and Y is written once.
+// The k range of a unit is dealt out in blocks of 64 (32 rows x 128 bytes) to the 8 consumer warps of the CTA in turn (phase 3: to
+// the 16 of the pair); a ninth warp fetches the blocks, one TMA copy each, up to 32 of them ahead.  It stops for nothing but a
+// full ring: it runs ahead across units and from phase 2 into phase 3, so the weights of phase 3 arrive during the second
+// meeting.  (Consumers that issued their own copies made the loops too large for the instruction cache: phase 3 of 64 tokens x
+// 128 experts of 2048 x 768 took 118 us.)
 //
 // The matrix instructions are mma.sync: with n = 8 columns a tcgen05 tile would be 128 rows high and leave most SMs without
 // work for one token; they are nowhere near their limit here.  Weights and tokens are both K-contiguous, so a lane may take any 8
-// consecutive k as its share of two k steps as long as both operands do: 16-byte shared-memory loads, no ldmatrix, and a
-// row pitch of 64 bytes more than a multiple of 128 keeps them free of bank conflicts.
+// consecutive k as its share of two k steps as long as both operands do: 16-byte loads, no ldmatrix.
+// h keeps 16 significant bits: it is stored as two bf16 rows (the rounded value and what the rounding left), side by side as two columns
+// of the same product, which the n = 8 columns have room for.
 #include <algorithm>
 #include <atomic>
 #include <chrono>
+#include <type_traits>
 
 #include "ccl_act.cuh"
 #include "ccl_tma.h"
 
 namespace ccl {
 
-constexpr int kMoeConsumers = 8;                         // warps
-constexpr int kMoeThreads = (kMoeConsumers + 2) * 32;
-constexpr int kMoeK = 512;                               // k elements of a slot
-constexpr int kMoePitch = kMoeK * 2 + 64;                // bytes between the rows of a slot
-constexpr int kMoeSlot = 16 * kMoePitch;
-constexpr int kMoeMaxSlots = 12, kMoeMaxHSlots = 8;
+constexpr int kMoeWarps = 8;                             // consumers
+constexpr int kMoeThreads = kMoeWarps * 32;
+constexpr int kMoeBlockThreads = kMoeThreads + 32;       // and the warp that fetches
+constexpr int kMoeRows = 32;                             // rows of a block,
+constexpr int kMoeBlockK = 64;                           // its k elements (128 bytes of a row)
+constexpr int kMoeBlock = kMoeRows * kMoeBlockK * 2;
+constexpr int kMoeDepth = 4;                             // blocks in a warp's ring
+constexpr int kMoeRing = kMoeWarps * kMoeDepth * kMoeBlock;
+constexpr int kMoeSmem = 226 * 1024;
 constexpr int64_t kMoeMaxT = 64, kMoeMaxE = 512, kMoeMaxK = 16;
 
 static __device__ int g_moe_status = 0;
 
 struct MoeParams {
     int32_t T, H, I, E, topk, norm;
-    int32_t gu_half, gu_strip;              // gate rows of a strip; rows of a strip
-    int64_t gu_stride, d_stride;            // bytes from one expert to the next
+    int32_t gu_half, strip_units;           // gate rows of a strip; units of a strip
     const uint16_t *x, *wr, *residual;
-    const unsigned char *wgu, *wd;
     uint16_t* y;
     int32_t* ids;
     float* weights;
     float* logits;                          // workspace: [T][E]
-    unsigned long long* flags;              // workspace: [2 meetings][CTAs]
-    unsigned char* h;                       // workspace: [pairs][h_pitch bytes] bf16
+    unsigned long long* flags;              // workspace: a flag per CTA (first meeting)
+    unsigned long long* gate;               // workspace: the word that ends the first meeting, the counter of the second
+    unsigned char* h;                       // workspace: [pairs][2 (value, remainder)][h_pitch bytes] bf16
     int64_t h_pitch;
     unsigned long long mark;                // this launch's mark in the flags
-    int32_t group;                          // tokens of an expert taken together (8, 16 or 32 columns)
-    int32_t slots, h_slots;
+    int32_t group;                          // most tokens of an expert taken together
+    int32_t all_x;                          // 1: the rows of all tokens are staged once; 0: those of an expert's tokens when it comes up
     int32_t x_pitch;                        // bytes between the token rows in shared memory
-    int32_t rows_per_block, blocks;         // phase 3: rows of Wd a CTA takes at a time, such blocks in all
+    int32_t rows_per_block, blocks;         // phase 3: rows of Wd a pair of CTAs takes at a time, such blocks in all
     // byte offsets in shared memory
-    int32_t at_region, at_hring, at_red, at_mask, at_off, at_ent, at_tok, at_wt, at_sel, at_selw, at_bars;
+    int32_t at_bars, at_region, at_red, at_mask, at_off, at_ent, at_sel, at_selw, at_pair;
 };
 
-__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     uint4 v;
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void st_release_u64(unsigned long long* p, unsigned long long v) {
-    asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(p), "l"(v) : "memory");
 }
 __device__ __forceinline__ unsigned long long ld_acquire_flag(const unsigned long long* p) {
     unsigned long long v;
     asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
     return v;
 }
-// One warp waits (bounded) until every CTA has set its flag to `mark`.
-__device__ __forceinline__ bool meet(const unsigned long long* flags, int ctas, unsigned long long mark, int lane) {
-    bool ok = true;
+// All consumer threads
+__device__ __forceinline__ void bar_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(kMoeThreads) : "memory"); }
+__device__ __forceinline__ bool bar_consumers_and(bool v) {
+    uint32_t r;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.and.pred q, 1, %2, p;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"((uint32_t)v), "n"(kMoeThreads) : "memory");
+    return r != 0;
+}
+// (out of line: the loops that wait must stay small)
+__device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity) { return mbar_wait_bounded_addr(bar, parity); }
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (!__all_sync(0xffffffffu, done)) done = __all_sync(0xffffffffu, wait_long(bar, parity));
+    return done;
+}
+// One thread waits (bounded) until the word is `mark` (exact) or at least that.
+__device__ __noinline__ bool wait_word(const unsigned long long* word, unsigned long long mark, bool exact) {
     const uint64_t t0 = global_timer_ns();
-    for (int i = lane; ok && i < ctas; i += 32)
-        for (uint32_t n = 1; ld_acquire_flag(flags + i) != mark; ++n)
-            if ((n & 255u) == 0 && global_timer_ns() - t0 > kWaitLimitNs) { ok = false; break; }
-    return __all_sync(0xffffffffu, ok);
+    for (;;) {
+        unsigned long long v;
+        asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(word) : "memory");
+        if (exact ? v == mark : v >= mark) return true;
+        if (global_timer_ns() - t0 > kWaitLimitNs) return false;
+    }
+}
+__device__ __forceinline__ void st_release(unsigned long long* p, unsigned long long v) { asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(p), "l"(v) : "memory"); }
+// The grid's meetings (all consumer threads call; what a CTA wrote before is seen by all behind it).  Measured, 148 CTAs: 1.3 us
+// when every CTA adds to one counter and one thread of each reads it; 4.9 us when 148 threads of every CTA read a flag of each.
+// The counter needs a start, so the first meeting has flags -- any contents but this launch's mark mean "not yet" -- that CTA 0 alone
+// reads, and a word by which it lets the others go; it clears the counter of the second on the way.
+__device__ __forceinline__ bool meet_first(const MoeParams& p) {
+    bar_consumers();
+    bool ok = true;
+    if (threadIdx.x == 0) st_release(p.flags + blockIdx.x, p.mark);
+    if (blockIdx.x == 0) {
+#pragma unroll 1
+        for (unsigned i = threadIdx.x; i < gridDim.x; i += kMoeThreads) ok = wait_word(p.flags + i, p.mark, true) && ok;
+        ok = bar_consumers_and(ok);
+        if (threadIdx.x == 0 && ok) { p.gate[1] = 0; st_release(p.gate, p.mark); }
+    } else {
+        if (threadIdx.x == 0) ok = wait_word(p.gate, p.mark, true);
+        ok = bar_consumers_and(ok);
+    }
+    if (!ok && threadIdx.x == 0) atomicExch(&g_moe_status, 8);
+    return ok;
+}
+__device__ __forceinline__ bool meet_second(const MoeParams& p) {
+    bar_consumers();
+    bool ok = true;
+    if (threadIdx.x == 0) {
+        asm volatile("red.release.gpu.global.add.u64 [%0], 1;" ::"l"(p.gate + 1) : "memory");
+        ok = wait_word(p.gate + 1, gridDim.x, false);
+        if (!ok) atomicExch(&g_moe_status, 8);
+    }
+    return bar_consumers_and(ok);
+}
+// All threads of the CTA pair
+__device__ __forceinline__ void pair_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// The consumers of a CTA pair meet at a barrier of each CTA's that one thread of the other CTA arrives at (the warps that fetch are
+// not to stop for it): what either wrote to its shared memory before is seen by the other behind the wait.
+__device__ __forceinline__ void tell_other(uint64_t* bar, uint32_t other) {
+    uint32_t remote;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_u32(bar)), "r"(other));
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
+}
+__device__ __noinline__ bool wait_other(uint64_t* bar, uint32_t parity) {
+    const uint64_t t0 = global_timer_ns();
+    for (;;) {
+        uint32_t done;
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+        if (done) return true;
+        if (global_timer_ns() - t0 > kWaitLimitNs) return false;
+    }
 }
 
 // Order-preserving integer image of a float; NaN below every number, 0 is left for "taken".
@@ -99,381 +166,554 @@ __device__ __forceinline__ uint32_t order_key(float f) {
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// The 32-element k steps of a slot that belong to this warp: acc += W[16 rows] * B[columns], both in shared memory at `w` (row
-// pitch kMoePitch) and `b`.  kc: valid k elements of the slot (a multiple of 8; both operands read as zero behind it); cols:
-// columns that exist (zero behind them; nothing is read there).
-template <int NT>
-__device__ __forceinline__ void slot_product(float (&acc)[NT][4], uint32_t w, uint32_t b, int b_pitch, int kc, int cols, int warp, int lane) {
-    const int g = lane >> 2, q = lane & 3;
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
+
+// Byte offset of the 16 bytes that row r, piece c (of 8) of a block are kept at (the TMA's 128-byte swizzle), and the row a lane
+// with g = lane / 4 takes as row g of a matrix fragment: consecutive g lie four rows apart, so that the 8 lanes of a 16-byte
+// load's phase (two g, four pieces each) hit different banks.
+__device__ __forceinline__ uint32_t block_at(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
+__device__ __forceinline__ int fragment_row(int g) { return (g & 1) << 2 | g >> 1; }
+
+// Sums of a token's rows r, r + 8, r + 16 and r + 24 (r < 8) lie side by side, turned by the token so that the tokens of a
+// product's columns meet in different banks.  Offset of the four, and the row of place `at` of a token's 32.
+__device__ __forceinline__ int sum_at(int t, int r) { return t * kMoeRows + ((r ^ (t & 7)) << 2); }
+__device__ __forceinline__ int sum_row(int t, int at) { return ((at >> 2) ^ (t & 7)) + (at & 3) * 8; }
+
+// The topk largest of one token's E logits, by one warp.  Every lane keeps V >= E / 32 of them (experts lane, lane + 32, ...);
+// lane k < topk gets the k-th choice.  SORTED: the lane's few are put in order first, so that a choice is one maximum over the
+// lanes' heads and the winner moves up by one; with many a lane the winner looks through all of its own again.
+struct Choice { int expert; float weight; };
+template <int V, bool SORTED, int TB>
+__device__ __forceinline__ void choose(const MoeParams& p, const float (&l)[TB][V], Choice (&c)[TB], int lane) {
+    uint32_t key[TB][V], mine[TB], first[TB];             // images of the logits; of the one this lane keeps; of the largest
+    int place[TB][V];                                     // (the lane's j-th: expert lane + 32 j)
+    bool nan[TB];
 #pragma unroll
-    for (int st = 0; st < kMoeK / 32 / kMoeConsumers; ++st) {
-        const int k = (st * kMoeConsumers + warp) * 32;
-        if (k >= kc) break;
-        const int kq = k + q * 8;
-        const bool ok = kq < kc;
-        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-        const uint4 lo = ok ? lds128(w + g * kMoePitch + kq * 2) : zero, hi = ok ? lds128(w + (g + 8) * kMoePitch + kq * 2) : zero;
+    for (int b = 0; b < TB; ++b) {
+        nan[b] = false;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if (n * 8 >= cols) break;
-            const uint4 t = ok && n * 8 + g < cols ? lds128(b + (n * 8 + g) * b_pitch + kq * 2) : zero;
-            mma_16x8x16(acc[n], lo.x, hi.x, lo.y, hi.y, t.x, t.y);
-            mma_16x8x16(acc[n], lo.z, hi.z, lo.w, hi.w, t.z, t.w);
+        for (int j = 0; j < V; ++j) {
+            key[b][j] = lane + 32 * j < p.E ? order_key(l[b][j]) : 0u;
+            place[b][j] = j;
+            nan[b] |= l[b][j] != l[b][j];
         }
+        nan[b] = __any_sync(0xffffffffu, nan[b]);
+        if (SORTED) {                                     // largest first, the lower expert first among equals
+#pragma unroll
+            for (int a = 0; a < V - 1; ++a)
+#pragma unroll
+                for (int j = V - 2; j >= a; --j) {
+                    const bool swap = key[b][j + 1] > key[b][j];
+                    const uint32_t k = swap ? key[b][j + 1] : key[b][j];
+                    const int q = swap ? place[b][j + 1] : place[b][j];
+                    if (swap) { key[b][j + 1] = key[b][j]; place[b][j + 1] = place[b][j]; }
+                    key[b][j] = k; place[b][j] = q;
+                }
+        }
+        c[b].expert = 0; mine[b] = first[b] = 0u;
+    }
+#pragma unroll 1
+    for (int k = 0; k < p.topk; ++k) {
+        uint32_t best[TB], top[TB];
+        int at[TB];
+#pragma unroll
+        for (int b = 0; b < TB; ++b) {
+            best[b] = key[b][0]; at[b] = place[b][0];
+            if (!SORTED) {
+#pragma unroll
+                for (int j = 1; j < V; ++j)
+                    if (key[b][j] > best[b]) { best[b] = key[b][j]; at[b] = j; }
+            }
+            top[b] = __reduce_max_sync(0xffffffffu, best[b]);
+        }
+#pragma unroll
+        for (int b = 0; b < TB; ++b) {
+            unsigned who = __ballot_sync(0xffffffffu, best[b] == top[b]);
+            if (who & (who - 1u)) {                       // equal logits in several lanes: the lowest expert
+                const uint32_t e = __reduce_min_sync(0xffffffffu, best[b] == top[b] ? (uint32_t)(lane + 32 * at[b]) : 0xffffffffu);
+                who = 1u << (e & 31u);
+            }
+            const int from = __ffs(who) - 1, e = __shfl_sync(0xffffffffu, lane + 32 * at[b], from);
+            if (k == 0) first[b] = top[b];
+            if (lane == k) { mine[b] = top[b]; c[b].expert = e; }
+            const bool out = lane == from;
+            if (SORTED) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    key[b][j] = out ? (j + 1 < V ? key[b][j + 1] : 0u) : key[b][j];
+                    place[b][j] = out && j + 1 < V ? place[b][j + 1] : place[b][j];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) if (out && j == at[b]) key[b][j] = 0u;
+            }
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < TB; ++b) {
+        const float top = key_value(first[b]);
+        float sum = 0.0f, w = 0.0f;
+        if (lane < p.topk) w = __expf(key_value(mine[b]) - top);
+        if (p.norm) sum = w;
+        else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (lane + 32 * j < p.E) sum += __expf(l[b][j] - top);
+        }
+#pragma unroll
+        for (int m = 16; m >= 1; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+        c[b].weight = nan[b] ? __int_as_float(0x7fffffff) : w / sum;
     }
 }
 
 // NT: most column groups of 8 an expert's tokens are taken in
 template <int NT>
-__global__ void __launch_bounds__(kMoeThreads, 1) moe_tokens_kernel(const __grid_constant__ MoeParams p) {
-    extern __shared__ __align__(128) unsigned char smem[];
+__global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const __grid_constant__ CUtensorMap map_gu, const __grid_constant__ CUtensorMap map_d, const __grid_constant__ MoeParams p) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x, ctas = gridDim.x;
-    constexpr int kConsumerThreads = kMoeConsumers * 32;
     unsigned long long* mask = reinterpret_cast<unsigned long long*>(smem + p.at_mask);      // per expert: the tokens that chose it
     uint16_t* off = reinterpret_cast<uint16_t*>(smem + p.at_off);                            // per expert: its first pair
-    uint32_t* ent = reinterpret_cast<uint32_t*>(smem + p.at_ent);                            // entries: expert | first pair << 9 | columns << 20
-    uint8_t* tok = smem + p.at_tok;                                                          // per pair (by expert): token
-    float* wt = reinterpret_cast<float*>(smem + p.at_wt);                                    // ... and its weight
+    uint32_t* ent = reinterpret_cast<uint32_t*>(smem + p.at_ent);                            // entries: expert | first pair << 9 | pairs << 19
     uint16_t* sel = reinterpret_cast<uint16_t*>(smem + p.at_sel);                            // per (token, choice): expert
-    float* selw = reinterpret_cast<float*>(smem + p.at_selw);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + p.at_bars);
-    uint64_t *wfull = bars, *wempty = wfull + p.slots, *hfull = wempty + p.slots, *hempty = hfull + p.h_slots, *rfull = hempty + p.h_slots, *rempty = rfull + 2;
-    int* shared = reinterpret_cast<int*>(rempty + 2);                                        // [0] entries, [1] gave up
-    const uint32_t ring0 = smem_u32(smem), x0 = smem_u32(smem + p.at_region), hring0 = smem_u32(smem + p.at_hring);
-    float* yacc = reinterpret_cast<float*>(smem + p.at_region);                              // phase 3, where x was: [warp][token][16]
+    float* selw = reinterpret_cast<float*>(smem + p.at_selw);                                // ... and weight
+    int2* pair = reinterpret_cast<int2*>(smem + p.at_pair);                                  // per pair, sorted by expert, then token: token, weight
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + p.at_bars);                          // [warp][slot]: a block has arrived; then: ... has been used
+    uint64_t* pair_bars = bars + 2 * kMoeWarps * kMoeDepth;                                  // the other CTA's sums are there; it has read this one's
+    int* shared = reinterpret_cast<int*>(pair_bars + 2);                  // [0] entries, [1] the first meeting came about
+    const int warp2 = (cta & 1) * kMoeWarps + warp;       // this warp's number in the CTA pair
+    const int pairs = p.T * p.topk, nb1 = (p.H + kMoeBlockK - 1) / kMoeBlockK, nb2 = (p.I + kMoeBlockK - 1) / kMoeBlockK, nfb = p.I / p.gu_half * p.strip_units;
+    const uint32_t x0 = smem_u32(smem + p.at_region);
+    float* yacc = reinterpret_cast<float*>(smem + p.at_region);                              // phase 3, where x was: [warp][token][32], see sum_at
 
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < p.slots; ++i) { mbar_init(&wfull[i], 1); mbar_init(&wempty[i], kMoeConsumers); }
-        for (int i = 0; i < p.h_slots; ++i) { mbar_init(&hfull[i], 1); mbar_init(&hempty[i], kMoeConsumers); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&rfull[i], kMoeConsumers); mbar_init(&rempty[i], 1); }
-        shared[1] = 0;
-        fence_barrier_init();
-        p.flags[ctas + cta] = 0;                          // the second meeting's flag; seen by all once the first meeting is over
-    }
-    for (int e = threadIdx.x; e < p.E; e += kMoeThreads) mask[e] = 0;
-    __syncthreads();
-    const int nch1 = (p.H + kMoeK - 1) / kMoeK, nch2 = (p.I + kMoeK - 1) / kMoeK, nfb = p.I / 8;
-    const bool fixed_x = p.T <= 8;                        // column = token for every expert: x is staged once
+    if (threadIdx.x == 0) { prefetch_tmap(&map_gu); prefetch_tmap(&map_d); }
+    if ((int)threadIdx.x < 2 * kMoeWarps * kMoeDepth + 2) { mbar_init(&bars[threadIdx.x], 1); fence_barrier_init(); }
+    if (warp < kMoeWarps)
+        for (int e = threadIdx.x; e < p.E; e += kMoeThreads) mask[e] = 0;
+    // rows of x (zeros behind H) in shared memory; row t is token `of(t)`
+    auto stage_x = [&](int rows, auto of) {
+        const int pieces = nb1 * (kMoeBlockK / 8);
+        for (int c = threadIdx.x; c < pieces; c += kMoeThreads)
+#pragma unroll 4
+            for (int t = 0; t < rows; ++t) {
+                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                if (c * 8 < p.H) v = __ldg(reinterpret_cast<const uint4*>(p.x + (int64_t)of(t) * p.H) + c);
+                *reinterpret_cast<uint4*>(smem + p.at_region + t * p.x_pitch + c * 16) = v;
+            }
+    };
 
     // ---- 1. router --------------------------------------------------------------------------------------------------
-    if (warp < kMoeConsumers) {
-        if (fixed_x)
-            for (int i = threadIdx.x; i < p.T * (p.H / 8); i += kConsumerThreads) {
-                const int t = i / (p.H / 8), c = i - t * (p.H / 8);
-                *reinterpret_cast<uint4*>(smem + p.at_region + t * p.x_pitch + c * 16) = __ldg(reinterpret_cast<const uint4*>(p.x + (int64_t)t * p.H) + c);
-            }
-        // an item is one expert's row times up to 8 tokens; with fewer tokens the warps split the row as well
-        float* part = reinterpret_cast<float*>(smem + p.at_red);
-        const int ntb = (p.T + 7) / 8;
-        int flip = 0;
-        for (int item = cta; item < p.E * ntb; item += ctas) {
-            const int tb = item / p.E, e = item - tb * p.E, nt = min(8, p.T - tb * 8);
-            const int np = nt > 4 ? 8 : (nt > 2 ? 4 : nt), nsl = kMoeConsumers / np, t = warp & (np - 1), sl = warp / np;
-            float s = 0.0f;
-            if (t < nt) {
-                const int pieces = p.H / 8, lo = pieces * sl / nsl, hi = pieces * (sl + 1) / nsl;
-                const uint4 *xr = reinterpret_cast<const uint4*>(p.x + (int64_t)(tb * 8 + t) * p.H), *wr = reinterpret_cast<const uint4*>(p.wr + (int64_t)e * p.H);
-#pragma unroll 4
-                for (int i = lo + lane; i < hi; i += 32) {
-                    float a[8], b[8];
-                    bf16x8_unpack(__ldg(xr + i), a);
-                    bf16x8_unpack(__ldg(wr + i), b);
+    // an item is 16 experts' rows times up to 8 tokens, one matrix product; the warps split its k range
+    if (warp < kMoeWarps) {
+    {
+        float4* part = reinterpret_cast<float4*>(smem + p.at_red);
+        const int g = lane >> 2, q = lane & 3, ne = (p.E + 15) / 16, ntb = (p.T + 7) / 8, steps = (p.H + 31) / 32;
+#pragma unroll 1
+        for (int item = cta; item < ne * ntb; item += ctas) {
+            const int tb = item / ne, e0 = (item - tb * ne) * 16, t0 = tb * 8;
+            const uint4 *wlo = reinterpret_cast<const uint4*>(p.wr + (int64_t)min(e0 + g, p.E - 1) * p.H) + q, *whi = reinterpret_cast<const uint4*>(p.wr + (int64_t)min(e0 + g + 8, p.E - 1) * p.H) + q;
+            const uint4* xr = reinterpret_cast<const uint4*>(p.x + (int64_t)min(t0 + g, p.T - 1) * p.H) + q;
+            float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+            for (int s0 = warp; s0 < steps; s0 += 8 * kMoeWarps) {       // eight steps' loads in flight together
+                uint4 a[8], b[8], c[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) s = fmaf(a[j], b[j], s);
+                for (int j = 0; j < 8; ++j) {
+                    const int s = s0 + j * kMoeWarps;
+                    a[j] = b[j] = c[j] = make_uint4(0u, 0u, 0u, 0u);
+                    if (s * 32 + q * 8 < p.H) { a[j] = __ldg(wlo + s * 4); b[j] = __ldg(whi + s * 4); c[j] = __ldg(xr + s * 4); }
                 }
 #pragma unroll
-                for (int m = 16; m >= 1; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
-            }
-            if (nsl == 1) {
-                if (lane == 0 && t < nt) p.logits[(int64_t)(tb * 8 + t) * p.E + e] = s;
-            } else {
-                if (lane == 0) part[flip + warp] = s;
-                bar_sync(1, kConsumerThreads);
-                if ((int)threadIdx.x < nt) {
-                    s = 0.0f;
-                    for (int i = 0; i < nsl; ++i) s += part[flip + i * np + threadIdx.x];
-                    p.logits[(int64_t)(tb * 8 + threadIdx.x) * p.E + e] = s;
-                }
-                flip ^= 8;
-            }
-        }
-        bar_sync(1, kConsumerThreads);
-        if (warp == 0) {
-            if (lane == 0) { __threadfence(); st_release_u64(p.flags + cta, p.mark); }
-            if (!meet(p.flags, ctas, p.mark, lane) && lane == 0) { shared[1] = 1; atomicExch(&g_moe_status, 8); }
-        }
-        bar_sync(1, kConsumerThreads);
-        // top-k, a warp per token
-        for (int t = warp; t < p.T; t += kMoeConsumers) {
-            constexpr int V = (int)(kMoeMaxE / 32);
-            float l[V];
-            uint32_t key[V];
-            bool nan = false;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int e = lane + 32 * j;
-                if (32 * j < p.E && e < p.E) { l[j] = __ldcg(p.logits + (int64_t)t * p.E + e); key[j] = order_key(l[j]); nan |= l[j] != l[j]; }
-                else { l[j] = 0.0f; key[j] = 0u; }
-            }
-            nan = __any_sync(0xffffffffu, nan);
-            float first = 0.0f, mine = 0.0f, sum = 0.0f;  // the largest logit; the chosen one this lane keeps; sum of exponentials
-            int mine_e = 0;
-            for (int k = 0; k < p.topk; ++k) {
-                uint32_t best = 0u;
-#pragma unroll
-                for (int j = 0; j < V; ++j) if (32 * j < p.E) best = max(best, key[j]);
-                best = __reduce_max_sync(0xffffffffu, best);
-                uint32_t at = 0xffffffffu;
-                float val = 0.0f;
-#pragma unroll
-                for (int j = V - 1; j >= 0; --j) if (32 * j < p.E && key[j] == best) { at = (uint32_t)(lane + 32 * j); val = l[j]; }
-                const uint32_t e = __reduce_min_sync(0xffffffffu, at);
-                val = __shfl_sync(0xffffffffu, val, (int)(e & 31u));
-#pragma unroll
-                for (int j = 0; j < V; ++j) if (32 * j < p.E && (uint32_t)(lane + 32 * j) == e) key[j] = 0u;
-                if (k == 0) first = val;
-                if (lane == k) { mine = val; mine_e = (int)e; }
-            }
-            if (p.norm) { if (lane < p.topk) sum = expf(mine - first); }
-            else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) if (32 * j < p.E && lane + 32 * j < p.E) sum += expf(l[j] - first);
-            }
-#pragma unroll
-            for (int m = 16; m >= 1; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-            if (lane < p.topk) {
-                const float w = nan ? __int_as_float(0x7fffffff) : expf(mine - first) / sum;
-                sel[t * p.topk + lane] = (uint16_t)mine_e;
-                selw[t * p.topk + lane] = w;
-                atomicOr(&mask[mine_e], 1ull << t);       // (the order of the bits' arrival does not matter)
-                if (cta == 0) {
-                    if (p.ids) p.ids[t * p.topk + lane] = mine_e;
-                    if (p.weights) p.weights[t * p.topk + lane] = w;
+                for (int j = 0; j < 8; ++j) {
+                    mma_16x8x16(acc, a[j].x, b[j].x, a[j].y, b[j].y, c[j].x, c[j].y);
+                    mma_16x8x16(acc, a[j].z, b[j].z, a[j].w, b[j].w, c[j].z, c[j].w);
                 }
             }
-        }
-        bar_sync(1, kConsumerThreads);
-        // pairs sorted by expert, then token; entries of at most `group` pairs of one expert
-        if (warp == 0) {
-            int pairs = 0, ents = 0;
-            for (int e0 = 0; e0 < p.E; e0 += 32) {
-                const int e = e0 + lane, cnt = e < p.E ? __popcll(mask[e]) : 0, ne = (cnt + p.group - 1) / p.group;
-                int sc = cnt, se = ne;
+            part[threadIdx.x] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            bar_consumers();
+            if (warp == 0) {
+                float4 v = part[lane];
 #pragma unroll
-                for (int m = 1; m < 32; m <<= 1) {
-                    const int a = __shfl_up_sync(0xffffffffu, sc, m), b = __shfl_up_sync(0xffffffffu, se, m);
-                    if (lane >= m) { sc += a; se += b; }
+                for (int w = 1; w < kMoeWarps; ++w) {
+                    const float4 z = part[w * 32 + lane];
+                    v.x += z.x; v.y += z.y; v.z += z.z; v.w += z.w;
                 }
-                const int o = pairs + sc - cnt, i0 = ents + se - ne;
-                if (e < p.E) off[e] = (uint16_t)o;
-                for (int i = 0; i < ne; ++i) ent[i0 + i] = (uint32_t)e | (uint32_t)(o + i * p.group) << 9 | (uint32_t)min(p.group, cnt - i * p.group) << 20;
-                pairs += __shfl_sync(0xffffffffu, sc, 31);
-                ents += __shfl_sync(0xffffffffu, se, 31);
+                const float l[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int t = t0 + 2 * q + (c & 1), e = e0 + g + (c >> 1) * 8;
+                    if (t < p.T && e < p.E) p.logits[(int64_t)t * p.E + e] = l[c];
+                }
             }
-            if (lane == 0) shared[0] = ents;
-        }
-        bar_sync(1, kConsumerThreads);
-        for (int i = threadIdx.x; i < p.T * p.topk; i += kConsumerThreads) {
-            const int t = i / p.topk, e = sel[i], s = off[e] + __popcll(mask[e] & ((1ull << t) - 1ull));
-            tok[s] = (uint8_t)t;
-            wt[s] = selw[i];
+            bar_consumers();
         }
     }
+    if (p.all_x) stage_x(p.T, [](int t) { return t; });
+    {   // h's rows end with whole blocks: zeros behind I
+        const int tail = nb2 * 8 - p.I / 8;
+        for (int j = cta * kMoeThreads + (int)threadIdx.x; j < 2 * pairs * tail; j += ctas * kMoeThreads) {
+            const int r = j / tail, c = p.I / 8 + j - r * tail;
+            *reinterpret_cast<uint4*>(p.h + (int64_t)r * p.h_pitch + c * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+    const bool met1 = meet_first(p);
+    if (threadIdx.x == 0) { shared[1] = met1; p.flags[cta] = 0; }        // (cleared for the next launch, which may be this one replayed)
+    // top-k, a warp per token; with many of them four at a time, whose chains of dependent steps (a choice waits for the one before)
+    // overlap
+    auto top_k = [&](auto v, auto sorted, auto tb) {
+        constexpr int V = decltype(v)::value, TB = decltype(tb)::value;
+#pragma unroll 1
+        for (int t0 = met1 ? warp * TB : p.T; t0 < p.T; t0 += kMoeWarps * TB) {
+            float l[TB][V];
+            Choice ch[TB];
+#pragma unroll
+            for (int b = 0; b < TB; ++b)
+#pragma unroll
+                for (int j = 0; j < V; ++j) l[b][j] = t0 + b < p.T && lane + 32 * j < p.E ? __ldcg(p.logits + (int64_t)(t0 + b) * p.E + lane + 32 * j) : 0.0f;
+            choose<V, decltype(sorted)::value, TB>(p, l, ch, lane);
+#pragma unroll
+            for (int b = 0; b < TB; ++b)
+                if (t0 + b < p.T && lane < p.topk) {
+                    const int at = (t0 + b) * p.topk + lane, e = ch[b].expert;
+                    sel[at] = (uint16_t)e;
+                    selw[at] = ch[b].weight;
+                    atomicOr(reinterpret_cast<uint32_t*>(mask + e) + ((t0 + b) >> 5), 1u << ((t0 + b) & 31));   // (in whatever order the bits arrive; 64-bit ones are emulated)
+                    if (cta == 0) {
+                        if (p.ids) p.ids[at] = e;
+                        if (p.weights) p.weights[at] = ch[b].weight;
+                    }
+                }
+        }
+    };
+    if (p.E > 128) top_k(std::integral_constant<int, (int)(kMoeMaxE / 32)>(), std::false_type(), std::integral_constant<int, 1>());
+    else if (p.T <= 8) top_k(std::integral_constant<int, 4>(), std::true_type(), std::integral_constant<int, 1>());
+    else top_k(std::integral_constant<int, 4>(), std::true_type(), std::integral_constant<int, 4>());
+    bar_consumers();
+    // pairs sorted by expert, then token: every expert's first one; entries of at most `group` pairs of one expert
+    if (warp == 0) {
+        int np = 0, ne = 0;
+#pragma unroll 1
+        for (int e = lane; e - lane < p.E; e += 32) {
+            const int cnt = e < p.E ? __popcll(mask[e]) : 0;
+            const int n = cnt <= p.group ? (cnt > 0) : (cnt + p.group - 1) / p.group;
+            int sum = cnt << 16 | n;                      // both prefix sums at once
+#pragma unroll
+            for (int m = 1; m < 32; m <<= 1) {
+                const int a = __shfl_up_sync(0xffffffffu, sum, m);
+                if (lane >= m) sum += a;
+            }
+            const int o = np + (sum >> 16) - cnt, i0 = ne + (sum & 0xffff) - n;
+            if (e < p.E) off[e] = (uint16_t)o;
+            for (int i = 0; i < n; ++i) ent[i0 + i] = (uint32_t)e | (uint32_t)(o + i * p.group) << 9 | (uint32_t)min(p.group, cnt - i * p.group) << 19;
+            sum = __shfl_sync(0xffffffffu, sum, 31);
+            np += sum >> 16; ne += sum & 0xffff;
+        }
+        if (lane == 0) shared[0] = ne;
+    }
+    bar_consumers();
+    for (int i = threadIdx.x; i < pairs; i += kMoeThreads) {
+        const int t = i / p.topk, e = sel[i], s = off[e] + __popcll(mask[e] & ((1ull << t) - 1ull));
+        pair[s] = make_int2(t, __float_as_int(selw[i]));
+    }
+    }
     __syncthreads();
-    if (shared[1]) return;                                // the first meeting did not come about: nothing is in flight yet
+    if (!shared[1]) { pair_sync(); return; }              // (the first meeting did not come about; nothing is in flight)
     const int ents = shared[0], units = ents * nfb;
     const int u0 = (int)((int64_t)units * cta / ctas), u1 = (int)((int64_t)units * (cta + 1) / ctas);
 
-    if (warp == kMoeConsumers) {
-        // ---- weight ring --------------------------------------------------------------------------------------------
-        int slot = 0, issued = 0;
-        uint32_t phase = 0;
+    const int per_row_block = ents * nb2;                // blocks of a row block in phase 3: number j goes to warp j % 16 of the pair
+
+    if (warp == kMoeWarps) {
+        // ---- the stream of weights -------------------------------------------------------------------------------------
+        // Lane w < 8 follows the blocks of consumer warp w: eight places are waited for, and eight copies started, at a time (one
+        // after the other they took 330 cycles a block, 170 ns, where the memory delivers one in 95 ns).
+        const uint32_t bar0 = smem_u32(bars + (lane & (kMoeWarps - 1)) * kMoeDepth), used0 = bar0 + kMoeWarps * kMoeDepth * 8;
+        unsigned char* ring = smem + (lane & (kMoeWarps - 1)) * kMoeDepth * kMoeBlock;
         bool ok = true;
-        auto fill = [&](const unsigned char* row, bool active, int rows, int kc) {      // this lane's row, if it has one
-            ok = __all_sync(0xffffffffu, mbar_wait_bounded(&wempty[slot], phase ^ 1));
-            if (!ok) { if (lane == 0) atomicExch(&g_moe_status, 8); return; }
-            if (lane == 0) mbar_expect_tx(&wfull[slot], (uint32_t)(rows * kc * 2));
-            if (active) bulk_load(ring0 + (uint32_t)(slot * kMoeSlot + lane * kMoePitch), row, (uint32_t)(kc * 2), smem_u32(&wfull[slot]));
-            ++issued;
-            if (++slot == p.slots) { slot = 0; phase ^= 1; }
+        int count = 0;                                    // blocks fetched for the warp so far
+        // The place for the next block of every lane that `has` one; false: a wait ran out
+        auto places = [&](bool has, int& at) {
+            at = count & (kMoeDepth - 1);
+            const uint32_t bar = used0 + at * 8, parity = (uint32_t)(count / kMoeDepth & 1) ^ 1u;
+            uint32_t done = !has;
+            if (has) asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+            if (!__all_sync(0xffffffffu, done)) {
+                if (has) done = wait_long(bar, parity);
+                ok = __all_sync(0xffffffffu, done);
+            }
+            count += has;
+            return ok;
         };
-        for (int u = u0; ok && u < u1; ++u) {
-            const int i = u / nfb, f = (u - i * nfb) * 8 + (lane & 7), g = f / p.gu_half;          // feature, and its strip
-            const unsigned char* row = p.wgu + (int64_t)(ent[i] & 511u) * p.gu_stride +
-                                       (int64_t)(g * p.gu_strip + (f - g * p.gu_half) + (lane >= 8 ? p.gu_half : 0)) * p.H * 2;
-            for (int c = 0; ok && c < nch1; ++c) fill(row + c * kMoeK * 2, lane < 16, 16, min(kMoeK, p.H - c * kMoeK));
-        }
-        for (int b = cta; ok && b < p.blocks; b += ctas) {
-            const int r0 = b * p.rows_per_block, rows = min(p.rows_per_block, p.H - r0);
-            for (int i = 0; ok && i < ents; ++i) {
-                const unsigned char* row = p.wd + (int64_t)(ent[i] & 511u) * p.d_stride + (int64_t)(r0 + lane) * p.I * 2;
-                for (int c = 0; ok && c < nch2; ++c) fill(row + c * kMoeK * 2, lane < rows, rows, min(kMoeK, p.I - c * kMoeK));
+        {
+            int u = u0, kb = lane, i = u0 / nfb, f = u0 - i * nfb, strip = f / p.strip_units, in_strip = f - strip * p.strip_units;
+#pragma unroll 1
+            while (ok) {
+                while (kb >= nb1 && u < u1) {
+                    kb -= nb1; ++u;
+                    if (++in_strip == p.strip_units) { in_strip = 0; ++strip; }
+                    if (++f == nfb) { f = 0; strip = 0; ++i; }
+                }
+                const bool has = lane < kMoeWarps && u < u1;
+                if (!__any_sync(0xffffffffu, has)) break;
+                int at;
+                if (places(has, at) && has) {
+                    mbar_expect_tx(bars + lane * kMoeDepth + at, kMoeBlock);
+                    tma_load_4d(ring + at * kMoeBlock, &map_gu, bars + lane * kMoeDepth + at, kb * kMoeBlockK, in_strip * 16, 2 * strip, (int)(ent[i] & 511u));
+                }
+                kb += kMoeWarps;
             }
         }
-        if (!ok)                                          // given up: the copies in flight land before the CTA may leave
-            for (int i = max(0, issued - p.slots); i < issued; ++i) mbar_wait_bounded(&wfull[i % p.slots], (uint32_t)(i / p.slots) & 1u);
-    } else if (warp == kMoeConsumers + 1) {
-        // ---- h ring -------------------------------------------------------------------------------------------------
-        bool ok = meet(p.flags + ctas, ctas, p.mark, lane);
-        if (!ok && lane == 0) atomicExch(&g_moe_status, 8);
-        if (ok && lane == 0) p.flags[cta] = 0;            // everyone is past the first meeting: its flag is cleared for the next launch
-        asm volatile("fence.proxy.async;" ::: "memory");  // h was written by ordinary stores and is fetched by the copy engine; x was read by ordinary loads
-        __syncwarp();
-        int slot = 0, issued = 0;
-        uint32_t phase = 0;
-        for (int b = cta; ok && b < p.blocks; b += ctas)
-            for (int i = 0; ok && i < ents; ++i) {
-                const uint32_t en = ent[i];
-                const int first = (int)(en >> 9 & 2047u), cnt = (int)(en >> 20);
-                for (int c = 0; ok && c < nch2; ++c) {
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&hempty[slot], phase ^ 1));
-                    if (!ok) { if (lane == 0) atomicExch(&g_moe_status, 8); break; }
-                    const int kc = min(kMoeK, p.I - c * kMoeK);
-                    if (lane == 0) mbar_expect_tx(&hfull[slot], (uint32_t)(cnt * kc * 2));
-                    if (lane < cnt)
-                        bulk_load(hring0 + (uint32_t)((slot * p.group + lane) * kMoePitch), p.h + (int64_t)(first + lane) * p.h_pitch + c * kMoeK * 2, (uint32_t)(kc * 2),
-                                  smem_u32(&hfull[slot]));
-                    ++issued;
-                    if (++slot == p.h_slots) { slot = 0; phase ^= 1; }
+#pragma unroll 1
+        for (int b = cta >> 1; ok && b < p.blocks; b += ctas >> 1) {
+            int j = (cta & 1) * kMoeWarps + lane, kb = j, i = 0;
+#pragma unroll 1
+            while (ok) {
+                const bool has = lane < kMoeWarps && j < per_row_block;
+                if (!__any_sync(0xffffffffu, has)) break;
+                while (kb >= nb2) { kb -= nb2; ++i; }
+                int at;
+                if (places(has, at) && has) {
+                    mbar_expect_tx(bars + lane * kMoeDepth + at, (uint32_t)(p.rows_per_block * 128));
+                    tma_load_3d(ring + at * kMoeBlock, &map_d, bars + lane * kMoeDepth + at, kb * kMoeBlockK, b * p.rows_per_block, (int)(ent[i] & 511u));
+                }
+                j += 2 * kMoeWarps; kb += 2 * kMoeWarps;
+            }
+        }
+        if (!ok && lane == 0) atomicExch(&g_moe_status, 9);
+        // whatever became of the consumers, every copy has landed before the CTA leaves
+        if (lane < kMoeWarps)
+            for (int m = max(0, count - kMoeDepth); m < count; ++m) wait_long(smem_u32(&bars[lane * kMoeDepth + (m & (kMoeDepth - 1))]), (uint32_t)(m / kMoeDepth) & 1u);
+        pair_sync();
+        return;
+    }
+
+    const int g = lane >> 2, q = lane & 3, fr = fragment_row(g);
+    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * kMoeDepth * kMoeBlock), full0 = smem_u32(bars + warp * kMoeDepth);
+    uint32_t slot = 0, parity = 0;
+    bool ok = true;                                       // no wait of this warp has run out
+    // The next block of the ring: wait for it, and give its place back.
+    auto block = [&]() {
+        ok = ok && wait_for(full0 + slot * 8, parity);
+        return ring + slot * kMoeBlock;
+    };
+    auto done_with_block = [&]() {
+        __syncwarp();                                     // every lane has read the block
+        if (lane == 0) mbar_arrive(&bars[(kMoeWarps + warp) * kMoeDepth + slot]);
+        if (++slot == kMoeDepth) { slot = 0; parity ^= 1; }
+    };
+
+    // ---- 2. gate and up ------------------------------------------------------------------------------------------------
+    {
+        float4* red = reinterpret_cast<float4*>(smem + p.at_red);                // [buffer][column group][warp][lane]
+        int i = u0 / nfb, f = u0 - i * nfb, cur = -1, first = 0, cnt = 0, kb = warp;     // kb: this warp's next block of the unit
+        uint32_t xrow[NT];                                // this lane's column of each group: its row of x
+#pragma unroll 1
+        for (int u = u0; u < u1; ++u) {
+            if (i != cur) {
+                first = (int)(ent[i] >> 9 & 1023u); cnt = (int)(ent[i] >> 19); cur = i;
+                if (!p.all_x) {
+                    bar_consumers();
+                    stage_x(cnt, [&](int t) { return pair[first + t].x; });
+                    bar_consumers();
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int col = min(n * 8 + g, cnt - 1);                     // (columns behind the last repeat it; nobody looks at them)
+                    xrow[n] = x0 + (uint32_t)((p.all_x ? pair[first + col].x : col) * p.x_pitch);
                 }
             }
-        if (!ok)
-            for (int i = max(0, issued - p.h_slots); i < issued; ++i) mbar_wait_bounded(&hfull[i % p.h_slots], (uint32_t)(i / p.h_slots) & 1u);
-    } else {
-        const int g = lane >> 2, q = lane & 3;
-        int slot = 0, cur = -1, cols = p.T, nt = (p.T + 7) / 8;      // columns staged (with more than 8 tokens: the entry's)
-        uint32_t phase = 0;
-        bool ok = true;
-        // ---- 2. gate and up -------------------------------------------------------------------------------------------
-        float* red = reinterpret_cast<float*>(smem + p.at_red);                  // [buffer][column group][warp][lane] float4
-        for (int u = u0; ok && u < u1; ++u) {
-            const int i = u / nfb, fb = u - i * nfb, n = u - u0, buf = n & 1;
-            const uint32_t en = ent[i];
-            const int first = (int)(en >> 9 & 2047u), cnt = (int)(en >> 20);
-            if (!fixed_x && i != cur) {                                          // another expert: its tokens' rows of x
-                bar_sync(1, kConsumerThreads);
-                for (int j = threadIdx.x; j < cnt * (p.H / 8); j += kConsumerThreads) {
-                    const int t = j / (p.H / 8), c = j - t * (p.H / 8);
-                    *reinterpret_cast<uint4*>(smem + p.at_region + t * p.x_pitch + c * 16) = __ldg(reinterpret_cast<const uint4*>(p.x + (int64_t)tok[first + t] * p.H) + c);
-                }
-                bar_sync(1, kConsumerThreads);
-                cur = i;
-                cols = cnt;
-                nt = (cnt + 7) / 8;
-            }
-            float acc[NT][4];
+            float gate[NT][4], up[NT][4];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
-            for (int c = 0; ok && c < nch1; ++c) {
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&wfull[slot], phase));
-                if (!ok) break;
-                slot_product<NT>(acc, ring0 + (uint32_t)(slot * kMoeSlot), x0 + (uint32_t)(c * kMoeK * 2), p.x_pitch, min(kMoeK, p.H - c * kMoeK), cols, warp, lane);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&wempty[slot]);
-                if (++slot == p.slots) { slot = 0; phase ^= 1; }
-            }
-            // the warps' partial sums meet in shared memory; the warps take turns in finishing a unit
-            const uint32_t rphase = (uint32_t)(n >> 1) & 1u;
-            ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&rempty[buf], rphase ^ 1));
-            if (!ok) break;
-            float4* out = reinterpret_cast<float4*>(red) + (size_t)buf * NT * kConsumerThreads;
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-                if (j < nt) out[j * kConsumerThreads + warp * 32 + lane] = make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&rfull[buf]);
-            if (warp == (n & (kMoeConsumers - 1))) {
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&rfull[buf], rphase));
-                if (!ok) break;
-                const unsigned long long em = mask[en & 511u];
+                for (int j = 0; j < 4; ++j) gate[n][j] = up[n][j] = 0.0f;
+#pragma unroll 1
+            for (; kb < nb1; kb += kMoeWarps) {
+                const uint32_t w = block();
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    if (j >= nt) break;
-                    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                for (int s = 0; s < 2; ++s) {
+                    const uint4 glo = lds128(w + block_at(fr, s * 4 + q)), ghi = lds128(w + block_at(fr + 8, s * 4 + q));
+                    const uint4 ulo = lds128(w + block_at(fr + 16, s * 4 + q)), uhi = lds128(w + block_at(fr + 24, s * 4 + q));
 #pragma unroll
-                    for (int w = 0; w < kMoeConsumers; ++w) {
-                        const float4 v = out[j * kConsumerThreads + w * 32 + lane];
-                        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-                    }
-                    const float h2[2] = {s.x * logistic(s.x) * s.z, s.y * logistic(s.y) * s.w};
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {                                // gate | up of feature g, columns 2q and 2q + 1
-                        const int col = j * 8 + 2 * q + c;
-                        const bool has = fixed_x ? (col < p.T && (em >> col & 1)) : col < cnt;
-                        const int pair = fixed_x ? first + __popcll(em & ((1ull << col) - 1ull)) : first + col;
-                        if (has) reinterpret_cast<__nv_bfloat16*>(p.h + (int64_t)pair * p.h_pitch)[fb * 8 + g] = __float2bfloat16_rn(h2[c]);
+                    for (int n = 0; n < NT; ++n) {
+                        if (n * 8 >= cnt) break;
+                        const uint4 b = lds128(xrow[n] + (uint32_t)(kb * 128 + s * 64 + q * 16));
+                        mma_16x8x16(gate[n], glo.x, ghi.x, glo.y, ghi.y, b.x, b.y);
+                        mma_16x8x16(up[n], ulo.x, uhi.x, ulo.y, uhi.y, b.x, b.y);
+                        mma_16x8x16(gate[n], glo.z, ghi.z, glo.w, ghi.w, b.z, b.w);
+                        mma_16x8x16(up[n], ulo.z, uhi.z, ulo.w, uhi.w, b.z, b.w);
                     }
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&rempty[buf]);
+                done_with_block();
             }
-        }
-        if (!ok && lane == 0) atomicExch(&g_moe_status, 8);
-        asm volatile("fence.proxy.async;" ::: "memory");
-        bar_sync(1, kConsumerThreads);
-        if (threadIdx.x == 0) { __threadfence(); st_release_u64(p.flags + ctas + cta, p.mark); }
-        // ---- 3. down --------------------------------------------------------------------------------------------------
-        for (int i = threadIdx.x; i < kMoeConsumers * p.T * 16; i += kConsumerThreads) yacc[i] = 0.0f;     // (x is no longer read)
-        bar_sync(1, kConsumerThreads);
-        float* ya = yacc + (size_t)warp * p.T * 16;
-        int hslot = 0;
-        uint32_t hphase = 0;
-        for (int b = cta; b < p.blocks; b += ctas) {
-            const int r0 = b * p.rows_per_block, rows = min(p.rows_per_block, p.H - r0);
-            for (int i = 0; ok && i < ents; ++i) {
-                const uint32_t en = ent[i];
-                const int first = (int)(en >> 9 & 2047u), cnt = (int)(en >> 20), n8 = (cnt + 7) / 8;
-                float acc[NT][4];
+            kb -= nb1;
+            // the warps' partial sums meet in shared memory (two buffers, one barrier a unit) and the warps take turns in
+            // finishing a unit: a buffer is written again only behind the next barrier, which its reader has reached by then
+            const int turn = u - u0;
+            float4* out = red + (size_t)(turn & 1) * 2 * NT * kMoeThreads;
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
-                for (int c = 0; ok && c < nch2; ++c) {
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&wfull[slot], phase) && mbar_wait_bounded(&hfull[hslot], hphase));
-                    if (!ok) break;
-                    slot_product<NT>(acc, ring0 + (uint32_t)(slot * kMoeSlot), hring0 + (uint32_t)(hslot * p.group * kMoePitch), kMoePitch, min(kMoeK, p.I - c * kMoeK), cnt, warp, lane);
-                    __syncwarp();
-                    if (lane == 0) { mbar_arrive(&wempty[slot]); mbar_arrive(&hempty[hslot]); }
-                    if (++slot == p.slots) { slot = 0; phase ^= 1; }
-                    if (++hslot == p.h_slots) { hslot = 0; hphase ^= 1; }
+            for (int n = 0; n < NT; ++n)
+                if (n * 8 < cnt) {
+                    out[2 * n * kMoeThreads + threadIdx.x] = make_float4(gate[n][0], gate[n][1], gate[n][2], gate[n][3]);
+                    out[(2 * n + 1) * kMoeThreads + threadIdx.x] = make_float4(up[n][0], up[n][1], up[n][2], up[n][3]);
                 }
-                // this warp's share of w * (Wd h), into its own sums: a token is in one column of an entry only
+            bar_consumers();
+            if (warp == (turn & (kMoeWarps - 1))) {
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    if (j >= n8) break;
+                for (int n = 0; n < NT; ++n) {
+                    if (n * 8 >= cnt) break;
+                    float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const int col = j * 8 + 2 * q + c;
-                        if (col < cnt) {
-                            float* a = ya + tok[first + col] * 16 + g;
-                            const float w = wt[first + col];
-                            a[0] = fmaf(w, acc[j][c], a[0]);
-                            a[8] = fmaf(w, acc[j][c + 2], a[8]);
+                    for (int w = 0; w < kMoeWarps; ++w) {
+                        const float4 v = out[2 * n * kMoeThreads + w * 32 + lane], z = out[(2 * n + 1) * kMoeThreads + w * 32 + lane];
+                        a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+                        b.x += z.x; b.y += z.y; b.z += z.z; b.w += z.w;
+                    }
+                    // gate and up of features fr (columns 2q and 2q + 1) and fr + 8 (the same columns) of the unit
+                    const int su = f / p.strip_units, in_strip = (f - su * p.strip_units) * 16 + fr;        // (strip, row in its half)
+                    const float h[4] = {a.x * logistic(a.x) * b.x, a.y * logistic(a.y) * b.y, a.z * logistic(a.z) * b.z, a.w * logistic(a.w) * b.w};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int col = n * 8 + 2 * q + (c & 1), feat = su * p.gu_half + in_strip + (c >> 1) * 8;
+                        if (col < cnt && in_strip + (c >> 1) * 8 < p.gu_half) {
+                            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.h + (int64_t)(first + col) * 2 * p.h_pitch) + feat;
+                            const __nv_bfloat16 v = __float2bfloat16_rn(h[c]);
+                            const float rest = h[c] - __bfloat162float(v);
+                            dst[0] = v;
+                            dst[p.h_pitch / 2] = __float2bfloat16_rn(rest == rest ? rest : 0.0f);     // (inf - inf: the value says it all)
                         }
                     }
                 }
-                __syncwarp();                             // (the next entry may hold the same token in another lane's column)
             }
-            if (!ok && lane == 0) atomicExch(&g_moe_status, 8);
-            bar_sync(1, kConsumerThreads);
-            for (int i = threadIdx.x; i < p.T * 16; i += kConsumerThreads) {
-                const int t = i >> 4, r = i & 15;
-                float s = 0.0f;
-#pragma unroll
-                for (int w = 0; w < kMoeConsumers; ++w) { s += yacc[(w * p.T) * 16 + i]; yacc[(w * p.T) * 16 + i] = 0.0f; }
-                if (r < rows) {
-                    const int64_t at = (int64_t)t * p.H + r0 + r;
-                    if (p.residual) s += bf16_lo(p.residual[at]);
-                    reinterpret_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(s);
-                }
-            }
-            bar_sync(1, kConsumerThreads);
+            if (++f == nfb) { f = 0; ++i; }
         }
     }
+    const bool met = meet_second(p);
+    if (cta == 0 && threadIdx.x == 0) p.gate[0] = 0;      // (everyone is past the first meeting)
+
+    // ---- 3. down -------------------------------------------------------------------------------------------------------
+    {
+        for (int i = threadIdx.x; i < kMoeWarps * p.T * kMoeRows; i += kMoeThreads) yacc[i] = 0.0f;   // (x is no longer read)
+        bar_consumers();
+        float* ya = yacc + (size_t)warp * p.T * kMoeRows;
+        constexpr int NH = 2 * NT;                        // column groups of 8: columns 2 j and 2 j + 1 are pair j's value and remainder
+        const unsigned char* hl = p.h + (int64_t)g * p.h_pitch + q * 16;
+        const int64_t hgroup = 8 * p.h_pitch;
+        // This lane's share of h comes straight from the L2, a block ahead (columns behind the entry's last read other pairs' rows, or
+        // the spare rows behind the last pair; nobody looks at them).  The loop is not unrolled: more blocks of h ahead, in registers
+        // of their own, made its code outgrow the instruction cache and took longer.
+        uint4 hn[2][NH];
+        uint32_t en = 0;
+        int turn = 0;                                     // row blocks done
+        auto load_h = [&](uint4 (&to)[2][NH], uint32_t e, int kb) {
+            const unsigned char* src = hl + (int64_t)(e >> 9 & 1023u) * 2 * p.h_pitch + kb * 128;
+#pragma unroll
+            for (int n = 0; n < NH; ++n) {
+                if (n * 4 >= (int)(e >> 19)) break;
+                to[0][n] = __ldcg(reinterpret_cast<const uint4*>(src + n * hgroup));
+                to[1][n] = __ldcg(reinterpret_cast<const uint4*>(src + n * hgroup + 64));
+            }
+        };
+#pragma unroll 1
+        for (int b = met ? cta >> 1 : p.blocks; b < p.blocks; b += ctas >> 1) {
+            const int r0 = b * p.rows_per_block, rows = min(p.rows_per_block, p.H - r0);
+            const int mine = ents * nb2 > warp2 ? (ents * nb2 - 1 - warp2) / (2 * kMoeWarps) + 1 : 0;      // this warp's blocks
+            int i = 0, kb = warp2;                        // the block whose h is loaded next
+            auto step = [&]() {
+                while (kb >= nb2) { kb -= nb2; ++i; }
+                en = ent[i];
+                load_h(hn, en, kb);
+                kb += 2 * kMoeWarps;
+            };
+            if (mine > 0) step();
+#pragma unroll 1
+            for (int j = 0; j < mine; ++j) {
+                {
+                    uint4 h[2][NH];
+#pragma unroll
+                    for (int n = 0; n < NH; ++n) { h[0][n] = hn[0][n]; h[1][n] = hn[1][n]; }
+                    const int cnt = (int)(en >> 19), first = (int)(en >> 9 & 1023u);
+                    if (j + 1 < mine) step();
+                    const uint32_t w = block();
+                    float acc[2][NH][4];
+#pragma unroll
+                    for (int n = 0; n < NH; ++n)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) acc[0][n][c] = acc[1][n][c] = 0.0f;
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            const uint4 lo = lds128(w + block_at(m * 16 + fr, s * 4 + q)), hi = lds128(w + block_at(m * 16 + fr + 8, s * 4 + q));
+#pragma unroll
+                            for (int n = 0; n < NH; ++n) {
+                                if (n * 4 >= cnt) break;
+                                mma_16x8x16(acc[m][n], lo.x, hi.x, lo.y, hi.y, h[s][n].x, h[s][n].y);
+                                mma_16x8x16(acc[m][n], lo.z, hi.z, lo.w, hi.w, h[s][n].z, h[s][n].w);
+                            }
+                        }
+                    done_with_block();
+                    // weight * (this block's share of Wd h) into the warp's own sums: a token is in one column of an entry only
+#pragma unroll
+                    for (int n = 0; n < NH; ++n) {
+                        if (n * 4 >= cnt) break;
+                        if (n * 4 + q < cnt) {
+                            const int2 pr = pair[first + n * 4 + q];
+                            float4* a = reinterpret_cast<float4*>(ya + sum_at(pr.x, fr));
+                            const float wj = __int_as_float(pr.y);
+                            float4 v = *a;
+                            v.x = fmaf(wj, acc[0][n][0] + acc[0][n][1], v.x);
+                            v.y = fmaf(wj, acc[0][n][2] + acc[0][n][3], v.y);
+                            v.z = fmaf(wj, acc[1][n][0] + acc[1][n][1], v.z);
+                            v.w = fmaf(wj, acc[1][n][2] + acc[1][n][3], v.w);
+                            *a = v;
+                        }
+                    }
+                }
+            }
+            // the warps' sums, then the pair's, in this order; CTA 0 of the pair finishes the even tokens, CTA 1 the odd ones
+            bar_consumers();
+            for (int j = threadIdx.x; j < p.T * kMoeRows; j += kMoeThreads) {
+                float s = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kMoeWarps; ++w) s += yacc[w * p.T * kMoeRows + j];
+                yacc[j] = s;
+            }
+            bar_consumers();
+            if (threadIdx.x == 0) tell_other(&pair_bars[0], ~cta & 1);
+            const bool there = wait_other(&pair_bars[0], turn & 1);
+            ok = ok && there;
+            for (int j = threadIdx.x; j < p.T * kMoeRows; j += kMoeThreads) {
+                const int t = j / kMoeRows, r = sum_row(t, j & (kMoeRows - 1));
+                if ((p.T > 1 && (t & 1) != (cta & 1)) || (p.T == 1 && (r & 1) != (cta & 1)) || r >= rows || !there) continue;
+                uint32_t remote;
+                float other;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_u32(&yacc[j])), "r"(~cta & 1));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(other) : "r"(remote) : "memory");
+                float s = cta & 1 ? other + yacc[j] : yacc[j] + other;
+                const int64_t at = (int64_t)t * p.H + r0 + r;
+                if (p.residual) s += bf16_lo(p.residual[at]);
+                reinterpret_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(s);
+            }
+            ++turn;
+            if (b + (ctas >> 1) < p.blocks) {              // another row block: the sums stay until the other CTA has read them
+                bar_consumers();
+                if (threadIdx.x == 0) tell_other(&pair_bars[1], ~cta & 1);
+                ok = wait_other(&pair_bars[1], (turn - 1) & 1) && ok;
+                for (int j = threadIdx.x; j < kMoeWarps * p.T * kMoeRows; j += kMoeThreads) yacc[j] = 0.0f;
+                bar_consumers();
+            }
+        }
+    }
+    if (!ok && lane == 0) atomicExch(&g_moe_status, 9);
+    pair_sync();                                          // (neither CTA leaves while the other may still read its sums)
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 struct MoePlan {
     MoeParams p;
     int nt, ctas;
+    int64_t gu_stride, d_stride;            // bytes from one expert to the next
     size_t smem, ws;
 };
 
@@ -495,47 +735,46 @@ static ccl_status plan_moe(const ccl_moe_desc* d, int sms, MoePlan* plan) {
     MoeParams& p = plan->p;
     p = MoeParams{};
     p.T = (int32_t)d->T; p.H = (int32_t)d->H; p.I = (int32_t)d->I; p.E = d->E; p.topk = d->topk; p.norm = d->norm_topk != 0;
-    p.gu_half = (int32_t)(d->I / d->gu_strips); p.gu_strip = 2 * p.gu_half;
-    p.gu_stride = d->gu_stride_bytes ? d->gu_stride_bytes : gu; p.d_stride = d->d_stride_bytes ? d->d_stride_bytes : dn;
-    plan->ctas = sms;
-    const int64_t per = (d->H + (int64_t)sms * 16 - 1) / ((int64_t)sms * 16);              // row blocks a CTA takes
-    p.rows_per_block = (int32_t)((d->H + sms * per - 1) / (sms * per));
+    p.gu_half = (int32_t)(d->I / d->gu_strips); p.strip_units = (p.gu_half + 15) / 16;
+    plan->gu_stride = d->gu_stride_bytes ? d->gu_stride_bytes : gu; plan->d_stride = d->d_stride_bytes ? d->d_stride_bytes : dn;
+    if (plan->gu_stride >= (INT64_C(1) << 40) || plan->d_stride >= (INT64_C(1) << 40)) return fail(CCL_ERR_UNSUPPORTED, "ccl_moe_tokens: an expert stride is too large for a tensor map");
+    plan->ctas = sms & ~1;                               // CTA pairs
+    const int64_t pr = sms / 2, per = (d->H + pr * kMoeRows - 1) / (pr * kMoeRows);          // row blocks a pair takes
+    p.rows_per_block = (int32_t)((d->H + pr * per - 1) / (pr * per));
     p.blocks = (int32_t)((d->H + p.rows_per_block - 1) / p.rows_per_block);
-    p.x_pitch = (int32_t)(up128((size_t)d->H * 2) + 64);
+    const int64_t nb1 = (d->H + kMoeBlockK - 1) / kMoeBlockK;
+    p.x_pitch = (int32_t)(nb1 * 128 + 64);               // (not a multiple of 128: neighbouring rows start in different banks)
     const int pairs = (int)(d->T * d->topk);
-    // Tokens of an expert taken together.  An expert with more is taken several times, its weights re-read (from the L2, they
-    // were just used); more columns cost shared memory that the ring of weights in flight would have.
-    const int64_t mean = (pairs + d->E - 1) / d->E;
-    for (p.group = d->T <= 8 ? 8 : (mean <= 8 ? 16 : 32);; p.group /= 2) {
-        const size_t yacc = up128((size_t)kMoeConsumers * (size_t)d->T * 16 * 4), hslot = (size_t)p.group * kMoePitch, xs = (size_t)std::min<int64_t>(p.group, d->T) * (size_t)p.x_pitch;
-        const int most = std::min(pairs, d->E) + pairs / p.group;                            // entries
-        size_t at = 0;
+    // Tokens of an expert taken together, in column groups of 8.  An expert with more is taken several times, its weights re-read
+    // (from the L2, they were just used); more columns cost registers, and shared memory for their rows of x.
+    for (plan->nt = d->T <= 8 ? 1 : 2;; plan->nt /= 2) {
+        const size_t red = (size_t)2 * 2 * plan->nt * kMoeThreads * 16, yacc = (size_t)kMoeWarps * (size_t)d->T * kMoeRows * 4;
+        const size_t lists = up128((size_t)2 * kMoeWarps * kMoeDepth * 8 + 32) + up128((size_t)d->E * 8) + up128((size_t)d->E * 2) + up128((size_t)(std::min(pairs, d->E) + pairs) * 4) + up128((size_t)pairs * 8) +
+                             up128((size_t)pairs * 4) + up128((size_t)pairs * 2);
+        const int64_t rows = ((int64_t)kMoeSmem - 1024 - kMoeRing - (int64_t)(red + lists)) / p.x_pitch;        // of x that there is room for
+        p.all_x = d->T <= rows;
+        p.group = (int32_t)std::min<int64_t>(plan->nt * 8, std::min(d->T, rows));
+        if (plan->nt > 1 && p.group <= plan->nt * 4) continue;
+        if (p.group < 1) return fail(CCL_ERR_UNSUPPORTED, "ccl_moe_tokens: this problem does not fit shared memory");
+        size_t at = kMoeRing;
         auto take = [&](size_t bytes) { const size_t a = at; at += up128(bytes); return (int32_t)a; };
-        // (the ring comes first; its size is what the rest leaves)
-        for (p.h_slots = kMoeMaxHSlots; p.h_slots > 2 && yacc + p.h_slots * hslot > xs; --p.h_slots) {}
-        p.at_region = take(std::max(xs, yacc + p.h_slots * hslot));
-        p.at_hring = p.at_region + (int32_t)yacc;
-        p.at_red = take((size_t)2 * (p.group / 8) * kMoeConsumers * 32 * 16);
+        p.at_bars = take((size_t)2 * kMoeWarps * kMoeDepth * 8 + 32);
+        // x and the units' partial sums; phase 3 has its sums where both were
+        p.at_region = take((size_t)(p.all_x ? d->T : p.group) * (size_t)p.x_pitch);
+        p.at_red = take(red);
+        at = std::max(at, (size_t)p.at_region + up128(yacc));
         p.at_mask = take((size_t)d->E * 8);
         p.at_off = take((size_t)d->E * 2);
-        p.at_ent = take((size_t)most * 4);
-        p.at_tok = take((size_t)pairs);
-        p.at_wt = take((size_t)pairs * 4);
+        p.at_ent = take((size_t)(std::min(pairs, d->E) + pairs / p.group) * 4);
         p.at_sel = take((size_t)pairs * 2);
         p.at_selw = take((size_t)pairs * 4);
-        p.at_bars = take((size_t)(2 * kMoeMaxSlots + 2 * kMoeMaxHSlots + 4) * 8 + 16);
-        const size_t room = 227 * 1024;
-        p.slots = at < room ? (int32_t)std::min<size_t>(kMoeMaxSlots, (room - at) / kMoeSlot) : 0;
-        if (p.slots < 4 && p.group > 8) continue;
-        if (p.slots < 2) return fail(CCL_ERR_UNSUPPORTED, "ccl_moe_tokens: this problem does not fit shared memory");
-        const int32_t ring = p.slots * kMoeSlot;
-        for (int32_t* a : {&p.at_region, &p.at_hring, &p.at_red, &p.at_mask, &p.at_off, &p.at_ent, &p.at_tok, &p.at_wt, &p.at_sel, &p.at_selw, &p.at_bars}) *a += ring;
-        plan->smem = at + (size_t)ring;
+        p.at_pair = take((size_t)pairs * 8);
+        plan->smem = at + 1024;                          // (the ring starts at a multiple of 1024)
+        if (plan->smem > kMoeSmem) return fail(CCL_ERR_UNSUPPORTED, "ccl_moe_tokens: this problem does not fit shared memory");
         break;
     }
-    plan->nt = p.group / 8;
     p.h_pitch = (int64_t)up128((size_t)d->I * 2);
-    plan->ws = up128((size_t)(d->T * d->E) * 4) + up128((size_t)sms * 2 * 8) + (size_t)pairs * (size_t)p.h_pitch;
+    plan->ws = up128((size_t)(d->T * d->E) * 4) + up128((size_t)(plan->ctas + 18) * 8) + (size_t)(pairs * 2 + 16 * plan->nt) * (size_t)p.h_pitch;
     return CCL_OK;
 }
 
@@ -547,25 +786,27 @@ static int moe_sms() {
 }
 
 template <int NT>
-static ccl_status launch_moe(const MoePlan& plan, cudaStream_t st) {
+static ccl_status launch_moe(const MoePlan& plan, const CUtensorMap& map_gu, const CUtensorMap& map_d, cudaStream_t st) {
     static std::atomic<uint64_t> configured{0};
     int dev = 0;
     CCL_CUDA_TRY(cudaGetDevice(&dev));
     if (dev >= 64 || !(configured.load() >> dev & 1)) {
-        CCL_CUDA_TRY(cudaFuncSetAttribute(moe_tokens_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
+        CCL_CUDA_TRY(cudaFuncSetAttribute(moe_tokens_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMoeSmem));
         if (dev < 64) configured.fetch_or(1ull << dev);
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)plan.ctas, 1, 1);
-    cfg.blockDim = dim3(kMoeThreads, 1, 1);
+    cfg.blockDim = dim3(kMoeBlockThreads, 1, 1);
     cfg.dynamicSmemBytes = plan.smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeCooperative;         // all CTAs resident at once, or the launch fails
     attr[0].val.cooperative = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, moe_tokens_kernel<NT>, plan.p));
+    cfg.numAttrs = 2;
+    CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, moe_tokens_kernel<NT>, map_gu, map_d, plan.p));
     count_launch();
     return CCL_OK;
 }
@@ -609,20 +850,31 @@ extern "C" ccl_status ccl_moe_tokens(const ccl_moe_desc* d, const void* X_dev, c
     if (ws_bytes < plan.ws) return fail(CCL_ERR_WORKSPACE, "ccl_moe_tokens: needs %zu bytes of workspace (got %zu)", plan.ws, ws_bytes);
     MoeParams& p = plan.p;
     p.x = static_cast<const uint16_t*>(X_dev); p.wr = static_cast<const uint16_t*>(Wr_dev); p.residual = static_cast<const uint16_t*>(residual_dev);
-    p.wgu = static_cast<const unsigned char*>(Wgu_dev); p.wd = static_cast<const unsigned char*>(Wd_dev);
     p.y = static_cast<uint16_t*>(Y_dev); p.ids = ids_dev; p.weights = weights_dev;
     unsigned char* ws = static_cast<unsigned char*>(ws_dev);
     p.logits = reinterpret_cast<float*>(ws);
     p.flags = reinterpret_cast<unsigned long long*>(ws + up128((size_t)p.T * p.E * 4));
-    p.h = ws + up128((size_t)p.T * p.E * 4) + up128((size_t)plan.ctas * 2 * 8);
-    // A mark that no workspace holds yet, whatever its contents.  A launch leaves the first meeting's flags cleared and clears the
-    // second's before the first meeting, so that a replayed CUDA graph may use its mark again.
+    p.gate = p.flags + plan.ctas + 16;                   // (in another line than the flags)
+    p.h = ws + up128((size_t)p.T * p.E * 4) + up128((size_t)(plan.ctas + 18) * 8);
+    // A mark that no workspace holds yet, whatever its contents.  A launch leaves the first meeting's flags and word cleared, so that a
+    // replayed CUDA graph may use its mark again.
     static std::atomic<unsigned long long> next{(unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull};
     do p.mark = next.fetch_add(0x9E3779B97F4A7C15ull); while (p.mark == 0);
+    // gate | up weights as {k, row of a strip's half, half of a strip, expert}: a block is the same 16 rows of a strip's gate and up
+    // half.  Down weights as {k, row, expert}.  Rows and k past the end read as zero.
+    CUtensorMap map_gu, map_d;
+    {
+        const uint64_t H = (uint64_t)p.H, I = (uint64_t)p.I, E = (uint64_t)p.E, half = (uint64_t)p.gu_half;
+        const uint64_t dims[4] = {H, half, 2 * (I / half), E}, strides[3] = {H * 2, half * H * 2, (uint64_t)plan.gu_stride};
+        const uint32_t box[4] = {kMoeBlockK, kMoeRows / 2, 2, 1};
+        if ((s = encode_tmap(&map_gu, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, Wgu_dev, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B))) return s;
+        const uint64_t ddims[3] = {I, H, E}, dstrides[2] = {I * 2, (uint64_t)plan.d_stride};
+        const uint32_t dbox[3] = {kMoeBlockK, (uint32_t)p.rows_per_block, 1};
+        if ((s = encode_tmap(&map_d, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, Wd_dev, ddims, dstrides, dbox, CU_TENSOR_MAP_SWIZZLE_128B))) return s;
+    }
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     switch (plan.nt) {
-        case 1: return launch_moe<1>(plan, st);
-        case 2: return launch_moe<2>(plan, st);
-        default: return launch_moe<4>(plan, st);
+        case 1: return launch_moe<1>(plan, map_gu, map_d, st);
+        default: return launch_moe<2>(plan, map_gu, map_d, st);
     }
 }

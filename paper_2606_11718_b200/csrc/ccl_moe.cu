@@ -25,7 +25,6 @@
 #include <algorithm>
 #include <atomic>
 #include <chrono>
-#include <type_traits>
 
 #include "ccl_act.cuh"
 #include "ccl_tma.h"
@@ -54,7 +53,8 @@ struct MoeParams {
     float* weights;
     float* logits;                          // workspace: [T][E]
     unsigned long long* flags;              // workspace: a flag per CTA (first meeting)
-    unsigned long long* gate;               // workspace: the word that ends the first meeting, the counter of the second
+    unsigned long long* gate;               // workspace: the word that ends the first meeting, the counters of the others
+    int2* choice;                           // workspace: [T][topk] expert, weight (more than 8 tokens)
     unsigned char* h;                       // workspace: [pairs][2 (value, remainder)][h_pitch bytes] bf16
     int64_t h_pitch;
     unsigned long long mark;                // this launch's mark in the flags
@@ -109,7 +109,7 @@ __device__ __forceinline__ void st_release(unsigned long long* p, unsigned long 
 // The grid's meetings (all consumer threads call; what a CTA wrote before is seen by all behind it).  Measured, 148 CTAs: 1.3 us
 // when every CTA adds to one counter and one thread of each reads it; 4.9 us when 148 threads of every CTA read a flag of each.
 // The counter needs a start, so the first meeting has flags -- any contents but this launch's mark mean "not yet" -- that CTA 0 alone
-// reads, and a word by which it lets the others go; it clears the counter of the second on the way.
+// reads, and a word by which it lets the others go; it clears the counters of the later ones on the way.
 __device__ __forceinline__ bool meet_first(const MoeParams& p) {
     bar_consumers();
     bool ok = true;
@@ -118,7 +118,7 @@ __device__ __forceinline__ bool meet_first(const MoeParams& p) {
 #pragma unroll 1
         for (unsigned i = threadIdx.x; i < gridDim.x; i += kMoeThreads) ok = wait_word(p.flags + i, p.mark, true) && ok;
         ok = bar_consumers_and(ok);
-        if (threadIdx.x == 0 && ok) { p.gate[1] = 0; st_release(p.gate, p.mark); }
+        if (threadIdx.x == 0 && ok) { p.gate[1] = p.gate[2] = 0; st_release(p.gate, p.mark); }
     } else {
         if (threadIdx.x == 0) ok = wait_word(p.gate, p.mark, true);
         ok = bar_consumers_and(ok);
@@ -126,12 +126,12 @@ __device__ __forceinline__ bool meet_first(const MoeParams& p) {
     if (!ok && threadIdx.x == 0) atomicExch(&g_moe_status, 8);
     return ok;
 }
-__device__ __forceinline__ bool meet_second(const MoeParams& p) {
+__device__ __forceinline__ bool meet_counted(unsigned long long* counter) {
     bar_consumers();
     bool ok = true;
     if (threadIdx.x == 0) {
-        asm volatile("red.release.gpu.global.add.u64 [%0], 1;" ::"l"(p.gate + 1) : "memory");
-        ok = wait_word(p.gate + 1, gridDim.x, false);
+        asm volatile("red.release.gpu.global.add.u64 [%0], 1;" ::"l"(counter) : "memory");
+        ok = wait_word(counter, gridDim.x, false);
         if (!ok) atomicExch(&g_moe_status, 8);
     }
     return bar_consumers_and(ok);
@@ -159,10 +159,10 @@ __device__ __noinline__ bool wait_other(uint64_t* bar, uint32_t parity) {
     }
 }
 
-// Order-preserving integer image of a float; NaN below every number, 0 is left for "taken".
+// Order-preserving integer image of a float; NaN below every number, 0 for no number at all.
 __device__ __forceinline__ uint32_t order_key(float f) {
     if (f != f) return 1u;
-    const uint32_t u = __float_as_uint(f);
+    const uint32_t u = __float_as_uint(f == 0.0f ? 0.0f : f);        // (-0 and 0 are equal)
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
@@ -178,93 +178,6 @@ __device__ __forceinline__ int fragment_row(int g) { return (g & 1) << 2 | g >> 
 // product's columns meet in different banks.  Offset of the four, and the row of place `at` of a token's 32.
 __device__ __forceinline__ int sum_at(int t, int r) { return t * kMoeRows + ((r ^ (t & 7)) << 2); }
 __device__ __forceinline__ int sum_row(int t, int at) { return ((at >> 2) ^ (t & 7)) + (at & 3) * 8; }
-
-// The topk largest of one token's E logits, by one warp.  Every lane keeps V >= E / 32 of them (experts lane, lane + 32, ...);
-// lane k < topk gets the k-th choice.  SORTED: the lane's few are put in order first, so that a choice is one maximum over the
-// lanes' heads and the winner moves up by one; with many a lane the winner looks through all of its own again.
-struct Choice { int expert; float weight; };
-template <int V, bool SORTED, int TB>
-__device__ __forceinline__ void choose(const MoeParams& p, const float (&l)[TB][V], Choice (&c)[TB], int lane) {
-    uint32_t key[TB][V], mine[TB], first[TB];             // images of the logits; of the one this lane keeps; of the largest
-    int place[TB][V];                                     // (the lane's j-th: expert lane + 32 j)
-    bool nan[TB];
-#pragma unroll
-    for (int b = 0; b < TB; ++b) {
-        nan[b] = false;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            key[b][j] = lane + 32 * j < p.E ? order_key(l[b][j]) : 0u;
-            place[b][j] = j;
-            nan[b] |= l[b][j] != l[b][j];
-        }
-        nan[b] = __any_sync(0xffffffffu, nan[b]);
-        if (SORTED) {                                     // largest first, the lower expert first among equals
-#pragma unroll
-            for (int a = 0; a < V - 1; ++a)
-#pragma unroll
-                for (int j = V - 2; j >= a; --j) {
-                    const bool swap = key[b][j + 1] > key[b][j];
-                    const uint32_t k = swap ? key[b][j + 1] : key[b][j];
-                    const int q = swap ? place[b][j + 1] : place[b][j];
-                    if (swap) { key[b][j + 1] = key[b][j]; place[b][j + 1] = place[b][j]; }
-                    key[b][j] = k; place[b][j] = q;
-                }
-        }
-        c[b].expert = 0; mine[b] = first[b] = 0u;
-    }
-#pragma unroll 1
-    for (int k = 0; k < p.topk; ++k) {
-        uint32_t best[TB], top[TB];
-        int at[TB];
-#pragma unroll
-        for (int b = 0; b < TB; ++b) {
-            best[b] = key[b][0]; at[b] = place[b][0];
-            if (!SORTED) {
-#pragma unroll
-                for (int j = 1; j < V; ++j)
-                    if (key[b][j] > best[b]) { best[b] = key[b][j]; at[b] = j; }
-            }
-            top[b] = __reduce_max_sync(0xffffffffu, best[b]);
-        }
-#pragma unroll
-        for (int b = 0; b < TB; ++b) {
-            unsigned who = __ballot_sync(0xffffffffu, best[b] == top[b]);
-            if (who & (who - 1u)) {                       // equal logits in several lanes: the lowest expert
-                const uint32_t e = __reduce_min_sync(0xffffffffu, best[b] == top[b] ? (uint32_t)(lane + 32 * at[b]) : 0xffffffffu);
-                who = 1u << (e & 31u);
-            }
-            const int from = __ffs(who) - 1, e = __shfl_sync(0xffffffffu, lane + 32 * at[b], from);
-            if (k == 0) first[b] = top[b];
-            if (lane == k) { mine[b] = top[b]; c[b].expert = e; }
-            const bool out = lane == from;
-            if (SORTED) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    key[b][j] = out ? (j + 1 < V ? key[b][j + 1] : 0u) : key[b][j];
-                    place[b][j] = out && j + 1 < V ? place[b][j + 1] : place[b][j];
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) if (out && j == at[b]) key[b][j] = 0u;
-            }
-        }
-    }
-#pragma unroll
-    for (int b = 0; b < TB; ++b) {
-        const float top = key_value(first[b]);
-        float sum = 0.0f, w = 0.0f;
-        if (lane < p.topk) w = __expf(key_value(mine[b]) - top);
-        if (p.norm) sum = w;
-        else {
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (lane + 32 * j < p.E) sum += __expf(l[b][j] - top);
-        }
-#pragma unroll
-        for (int m = 16; m >= 1; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-        c[b].weight = nan[b] ? __int_as_float(0x7fffffff) : w / sum;
-    }
-}
 
 // NT: most column groups of 8 an expert's tokens are taken in
 template <int NT>
@@ -356,38 +269,80 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
             *reinterpret_cast<uint4*>(p.h + (int64_t)r * p.h_pitch + c * 16) = make_uint4(0u, 0u, 0u, 0u);
         }
     }
-    const bool met1 = meet_first(p);
+    bool met1 = meet_first(p);
     if (threadIdx.x == 0) { shared[1] = met1; p.flags[cta] = 0; }        // (cleared for the next launch, which may be this one replayed)
-    // top-k, a warp per token; with many of them four at a time, whose chains of dependent steps (a choice waits for the one before)
-    // overlap
-    auto top_k = [&](auto v, auto sorted, auto tb) {
-        constexpr int V = decltype(v)::value, TB = decltype(tb)::value;
-#pragma unroll 1
-        for (int t0 = met1 ? warp * TB : p.T; t0 < p.T; t0 += kMoeWarps * TB) {
-            float l[TB][V];
-            Choice ch[TB];
+    // top-k of a token: an expert's place is the number of those before it (a larger logit, or an equal one of a lower expert), a
+    // thread an expert against all of them in shared memory.  Up to 8 tokens are worked out by every CTA for itself; of more, each
+    // by one CTA, and the grid meets once more: 64 tokens x 128 experts took 10 us the first way, a warp a token.
+    {
+        const bool every = p.T <= 8;
+        const int first = every ? 0 : cta, nt = !met1 ? 0 : (every ? p.T : (cta < p.T ? 1 : 0)), ep = (p.E + 3) / 4 * 4;     // tokens at hand
+        uint32_t* keys = reinterpret_cast<uint32_t*>(smem + p.at_red);           // [token][ep]
+        float* vals = reinterpret_cast<float*>(keys + nt * ep);                  // [token][16]: the chosen logits, best first
+        int* who = reinterpret_cast<int*>(vals + nt * kMoeMaxK);                 // ... and their experts
+        for (int i = threadIdx.x; i < nt * ep; i += kMoeThreads) {
+            const int t = i / ep, e = i - t * ep;
+            keys[i] = e < p.E ? order_key(__ldcg(p.logits + (int64_t)(first + t) * p.E + e)) : 0u;
+        }
+        bar_consumers();
+        for (int i = threadIdx.x; i < nt * p.E; i += kMoeThreads) {
+            const int t = i / p.E, e = i - t * p.E;
+            const uint32_t* kt = keys + t * ep;
+            const uint32_t k = kt[e];
+            int place[4] = {0, 0, 0, 0};
+#pragma unroll 4
+            for (int o = 0; o < p.E; o += 4) {
+                const uint4 v = *reinterpret_cast<const uint4*>(kt + o);
+                place[0] += v.x >= (o < e ? k : k + 1u); place[1] += v.y >= (o + 1 < e ? k : k + 1u);
+                place[2] += v.z >= (o + 2 < e ? k : k + 1u); place[3] += v.w >= (o + 3 < e ? k : k + 1u);
+            }
+            const int at = place[0] + place[1] + place[2] + place[3];
+            if (at < p.topk) { vals[t * kMoeMaxK + at] = key_value(k); who[t * kMoeMaxK + at] = e; }
+        }
+        bar_consumers();
+        if (warp < nt) {
+            const int t = first + warp;
+            keys += warp * ep; vals += warp * kMoeMaxK; who += warp * kMoeMaxK;
+            {
+                const float top = vals[0];
+                float sum = 0.0f, w = 0.0f;
+                bool nan = false;
+                if (lane < p.topk) w = __expf(vals[lane] - top);
+                for (int e = lane; e < p.E; e += 32) {
+                    nan |= keys[e] == 1u;
+                    if (!p.norm) sum += __expf(key_value(keys[e]) - top);
+                }
+                if (p.norm) sum = w;
 #pragma unroll
-            for (int b = 0; b < TB; ++b)
-#pragma unroll
-                for (int j = 0; j < V; ++j) l[b][j] = t0 + b < p.T && lane + 32 * j < p.E ? __ldcg(p.logits + (int64_t)(t0 + b) * p.E + lane + 32 * j) : 0.0f;
-            choose<V, decltype(sorted)::value, TB>(p, l, ch, lane);
-#pragma unroll
-            for (int b = 0; b < TB; ++b)
-                if (t0 + b < p.T && lane < p.topk) {
-                    const int at = (t0 + b) * p.topk + lane, e = ch[b].expert;
-                    sel[at] = (uint16_t)e;
-                    selw[at] = ch[b].weight;
-                    atomicOr(reinterpret_cast<uint32_t*>(mask + e) + ((t0 + b) >> 5), 1u << ((t0 + b) & 31));   // (in whatever order the bits arrive; 64-bit ones are emulated)
-                    if (cta == 0) {
+                for (int m = 16; m >= 1; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+                nan = __any_sync(0xffffffffu, nan);
+                if (lane < p.topk) {
+                    const int at = t * p.topk + lane, e = who[lane];
+                    w = nan ? __int_as_float(0x7fffffff) : w / sum;
+                    if (every) {
+                        sel[at] = (uint16_t)e;
+                        selw[at] = w;
+                        atomicOr(reinterpret_cast<uint32_t*>(mask + e), 1u << t);    // (in whatever order the bits arrive; 64-bit ones are emulated)
+                    } else p.choice[at] = make_int2(e, __float_as_int(w));
+                    if (!every || cta == 0) {
                         if (p.ids) p.ids[at] = e;
-                        if (p.weights) p.weights[at] = ch[b].weight;
+                        if (p.weights) p.weights[at] = w;
                     }
                 }
+            }
         }
-    };
-    if (p.E > 128) top_k(std::integral_constant<int, (int)(kMoeMaxE / 32)>(), std::false_type(), std::integral_constant<int, 1>());
-    else if (p.T <= 8) top_k(std::integral_constant<int, 4>(), std::true_type(), std::integral_constant<int, 1>());
-    else top_k(std::integral_constant<int, 4>(), std::true_type(), std::integral_constant<int, 4>());
+        if (!every) {
+            met1 = met1 && meet_counted(p.gate + 2);
+            if (threadIdx.x == 0) shared[1] = met1;
+            for (int i = threadIdx.x; met1 && i < pairs; i += kMoeThreads) {
+                const int2 c = __ldcg(p.choice + i);
+                const int t = i / p.topk;
+                sel[i] = (uint16_t)c.x;
+                selw[i] = __int_as_float(c.y);
+                atomicOr(reinterpret_cast<uint32_t*>(mask + c.x) + (t >> 5), 1u << (t & 31));
+            }
+        }
+    }
     bar_consumers();
     // pairs sorted by expert, then token: every expert's first one; entries of at most `group` pairs of one expert
     if (warp == 0) {
@@ -588,7 +543,7 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
             if (++f == nfb) { f = 0; ++i; }
         }
     }
-    const bool met = meet_second(p);
+    const bool met = meet_counted(p.gate + 1);
     if (cta == 0 && threadIdx.x == 0) p.gate[0] = 0;      // (everyone is past the first meeting)
 
     // ---- 3. down -------------------------------------------------------------------------------------------------------
@@ -748,7 +703,8 @@ static ccl_status plan_moe(const ccl_moe_desc* d, int sms, MoePlan* plan) {
     // Tokens of an expert taken together, in column groups of 8.  An expert with more is taken several times, its weights re-read
     // (from the L2, they were just used); more columns cost registers, and shared memory for their rows of x.
     for (plan->nt = d->T <= 8 ? 1 : 2;; plan->nt /= 2) {
-        const size_t red = (size_t)2 * 2 * plan->nt * kMoeThreads * 16, yacc = (size_t)kMoeWarps * (size_t)d->T * kMoeRows * 4;
+        const size_t keys = (size_t)(d->T <= 8 ? d->T : 1) * (size_t)((d->E + 3) / 4 * 16 + kMoeMaxK * 8);   // the top-k's
+        const size_t red = std::max((size_t)2 * 2 * plan->nt * kMoeThreads * 16, up128(keys)), yacc = (size_t)kMoeWarps * (size_t)d->T * kMoeRows * 4;
         const size_t lists = up128((size_t)2 * kMoeWarps * kMoeDepth * 8 + 32) + up128((size_t)d->E * 8) + up128((size_t)d->E * 2) + up128((size_t)(std::min(pairs, d->E) + pairs) * 4) + up128((size_t)pairs * 8) +
                              up128((size_t)pairs * 4) + up128((size_t)pairs * 2);
         const int64_t rows = ((int64_t)kMoeSmem - 1024 - kMoeRing - (int64_t)(red + lists)) / p.x_pitch;        // of x that there is room for
@@ -774,7 +730,7 @@ static ccl_status plan_moe(const ccl_moe_desc* d, int sms, MoePlan* plan) {
         break;
     }
     p.h_pitch = (int64_t)up128((size_t)d->I * 2);
-    plan->ws = up128((size_t)(d->T * d->E) * 4) + up128((size_t)(plan->ctas + 18) * 8) + (size_t)(pairs * 2 + 16 * plan->nt) * (size_t)p.h_pitch;
+    plan->ws = up128((size_t)(d->T * d->E) * 4) + up128((size_t)(plan->ctas + 32 + pairs) * 8) + (size_t)(pairs * 2 + 16 * plan->nt) * (size_t)p.h_pitch;
     return CCL_OK;
 }
 
@@ -855,7 +811,8 @@ extern "C" ccl_status ccl_moe_tokens(const ccl_moe_desc* d, const void* X_dev, c
     p.logits = reinterpret_cast<float*>(ws);
     p.flags = reinterpret_cast<unsigned long long*>(ws + up128((size_t)p.T * p.E * 4));
     p.gate = p.flags + plan.ctas + 16;                   // (in another line than the flags)
-    p.h = ws + up128((size_t)p.T * p.E * 4) + up128((size_t)(plan.ctas + 18) * 8);
+    p.choice = reinterpret_cast<int2*>(p.gate + 16);
+    p.h = ws + up128((size_t)p.T * p.E * 4) + up128((size_t)(plan.ctas + 32 + p.T * p.topk) * 8);
     // A mark that no workspace holds yet, whatever its contents.  A launch leaves the first meeting's flags and word cleared, so that a
     // replayed CUDA graph may use its mark again.
     static std::atomic<unsigned long long> next{(unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull};

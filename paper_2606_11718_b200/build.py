@@ -22,15 +22,31 @@ def _stale():
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    """Compiles the sources side by side (one object each) and links them into libccl.so."""
     if not force and not _stale():
         return LIB
-    cmd = [NVCC, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
-           "-Xcompiler", "-fPIC,-Wall", "-x", "cu", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           "-cudart", "static", "-o", LIB]
+    objdir = os.path.join(HERE, "build")
+    os.makedirs(objdir, exist_ok=True)
+    flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC,-Wall", "-x", "cu",
+             "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     if verbose:
-        cmd += ["-Xptxas", "-v"]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    subprocess.run(cmd, check=True)
+        flags += ["-Xptxas", "-v"]
+    headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))] + [os.path.join(ROOT, "include", "ccl.h")]
+    newest = max(os.path.getmtime(h) for h in headers)
+    objects, running = [], []
+    for src in SOURCES:
+        path, obj = os.path.join(CSRC, src), os.path.join(objdir, src + ".o")
+        objects.append(obj)
+        if force or not os.path.exists(obj) or os.path.getmtime(obj) < max(newest, os.path.getmtime(path)):
+            cmd = [NVCC] + flags + ["-c", path, "-o", obj]
+            running.append((cmd, obj, subprocess.Popen(cmd)))
+    failed = [(p.returncode, cmd, obj) for cmd, obj, p in running if p.wait()]
+    for rc, cmd, obj in failed:
+        if os.path.exists(obj):
+            os.remove(obj)
+    if failed:
+        raise subprocess.CalledProcessError(failed[0][0], failed[0][1])
+    subprocess.run([NVCC, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-cudart", "static", "-o", LIB] + objects, check=True)
     return LIB
 
 

@@ -9,41 +9,117 @@
 
 namespace ccl {
 
-// What is computed and how exactly.  The logistic function s(t) = 1 / (1 + exp(-t)) is taken with the hardware's exponential and
+// Two fp32 values in one 64-bit register: sm_100 multiplies and adds such pairs in one instruction.  Under a GEMM that runs at the
+// power limit an epilogue costs what its instructions cost in energy, whether or not there is time for them (measured,
+// 4096 x 8192 x 2048: the clock falls from 1.5 to 1.25 GHz behind gelu's slope): about 0.8 us an instruction a value there.
+struct f32x2 { uint64_t v; };
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ f32x2 both(float x) { return pair(x, x); }
+__device__ __forceinline__ void split(f32x2 a, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
+__device__ __forceinline__ f32x2 operator*(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ f32x2 operator+(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ float exp2_fast(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float rcp_fast(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ f32x2 exp2_fast(f32x2 a) { float x, y; split(a, x, y); return pair(exp2_fast(x), exp2_fast(y)); }
+__device__ __forceinline__ f32x2 rcp_fast(f32x2 a) { float x, y; split(a, x, y); return pair(rcp_fast(x), rcp_fast(y)); }
+
+// What is computed and how exactly.  The logistic function s(t) = 1 / (1 + 2^(-t log2 e)) is taken with the hardware's exponential and
 // reciprocal (a few units of 2^-22): every result below is rounded to bf16 (2^-9) or summed in fp32.
 //   relu       max(z, 0), NaN kept           slope 1 for z > 0, 0 for z <= 0
 //   gelu_tanh  z/2 (1 + tanh(t/2)) = z s(t), t = 2 sqrt(2/pi) (z + 0.044715 z^3)    slope s + z s (1 - s) dt/dz
-//   gelu_erf   z/2 (1 + erf(z/sqrt 2))       slope of that: 1/2 (1 + erf(z/sqrt 2)) + z exp(-z^2/2) / sqrt(2 pi)
+//   gelu_erf   z P(z), P(z) = 1/2 (1 + erf(z/sqrt 2))                                slope P + z exp(-z^2/2) / sqrt(2 pi)
 //   silu       z s(z)                        slope s (1 + z (1 - s))
-// The product form z s(t) costs one exponential and one reciprocal where tanh takes several steps.
-__device__ __forceinline__ float logistic(float t) { return __fdividef(1.0f, 1.0f + __expf(-t)); }
+// The product form z s(t) costs one exponential and one reciprocal where tanh takes several steps.  P(z) is formula 7.1.26 of Abramowitz
+// and Stegun, Handbook of Mathematical Functions (C. Hastings): for x >= 0, erf(x) = 1 - (a1 k + ... + a5 k^5) exp(-x^2) with
+// k = 1 / (1 + 0.3275911 x), off by at most 1.5e-7; its exponential is the slope's as well.
+__device__ __forceinline__ float logistic(float t) { return rcp_fast(1.0f + exp2_fast(t * -1.4426950408889634f)); }
 
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGeluA = 1.5957691216057308f;            // 2 sqrt(2 / pi)
 constexpr float kGeluB = 0.044715f;
 
+// 1 - P(|z|) and exp(-z^2 / 2)
+__device__ __forceinline__ f32x2 normal_tail(f32x2 z, f32x2& density) {
+    float x, y;
+    split(z, x, y);
+    const f32x2 k = rcp_fast(fma2(pair(fabsf(x), fabsf(y)), both(0.3275911f * 0.70710678118654752f), both(1.0f)));
+    density = exp2_fast(z * (z * both(-0.5f * kLog2e)));
+    f32x2 p = fma2(k, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+    p = fma2(k, p, both(0.5f * 1.421413741f));
+    p = fma2(k, p, both(0.5f * -0.284496736f));
+    p = fma2(k, p, both(0.5f * 0.254829592f));
+    return k * p * density;
+}
+// P(z) from the tail on z's side
+__device__ __forceinline__ f32x2 normal_cdf(f32x2 z, f32x2 tail) {
+    float x, y, a, b;
+    split(z, x, y);
+    split(tail, a, b);
+    return pair(x < 0.0f ? a : 1.0f - a, y < 0.0f ? b : 1.0f - b);
+}
+
 template <int ACT>
-__device__ __forceinline__ float act_value(float z) {
-    if (ACT == CCL_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (ACT == CCL_ACT_GELU_TANH) return z * logistic(kGeluA * z * fmaf(kGeluB * z, z, 1.0f));
-    if (ACT == CCL_ACT_GELU_ERF) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    if (ACT == CCL_ACT_SILU) return z * logistic(z);
+__device__ __forceinline__ f32x2 act_value(f32x2 z) {
+    if (ACT == CCL_ACT_RELU) {
+        float x, y;
+        split(z, x, y);
+        return pair(x < 0.0f ? 0.0f : x, y < 0.0f ? 0.0f : y);
+    }
+    if (ACT == CCL_ACT_GELU_TANH) {                      // (z^2 = infinity leaves s at 0 or 1)
+        const f32x2 e = exp2_fast(z * fma2(z * z, both(-kLog2e * kGeluA * kGeluB), both(-kLog2e * kGeluA)));
+        return z * rcp_fast(e + both(1.0f));
+    }
+    if (ACT == CCL_ACT_GELU_ERF) {
+        f32x2 d;
+        const f32x2 tail = normal_tail(z, d);
+        return z * normal_cdf(z, tail);
+    }
+    if (ACT == CCL_ACT_SILU) return z * rcp_fast(exp2_fast(z * both(-kLog2e)) + both(1.0f));
     return z;
 }
+// The slope at two values of z given as a bf16 pair
 template <int ACT>
-__device__ __forceinline__ float act_slope(float z) {
-    if (ACT == CCL_ACT_RELU) return z <= 0.0f ? 0.0f : 1.0f;
+__device__ __forceinline__ f32x2 act_slope(uint32_t zz) {
     if (ACT == CCL_ACT_GELU_TANH) {
-        const float s = logistic(kGeluA * z * fmaf(kGeluB * z, z, 1.0f));
-        const float c = fminf(fmaxf(z, -12.0f), 12.0f);  // s (1 - s) is 0 in fp32 beyond that, and z^2 must not reach infinity: 0 * inf
-        return fmaf(c * s * (1.0f - s), kGeluA * fmaf(3.0f * kGeluB * c, c, 1.0f), s);
+        // beyond 12 the slope is 0 or 1 in fp32, and z^2 must not reach infinity: 0 * inf (NaN passes both limits)
+        asm("min.NaN.bf16x2 %0, %0, %1;" : "+r"(zz) : "r"(0x41404140u));
+        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(zz) : "r"(0xC140C140u));
     }
-    if (ACT == CCL_ACT_GELU_ERF)
-        return fmaf(z * 0.39894228040143268f, __expf(-0.5f * z * z), 0.5f * (1.0f + erff(z * 0.70710678118654752f)));
+    const float x = __uint_as_float(zz << 16), y = __uint_as_float(zz & 0xFFFF0000u);
+    const f32x2 z = pair(x, y);
+    if (ACT == CCL_ACT_RELU) return pair(x <= 0.0f ? 0.0f : 1.0f, y <= 0.0f ? 0.0f : 1.0f);
+    if (ACT == CCL_ACT_GELU_TANH) {
+        const f32x2 q = z * z, e = exp2_fast(z * fma2(q, both(-kLog2e * kGeluA * kGeluB), both(-kLog2e * kGeluA)));
+        const f32x2 s = rcp_fast(e + both(1.0f)), dt = fma2(q, both(3.0f * kGeluA * kGeluB), both(kGeluA));
+        return fma2(fma2(s * both(-1.0f), s, s), z * dt, s);
+    }
+    if (ACT == CCL_ACT_GELU_ERF) {
+        f32x2 d;
+        const f32x2 tail = normal_tail(z, d);
+        return fma2(z * both(0.39894228040143268f), d, normal_cdf(z, tail));
+    }
     if (ACT == CCL_ACT_SILU) {
-        const float s = logistic(z);
-        return s * fmaf(z, 1.0f - s, 1.0f);
+        const f32x2 s = rcp_fast(exp2_fast(z * both(-kLog2e)) + both(1.0f));
+        return s * fma2(z, fma2(s, both(-1.0f), both(1.0f)), both(1.0f));
     }
-    return 1.0f;
+    return both(1.0f);
 }
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
@@ -52,40 +128,41 @@ __device__ __forceinline__ uint32_t bf16_pack(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ void bf16x8_unpack(const uint4& w, float (&v)[8]) {
-    v[0] = bf16_lo(w.x); v[1] = bf16_hi(w.x); v[2] = bf16_lo(w.y); v[3] = bf16_hi(w.y);
-    v[4] = bf16_lo(w.z); v[5] = bf16_hi(w.z); v[6] = bf16_lo(w.w); v[7] = bf16_hi(w.w);
+__device__ __forceinline__ uint32_t bf16_pack(f32x2 a) {
+    float x, y;
+    split(a, x, y);
+    return bf16_pack(x, y);
 }
-__device__ __forceinline__ uint4 bf16x8_pack(const float (&v)[8]) {
-    return make_uint4(bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]), bf16_pack(v[4], v[5]), bf16_pack(v[6], v[7]));
+__device__ __forceinline__ f32x2 bf16_unpack(uint32_t w) { return pair(bf16_lo(w), bf16_hi(w)); }
+__device__ __forceinline__ uint4 bf16x8_pack(const f32x2* v) { return make_uint4(bf16_pack(v[0]), bf16_pack(v[1]), bf16_pack(v[2]), bf16_pack(v[3])); }
+
+// v <- act(v), v <- v * act'(z) for 2 N values; the branch is the same for the whole launch
+template <int N>
+__device__ __forceinline__ void act_pairs(int act, f32x2 (&v)[N]) {
+#define CCL_ACT_N(A) case A: _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = act_value<A>(v[i]); break
+    switch (act) { CCL_ACT_N(CCL_ACT_RELU); CCL_ACT_N(CCL_ACT_GELU_TANH); CCL_ACT_N(CCL_ACT_GELU_ERF); CCL_ACT_N(CCL_ACT_SILU); default: break; }
+#undef CCL_ACT_N
+}
+template <int N>
+__device__ __forceinline__ void slope_pairs(int act, f32x2 (&v)[N], const uint32_t (&z)[N]) {
+#define CCL_ACT_N(A) case A: _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = v[i] * act_slope<A>(z[i]); break
+    switch (act) { CCL_ACT_N(CCL_ACT_RELU); CCL_ACT_N(CCL_ACT_GELU_TANH); CCL_ACT_N(CCL_ACT_GELU_ERF); CCL_ACT_N(CCL_ACT_SILU); default: break; }
+#undef CCL_ACT_N
 }
 
-// v <- act(v); the branch is the same for the whole launch
-__device__ __forceinline__ void act8(int act, float (&v)[8]) {
-#define CCL_ACT8(A) case A: _Pragma("unroll") for (int i = 0; i < 8; ++i) v[i] = act_value<A>(v[i]); break
-    switch (act) { CCL_ACT8(CCL_ACT_RELU); CCL_ACT8(CCL_ACT_GELU_TANH); CCL_ACT8(CCL_ACT_GELU_ERF); CCL_ACT8(CCL_ACT_SILU); default: break; }
-#undef CCL_ACT8
-}
-// v <- v * act'(z)
-__device__ __forceinline__ void slope8(int act, float (&v)[8], const float (&z)[8]) {
-#define CCL_ACT8(A) case A: _Pragma("unroll") for (int i = 0; i < 8; ++i) v[i] *= act_slope<A>(z[i]); break
-    switch (act) { CCL_ACT8(CCL_ACT_RELU); CCL_ACT8(CCL_ACT_GELU_TANH); CCL_ACT8(CCL_ACT_GELU_ERF); CCL_ACT8(CCL_ACT_SILU); default: break; }
-#undef CCL_ACT8
-}
-
-// Column sums of a warp's 32 rows (one per lane) over 2 W columns: halves are exchanged with the lane across and added, W
-// steps in all instead of 5 for each column.  Afterwards lane L holds the sums of columns (2 W / 32) L ... of the 2 W, for
-// 2 W = 64: columns 2 L and 2 L + 1, in v[0] and v[1].  The order of the additions is fixed.
-__device__ __forceinline__ void column_sums64(float (&v)[64], int lane) {
+// Sums of 16 columns over a warp's 32 rows (one per lane): halves are exchanged with the lane across and added, 16 exchanges in
+// all instead of 5 for each column.  Every lane ends up with the sum of column lane / 2.  The order of the additions is fixed.
+__device__ __forceinline__ float column_sums16(float (&v)[16], int lane) {
 #pragma unroll
-    for (int w = 32; w >= 2; w >>= 1) {
-        const bool up = lane & (w >> 1);
+    for (int w = 8; w >= 1; w >>= 1) {
+        const bool up = lane & (w << 1);
 #pragma unroll
         for (int i = 0; i < w; ++i) {
             const float send = up ? v[i] : v[i + w], keep = up ? v[i + w] : v[i];
-            v[i] = keep + __shfl_xor_sync(0xffffffffu, send, w >> 1);
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, send, w << 1);
         }
     }
+    return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 1);
 }
 // The same for 8 columns: every lane ends up with the sum of column lane / 4.
 __device__ __forceinline__ float column_sums8(float (&v)[8], int lane) {

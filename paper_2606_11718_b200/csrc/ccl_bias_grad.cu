@@ -21,11 +21,13 @@ struct BiasGradParams {
     int64_t rows_per_cta;
 };
 
+// A thread's columns of a row as bf16 pairs (VEC = 1: one value, the other zero)
 template <int VEC>
-__device__ __forceinline__ void load_cols(const uint16_t* p, float (&v)[VEC]) {
+__device__ __forceinline__ void load_cols(const uint16_t* p, uint32_t (&v)[(VEC + 1) / 2]) {
     if constexpr (VEC == 8) {
-        bf16x8_unpack(*reinterpret_cast<const uint4*>(p), v);
-    } else v[0] = bf16_lo(*p);
+        const uint4 w = *reinterpret_cast<const uint4*>(p);
+        v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+    } else v[0] = *p;
 }
 
 // VEC: columns of a thread: 8 (16-byte accesses) or 1.  LINEAR: a column strip's rows follow each other at one pitch (row-major
@@ -39,9 +41,10 @@ __global__ void __launch_bounds__(kBiasThreads) bias_act_grad_kernel(const BiasG
     const int L = p.lanes, R = kBiasThreads / L, lx = threadIdx.x & (L - 1), ly = threadIdx.x / L;
     const int64_t tile = blockIdx.x / ctas, col = (tile * L + lx) * VEC;
     const bool col_ok = col < p.v.cols;
-    float sum[VEC];
+    constexpr int PR = (VEC + 1) / 2;
+    f32x2 sum2[PR];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) sum[i] = 0.0f;
+    for (int i = 0; i < PR; ++i) sum2[i] = both(0.0f);
     if (col_ok) {
         const int64_t r1 = min(p.v.rows, (int64_t)(rank + 1) * p.rows_per_cta);
         int64_t r = (int64_t)rank * p.rows_per_cta + ly;
@@ -50,7 +53,7 @@ __global__ void __launch_bounds__(kBiasThreads) bias_act_grad_kernel(const BiasG
         // U rows at a time: their loads are all in flight before the first is used
         constexpr int U = 4;
         for (; r < r1; r += (int64_t)U * R) {
-            float g[U][VEC], z[U][VEC];
+            uint32_t g[U][PR], z[U][PR];
             int64_t off[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -62,20 +65,25 @@ __global__ void __launch_bounds__(kBiasThreads) bias_act_grad_kernel(const BiasG
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (r + (int64_t)u * R >= r1) break;
+                f32x2 d[PR];
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    if (ACT != CCL_ACT_NONE) g[u][i] *= act_slope<ACT>(z[u][i]);
-                    sum[i] += g[u][i];
+                for (int i = 0; i < PR; ++i) {
+                    d[i] = bf16_unpack(g[u][i]);
+                    if (ACT != CCL_ACT_NONE) d[i] = d[i] * act_slope<ACT>(z[u][i]);
+                    sum2[i] = sum2[i] + d[i];
                 }
                 if (p.dz) {
-                    if constexpr (VEC == 8) *reinterpret_cast<uint4*>(p.dz + off[u]) = bf16x8_pack(g[u]);
-                    else p.dz[off[u]] = (uint16_t)bf16_pack(g[u][0], 0.0f);
+                    if constexpr (VEC == 8) *reinterpret_cast<uint4*>(p.dz + off[u]) = bf16x8_pack(d);
+                    else p.dz[off[u]] = (uint16_t)bf16_pack(d[0]);
                 }
             }
         }
     }
     if (!p.dbias) return;                                // (the same for every CTA)
     const int cols = L * VEC;
+    float sum[2 * PR];
+#pragma unroll
+    for (int i = 0; i < PR; ++i) split(sum2[i], sum[2 * i], sum[2 * i + 1]);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) part[ly * cols + lx * VEC + i] = sum[i];
     __syncthreads();

@@ -66,7 +66,7 @@ static ccl_status launch(const GemmPlan& plan, const CUtensorMap& ma, const CUte
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.numAttrs = 2;
     }
-    CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, ccl_gemm_kernel<BN, CTAS, SWIGLU, RAG, FULL, KS>, ma, mb, mc, plan.ma2, plan.mb2, plan.mc2, plan.p));
+    CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, ccl_gemm_kernel<BN, CTAS, SWIGLU, RAG, FULL, KS>, ma, mb, mc, plan.ma2, plan.mb2, plan.mc2, plan.p, EpiMaps<0>{}));
     count_launch();
     return CCL_OK;
 }

@@ -10,18 +10,18 @@
 namespace ccl {
 
 template <int BN, int CTAS, bool FULL, int KS, int EPI>
-static ccl_status launch_epi(const GemmPlan& plan, const CUtensorMap* maps, cudaStream_t st) {
+static ccl_status launch_epi(const GemmPlan& plan, const CUtensorMap* maps, const EpiMaps<EPI>& em, cudaStream_t st) {
     auto kernel = ccl_gemm_kernel<BN, CTAS, false, 0, FULL, KS, EPI>;
     static std::atomic<uint64_t> configured{0};                 // bit per device: the shared-memory limit has been raised
     int dev = 0;
     CCL_CUDA_TRY(cudaGetDevice(&dev));
     if (dev >= 64 || !(configured.load() >> dev & 1)) {
-        CCL_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmemBudget + kEpiBytes + 2048)));
+        CCL_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmemBudgetOp + kEpiBytesOp + 2048)));
         if (dev < 64) configured.fetch_or(1ull << dev);
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(plan.grid, 1, 1);
-    cfg.blockDim = dim3(kGemmThreads, 1, 1);
+    cfg.blockDim = dim3(gemm_threads<EPI>, 1, 1);
     cfg.dynamicSmemBytes = plan.smem_bytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -35,39 +35,39 @@ static ccl_status launch_epi(const GemmPlan& plan, const CUtensorMap* maps, cuda
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.numAttrs = 2;
     }
-    CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], plan.p));
+    CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], plan.p, em));
     count_launch();
     return CCL_OK;
 }
 
 template <int EPI>
-static ccl_status launch_variant(const GemmPlan& plan, const CUtensorMap* maps, cudaStream_t st) {
+static ccl_status launch_variant(const GemmPlan& plan, const CUtensorMap* maps, const EpiMaps<EPI>& em, cudaStream_t st) {
     if (plan.ks) {
         switch (plan.bn * 10 + plan.ks) {
-            case 2562: return launch_epi<256, 1, false, 2, EPI>(plan, maps, st);
-            case 2564: return launch_epi<256, 1, false, 4, EPI>(plan, maps, st);
-            case 2568: return launch_epi<256, 1, false, 8, EPI>(plan, maps, st);
-            case 1922: return launch_epi<192, 1, false, 2, EPI>(plan, maps, st);
-            case 1924: return launch_epi<192, 1, false, 4, EPI>(plan, maps, st);
-            case 1928: return launch_epi<192, 1, false, 8, EPI>(plan, maps, st);
-            case 1282: return launch_epi<128, 1, false, 2, EPI>(plan, maps, st);
-            case 1284: return launch_epi<128, 1, false, 4, EPI>(plan, maps, st);
-            default: return launch_epi<128, 1, false, 8, EPI>(plan, maps, st);
+            case 2562: return launch_epi<256, 1, false, 2, EPI>(plan, maps, em, st);
+            case 2564: return launch_epi<256, 1, false, 4, EPI>(plan, maps, em, st);
+            case 2568: return launch_epi<256, 1, false, 8, EPI>(plan, maps, em, st);
+            case 1922: return launch_epi<192, 1, false, 2, EPI>(plan, maps, em, st);
+            case 1924: return launch_epi<192, 1, false, 4, EPI>(plan, maps, em, st);
+            case 1928: return launch_epi<192, 1, false, 8, EPI>(plan, maps, em, st);
+            case 1282: return launch_epi<128, 1, false, 2, EPI>(plan, maps, em, st);
+            case 1284: return launch_epi<128, 1, false, 4, EPI>(plan, maps, em, st);
+            default: return launch_epi<128, 1, false, 8, EPI>(plan, maps, em, st);
         }
     }
     if (!plan.lean) {                                           // (make_plan offers these two widths only)
-        if (plan.ctas == 2) return plan.bn == 256 ? launch_epi<256, 2, true, 0, EPI>(plan, maps, st) : launch_epi<128, 2, true, 0, EPI>(plan, maps, st);
-        return plan.bn == 256 ? launch_epi<256, 1, true, 0, EPI>(plan, maps, st) : launch_epi<128, 1, true, 0, EPI>(plan, maps, st);
+        if (plan.ctas == 2) return plan.bn == 256 ? launch_epi<256, 2, true, 0, EPI>(plan, maps, em, st) : launch_epi<128, 2, true, 0, EPI>(plan, maps, em, st);
+        return plan.bn == 256 ? launch_epi<256, 1, true, 0, EPI>(plan, maps, em, st) : launch_epi<128, 1, true, 0, EPI>(plan, maps, em, st);
     }
     switch (plan.bn * 10 + plan.ctas) {
-        case 5122: return launch_epi<512, 2, false, 0, EPI>(plan, maps, st);
-        case 3842: return launch_epi<384, 2, false, 0, EPI>(plan, maps, st);
-        case 2562: return launch_epi<256, 2, false, 0, EPI>(plan, maps, st);
-        case 1922: return launch_epi<192, 2, false, 0, EPI>(plan, maps, st);
-        case 1282: return launch_epi<128, 2, false, 0, EPI>(plan, maps, st);
-        case 2561: return launch_epi<256, 1, false, 0, EPI>(plan, maps, st);
-        case 1921: return launch_epi<192, 1, false, 0, EPI>(plan, maps, st);
-        default: return launch_epi<128, 1, false, 0, EPI>(plan, maps, st);
+        case 5122: return launch_epi<512, 2, false, 0, EPI>(plan, maps, em, st);
+        case 3842: return launch_epi<384, 2, false, 0, EPI>(plan, maps, em, st);
+        case 2562: return launch_epi<256, 2, false, 0, EPI>(plan, maps, em, st);
+        case 1922: return launch_epi<192, 2, false, 0, EPI>(plan, maps, em, st);
+        case 1282: return launch_epi<128, 2, false, 0, EPI>(plan, maps, em, st);
+        case 2561: return launch_epi<256, 1, false, 0, EPI>(plan, maps, em, st);
+        case 1921: return launch_epi<192, 1, false, 0, EPI>(plan, maps, em, st);
+        default: return launch_epi<128, 1, false, 0, EPI>(plan, maps, em, st);
     }
 }
 
@@ -203,6 +203,23 @@ int64_t row_blocks(const GemmPlan& plan) {
 }
 size_t partial_sums_at(const GemmPlan& plan) { return (plan.ws_bytes + 255) & ~(size_t)255; }
 
+// A matrix laid out like C, in C's boxes: its map, and that of its last strip
+ccl_status encode_like_c(const GemmPlan& plan, const void* base, CUtensorMap* m, CUtensorMap* m2) {
+    ccl_status s = operand_tmap(m, plan.vc, base, 64, 32, 1, 0);
+    if (s) return s;
+    *m2 = *m;
+    return ragged(plan.vc) ? operand_tmap(m2, plan.vc, base, 64, 32, 1, 0, true) : CCL_OK;
+}
+
+template <int EPI>
+ccl_status launch_with_maps(const GemmPlan& plan, const CUtensorMap* maps, cudaStream_t st) {
+    EpiMaps<EPI> em;
+    ccl_status s;
+    std::memset(&em, 0, sizeof(em));
+    if (plan.p.addend && (s = encode_like_c(plan, plan.p.addend, &em.addend, &em.addend2))) return s;
+    return launch_variant<EPI>(plan, maps, em, st);
+}
+
 ccl_status encode_maps(const GemmPlan& plan, const void* A, const void* B, void* C, CUtensorMap* m) {
     const GemmParams& p = plan.p;
     const uint32_t bnh = plan.bn == 384 ? 64u : (uint32_t)(plan.subn / plan.ctas);   // B rows of one K-major box
@@ -248,11 +265,12 @@ ccl_status run_epi(const char* who, int epi, const ccl_gemm_desc* d, int act, co
     p.ws = static_cast<float*>(ws);
     p.act = act;
     p.bias = static_cast<const uint16_t*>(bias);
-    p.addend = static_cast<const uint16_t*>(addend);
+    p.addend = epi == 2 && act == CCL_ACT_NONE ? nullptr : static_cast<const uint16_t*>(addend);
     p.preact = static_cast<uint16_t*>(preact);
+    p.addend_tma = p.c.il_mode != 3;
     p.colsum = dbias ? reinterpret_cast<float*>(static_cast<char*>(ws) + sums_at) : nullptr;
     if ((s = wave_barrier(plan, true, st))) return s;
-    if ((s = epi == 1 ? launch_variant<1>(plan, maps, st) : launch_variant<2>(plan, maps, st))) return s;
+    if ((s = epi == 1 ? launch_with_maps<1>(plan, maps, st) : launch_with_maps<2>(plan, maps, st))) return s;
     if (p.splits > 1) {
         const dim3 grid((unsigned)((p.N + 63) / 64), (unsigned)((p.M + 31) / 32));
         if (epi == 1) splitk_epilogue_kernel<1><<<grid, 256, 0, st>>>(p);

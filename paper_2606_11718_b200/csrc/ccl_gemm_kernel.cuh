@@ -27,10 +27,18 @@ constexpr int BK = 64;
 #endif
 constexpr int kEpiWarps = CCL_EPI_WARPS;        // 4, or 8: two warps per TMEM lane quadrant taking alternate 64-column pieces
 constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
+// The kernels with an operator in the epilogue (EPI != 0) drain with sixteen warps, one 64-column piece of a 256-wide tile each:
+// their arithmetic -- an exponential, a reciprocal and some twenty instructions a value -- has the time of the next tile's product,
+// and what eight warps lost was latency (4096 x 8192 x 2048 with gelu's slope: 140 us with eight, 94 for the plain product).
+constexpr int kEpiOpWarps = 16;
+template <int EPI> constexpr int epi_warps = EPI ? kEpiOpWarps : kEpiWarps;
+template <int EPI> constexpr int gemm_threads = 64 + 32 * epi_warps<EPI>;
 constexpr int kTmemCols = 512;
 constexpr uint32_t kSmemBudget = 192 * 1024;    // ring of operand stages
 constexpr int64_t kRaggedDense = 4096;         // problems of a ragged batch whose tile prefix is kept in shared memory
 constexpr uint32_t kEpiBytes = 4 * 2 * 32 * 128; // epilogue staging: per warp two buffers of 32 rows x 128 B
+constexpr uint32_t kSmemBudgetOp = 160 * 1024;  // EPI: a shorter ring,
+constexpr uint32_t kEpiBytesOp = kEpiOpWarps * 32 * 128;       // and a buffer for each of the sixteen warps, in which an addend's piece becomes C's
 
 static __device__ int g_gemm_status = 0;
 
@@ -146,7 +154,12 @@ struct GemmParams {
     const uint16_t* addend;         // EPI 1: the residual or NULL; EPI 2: the pre-activation Z
     uint16_t* preact;               // EPI 1: receives the pre-activation, or NULL
     float* colsum;                  // EPI 2: partial column sums [row blocks][N] fp32, or NULL
+    int32_t addend_tma;             // the addend comes by TMA, a piece ahead (else by ordinary loads: see line_of())
 };
+
+// Tensor maps of the epilogue operators: the addend (residual / Z), boxes as C's, and its last strip where that differs
+template <int EPI> struct EpiMaps { CUtensorMap addend, addend2; };
+template <> struct EpiMaps<0> {};
 
 // ---- PTX wrappers ---------------------------------------------------------------------------
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -270,6 +283,13 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
           "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr) : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
 // 16-byte global store under a predicate, without a branch: the epilogue's TMEM loads and waits are warp-wide
 // (.sync.aligned) and must never be reached by a warp that the compiler has split by a per-lane row test.
 __device__ __forceinline__ void st_global_v4_if(void* ptr, uint4 v, bool pred) {
@@ -287,6 +307,9 @@ __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.
 // The loaded registers only hold their values once the wait above has run, but to the compiler they were defined by
 // the load statement: nothing stops it from moving an instruction that reads them above the wait.  Passing them
 // through an (empty) volatile statement placed after the wait makes every later use depend on that statement.
+__device__ __forceinline__ void tmem_regs_ready(uint32_t (&r)[16]) {
+    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
 __device__ __forceinline__ void tmem_regs_ready(uint32_t (&r)[64]) {
     asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
     asm volatile("" : "+r"(r[32]), "+r"(r[33]), "+r"(r[34]), "+r"(r[35]), "+r"(r[36]), "+r"(r[37]), "+r"(r[38]), "+r"(r[39]), "+r"(r[40]), "+r"(r[41]), "+r"(r[42]), "+r"(r[43]), "+r"(r[44]), "+r"(r[45]), "+r"(r[46]), "+r"(r[47]), "+r"(r[48]), "+r"(r[49]), "+r"(r[50]), "+r"(r[51]), "+r"(r[52]), "+r"(r[53]), "+r"(r[54]), "+r"(r[55]), "+r"(r[56]), "+r"(r[57]), "+r"(r[58]), "+r"(r[59]), "+r"(r[60]), "+r"(r[61]), "+r"(r[62]), "+r"(r[63]));
@@ -356,32 +379,34 @@ __device__ __forceinline__ int64_t c_offset(const GemmParams& p, int64_t m, int6
 // `ok` off: nothing is stored and, for EPI 2, v becomes zero (it goes into column sums).
 template <int EPI>
 __device__ __forceinline__ void epilogue8(const GemmParams& p, float (&v)[8], int64_t off, int n, bool ok) {
-    float x[8];
+    f32x2 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pair(v[2 * i], v[2 * i + 1]);
     if (EPI == 1) {
         if (p.bias) {
-            bf16x8_unpack(ld_global_v4_if(p.bias + n, ok), x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += x[i];
+            const uint4 b = ld_global_v4_if(p.bias + n, ok);
+            w[0] = w[0] + bf16_unpack(b.x); w[1] = w[1] + bf16_unpack(b.y); w[2] = w[2] + bf16_unpack(b.z); w[3] = w[3] + bf16_unpack(b.w);
         }
-        if (p.preact) st_global_v4_if(p.preact + off, bf16x8_pack(v), ok);
-        act8(p.act, v);
+        if (p.preact) st_global_v4_if(p.preact + off, bf16x8_pack(w), ok);
+        act_pairs(p.act, w);
         if (p.addend) {
-            bf16x8_unpack(ld_global_v4_if(p.addend + off, ok), x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += x[i];
+            const uint4 x = ld_global_v4_if(p.addend + off, ok);
+            w[0] = w[0] + bf16_unpack(x.x); w[1] = w[1] + bf16_unpack(x.y); w[2] = w[2] + bf16_unpack(x.z); w[3] = w[3] + bf16_unpack(x.w);
         }
     }
-    if (EPI == 2) {
-        if (p.act != CCL_ACT_NONE) {
-            bf16x8_unpack(ld_global_v4_if(p.addend + off, ok), x);
-            slope8(p.act, v, x);
-        }
-        if (!ok) {
+    if (EPI == 2 && p.act != CCL_ACT_NONE) {
+        const uint4 x = ld_global_v4_if(p.addend + off, ok);
+        const uint32_t z[4] = {x.x, x.y, x.z, x.w};
+        slope_pairs(p.act, w, z);
+    }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-        }
+    for (int i = 0; i < 4; ++i) split(w[i], v[2 * i], v[2 * i + 1]);
+    if (EPI == 2 && !ok) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
     }
 }
+__device__ __forceinline__ uint4 bf16x8_pack(const float (&v)[8]) { return make_uint4(bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]), bf16_pack(v[4], v[5]), bf16_pack(v[6], v[7])); }
 
 // Ragged K: first row, k blocks and rows of the last block of problem e (an empty or out-of-range problem: one block of
 // zero rows, so that its output is written as zeros).
@@ -549,11 +574,11 @@ struct Scheduler {
 // EPI: 1 = bias, activation and residual in the epilogue (ccl_gemm_epilogue), 2 = activation slope and column sums
 // (ccl_gemm_act_grad)
 template <int BN, int CTAS, bool SWIGLU = false, int RAG = 0, bool FULL = true, int KS = 0, int EPI = 0>
-__global__ void __launch_bounds__(kGemmThreads, 1)
+__global__ void __launch_bounds__(gemm_threads<EPI>, 1)
 ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                 const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_a2,
                 const __grid_constant__ CUtensorMap map_b2, const __grid_constant__ CUtensorMap map_c2,
-                const __grid_constant__ GemmParams gp) {
+                const __grid_constant__ GemmParams gp, const __grid_constant__ EpiMaps<EPI> em) {
     // map_a2 / map_b2 / map_c2: the last strip of an operand whose strips are not all alike (OpMap::rag); copies of the
     // first three otherwise
     // The parameters are read from shared memory: the threads fetch the block's words side by side, so
@@ -564,7 +589,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         static_assert(sizeof(GemmParams) % 4 == 0, "GemmParams is copied word by word");
         const uint32_t* src = reinterpret_cast<const uint32_t*>(&gp);
         uint32_t* dst = reinterpret_cast<uint32_t*>(&p);
-        for (int i = threadIdx.x; i < (int)(sizeof(GemmParams) / 4); i += kGemmThreads) dst[i] = src[i];
+        for (int i = threadIdx.x; i < (int)(sizeof(GemmParams) / 4); i += gemm_threads<EPI>) dst[i] = src[i];
     }
     // A tile wider than 256 columns is computed as two sub-tiles (one MMA each per k step), the first 256 columns wide,
     // the second the rest (256 or 128), each with a 256-column half of TMEM; narrower tiles use the two halves as a
@@ -587,12 +612,13 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     unsigned char* epi = smem + (size_t)gp.stages * gp.stage_bytes;     // 1024-byte aligned: stage sizes are multiples of 1 KB
-    uint64_t* bars = reinterpret_cast<uint64_t*>(epi + kEpiBytes);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(epi + (EPI ? kEpiBytesOp : kEpiBytes));
     uint64_t* full = bars;                           // used in the leader CTA only
     uint64_t* empty = bars + gp.stages;               // one set per CTA
     uint64_t* tmem_full = bars + 2 * gp.stages;       // one set per CTA
     uint64_t* tmem_empty = tmem_full + 4;            // used in the leader CTA only
-    uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(tmem_empty + 4);
+    uint64_t* addend_full = tmem_empty + 4;          // EPI: one per epilogue warp
+    uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(addend_full + (EPI ? kEpiOpWarps : 0));
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0;
@@ -605,7 +631,9 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         prefetch_tmap(&map_b);
         prefetch_tmap(&map_c);
         for (int s = 0; s < gp.stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int a = 0; a < NACC; ++a) { mbar_init(&tmem_full[a], 1); mbar_init(&tmem_empty[a], kEpiWarps * CTAS); }
+        for (int a = 0; a < NACC; ++a) { mbar_init(&tmem_full[a], 1); mbar_init(&tmem_empty[a], epi_warps<EPI> * CTAS); }
+        if constexpr (EPI != 0)
+            for (int w = 0; w < kEpiOpWarps; ++w) mbar_init(&addend_full[w], 1);
         fence_barrier_init();
     }
     if (warp == 1) tmem_alloc<CTAS>(tmem_ptr, kTmemCols);
@@ -863,7 +891,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         // ------------------------------------------------------------------ epilogue (warps 2..5)
         if (RAG == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
         const int quad = warp & 3;                       // TMEM lane quadrant this warp may read
-        constexpr int EW = kEpiWarps / 4;                // warps per quadrant
+        constexpr int EW = epi_warps<EPI> / 4;         // warps per quadrant
         const int hf = (warp - 2) >> 2;                  // which of them this one is
         const uint32_t tmem_empty0 = CTAS == 2 ? map_to_cta(smem_u32(&tmem_empty[0]), 0) : smem_u32(&tmem_empty[0]);
         TileCoord t;
@@ -872,6 +900,42 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         int done = 0;                                    // tiles drained so far
         TileCoord pend[2];                               // balanced split: shares written but not yet reduced
         int npend = 0;
+        // EPI: the addend's part of this warp's next piece (32 rows x 64 columns) is fetched into the warp's buffer as soon as the
+        // piece before has been stored from it; the cursor `ap` runs one piece ahead, into the next tile.
+        constexpr bool kOp = EPI != 0 && KS == 0;
+        unsigned char* op_buf = epi + (size_t)(warp - 2) * (32 * 128);
+        uint32_t addend_phase = 0;
+        [[maybe_unused]] struct { int it, h, c; bool ok, out; TileCoord t; } ap = {};       // out: a fetch is under way
+        auto fetch_addend = [&]() {
+            if constexpr (kOp) {
+                while (ap.ok) {                          // the next piece that exists
+                    const int n0 = ap.t.n0 + ap.h * SUBN;
+                    if (!ap.t.skip && ap.h < NSUB && ap.c < ((ap.h == 0 ? SUBN : SUBN1) / 64) && n0 + ap.c * 64 < ap.t.n1) break;
+                    if (!ap.t.skip && ap.h + 1 < NSUB) { ++ap.h; ap.c = hf; continue; }
+                    ap.h = 0; ap.c = hf;
+                    ap.ok = sched.template get<RAG, FULL>(++ap.it, ap.t);
+                }
+                if (!ap.ok) return;
+                if (lane == 0) {
+                    const int r = ap.t.m0 + (int)rank * BM + quad * 32, n = ap.t.n0 + ap.h * SUBN + ap.c * 64;
+                    int x, y, z, u;
+                    to_coords<FULL>(p.c, r, n, x, y, z, u);
+                    const CUtensorMap* map = &em.addend;
+                    if (FULL && p.c.rag && z == p.c.nstrips - 1) { map = &em.addend2; z = 0; }
+                    mbar_expect_tx(&addend_full[warp - 2], 32 * 128);
+                    tma_load_5d(op_buf, map, &addend_full[warp - 2], x, y, z, u, 0);
+                }
+                ap.c += EW;
+                ap.out = true;
+            }
+        };
+        const bool addend_ahead = kOp && p.addend && p.addend_tma && p.splits == 1;
+        if constexpr (kOp)
+            if (addend_ahead) {
+                ap.it = 0; ap.h = 0; ap.c = hf;
+                ap.ok = sched.template get<RAG, FULL>(0, ap.t);
+                fetch_addend();
+            }
         for (int it = 0; alive && sched.template get<RAG, FULL>(it, t); ++it) {
           if (t.skip) continue;
           const int tile_no = done++;
@@ -889,7 +953,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 alive = false; break;
             }
             tc_fence_after();
-            const bool bal = RAG == 0 && !SWIGLU && p.bal;
+            const bool bal = RAG == 0 && EPI == 0 && !SWIGLU && p.bal;
             bool released = false;                                 // the accumulator has been handed back already
             const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * ACC_COLS);
             // Full 32-row x 64-column pieces go through shared memory (128-byte swizzle) and a TMA tile store
@@ -975,36 +1039,119 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     }
                 }
             };
-            // EPI: this lane's 64 accumulators through the epilogue, 8 columns at a time, and the piece's column sums into
-            // the row block's line of the partial sums (block = the 32 rows of this warp in this tile)
-            auto epilogue_piece = [&](uint32_t (&r)[64], int c) {
+            // EPI: a 64-column piece through the epilogue, 16 columns at a time.  The loop is not unrolled: eight times 8 columns of
+            // straight-line arithmetic (30 KB of code) ran at the speed of the instruction fetch, 84 us of 175 on 4096 x 8192 x 2048
+            // with gelu's slope.  The next 16 accumulators are on their way while these are worked on; the addend's next piece
+            // as soon as this one has been read.
+            auto epilogue_piece = [&](int c) {
                 const int n64 = nb + c * 64;
                 const bool row_ok = m < t.m1;
+                const bool full = rows_full && n64 + 64 <= t.n1 && !(FULL && p.c.il_mode == 3);
                 const int64_t off = c_offset<FULL>(p, min(m, t.m1 - 1), n64);
-                float v[64];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    float (&v8)[8] = *reinterpret_cast<float(*)[8]>(&v[8 * j]);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v8[i] = __uint_as_float(r[8 * j + i]);
-                    epilogue8<EPI>(p, v8, off + 8 * j, n64 + 8 * j, row_ok && n64 + 8 * j < t.n1);
-                }
-                uint32_t pk[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) pk[i] = bf16_pack(v[2 * i], v[2 * i + 1]);
-                store_packed(pk, c);
+                if (addend_ahead) {
+                    if (!mbar_wait_bounded(&addend_full[warp - 2], addend_phase) && lane == 0) atomicExch(&g_gemm_status, 4);
+                    addend_phase ^= 1;
+                    ap.out = false;
+                } else if (full) { if (lane == 0) tma_store_wait_read<0>(); __syncwarp(); }       // the buffer's last piece has been stored
+                int64_t blk = 0;
                 if (EPI == 2 && p.colsum) {
-                    column_sums64(v, lane);
                     int sm, jm;
                     p.fd_wm.divmod(t.m0, sm, jm);
-                    const int64_t blk = ((int64_t)sm * p.tps_m + jm / (BM * CTAS)) * (4 * CTAS) + rank * 4 + quad;
-                    if (n64 + 2 * lane < t.n1)           // (n1 - n64 is a multiple of 8)
-                        *reinterpret_cast<float2*>(p.colsum + blk * p.N + n64 + 2 * lane) = make_float2(v[0], v[1]);
+                    blk = ((int64_t)sm * p.tps_m + jm / (BM * CTAS)) * (4 * CTAS) + rank * 4 + quad;
+                }
+                uint32_t nx[16];
+                tmem_ld16(taddr + (uint32_t)(c * 64), nx);
+#pragma unroll 1
+                for (int q = 0; q < 4; ++q) {
+                    const int n16 = n64 + q * 16;
+                    const bool ok0 = row_ok && n16 < t.n1, ok1 = row_ok && n16 + 8 < t.n1;
+                    uint4 x0 = make_uint4(0u, 0u, 0u, 0u), x1 = x0, b0 = x0, b1 = x0;
+                    if (addend_ahead) {
+                        x0 = *reinterpret_cast<const uint4*>(op_buf + lane * 128 + (((2 * q) ^ (lane & 7)) << 4));
+                        x1 = *reinterpret_cast<const uint4*>(op_buf + lane * 128 + (((2 * q + 1) ^ (lane & 7)) << 4));
+                    } else if (p.addend) {
+                        x0 = ld_global_v4_if(p.addend + off + q * 16, ok0);
+                        x1 = ld_global_v4_if(p.addend + off + q * 16 + 8, ok1);
+                    }
+                    if (EPI == 1 && p.bias) {
+                        b0 = ld_global_v4_if(p.bias + n16, n16 < t.n1);
+                        b1 = ld_global_v4_if(p.bias + n16 + 8, n16 + 8 < t.n1);
+                    }
+                    tmem_ld_wait();
+                    tmem_regs_ready(nx);
+                    f32x2 v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = pair(__uint_as_float(nx[2 * i]), __uint_as_float(nx[2 * i + 1]));
+                    tmem_ld16(taddr + (uint32_t)(c * 64 + min(q + 1, 3) * 16), nx);       // (the last one again: no branch around a warp-wide load)
+                    const int u0 = lane * 128 + (((2 * q) ^ (lane & 7)) << 4), u1 = lane * 128 + (((2 * q + 1) ^ (lane & 7)) << 4);
+                    const uint32_t x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+                    if (EPI == 1) {
+                        if (p.bias) {
+                            const uint32_t b[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) v[i] = v[i] + bf16_unpack(b[i]);
+                        }
+                        if (p.preact) {
+                            st_global_v4_if(p.preact + off + q * 16, bf16x8_pack(v), ok0);
+                            st_global_v4_if(p.preact + off + q * 16 + 8, bf16x8_pack(v + 4), ok1);
+                        }
+                        act_pairs(p.act, v);
+                        if (p.addend) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) v[i] = v[i] + bf16_unpack(x[i]);
+                        }
+                    } else {
+                        if (p.act != CCL_ACT_NONE) slope_pairs(p.act, v, x);
+                        if (!rows_full && !row_ok) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) v[i] = both(0.0f);
+                        }
+                    }
+                    const uint4 o0 = bf16x8_pack(v), o1 = bf16x8_pack(v + 4);
+                    if (full) {
+                        *reinterpret_cast<uint4*>(op_buf + u0) = o0;
+                        *reinterpret_cast<uint4*>(op_buf + u1) = o1;
+                    } else { st_global_v4_if(p.C + off + q * 16, o0, ok0); st_global_v4_if(p.C + off + q * 16 + 8, o1, ok1); }
+                    if (EPI == 2 && p.colsum) {
+                        float f[16];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) split(v[i], f[2 * i], f[2 * i + 1]);
+                        const float sum = column_sums16(f, lane);
+                        if ((lane & 1) == 0 && n16 + (lane >> 1) < t.n1) p.colsum[blk * p.N + n16 + (lane >> 1)] = sum;
+                    }
+                }
+                tmem_ld_wait();
+                tmem_regs_ready(nx);
+                if (full) {
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        int cx = cx0 + c * 64, cy = cy0, cz = cz0, cu = cu0;
+                        if (c_chunked) to_coords<FULL>(p.c, row0, n64, cx, cy, cz, cu);
+                        tma_store_5d(mpc, op_buf, cx, cy, cz, cu, 0);
+                        tma_store_commit();
+                        if (addend_ahead) tma_store_wait_read<0>();
+                    }
+                }
+                if (addend_ahead) { __syncwarp(); fetch_addend(); }
+            };
+            // EPI: the fp32 partial sums of a piece of a K split
+            auto partial_piece = [&](int c) {
+                float* wrow = p.ws + ((int64_t)t.split * p.M + min(m, t.m1 - 1)) * (int64_t)p.N;
+#pragma unroll 1
+                for (int q = 0; q < 4; ++q) {
+                    const int n16 = nb + c * 64 + q * 16;
+                    uint32_t r[16];
+                    tmem_ld16(taddr + (uint32_t)(c * 64 + q * 16), r);
+                    tmem_ld_wait();
+                    tmem_regs_ready(r);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (n16 + j * 4 < t.n1) st_global_v4_if(wrow + n16 + j * 4, make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]), m < t.m1);
                 }
             };
             auto store_piece = [&](uint32_t (&r)[64], int c) {
                 if (p.splits > 1) { store_partial(r, c); return; }
-                if (EPI != 0) { epilogue_piece(r, c); return; }
                 if (FULL && p.axpby) axpby_piece(r, c);
                 uint32_t pk[32];
                 pack(r, pk);
@@ -1053,7 +1200,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 cluster_sync();
                 float* rbuf = reinterpret_cast<float*>(smem);                       // [source][quarter][piece][group in slice][lane] float4
 #pragma unroll 1
-                for (int c = 0; c < npieces; ++c) {
+                for (int c = hf; c < npieces; c += EW) {
                     load_piece(ra, c);
                     tmem_ld_wait();
                     tmem_regs_ready(ra);
@@ -1071,7 +1218,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const int64_t coff = c_offset<FULL>(p, min(row, t.m1 - 1), nb) + (int)krank * JS * 4;
                 unsigned short* crow = p.C + coff;
 #pragma unroll 1
-                for (int c = 0; c < npieces; ++c)
+                for (int c = hf; c < npieces; c += EW)
 #pragma unroll
                     for (int js = 0; js < JS; js += 2) {           // two 4-column groups = one 16-byte store
                         float4 a0 = make_float4(0.0f, 0.0f, 0.0f, 0.0f), a1 = a0;
@@ -1204,6 +1351,11 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         if (!alive) break;
                     }
                 }
+            } else if constexpr (EPI != 0) {
+#pragma unroll 1
+                for (int c = hf; c < npieces; c += EW) {
+                    if (p.splits > 1) partial_piece(c); else epilogue_piece(c);
+                }
             } else if (EW > 1) {
 #pragma unroll 1
                 for (int c = hf; c < npieces; c += EW) {
@@ -1240,6 +1392,8 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             }
           }
         }
+        if constexpr (kOp)
+            if (ap.out) mbar_wait_bounded(&addend_full[warp - 2], addend_phase);     // (left early: the copy lands before the CTA does)
         // every tile store has read its shared-memory source; the writes themselves are complete, like any other
         // store of the kernel, when the kernel is
         if (lane == 0) tma_store_wait_read<0>();

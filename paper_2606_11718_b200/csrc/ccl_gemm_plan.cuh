@@ -406,7 +406,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     const char* rag_env = std::getenv("CCL_GEMM_RAGGED_DENSE");
     const uint32_t rag_bytes = cap > 0 && batch <= kRaggedDense && !(rag_env && atoi(rag_env) == 0) ? (uint32_t)(4 * (kGemmThreads + batch + 1) + 1023) & ~1023u : 0;
     p.rag_dense = rag_bytes ? 1 : 0;
-    p.stages = (int32_t)((kSmemBudget - rag_bytes) / p.stage_bytes);
+    p.stages = (int32_t)(((epi ? kSmemBudgetOp : kSmemBudget) - rag_bytes) / p.stage_bytes);
     if (p.stages > 8) p.stages = 8;
     int64_t ntiles = (int64_t)p.tiles_m * p.tiles_n * splits * batch;
     p.batch = (int32_t)batch;
@@ -469,7 +469,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     p.fd_upg = make_fastdiv(p.sch_upg); p.fd_groups = make_fastdiv(p.groups); p.fd_splits = make_fastdiv(p.splits);
     p.fd_per_panel = make_fastdiv((int64_t)p.panel * p.sch_gn); p.fd_panel = make_fastdiv(p.panel);
     p.fd_tps_m = make_fastdiv(p.tps_m); p.fd_tps_n = make_fastdiv(p.tps_n);
-    plan->smem_bytes = (uint32_t)p.stages * p.stage_bytes + kEpiBytes + 1024 + (2 * p.stages + 8) * 8 + 16 + rag_bytes;
+    plan->smem_bytes = (uint32_t)p.stages * p.stage_bytes + (epi ? kEpiBytesOp + kEpiOpWarps * 8 : kEpiBytes) + 1024 + (2 * p.stages + 8) * 8 + 16 + rag_bytes;
     p.fd_tiles_n = make_fastdiv(p.tiles_n);
     return CCL_OK;
 }

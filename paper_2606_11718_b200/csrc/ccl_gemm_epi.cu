@@ -16,7 +16,7 @@ static ccl_status launch_epi(const GemmPlan& plan, const CUtensorMap* maps, cons
     int dev = 0;
     CCL_CUDA_TRY(cudaGetDevice(&dev));
     if (dev >= 64 || !(configured.load() >> dev & 1)) {
-        CCL_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmemBudgetOp + kEpiBytesOp + 2048)));
+        CCL_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((KS ? kSmemBudgetOpKs : kSmemBudgetOp) + staging_bytes<EPI, KS> + 2048)));
         if (dev < 64) configured.fetch_or(1ull << dev);
     }
     cudaLaunchConfig_t cfg = {};
@@ -75,6 +75,8 @@ static ccl_status launch_variant(const GemmPlan& plan, const CUtensorMap* maps, 
 // columns of a row.  Column sums of the block go to its line of the partial sums, as in the GEMM kernel.
 template <int EPI>
 static __global__ void __launch_bounds__(256) splitk_epilogue_kernel(const GemmParams p) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");            // the GEMM has completed
     const int row = blockIdx.y * 32 + (threadIdx.x >> 3), n = blockIdx.x * 64 + (threadIdx.x & 7) * 8;
     const bool ok = row < p.M && n < p.N;
     const int r = min(row, p.M - 1), c = min(n, p.N - 8);
@@ -108,6 +110,8 @@ static __global__ void __launch_bounds__(256) splitk_epilogue_kernel(const GemmP
 // dbias[n] = bf16(sum over the row blocks of partial[block][n]): 32 columns a block, eight warps over the row blocks, their
 // sums added in a fixed order.  Reads blocks x N floats once (4 bytes for every 64 of dZ).
 __global__ void __launch_bounds__(256) column_sum_finish_kernel(const float* partial, int blocks, int N, uint16_t* dbias) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");            // the kernel that writes the partial sums has completed
     __shared__ float part[8][32];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, n = blockIdx.x * 32 + lane;
     float s = 0.0f;
@@ -124,10 +128,20 @@ __global__ void __launch_bounds__(256) column_sum_finish_kernel(const float* par
     }
 }
 
-ccl_status column_sum_finish(const float* partial, int blocks, int N, void* dbias, cudaStream_t st) {
-    column_sum_finish_kernel<<<(unsigned)((N + 31) / 32), 256, 0, st>>>(partial, blocks, N, static_cast<uint16_t*>(dbias));
+// A kernel of this file behind the GEMM: placed early (its CTAs wait for the GEMM's completion themselves)
+template <typename... Params, typename... Args>
+static ccl_status launch_behind(void (*kernel)(Params...), dim3 grid, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(256, 1, 1);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
     count_launch();
-    CCL_CUDA_TRY(cudaGetLastError());
     return CCL_OK;
 }
 
@@ -273,12 +287,10 @@ ccl_status run_epi(const char* who, int epi, const ccl_gemm_desc* d, int act, co
     if ((s = epi == 1 ? launch_with_maps<1>(plan, maps, st) : launch_with_maps<2>(plan, maps, st))) return s;
     if (p.splits > 1) {
         const dim3 grid((unsigned)((p.N + 63) / 64), (unsigned)((p.M + 31) / 32));
-        if (epi == 1) splitk_epilogue_kernel<1><<<grid, 256, 0, st>>>(p);
-        else splitk_epilogue_kernel<2><<<grid, 256, 0, st>>>(p);
-        count_launch();
-        CCL_CUDA_TRY(cudaGetLastError());
+        if ((s = epi == 1 ? launch_behind(splitk_epilogue_kernel<1>, grid, st, p) : launch_behind(splitk_epilogue_kernel<2>, grid, st, p))) return s;
     }
-    return dbias ? column_sum_finish(p.colsum, (int)row_blocks(plan), p.N, dbias, st) : CCL_OK;
+    if (!dbias) return CCL_OK;
+    return launch_behind(column_sum_finish_kernel, dim3((unsigned)((p.N + 31) / 32)), st, (const float*)p.colsum, (int)row_blocks(plan), (int)p.N, static_cast<uint16_t*>(dbias));
 }
 }  // namespace
 

@@ -31,12 +31,15 @@ constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
 // their arithmetic -- an exponential, a reciprocal and some twenty instructions a value -- has the time of the next tile's product,
 // and what eight warps lost was latency (4096 x 8192 x 2048 with gelu's slope: 140 us with eight, 94 for the plain product).
 constexpr int kEpiOpWarps = 16;
+// (the cluster split exchanges its partial sums in the ring and stores from registers: no staging, a longer ring)
+template <int EPI, int KS> constexpr uint32_t staging_bytes = EPI ? (KS ? 0u : kEpiOpWarps * 32u * 128u) : 4u * 2 * 32 * 128;
 template <int EPI> constexpr int epi_warps = EPI ? kEpiOpWarps : kEpiWarps;
 template <int EPI> constexpr int gemm_threads = 64 + 32 * epi_warps<EPI>;
 constexpr int kTmemCols = 512;
 constexpr uint32_t kSmemBudget = 192 * 1024;    // ring of operand stages
 constexpr int64_t kRaggedDense = 4096;         // problems of a ragged batch whose tile prefix is kept in shared memory
 constexpr uint32_t kEpiBytes = 4 * 2 * 32 * 128; // epilogue staging: per warp two buffers of 32 rows x 128 B
+constexpr uint32_t kSmemBudgetOpKs = 224 * 1024;
 constexpr uint32_t kSmemBudgetOp = 160 * 1024;  // EPI: a shorter ring,
 constexpr uint32_t kEpiBytesOp = kEpiOpWarps * 32 * 128;       // and a buffer for each of the sixteen warps, in which an addend's piece becomes C's
 
@@ -612,7 +615,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     unsigned char* epi = smem + (size_t)gp.stages * gp.stage_bytes;     // 1024-byte aligned: stage sizes are multiples of 1 KB
-    uint64_t* bars = reinterpret_cast<uint64_t*>(epi + (EPI ? kEpiBytesOp : kEpiBytes));
+    uint64_t* bars = reinterpret_cast<uint64_t*>(epi + staging_bytes<EPI, KS>);
     uint64_t* full = bars;                           // used in the leader CTA only
     uint64_t* empty = bars + gp.stages;               // one set per CTA
     uint64_t* tmem_full = bars + 2 * gp.stages;       // one set per CTA

@@ -254,8 +254,13 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
                 const int64_t waves = (tiles * sp + units - 1) / units;
                 // (a last wave that leaves SMs idle streams a little slower: measured ~5 % between 96 and 128 busy SMs)
                 const double last = (double)(tiles * sp - (waves - 1) * units) / (double)units;
-                double cost = std::max((double)waves * ((double)kbps * t_kb + (sp > 1 ? 2.0 * t_drain : t_drain)),
-                                       stream_clk * (1.0 + 0.1 * (1.0 - last))) + 3000.0;
+                // an operator in the epilogue: ~6000 cycles a piece and warp (four pieces side by side), behind the next tile's
+                // product where the accumulator is double-buffered, in the open otherwise (measured, 4096 x 28672 x 8192: 1363 us
+                // with 256 x 256 pair tiles, 1469 with 256 x 512, which ccl_gemm prefers)
+                const double t_op = epi ? 6000.0 * ((b + 255) / 256) : 0.0;
+                const double per_tile = !epi || sp > 1 ? (double)kbps * t_kb + (sp > 1 ? 2.0 * t_drain : t_drain)
+                                                       : (b <= 256 ? std::max((double)kbps * t_kb, t_op) + 500.0 : (double)kbps * t_kb + t_op + t_drain);
+                double cost = std::max((double)waves * per_tile + (epi && b <= 256 ? t_op : 0.0), stream_clk * (1.0 + 0.1 * (1.0 - last))) + 3000.0;
                 // a problem that runs for long runs at the power cap, where the clock follows the energy a k block costs:
                 // measured, 256 x 256 pair tiles (a third more operand bytes per flop than 256 x 512) take 3-6 % longer on
                 // the Llama-size GEMMs although they need fewer cycles
@@ -406,7 +411,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     const char* rag_env = std::getenv("CCL_GEMM_RAGGED_DENSE");
     const uint32_t rag_bytes = cap > 0 && batch <= kRaggedDense && !(rag_env && atoi(rag_env) == 0) ? (uint32_t)(4 * (kGemmThreads + batch + 1) + 1023) & ~1023u : 0;
     p.rag_dense = rag_bytes ? 1 : 0;
-    p.stages = (int32_t)(((epi ? kSmemBudgetOp : kSmemBudget) - rag_bytes) / p.stage_bytes);
+    p.stages = (int32_t)(((epi ? (ks ? kSmemBudgetOpKs : kSmemBudgetOp) : kSmemBudget) - rag_bytes) / p.stage_bytes);
     if (p.stages > 8) p.stages = 8;
     int64_t ntiles = (int64_t)p.tiles_m * p.tiles_n * splits * batch;
     p.batch = (int32_t)batch;
@@ -469,7 +474,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     p.fd_upg = make_fastdiv(p.sch_upg); p.fd_groups = make_fastdiv(p.groups); p.fd_splits = make_fastdiv(p.splits);
     p.fd_per_panel = make_fastdiv((int64_t)p.panel * p.sch_gn); p.fd_panel = make_fastdiv(p.panel);
     p.fd_tps_m = make_fastdiv(p.tps_m); p.fd_tps_n = make_fastdiv(p.tps_n);
-    plan->smem_bytes = (uint32_t)p.stages * p.stage_bytes + (epi ? kEpiBytesOp + kEpiOpWarps * 8 : kEpiBytes) + 1024 + (2 * p.stages + 8) * 8 + 16 + rag_bytes;
+    plan->smem_bytes = (uint32_t)p.stages * p.stage_bytes + (epi ? (ks ? 0u : kEpiBytesOp) + kEpiOpWarps * 8 : kEpiBytes) + 1024 + (2 * p.stages + 8) * 8 + 16 + rag_bytes;
     p.fd_tiles_n = make_fastdiv(p.tiles_n);
     return CCL_OK;
 }

@@ -135,11 +135,12 @@ def _check(status):
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    """Handle of torch's current stream (an int; torch.cuda.current_stream() builds an object around it, 3 us)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _ptr(t):
-    return C.c_void_p(t.data_ptr()) if t is not None else None
+    return t.data_ptr() if t is not None else None
 
 
 def ccl_version():
@@ -285,19 +286,28 @@ def ccl_gemm_swiglu(d, A, B, Cout):
     _check(lib().ccl_gemm_swiglu(C.byref(d), _ptr(A), _ptr(B), _ptr(Cout), _stream()))
 
 
-def _holds(t, nbytes):
-    return t.is_cuda and t.is_contiguous() and t.numel() * t.element_size() >= nbytes
+def _check_operands(what, *pairs):
+    """Every (tensor or None, bytes) pair: a contiguous CUDA tensor with at least that many bytes."""
+    for t, nbytes in pairs:
+        if t is not None and (t.nbytes < nbytes or not t.is_cuda or not t.is_contiguous()):
+            raise ValueError(f"{what}: an operand must be a contiguous CUDA tensor that holds what the descriptor says")
 
 
-def _vector(t, n, what):
-    if t is not None and not (t.dtype == torch.bfloat16 and _holds(t, 2 * n)):
+def _check_vector(t, n, what):
+    if t is not None and (t.dtype != torch.bfloat16 or t.nbytes < 2 * n or not t.is_cuda or not t.is_contiguous()):
         raise ValueError(f"{what} must be a contiguous bfloat16 CUDA tensor with at least {n} entries")
 
 
-def _operands(what, *pairs):
-    for t, nbytes in pairs:
-        if t is not None and not _holds(t, nbytes):
-            raise ValueError(f"{what}: an operand must be a contiguous CUDA tensor that holds what the descriptor says")
+_gemm_bytes_cache = {}
+
+
+def _gemm_bytes(d):
+    """Bytes of the buffers of A, B and C that a GEMM descriptor addresses (kept by the descriptor's contents)."""
+    key = bytes(d)
+    v = _gemm_bytes_cache.get(key)
+    if v is None:
+        v = _gemm_bytes_cache[key] = tuple(ccl_buffer_bytes(m) for m in (d.A, d.B, d.C))
+    return v
 
 
 def _size(fn, d):
@@ -312,11 +322,11 @@ def ccl_gemm_epilogue_workspace(d):
 
 def ccl_gemm_epilogue(d, A, B, Cout, ws=None, act=ACT_NONE, bias=None, residual=None, preact=None):
     """C = act(A*B + bias) + residual; preact receives A*B + bias.  bias: [N] bfloat16; residual (may be Cout) and preact in C's layout."""
-    c_bytes = ccl_buffer_bytes(d.C)
-    _operands("ccl_gemm_epilogue", (A, ccl_buffer_bytes(d.A)), (B, ccl_buffer_bytes(d.B)), (Cout, c_bytes), (residual, c_bytes), (preact, c_bytes))
-    _vector(bias, d.N, "ccl_gemm_epilogue: bias")
+    a_bytes, b_bytes, c_bytes = _gemm_bytes(d)
+    _check_operands("ccl_gemm_epilogue", (A, a_bytes), (B, b_bytes), (Cout, c_bytes), (residual, c_bytes), (preact, c_bytes))
+    _check_vector(bias, d.N, "ccl_gemm_epilogue: bias")
     e = Epilogue(act, _ptr(bias), _ptr(residual), _ptr(preact))
-    ws_bytes = ws.numel() * ws.element_size() if ws is not None else 0
+    ws_bytes = ws.nbytes if ws is not None else 0
     _check(lib().ccl_gemm_epilogue(C.byref(d), C.byref(e), _ptr(A), _ptr(B), _ptr(Cout), _ptr(ws), ws_bytes, _stream()))
 
 
@@ -326,18 +336,18 @@ def ccl_gemm_act_grad_workspace(d):
 
 def ccl_gemm_act_grad(d, A, B, preact, dz, ws=None, act=ACT_NONE, dbias=None):
     """dz = (A*B) * act'(preact), dbias = its column sums.  preact and dz in C's layout; dbias: [N] bfloat16."""
-    c_bytes = ccl_buffer_bytes(d.C)
-    _operands("ccl_gemm_act_grad", (A, ccl_buffer_bytes(d.A)), (B, ccl_buffer_bytes(d.B)), (preact, c_bytes), (dz, c_bytes))
-    _vector(dbias, d.N, "ccl_gemm_act_grad: dbias")
-    ws_bytes = ws.numel() * ws.element_size() if ws is not None else 0
+    a_bytes, b_bytes, c_bytes = _gemm_bytes(d)
+    _check_operands("ccl_gemm_act_grad", (A, a_bytes), (B, b_bytes), (preact, c_bytes), (dz, c_bytes))
+    _check_vector(dbias, d.N, "ccl_gemm_act_grad: dbias")
+    ws_bytes = ws.nbytes if ws is not None else 0
     _check(lib().ccl_gemm_act_grad(C.byref(d), act, _ptr(A), _ptr(B), _ptr(preact), _ptr(dz), _ptr(dbias), _ptr(ws), ws_bytes, _stream()))
 
 
 def ccl_bias_act_grad(m, dy, preact, dz, dbias=None, act=ACT_NONE):
     """dz = dy * act'(preact) (None: not wanted), dbias = its column sums; dy, preact and dz as `m` describes, dbias: [cols] bfloat16."""
     nbytes = ccl_buffer_bytes(m)
-    _operands("ccl_bias_act_grad", (dy, nbytes), (preact, nbytes), (dz, nbytes))
-    _vector(dbias, m.cols, "ccl_bias_act_grad: dbias")
+    _check_operands("ccl_bias_act_grad", (dy, nbytes), (preact, nbytes), (dz, nbytes))
+    _check_vector(dbias, m.cols, "ccl_bias_act_grad: dbias")
     _check(lib().ccl_bias_act_grad(C.byref(m), act, _ptr(dy), _ptr(preact), _ptr(dz), _ptr(dbias), _stream()))
 
 
@@ -349,11 +359,11 @@ def ccl_moe_tokens(d, X, Wr, Wgu, Wd, Y, ws, residual=None, ids=None, weights=No
     """A mixture-of-experts layer for d.T tokens: Y = residual + sum over each token's topk experts.  Wr [E x H], Wgu per expert
     [2I x H], Wd per expert [H x I]; ids int32 / weights float32 [T x topk] receive the choice if wanted."""
     th, gu, dn = 2 * d.T * d.H, 4 * d.I * d.H, 2 * d.I * d.H
-    _operands("ccl_moe_tokens", (X, th), (Y, th), (residual, th), (Wr, 2 * d.E * d.H), (Wgu, (d.E - 1) * (d.gu_stride_bytes or gu) + gu),
+    _check_operands("ccl_moe_tokens", (X, th), (Y, th), (residual, th), (Wr, 2 * d.E * d.H), (Wgu, (d.E - 1) * (d.gu_stride_bytes or gu) + gu),
               (Wd, (d.E - 1) * (d.d_stride_bytes or dn) + dn), (ids, 4 * d.T * d.topk), (weights, 4 * d.T * d.topk))
     if (ids is not None and ids.dtype != torch.int32) or (weights is not None and weights.dtype != torch.float32):
         raise ValueError("ccl_moe_tokens: ids must be int32 and weights float32")
-    ws_bytes = ws.numel() * ws.element_size() if ws is not None else 0
+    ws_bytes = ws.nbytes if ws is not None else 0
     _check(lib().ccl_moe_tokens(C.byref(d), _ptr(X), _ptr(Wr), _ptr(Wgu), _ptr(Wd), _ptr(residual), _ptr(Y), _ptr(ids), _ptr(weights), _ptr(ws), ws_bytes,
                                 _stream()))
 

@@ -33,7 +33,7 @@ __device__ __forceinline__ void load_cols(const uint16_t* p, uint32_t (&v)[(VEC 
 // VEC: columns of a thread: 8 (16-byte accesses) or 1.  LINEAR: a column strip's rows follow each other at one pitch (row-major
 // and CCL split along the columns); otherwise every element is looked up in the address map.
 template <int ACT, int VEC, bool LINEAR>
-__global__ void __launch_bounds__(kBiasThreads) bias_act_grad_kernel(const BiasGradParams p) {
+__global__ void __launch_bounds__(kBiasThreads, 4) bias_act_grad_kernel(const BiasGradParams p) {
     __shared__ float part[kBiasThreads * VEC];
     uint32_t rank, ctas;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -149,7 +149,7 @@ extern "C" ccl_status ccl_bias_act_grad(const ccl_mat* m, int32_t act, const voi
     const bool vec = (any & 15) == 0 && v.cols % 8 == 0 && (v.split != 2 || (v.w % 8 == 0 && v.wlast % 8 == 0)) && v.stride % 8 == 0 && v.ichunk % 8 == 0;
     const bool linear = !v.ichunk && v.split != 1;
     const int64_t groups = vec ? v.cols / 8 : v.cols;    // threads needed for one row
-    // As many threads along a row as leave every SM a few CTAs: 16 of them read 256 contiguous bytes
+    // As many threads along a row as leave every SM three CTAs or more (four fit at a time): 16 of them read 256 contiguous bytes
     int lanes = 32, ctas = 8;
     while (ctas > 1 && v.rows < (int64_t)ctas * 32) ctas /= 2;
     while (lanes > 2 && (groups + lanes - 1) / lanes * ctas < 148 * 3) lanes /= 2;

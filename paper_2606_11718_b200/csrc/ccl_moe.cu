@@ -168,6 +168,12 @@ __device__ __forceinline__ uint32_t order_key(float f) {
 
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
 
+// d = A B for a block's 16 rows (m) of one of its two halves of 32 k: two k steps
+__device__ __forceinline__ void mma_half(float (&d)[4], const uint4& lo, const uint4& hi, const uint4& b) {
+    mma_16x8x16(d, lo.x, hi.x, lo.y, hi.y, b.x, b.y);
+    mma_16x8x16(d, lo.z, hi.z, lo.w, hi.w, b.z, b.w);
+}
+
 // Byte offset of the 16 bytes that row r, piece c (of 8) of a block are kept at (the TMA's 128-byte swizzle), and the row a lane
 // with g = lane / 4 takes as row g of a matrix fragment: consecutive g lie four rows apart, so that the 8 lanes of a 16-byte
 // load's phase (two g, four pieces each) hit different banks.
@@ -457,6 +463,22 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
         if (++slot == kMoeDepth) { slot = 0; parity ^= 1; }
     };
 
+    // A block's weights as matrix fragments: [half of its k][16 rows of its 32], rows fr and fr + 8.  All eight loads are under way
+    // before the first product waits for one; the two halves have sums of their own, so that no product waits for more than one other.
+    // (With loads and products in turn a block took 1350 cycles.)
+    struct Fragments { uint4 lo[2][2], hi[2][2]; };
+    auto fragments = [&](uint32_t w) {
+        Fragments a;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                a.lo[s][m] = lds128(w + block_at(m * 16 + fr, s * 4 + q));
+                a.hi[s][m] = lds128(w + block_at(m * 16 + fr + 8, s * 4 + q));
+            }
+        return a;
+    };
+
     // ---- 2. gate and up ------------------------------------------------------------------------------------------------
     {
         float4* red = reinterpret_cast<float4*>(smem + p.at_red);                // [buffer][column group][warp][lane]
@@ -477,27 +499,22 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
                     xrow[n] = x0 + (uint32_t)((p.all_x ? pair[first + col].x : col) * p.x_pitch);
                 }
             }
-            float gate[NT][4], up[NT][4];
+            float acc[NT][2][2][4];                       // [column group][half of k][gate, up]
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) gate[n][j] = up[n][j] = 0.0f;
+                for (int j = 0; j < 16; ++j) acc[n][j >> 3][j >> 2 & 1][j & 3] = 0.0f;
 #pragma unroll 1
             for (; kb < nb1; kb += kMoeWarps) {
-                const uint32_t w = block();
+                const Fragments a = fragments(block());
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const uint4 glo = lds128(w + block_at(fr, s * 4 + q)), ghi = lds128(w + block_at(fr + 8, s * 4 + q));
-                    const uint4 ulo = lds128(w + block_at(fr + 16, s * 4 + q)), uhi = lds128(w + block_at(fr + 24, s * 4 + q));
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        if (n * 8 >= cnt) break;
-                        const uint4 b = lds128(xrow[n] + (uint32_t)(kb * 128 + s * 64 + q * 16));
-                        mma_16x8x16(gate[n], glo.x, ghi.x, glo.y, ghi.y, b.x, b.y);
-                        mma_16x8x16(up[n], ulo.x, uhi.x, ulo.y, uhi.y, b.x, b.y);
-                        mma_16x8x16(gate[n], glo.z, ghi.z, glo.w, ghi.w, b.z, b.w);
-                        mma_16x8x16(up[n], ulo.z, uhi.z, ulo.w, uhi.w, b.z, b.w);
-                    }
+                for (int n = 0; n < NT; ++n) {
+                    if (n * 8 >= cnt) break;
+                    const uint4 b0 = lds128(xrow[n] + (uint32_t)(kb * 128 + q * 16)), b1 = lds128(xrow[n] + (uint32_t)(kb * 128 + 64 + q * 16));
+                    mma_half(acc[n][0][0], a.lo[0][0], a.hi[0][0], b0);
+                    mma_half(acc[n][0][1], a.lo[0][1], a.hi[0][1], b0);
+                    mma_half(acc[n][1][0], a.lo[1][0], a.hi[1][0], b1);
+                    mma_half(acc[n][1][1], a.lo[1][1], a.hi[1][1], b1);
                 }
                 done_with_block();
             }
@@ -509,8 +526,10 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
 #pragma unroll
             for (int n = 0; n < NT; ++n)
                 if (n * 8 < cnt) {
-                    out[2 * n * kMoeThreads + threadIdx.x] = make_float4(gate[n][0], gate[n][1], gate[n][2], gate[n][3]);
-                    out[(2 * n + 1) * kMoeThreads + threadIdx.x] = make_float4(up[n][0], up[n][1], up[n][2], up[n][3]);
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+                        out[(2 * n + m) * kMoeThreads + threadIdx.x] = make_float4(acc[n][0][m][0] + acc[n][1][m][0], acc[n][0][m][1] + acc[n][1][m][1],
+                                                                                   acc[n][0][m][2] + acc[n][1][m][2], acc[n][0][m][3] + acc[n][1][m][3]);
                 }
             bar_consumers();
             if (warp == (turn & (kMoeWarps - 1))) {
@@ -558,15 +577,18 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
         // the spare rows behind the last pair; nobody looks at them).  The loop is not unrolled: more blocks of h ahead, in registers
         // of their own, made its code outgrow the instruction cache and took longer.
         uint4 hn[2][NH];
+        int2 pn[NH];                                      // token and weight of this lane's column of each group
         uint32_t en = 0;
         int turn = 0;                                     // row blocks done
-        auto load_h = [&](uint4 (&to)[2][NH], uint32_t e, int kb) {
-            const unsigned char* src = hl + (int64_t)(e >> 9 & 1023u) * 2 * p.h_pitch + kb * 128;
+        auto load_h = [&](uint32_t e, int kb) {
+            const int first = (int)(e >> 9 & 1023u), cnt = (int)(e >> 19);
+            const unsigned char* src = hl + (int64_t)first * 2 * p.h_pitch + kb * 128;
 #pragma unroll
             for (int n = 0; n < NH; ++n) {
-                if (n * 4 >= (int)(e >> 19)) break;
-                to[0][n] = __ldcg(reinterpret_cast<const uint4*>(src + n * hgroup));
-                to[1][n] = __ldcg(reinterpret_cast<const uint4*>(src + n * hgroup + 64));
+                if (n * 4 >= cnt) break;
+                hn[0][n] = __ldcg(reinterpret_cast<const uint4*>(src + n * hgroup));
+                hn[1][n] = __ldcg(reinterpret_cast<const uint4*>(src + n * hgroup + 64));
+                pn[n] = pair[min(first + n * 4 + q, pairs - 1)];
             }
         };
 #pragma unroll 1
@@ -577,7 +599,7 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
             auto step = [&]() {
                 while (kb >= nb2) { kb -= nb2; ++i; }
                 en = ent[i];
-                load_h(hn, en, kb);
+                load_h(en, kb);
                 kb += 2 * kMoeWarps;
             };
             if (mine > 0) step();
@@ -585,45 +607,35 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
             for (int j = 0; j < mine; ++j) {
                 {
                     uint4 h[2][NH];
+                    int2 pr[NH];
 #pragma unroll
-                    for (int n = 0; n < NH; ++n) { h[0][n] = hn[0][n]; h[1][n] = hn[1][n]; }
-                    const int cnt = (int)(en >> 19), first = (int)(en >> 9 & 1023u);
+                    for (int n = 0; n < NH; ++n) { h[0][n] = hn[0][n]; h[1][n] = hn[1][n]; pr[n] = pn[n]; }
+                    const int cnt = (int)(en >> 19);
                     if (j + 1 < mine) step();
-                    const uint32_t w = block();
-                    float acc[2][NH][4];
-#pragma unroll
-                    for (int n = 0; n < NH; ++n)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) acc[0][n][c] = acc[1][n][c] = 0.0f;
-#pragma unroll
-                    for (int s = 0; s < 2; ++s)
-#pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            const uint4 lo = lds128(w + block_at(m * 16 + fr, s * 4 + q)), hi = lds128(w + block_at(m * 16 + fr + 8, s * 4 + q));
-#pragma unroll
-                            for (int n = 0; n < NH; ++n) {
-                                if (n * 4 >= cnt) break;
-                                mma_16x8x16(acc[m][n], lo.x, hi.x, lo.y, hi.y, h[s][n].x, h[s][n].y);
-                                mma_16x8x16(acc[m][n], lo.z, hi.z, lo.w, hi.w, h[s][n].z, h[s][n].w);
-                            }
-                        }
-                    done_with_block();
-                    // weight * (this block's share of Wd h) into the warp's own sums: a token is in one column of an entry only
+                    const Fragments a = fragments(block());
 #pragma unroll
                     for (int n = 0; n < NH; ++n) {
                         if (n * 4 >= cnt) break;
+                        float acc[2][2][4];
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) acc[c >> 3][c >> 2 & 1][c & 3] = 0.0f;
+#pragma unroll
+                        for (int s = 0; s < 2; ++s)
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) mma_half(acc[s][m], a.lo[s][m], a.hi[s][m], h[s][n]);
+                        // weight * (this block's share of Wd h) into the warp's own sums: a token is in one column of an entry only
                         if (n * 4 + q < cnt) {
-                            const int2 pr = pair[first + n * 4 + q];
-                            float4* a = reinterpret_cast<float4*>(ya + sum_at(pr.x, fr));
-                            const float wj = __int_as_float(pr.y);
-                            float4 v = *a;
-                            v.x = fmaf(wj, acc[0][n][0] + acc[0][n][1], v.x);
-                            v.y = fmaf(wj, acc[0][n][2] + acc[0][n][3], v.y);
-                            v.z = fmaf(wj, acc[1][n][0] + acc[1][n][1], v.z);
-                            v.w = fmaf(wj, acc[1][n][2] + acc[1][n][3], v.w);
-                            *a = v;
+                            float4* to = reinterpret_cast<float4*>(ya + sum_at(pr[n].x, fr));
+                            const float wj = __int_as_float(pr[n].y);
+                            float4 v = *to;
+                            v.x = fmaf(wj, acc[0][0][0] + acc[0][0][1] + (acc[1][0][0] + acc[1][0][1]), v.x);
+                            v.y = fmaf(wj, acc[0][0][2] + acc[0][0][3] + (acc[1][0][2] + acc[1][0][3]), v.y);
+                            v.z = fmaf(wj, acc[0][1][0] + acc[0][1][1] + (acc[1][1][0] + acc[1][1][1]), v.z);
+                            v.w = fmaf(wj, acc[0][1][2] + acc[0][1][3] + (acc[1][1][2] + acc[1][1][3]), v.w);
+                            *to = v;
                         }
                     }
+                    done_with_block();
                 }
             }
             // the warps' sums, then the pair's, in this order; CTA 0 of the pair finishes the even tokens, CTA 1 the odd ones

@@ -12,16 +12,17 @@
 //   3. down: a pair of CTAs (a cluster) owns a few rows of Wd (2 H / #SMs of them, at most 32) and takes every chosen expert's:
 //      the sum over a token's experts stays inside the pair, in a fixed order, and Y is written once.
 // The k range of a unit is dealt out in blocks of 64 (32 rows x 128 bytes) to the 8 consumer warps of the CTA in turn (phase 3: to
-// the 16 of the pair); a ninth warp fetches the blocks, one TMA copy each, up to 32 of them ahead.  It stops for nothing but a
-// full ring: it runs ahead across units and from phase 2 into phase 3, so the weights of phase 3 arrive during the second
-// meeting.  (Consumers that issued their own copies made the loops too large for the instruction cache: phase 3 of 64 tokens x
-// 128 experts of 2048 x 768 took 118 us.)
+// the 16 of the pair).  A ninth warp fetches the blocks, one TMA copy each, up to 32 of them ahead: it stops for nothing but a
+// full ring, runs ahead across units and from phase 2 into phase 3, so the weights of phase 3 arrive during the second meeting.
+// A tenth fetches the h that goes with phase 3's blocks, by cp.async: the TMA takes ~60 ns a block as it is (a 128-byte row every four
+// cycles), and h by TMA as well had the products wait.  (Consumers that issued their own copies, or read h themselves, made loops
+// that were slower to run than the weights to come: phase 3 of 64 tokens x 128 experts of 2048 x 768 took 118 and 86 us.)
 //
 // The matrix instructions are mma.sync: with n = 8 columns a tcgen05 tile would be 128 rows high and leave most SMs without
 // work for one token; they are nowhere near their limit here.  Weights and tokens are both K-contiguous, so a lane may take any 8
 // consecutive k as its share of two k steps as long as both operands do: 16-byte loads, no ldmatrix.
-// h keeps 16 significant bits: it is stored as two bf16 rows (the rounded value and what the rounding left), side by side as two columns
-// of the same product, which the n = 8 columns have room for.
+// h keeps 16 significant bits: it is stored as two bf16 rows (the rounded value and what the rounding left), two columns of the same
+// product, which the n = 8 columns have room for.
 #include <algorithm>
 #include <atomic>
 #include <chrono>
@@ -33,13 +34,15 @@ namespace ccl {
 
 constexpr int kMoeWarps = 8;                             // consumers
 constexpr int kMoeThreads = kMoeWarps * 32;
-constexpr int kMoeBlockThreads = kMoeThreads + 32;       // and the warp that fetches
+constexpr int kMoeHWarps = 4;                            // warps that fetch h, for two consumers each
+constexpr int kMoeBlockThreads = kMoeThreads + 32 + 32 * kMoeHWarps;         // and the one that fetches weights
 constexpr int kMoeRows = 32;                             // rows of a block,
 constexpr int kMoeBlockK = 64;                           // its k elements (128 bytes of a row)
 constexpr int kMoeBlock = kMoeRows * kMoeBlockK * 2;
-constexpr int kMoeDepth = 4;                             // blocks in a warp's ring
-constexpr int kMoeRing = kMoeWarps * kMoeDepth * kMoeBlock;
-constexpr int kMoeSmem = 226 * 1024;
+constexpr int kMoeDepth = 4;                             // most blocks in a warp's ring
+constexpr int kMoeGroup = 8;                             // most tokens of an expert taken together: two groups of 4, each 8 columns of phase 3
+constexpr int kMoeHBlock = 2 * 8 * kMoeBlockK * 2;       // h for a block
+constexpr size_t kMoeSmem = 227 * 1024;
 constexpr int64_t kMoeMaxT = 64, kMoeMaxE = 512, kMoeMaxK = 16;
 
 static __device__ int g_moe_status = 0;
@@ -55,21 +58,26 @@ struct MoeParams {
     unsigned long long* flags;              // workspace: a flag per CTA (first meeting)
     unsigned long long* gate;               // workspace: the word that ends the first meeting, the counters of the others
     int2* choice;                           // workspace: [T][topk] expert, weight (more than 8 tokens)
-    unsigned char* h;                       // workspace: [pairs][2 (value, remainder)][h_pitch bytes] bf16
+    unsigned char* h;                       // workspace: [groups of 4 pairs][value, remainder][4][h_pitch bytes] bf16
     int64_t h_pitch;
     unsigned long long mark;                // this launch's mark in the flags
-    int32_t group;                          // most tokens of an expert taken together
+    int32_t group;                          // most tokens of an expert taken together (8 or 4)
+    int32_t depth;                          // blocks in a warp's ring
     int32_t all_x;                          // 1: the rows of all tokens are staged once; 0: those of an expert's tokens when it comes up
     int32_t x_pitch;                        // bytes between the token rows in shared memory
     int32_t rows_per_block, blocks;         // phase 3: rows of Wd a pair of CTAs takes at a time, such blocks in all
     // byte offsets in shared memory
-    int32_t at_bars, at_region, at_red, at_mask, at_off, at_ent, at_sel, at_selw, at_pair;
+    int32_t at_bars, at_region, at_hring, at_red, at_mask, at_off, at_ent, at_hgroup, at_sel, at_selw, at_pair;
 };
 
 __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     uint4 v;
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
+}
+// 16 bytes, or zeros where `ok` is off (nothing is read then)
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool ok) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -185,28 +193,30 @@ __device__ __forceinline__ int fragment_row(int g) { return (g & 1) << 2 | g >> 
 __device__ __forceinline__ int sum_at(int t, int r) { return t * kMoeRows + ((r ^ (t & 7)) << 2); }
 __device__ __forceinline__ int sum_row(int t, int at) { return ((at >> 2) ^ (t & 7)) + (at & 3) * 8; }
 
-// NT: most column groups of 8 an expert's tokens are taken in
-template <int NT>
-__global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const __grid_constant__ CUtensorMap map_gu, const __grid_constant__ CUtensorMap map_d, const __grid_constant__ MoeParams p) {
+__global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const __grid_constant__ CUtensorMap map_gu, const __grid_constant__ CUtensorMap map_d,
+                                                                        const __grid_constant__ MoeParams p) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x, ctas = gridDim.x;
     unsigned long long* mask = reinterpret_cast<unsigned long long*>(smem + p.at_mask);      // per expert: the tokens that chose it
     uint16_t* off = reinterpret_cast<uint16_t*>(smem + p.at_off);                            // per expert: its first pair
+    uint16_t* hgroup = reinterpret_cast<uint16_t*>(smem + p.at_hgroup);                      // per entry: its first group of h
     uint32_t* ent = reinterpret_cast<uint32_t*>(smem + p.at_ent);                            // entries: expert | first pair << 9 | pairs << 19
     uint16_t* sel = reinterpret_cast<uint16_t*>(smem + p.at_sel);                            // per (token, choice): expert
     float* selw = reinterpret_cast<float*>(smem + p.at_selw);                                // ... and weight
     int2* pair = reinterpret_cast<int2*>(smem + p.at_pair);                                  // per pair, sorted by expert, then token: token, weight
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + p.at_bars);                          // [warp][slot]: a block has arrived; then: ... has been used
-    uint64_t* pair_bars = bars + 2 * kMoeWarps * kMoeDepth;                                  // the other CTA's sums are there; it has read this one's
-    int* shared = reinterpret_cast<int*>(pair_bars + 2);                  // [0] entries, [1] the first meeting came about
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + p.at_bars);                          // [warp][slot]: a block has arrived; then: ... has been used; its h has
+    uint64_t *used = bars + kMoeWarps * kMoeDepth, *h_bars = used + kMoeWarps * kMoeDepth;
+    uint64_t* pair_bars = h_bars + kMoeWarps * kMoeDepth;                                    // the other CTA's sums are there; it has read this one's
+    uint64_t* met_bar = pair_bars + 2;                                                       // the second meeting is over
+    int* shared = reinterpret_cast<int*>(met_bar + 1);                                       // [0] entries, [1] the first meeting came about, [2] the second
     const int warp2 = (cta & 1) * kMoeWarps + warp;       // this warp's number in the CTA pair
     const int pairs = p.T * p.topk, nb1 = (p.H + kMoeBlockK - 1) / kMoeBlockK, nb2 = (p.I + kMoeBlockK - 1) / kMoeBlockK, nfb = p.I / p.gu_half * p.strip_units;
     const uint32_t x0 = smem_u32(smem + p.at_region);
     float* yacc = reinterpret_cast<float*>(smem + p.at_region);                              // phase 3, where x was: [warp][token][32], see sum_at
 
     if (threadIdx.x == 0) { prefetch_tmap(&map_gu); prefetch_tmap(&map_d); }
-    if ((int)threadIdx.x < 2 * kMoeWarps * kMoeDepth + 2) { mbar_init(&bars[threadIdx.x], 1); fence_barrier_init(); }
+    if ((int)threadIdx.x < 3 * kMoeWarps * kMoeDepth + 3) { mbar_init(&bars[threadIdx.x], (int)threadIdx.x >= 2 * kMoeWarps * kMoeDepth && (int)threadIdx.x < 3 * kMoeWarps * kMoeDepth ? 32 : 1); fence_barrier_init(); }
     if (warp < kMoeWarps)
         for (int e = threadIdx.x; e < p.E; e += kMoeThreads) mask[e] = 0;
     // rows of x (zeros behind H) in shared memory; row t is token `of(t)`
@@ -268,13 +278,6 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
         }
     }
     if (p.all_x) stage_x(p.T, [](int t) { return t; });
-    {   // h's rows end with whole blocks: zeros behind I
-        const int tail = nb2 * 8 - p.I / 8;
-        for (int j = cta * kMoeThreads + (int)threadIdx.x; j < 2 * pairs * tail; j += ctas * kMoeThreads) {
-            const int r = j / tail, c = p.I / 8 + j - r * tail;
-            *reinterpret_cast<uint4*>(p.h + (int64_t)r * p.h_pitch + c * 16) = make_uint4(0u, 0u, 0u, 0u);
-        }
-    }
     bool met1 = meet_first(p);
     if (threadIdx.x == 0) { shared[1] = met1; p.flags[cta] = 0; }        // (cleared for the next launch, which may be this one replayed)
     // top-k of a token: an expert's place is the number of those before it (a larger logit, or an equal one of a lower expert), a
@@ -352,22 +355,25 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
     bar_consumers();
     // pairs sorted by expert, then token: every expert's first one; entries of at most `group` pairs of one expert
     if (warp == 0) {
-        int np = 0, ne = 0;
+        int np = 0, ne = 0, nh = 0;                       // pairs, entries and groups of h so far
 #pragma unroll 1
         for (int e = lane; e - lane < p.E; e += 32) {
-            const int cnt = e < p.E ? __popcll(mask[e]) : 0;
+            const int cnt = e < p.E ? __popcll(mask[e]) : 0, gr = (cnt + 3) / 4;
             const int n = cnt <= p.group ? (cnt > 0) : (cnt + p.group - 1) / p.group;
-            int sum = cnt << 16 | n;                      // both prefix sums at once
+            int sum = cnt << 16 | n, sumh = gr;           // the prefix sums (two at once)
 #pragma unroll
             for (int m = 1; m < 32; m <<= 1) {
-                const int a = __shfl_up_sync(0xffffffffu, sum, m);
-                if (lane >= m) sum += a;
+                const int a = __shfl_up_sync(0xffffffffu, sum, m), b = __shfl_up_sync(0xffffffffu, sumh, m);
+                if (lane >= m) { sum += a; sumh += b; }
             }
-            const int o = np + (sum >> 16) - cnt, i0 = ne + (sum & 0xffff) - n;
+            const int o = np + (sum >> 16) - cnt, i0 = ne + (sum & 0xffff) - n, h0 = nh + sumh - gr;
             if (e < p.E) off[e] = (uint16_t)o;
-            for (int i = 0; i < n; ++i) ent[i0 + i] = (uint32_t)e | (uint32_t)(o + i * p.group) << 9 | (uint32_t)min(p.group, cnt - i * p.group) << 19;
+            for (int i = 0; i < n; ++i) {
+                ent[i0 + i] = (uint32_t)e | (uint32_t)(o + i * p.group) << 9 | (uint32_t)min(p.group, cnt - i * p.group) << 19;
+                hgroup[i0 + i] = (uint16_t)(h0 + i * (p.group / 4));
+            }
             sum = __shfl_sync(0xffffffffu, sum, 31);
-            np += sum >> 16; ne += sum & 0xffff;
+            np += sum >> 16; ne += sum & 0xffff; nh += __shfl_sync(0xffffffffu, sumh, 31);
         }
         if (lane == 0) shared[0] = ne;
     }
@@ -384,28 +390,37 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
 
     const int per_row_block = ents * nb2;                // blocks of a row block in phase 3: number j goes to warp j % 16 of the pair
 
-    if (warp == kMoeWarps) {
-        // ---- the stream of weights -------------------------------------------------------------------------------------
+    if (warp >= kMoeWarps) {
+        // ---- the streams of weights and of h ---------------------------------------------------------------------------
         // Lane w < 8 follows the blocks of consumer warp w: eight places are waited for, and eight copies started, at a time (one
         // after the other they took 330 cycles a block, 170 ns, where the memory delivers one in 95 ns).
-        const uint32_t bar0 = smem_u32(bars + (lane & (kMoeWarps - 1)) * kMoeDepth), used0 = bar0 + kMoeWarps * kMoeDepth * 8;
-        unsigned char* ring = smem + (lane & (kMoeWarps - 1)) * kMoeDepth * kMoeBlock;
+        const bool weights = warp == kMoeWarps;
+        constexpr int kPer = kMoeWarps / kMoeHWarps;      // consumers a warp fetches h for, from number v0 on
+        const int v0 = weights ? 0 : (warp - kMoeWarps - 1) * kPer, v1 = weights ? kMoeWarps : v0 + kPer;
+        const int w = lane & (kMoeWarps - 1), in_phase2 = ((u1 - u0) * nb1 + kMoeWarps - 1 - w) / kMoeWarps;       // the warp's blocks there
+        uint64_t* full = bars + w * kMoeDepth;
+        unsigned char* ring = smem + w * p.depth * kMoeBlock;
         bool ok = true;
-        int count = 0;                                    // blocks fetched for the warp so far
-        // The place for the next block of every lane that `has` one; false: a wait ran out
-        auto places = [&](bool has, int& at) {
-            at = count & (kMoeDepth - 1);
-            const uint32_t bar = used0 + at * 8, parity = (uint32_t)(count / kMoeDepth & 1) ^ 1u;
+        int count = 0;                                    // copies started for the warp
+        int at = weights ? 0 : in_phase2 % p.depth;       // the place of the next one; how often it has been around, mod 2
+        uint32_t turn = weights ? 0u : (uint32_t)(in_phase2 / p.depth) & 1u;
+        const uint32_t used0 = smem_u32(used + w * kMoeDepth);
+        // Waits for the place of the next block of every lane that `has` one; false: a wait ran out
+        auto places = [&](bool has) {
             uint32_t done = !has;
-            if (has) asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+            if (has) asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(used0 + at * 8), "r"(turn ^ 1u) : "memory");
             if (!__all_sync(0xffffffffu, done)) {
-                if (has) done = wait_long(bar, parity);
+                if (has) done = wait_long(used0 + at * 8, turn ^ 1u);
                 ok = __all_sync(0xffffffffu, done);
             }
-            count += has;
             return ok;
         };
-        {
+        auto next_place = [&](bool has) {
+            if (!has) return;
+            ++count;
+            if (++at == p.depth) { at = 0; turn ^= 1u; }
+        };
+        if (weights) {
             int u = u0, kb = lane, i = u0 / nfb, f = u0 - i * nfb, strip = f / p.strip_units, in_strip = f - strip * p.strip_units;
 #pragma unroll 1
             while (ok) {
@@ -416,40 +431,65 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
                 }
                 const bool has = lane < kMoeWarps && u < u1;
                 if (!__any_sync(0xffffffffu, has)) break;
-                int at;
-                if (places(has, at) && has) {
-                    mbar_expect_tx(bars + lane * kMoeDepth + at, kMoeBlock);
-                    tma_load_4d(ring + at * kMoeBlock, &map_gu, bars + lane * kMoeDepth + at, kb * kMoeBlockK, in_strip * 16, 2 * strip, (int)(ent[i] & 511u));
+                if (places(has) && has) {
+                    mbar_expect_tx(full + at, kMoeBlock);
+                    tma_load_4d(ring + at * kMoeBlock, &map_gu, full + at, kb * kMoeBlockK, in_strip * 16, 2 * strip, (int)(ent[i] & 511u));
+                    next_place(has);
                 }
                 kb += kMoeWarps;
             }
+        } else {
+            ok = wait_long(smem_u32(met_bar), 0u) && shared[2];      // h is complete when the second meeting is over
         }
 #pragma unroll 1
         for (int b = cta >> 1; ok && b < p.blocks; b += ctas >> 1) {
             int j = (cta & 1) * kMoeWarps + lane, kb = j, i = 0;
 #pragma unroll 1
             while (ok) {
-                const bool has = lane < kMoeWarps && j < per_row_block;
+                const bool has = lane >= v0 && lane < v1 && j < per_row_block;
                 if (!__any_sync(0xffffffffu, has)) break;
                 while (kb >= nb2) { kb -= nb2; ++i; }
-                int at;
-                if (places(has, at) && has) {
-                    mbar_expect_tx(bars + lane * kMoeDepth + at, (uint32_t)(p.rows_per_block * 128));
-                    tma_load_3d(ring + at * kMoeBlock, &map_d, bars + lane * kMoeDepth + at, kb * kMoeBlockK, b * p.rows_per_block, (int)(ent[i] & 511u));
+                if (!places(has)) break;
+                if (weights) {
+                    if (has) {
+                        mbar_expect_tx(full + at, (uint32_t)(p.rows_per_block * 128));
+                        tma_load_3d(ring + at * kMoeBlock, &map_d, full + at, kb * kMoeBlockK, b * p.rows_per_block, (int)(ent[i] & 511u));
+                    }
+                } else {
+                    // Lane v describes consumer v's block -- where its h starts, how many rows and pieces of 8 there are, the place in the
+                    // ring -- and the whole warp copies one after the other; nothing waits, so they overlap.
+                    const int ii = min(i, ents - 1), cnt = (int)(ent[ii] >> 19);
+                    const uint32_t from = (uint32_t)((int64_t)hgroup[ii] * 8 * p.h_pitch / 16) + (uint32_t)kb * 8u;       // in 16-byte units
+                    const uint32_t what = has ? (uint32_t)cnt | (uint32_t)min(8, (p.I - kb * kMoeBlockK) / 8) << 8 | (uint32_t)at << 16 : 0u;
+                    const int c = lane & 7, r = lane >> 3;
+#pragma unroll
+                    for (int vv = 0; vv < kPer; ++vv) {
+                        const int v = v0 + vv;
+                        const uint32_t fv = __shfl_sync(0xffffffffu, from, v), wv = __shfl_sync(0xffffffffu, what, v);
+                        const int n = (int)(wv & 255u), pieces = (int)(wv >> 8 & 255u), slot = v * p.depth + (int)(wv >> 16);
+                        const unsigned char* src = p.h + ((int64_t)fv + c) * 16 + (int64_t)r * p.h_pitch;
+                        const uint32_t dst = smem_u32(smem + p.at_hring) + (uint32_t)(slot * kMoeHBlock);
+#pragma unroll
+                        for (int t = 0; t < 4; ++t)                  // rows 4 t ... 4 t + 3: values (t even) or remainders of group t / 2
+                            if ((t >> 1) * 4 + r < n) copy_async(dst + block_at(t * 4 + r, c), c < pieces ? src + (int64_t)(t * 4) * p.h_pitch : p.h, c < pieces);
+                        if (n) asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(h_bars + v * kMoeDepth + (int)(wv >> 16))) : "memory");
+                    }
                 }
+                next_place(has);
                 j += 2 * kMoeWarps; kb += 2 * kMoeWarps;
             }
         }
         if (!ok && lane == 0) atomicExch(&g_moe_status, 9);
         // whatever became of the consumers, every copy has landed before the CTA leaves
-        if (lane < kMoeWarps)
-            for (int m = max(0, count - kMoeDepth); m < count; ++m) wait_long(smem_u32(&bars[lane * kMoeDepth + (m & (kMoeDepth - 1))]), (uint32_t)(m / kMoeDepth) & 1u);
+        if (!weights) asm volatile("cp.async.wait_all;" ::: "memory");
+        else if (lane < kMoeWarps)
+            for (int m = max(0, count - p.depth); m < count; ++m) wait_long(smem_u32(full + m % p.depth), (uint32_t)(m / p.depth) & 1u);
         pair_sync();
         return;
     }
 
     const int g = lane >> 2, q = lane & 3, fr = fragment_row(g);
-    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * kMoeDepth * kMoeBlock), full0 = smem_u32(bars + warp * kMoeDepth);
+    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * p.depth * kMoeBlock), hring = smem_u32(smem) + (uint32_t)(p.at_hring + warp * p.depth * kMoeHBlock), full0 = smem_u32(bars + warp * kMoeDepth);
     uint32_t slot = 0, parity = 0;
     bool ok = true;                                       // no wait of this warp has run out
     // The next block of the ring: wait for it, and give its place back.
@@ -459,8 +499,8 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
     };
     auto done_with_block = [&]() {
         __syncwarp();                                     // every lane has read the block
-        if (lane == 0) mbar_arrive(&bars[(kMoeWarps + warp) * kMoeDepth + slot]);
-        if (++slot == kMoeDepth) { slot = 0; parity ^= 1; }
+        if (lane == 0) mbar_arrive(&used[warp * kMoeDepth + slot]);
+        if (++slot == (uint32_t)p.depth) { slot = 0; parity ^= 1; }
     };
 
     // A block's weights as matrix fragments: [half of its k][16 rows of its 32], rows fr and fr + 8.  All eight loads are under way
@@ -483,7 +523,7 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
     {
         float4* red = reinterpret_cast<float4*>(smem + p.at_red);                // [buffer][column group][warp][lane]
         int i = u0 / nfb, f = u0 - i * nfb, cur = -1, first = 0, cnt = 0, kb = warp;     // kb: this warp's next block of the unit
-        uint32_t xrow[NT];                                // this lane's column of each group: its row of x
+        uint32_t xrow = 0;                                // this lane's column: its row of x
 #pragma unroll 1
         for (int u = u0; u < u1; ++u) {
             if (i != cur) {
@@ -493,28 +533,20 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
                     stage_x(cnt, [&](int t) { return pair[first + t].x; });
                     bar_consumers();
                 }
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const int col = min(n * 8 + g, cnt - 1);                     // (columns behind the last repeat it; nobody looks at them)
-                    xrow[n] = x0 + (uint32_t)((p.all_x ? pair[first + col].x : col) * p.x_pitch);
-                }
+                const int col = min(g, cnt - 1);                                 // (columns behind the last repeat it; nobody looks at them)
+                xrow = x0 + (uint32_t)((p.all_x ? pair[first + col].x : col) * p.x_pitch);
             }
-            float acc[NT][2][2][4];                       // [column group][half of k][gate, up]
+            float acc[2][2][4];                           // [half of k][gate, up]
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) acc[n][j >> 3][j >> 2 & 1][j & 3] = 0.0f;
+            for (int j = 0; j < 16; ++j) acc[j >> 3][j >> 2 & 1][j & 3] = 0.0f;
 #pragma unroll 1
             for (; kb < nb1; kb += kMoeWarps) {
                 const Fragments a = fragments(block());
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if (n * 8 >= cnt) break;
-                    const uint4 b0 = lds128(xrow[n] + (uint32_t)(kb * 128 + q * 16)), b1 = lds128(xrow[n] + (uint32_t)(kb * 128 + 64 + q * 16));
-                    mma_half(acc[n][0][0], a.lo[0][0], a.hi[0][0], b0);
-                    mma_half(acc[n][0][1], a.lo[0][1], a.hi[0][1], b0);
-                    mma_half(acc[n][1][0], a.lo[1][0], a.hi[1][0], b1);
-                    mma_half(acc[n][1][1], a.lo[1][1], a.hi[1][1], b1);
+                for (int s = 0; s < 2; ++s) {
+                    const uint4 b = lds128(xrow + (uint32_t)(kb * 128 + s * 64 + q * 16));
+                    mma_half(acc[s][0], a.lo[s][0], a.hi[s][0], b);
+                    mma_half(acc[s][1], a.lo[s][1], a.hi[s][1], b);
                 }
                 done_with_block();
             }
@@ -522,40 +554,31 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
             // the warps' partial sums meet in shared memory (two buffers, one barrier a unit) and the warps take turns in
             // finishing a unit: a buffer is written again only behind the next barrier, which its reader has reached by then
             const int turn = u - u0;
-            float4* out = red + (size_t)(turn & 1) * 2 * NT * kMoeThreads;
+            float4* out = red + (size_t)(turn & 1) * 2 * kMoeThreads;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-                if (n * 8 < cnt) {
-#pragma unroll
-                    for (int m = 0; m < 2; ++m)
-                        out[(2 * n + m) * kMoeThreads + threadIdx.x] = make_float4(acc[n][0][m][0] + acc[n][1][m][0], acc[n][0][m][1] + acc[n][1][m][1],
-                                                                                   acc[n][0][m][2] + acc[n][1][m][2], acc[n][0][m][3] + acc[n][1][m][3]);
-                }
+            for (int m = 0; m < 2; ++m)
+                out[m * kMoeThreads + threadIdx.x] = make_float4(acc[0][m][0] + acc[1][m][0], acc[0][m][1] + acc[1][m][1], acc[0][m][2] + acc[1][m][2], acc[0][m][3] + acc[1][m][3]);
             bar_consumers();
             if (warp == (turn & (kMoeWarps - 1))) {
+                float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if (n * 8 >= cnt) break;
-                    float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
+                for (int w = 0; w < kMoeWarps; ++w) {
+                    const float4 v = out[w * 32 + lane], z = out[kMoeThreads + w * 32 + lane];
+                    a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+                    b.x += z.x; b.y += z.y; b.z += z.z; b.w += z.w;
+                }
+                // gate and up of features fr (columns 2q and 2q + 1) and fr + 8 (the same columns) of the unit
+                const int su = f / p.strip_units, in_strip = (f - su * p.strip_units) * 16 + fr;        // (strip, row in its half)
+                const float h[4] = {a.x * logistic(a.x) * b.x, a.y * logistic(a.y) * b.y, a.z * logistic(a.z) * b.z, a.w * logistic(a.w) * b.w};
 #pragma unroll
-                    for (int w = 0; w < kMoeWarps; ++w) {
-                        const float4 v = out[2 * n * kMoeThreads + w * 32 + lane], z = out[(2 * n + 1) * kMoeThreads + w * 32 + lane];
-                        a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
-                        b.x += z.x; b.y += z.y; b.z += z.z; b.w += z.w;
-                    }
-                    // gate and up of features fr (columns 2q and 2q + 1) and fr + 8 (the same columns) of the unit
-                    const int su = f / p.strip_units, in_strip = (f - su * p.strip_units) * 16 + fr;        // (strip, row in its half)
-                    const float h[4] = {a.x * logistic(a.x) * b.x, a.y * logistic(a.y) * b.y, a.z * logistic(a.z) * b.z, a.w * logistic(a.w) * b.w};
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const int col = n * 8 + 2 * q + (c & 1), feat = su * p.gu_half + in_strip + (c >> 1) * 8;
-                        if (col < cnt && in_strip + (c >> 1) * 8 < p.gu_half) {
-                            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.h + (int64_t)(first + col) * 2 * p.h_pitch) + feat;
-                            const __nv_bfloat16 v = __float2bfloat16_rn(h[c]);
-                            const float rest = h[c] - __bfloat162float(v);
-                            dst[0] = v;
-                            dst[p.h_pitch / 2] = __float2bfloat16_rn(rest == rest ? rest : 0.0f);     // (inf - inf: the value says it all)
-                        }
+                for (int c = 0; c < 4; ++c) {
+                    const int col = 2 * q + (c & 1), feat = su * p.gu_half + in_strip + (c >> 1) * 8;
+                    if (col < cnt && in_strip + (c >> 1) * 8 < p.gu_half) {
+                        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.h + (int64_t)((hgroup[i] + (col >> 2)) * 8 + (col & 3)) * p.h_pitch) + feat;
+                        const __nv_bfloat16 v = __float2bfloat16_rn(h[c]);
+                        const float rest = h[c] - __bfloat162float(v);
+                        dst[0] = v;
+                        dst[2 * p.h_pitch] = __float2bfloat16_rn(rest == rest ? rest : 0.0f);     // (four rows on; inf - inf: the value says it all)
                     }
                 }
             }
@@ -563,6 +586,7 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
         }
     }
     const bool met = meet_counted(p.gate + 1);
+    if (threadIdx.x == 0) { shared[2] = met; mbar_arrive(met_bar); }
     if (cta == 0 && threadIdx.x == 0) p.gate[0] = 0;      // (everyone is past the first meeting)
 
     // ---- 3. down -------------------------------------------------------------------------------------------------------
@@ -570,73 +594,48 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
         for (int i = threadIdx.x; i < kMoeWarps * p.T * kMoeRows; i += kMoeThreads) yacc[i] = 0.0f;   // (x is no longer read)
         bar_consumers();
         float* ya = yacc + (size_t)warp * p.T * kMoeRows;
-        constexpr int NH = 2 * NT;                        // column groups of 8: columns 2 j and 2 j + 1 are pair j's value and remainder
-        const unsigned char* hl = p.h + (int64_t)g * p.h_pitch + q * 16;
-        const int64_t hgroup = 8 * p.h_pitch;
-        // This lane's share of h comes straight from the L2, a block ahead (columns behind the entry's last read other pairs' rows, or
-        // the spare rows behind the last pair; nobody looks at them).  The loop is not unrolled: more blocks of h ahead, in registers
-        // of their own, made its code outgrow the instruction cache and took longer.
-        uint4 hn[2][NH];
-        int2 pn[NH];                                      // token and weight of this lane's column of each group
-        uint32_t en = 0;
         int turn = 0;                                     // row blocks done
-        auto load_h = [&](uint32_t e, int kb) {
-            const int first = (int)(e >> 9 & 1023u), cnt = (int)(e >> 19);
-            const unsigned char* src = hl + (int64_t)first * 2 * p.h_pitch + kb * 128;
-#pragma unroll
-            for (int n = 0; n < NH; ++n) {
-                if (n * 4 >= cnt) break;
-                hn[0][n] = __ldcg(reinterpret_cast<const uint4*>(src + n * hgroup));
-                hn[1][n] = __ldcg(reinterpret_cast<const uint4*>(src + n * hgroup + 64));
-                pn[n] = pair[min(first + n * 4 + q, pairs - 1)];
-            }
-        };
+        uint32_t hphase = 0, hcount = 0;                  // of the ring of h
 #pragma unroll 1
         for (int b = met ? cta >> 1 : p.blocks; b < p.blocks; b += ctas >> 1) {
             const int r0 = b * p.rows_per_block, rows = min(p.rows_per_block, p.H - r0);
-            const int mine = ents * nb2 > warp2 ? (ents * nb2 - 1 - warp2) / (2 * kMoeWarps) + 1 : 0;      // this warp's blocks
-            int i = 0, kb = warp2;                        // the block whose h is loaded next
-            auto step = [&]() {
-                while (kb >= nb2) { kb -= nb2; ++i; }
-                en = ent[i];
-                load_h(en, kb);
-                kb += 2 * kMoeWarps;
-            };
-            if (mine > 0) step();
+            int i = 0, kb = warp2;
 #pragma unroll 1
-            for (int j = 0; j < mine; ++j) {
-                {
-                    uint4 h[2][NH];
-                    int2 pr[NH];
+            for (int j = warp2; j < per_row_block; j += 2 * kMoeWarps, kb += 2 * kMoeWarps) {
+                while (kb >= nb2) { kb -= nb2; ++i; }
+                const uint32_t en = ent[i];
+                const int first = (int)(en >> 9 & 1023u), cnt = (int)(en >> 19);
+                const int2 p0 = pair[first + min(q, cnt - 1)], p1 = pair[first + min(4 + q, cnt - 1)];      // token and weight of this lane's columns
+                const uint32_t wb = block();
+                ok = ok && wait_for(smem_u32(h_bars + warp * kMoeDepth + slot), hphase);
+                const Fragments a = fragments(wb);
+                const uint32_t hb = hring + slot * kMoeHBlock;
+                auto product = [&](int n, const int2& pr) {
+                    const uint4 h0 = lds128(hb + block_at(n * 8 + fr, q)), h1 = lds128(hb + block_at(n * 8 + fr, 4 + q));
+                    float4* to = reinterpret_cast<float4*>(ya + sum_at(pr.x, fr));
+                    float4 v = *to;
+                    float acc[2][2][4];
 #pragma unroll
-                    for (int n = 0; n < NH; ++n) { h[0][n] = hn[0][n]; h[1][n] = hn[1][n]; pr[n] = pn[n]; }
-                    const int cnt = (int)(en >> 19);
-                    if (j + 1 < mine) step();
-                    const Fragments a = fragments(block());
-#pragma unroll
-                    for (int n = 0; n < NH; ++n) {
-                        if (n * 4 >= cnt) break;
-                        float acc[2][2][4];
-#pragma unroll
-                        for (int c = 0; c < 16; ++c) acc[c >> 3][c >> 2 & 1][c & 3] = 0.0f;
-#pragma unroll
-                        for (int s = 0; s < 2; ++s)
-#pragma unroll
-                            for (int m = 0; m < 2; ++m) mma_half(acc[s][m], a.lo[s][m], a.hi[s][m], h[s][n]);
-                        // weight * (this block's share of Wd h) into the warp's own sums: a token is in one column of an entry only
-                        if (n * 4 + q < cnt) {
-                            float4* to = reinterpret_cast<float4*>(ya + sum_at(pr[n].x, fr));
-                            const float wj = __int_as_float(pr[n].y);
-                            float4 v = *to;
-                            v.x = fmaf(wj, acc[0][0][0] + acc[0][0][1] + (acc[1][0][0] + acc[1][0][1]), v.x);
-                            v.y = fmaf(wj, acc[0][0][2] + acc[0][0][3] + (acc[1][0][2] + acc[1][0][3]), v.y);
-                            v.z = fmaf(wj, acc[0][1][0] + acc[0][1][1] + (acc[1][1][0] + acc[1][1][1]), v.z);
-                            v.w = fmaf(wj, acc[0][1][2] + acc[0][1][3] + (acc[1][1][2] + acc[1][1][3]), v.w);
-                            *to = v;
-                        }
+                    for (int c = 0; c < 16; ++c) acc[c >> 3][c >> 2 & 1][c & 3] = 0.0f;
+                    mma_half(acc[0][0], a.lo[0][0], a.hi[0][0], h0);
+                    mma_half(acc[0][1], a.lo[0][1], a.hi[0][1], h0);
+                    mma_half(acc[1][0], a.lo[1][0], a.hi[1][0], h1);
+                    mma_half(acc[1][1], a.lo[1][1], a.hi[1][1], h1);
+                    // weight * (this block's share of Wd h) into the warp's own sums: a token is in one column of an entry only.  (Columns
+                    // 2 q and 2 q + 1 are h's rows fragment_row(2 q) = q and fragment_row(2 q + 1) = q + 4: a pair's value and remainder.)
+                    if (n * 4 + q < cnt) {
+                        const float wj = __int_as_float(pr.y);
+                        v.x = fmaf(wj, acc[0][0][0] + acc[0][0][1] + (acc[1][0][0] + acc[1][0][1]), v.x);
+                        v.y = fmaf(wj, acc[0][0][2] + acc[0][0][3] + (acc[1][0][2] + acc[1][0][3]), v.y);
+                        v.z = fmaf(wj, acc[0][1][0] + acc[0][1][1] + (acc[1][1][0] + acc[1][1][1]), v.z);
+                        v.w = fmaf(wj, acc[0][1][2] + acc[0][1][3] + (acc[1][1][2] + acc[1][1][3]), v.w);
+                        *to = v;
                     }
-                    done_with_block();
-                }
+                };
+                product(0, p0);
+                if (cnt > 4) product(1, p1);
+                done_with_block();
+                if (++hcount == (uint32_t)p.depth) { hcount = 0; hphase ^= 1; }
             }
             // the warps' sums, then the pair's, in this order; CTA 0 of the pair finishes the even tokens, CTA 1 the odd ones
             bar_consumers();
@@ -679,7 +678,7 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
 // ---- host ------------------------------------------------------------------------------------------------------------
 struct MoePlan {
     MoeParams p;
-    int nt, ctas;
+    int ctas, h_groups;
     int64_t gu_stride, d_stride;            // bytes from one expert to the next
     size_t smem, ws;
 };
@@ -712,37 +711,40 @@ static ccl_status plan_moe(const ccl_moe_desc* d, int sms, MoePlan* plan) {
     const int64_t nb1 = (d->H + kMoeBlockK - 1) / kMoeBlockK;
     p.x_pitch = (int32_t)(nb1 * 128 + 64);               // (not a multiple of 128: neighbouring rows start in different banks)
     const int pairs = (int)(d->T * d->topk);
-    // Tokens of an expert taken together, in column groups of 8.  An expert with more is taken several times, its weights re-read
-    // (from the L2, they were just used); more columns cost registers, and shared memory for their rows of x.
-    for (plan->nt = d->T <= 8 ? 1 : 2;; plan->nt /= 2) {
-        const size_t keys = (size_t)(d->T <= 8 ? d->T : 1) * (size_t)((d->E + 3) / 4 * 16 + kMoeMaxK * 8);   // the top-k's
-        const size_t red = std::max((size_t)2 * 2 * plan->nt * kMoeThreads * 16, up128(keys)), yacc = (size_t)kMoeWarps * (size_t)d->T * kMoeRows * 4;
-        const size_t lists = up128((size_t)2 * kMoeWarps * kMoeDepth * 8 + 32) + up128((size_t)d->E * 8) + up128((size_t)d->E * 2) + up128((size_t)(std::min(pairs, d->E) + pairs) * 4) + up128((size_t)pairs * 8) +
-                             up128((size_t)pairs * 4) + up128((size_t)pairs * 2);
-        const int64_t rows = ((int64_t)kMoeSmem - 1024 - kMoeRing - (int64_t)(red + lists)) / p.x_pitch;        // of x that there is room for
-        p.all_x = d->T <= rows;
-        p.group = (int32_t)std::min<int64_t>(plan->nt * 8, std::min(d->T, rows));
-        if (plan->nt > 1 && p.group <= plan->nt * 4) continue;
-        if (p.group < 1) return fail(CCL_ERR_UNSUPPORTED, "ccl_moe_tokens: this problem does not fit shared memory");
-        size_t at = kMoeRing;
+    // Groups of 4 of an expert's tokens, at most
+    plan->h_groups = (pairs + 3 * std::min(pairs, d->E)) / 4;
+    for (p.depth = kMoeDepth;; --p.depth) {
+        if (p.depth < 2) return fail(CCL_ERR_UNSUPPORTED, "ccl_moe_tokens: this problem does not fit shared memory");
+        const size_t room = kMoeSmem - 1024, ring = (size_t)kMoeWarps * p.depth * kMoeBlock;       // (the rings start at multiples of 1024)
+        size_t at = ring;
         auto take = [&](size_t bytes) { const size_t a = at; at += up128(bytes); return (int32_t)a; };
-        p.at_bars = take((size_t)2 * kMoeWarps * kMoeDepth * 8 + 32);
-        // x and the units' partial sums; phase 3 has its sums where both were
-        p.at_region = take((size_t)(p.all_x ? d->T : p.group) * (size_t)p.x_pitch);
-        p.at_red = take(red);
-        at = std::max(at, (size_t)p.at_region + up128(yacc));
+        p.at_bars = take((size_t)(3 * kMoeWarps * kMoeDepth + 3) * 8 + 16);
         p.at_mask = take((size_t)d->E * 8);
         p.at_off = take((size_t)d->E * 2);
-        p.at_ent = take((size_t)(std::min(pairs, d->E) + pairs / p.group) * 4);
         p.at_sel = take((size_t)pairs * 2);
         p.at_selw = take((size_t)pairs * 4);
         p.at_pair = take((size_t)pairs * 8);
-        plan->smem = at + 1024;                          // (the ring starts at a multiple of 1024)
-        if (plan->smem > kMoeSmem) return fail(CCL_ERR_UNSUPPORTED, "ccl_moe_tokens: this problem does not fit shared memory");
-        break;
+        const int most = std::min(pairs, d->E) + pairs / 4;                                        // entries
+        p.at_ent = take((size_t)most * 4);
+        p.at_hgroup = take((size_t)most * 2);
+        at = (at + 1023) & ~(size_t)1023;
+        // x and the units' partial sums (before them the top-k's keys); in phase 3 its own sums and h where both were
+        const size_t keys = (size_t)(d->T <= 8 ? d->T : 1) * (size_t)((d->E + 3) / 4 * 16 + kMoeMaxK * 8);
+        const size_t red = std::max((size_t)2 * 2 * kMoeThreads * 16, up128(keys)), yacc = ((size_t)kMoeWarps * (size_t)d->T * kMoeRows * 4 + 1023) & ~(size_t)1023;
+        if (at + red > room) continue;
+        const int64_t rows = (int64_t)((room - at - red) / (size_t)p.x_pitch);                     // of x that there is room for
+        p.all_x = d->T <= rows;
+        p.group = rows >= kMoeGroup || p.all_x ? kMoeGroup : 4;
+        if (rows < std::min<int64_t>(4, d->T)) continue;
+        p.at_region = (int32_t)at;
+        p.at_hring = (int32_t)(at + yacc);
+        p.at_red = take((size_t)(p.all_x ? d->T : p.group) * (size_t)p.x_pitch);                   // (x)
+        p.at_red = take(red);
+        plan->smem = std::max(at, (size_t)p.at_hring + (size_t)kMoeWarps * p.depth * kMoeHBlock) + 1024;
+        if (plan->smem <= kMoeSmem) break;
     }
     p.h_pitch = (int64_t)up128((size_t)d->I * 2);
-    plan->ws = up128((size_t)(d->T * d->E) * 4) + up128((size_t)(plan->ctas + 32 + pairs) * 8) + (size_t)(pairs * 2 + 16 * plan->nt) * (size_t)p.h_pitch;
+    plan->ws = up128((size_t)(d->T * d->E) * 4) + up128((size_t)(plan->ctas + 32 + pairs) * 8) + (size_t)plan->h_groups * 8 * (size_t)p.h_pitch;
     return CCL_OK;
 }
 
@@ -753,13 +755,12 @@ static int moe_sms() {
     return 148;
 }
 
-template <int NT>
 static ccl_status launch_moe(const MoePlan& plan, const CUtensorMap& map_gu, const CUtensorMap& map_d, cudaStream_t st) {
     static std::atomic<uint64_t> configured{0};
     int dev = 0;
     CCL_CUDA_TRY(cudaGetDevice(&dev));
     if (dev >= 64 || !(configured.load() >> dev & 1)) {
-        CCL_CUDA_TRY(cudaFuncSetAttribute(moe_tokens_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMoeSmem));
+        CCL_CUDA_TRY(cudaFuncSetAttribute(moe_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMoeSmem));
         if (dev < 64) configured.fetch_or(1ull << dev);
     }
     cudaLaunchConfig_t cfg = {};
@@ -774,7 +775,7 @@ static ccl_status launch_moe(const MoePlan& plan, const CUtensorMap& map_gu, con
     attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, moe_tokens_kernel<NT>, map_gu, map_d, plan.p));
+    CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, moe_tokens_kernel, map_gu, map_d, plan.p));
     count_launch();
     return CCL_OK;
 }
@@ -841,9 +842,5 @@ extern "C" ccl_status ccl_moe_tokens(const ccl_moe_desc* d, const void* X_dev, c
         const uint32_t dbox[3] = {kMoeBlockK, (uint32_t)p.rows_per_block, 1};
         if ((s = encode_tmap(&map_d, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, Wd_dev, ddims, dstrides, dbox, CU_TENSOR_MAP_SWIZZLE_128B))) return s;
     }
-    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-    switch (plan.nt) {
-        case 1: return launch_moe<1>(plan, map_gu, map_d, st);
-        default: return launch_moe<2>(plan, map_gu, map_d, st);
-    }
+    return launch_moe(plan, map_gu, map_d, reinterpret_cast<cudaStream_t>(cuda_stream));
 }

@@ -118,10 +118,13 @@ __device__ __forceinline__ void st_release(unsigned long long* p, unsigned long 
 // when every CTA adds to one counter and one thread of each reads it; 4.9 us when 148 threads of every CTA read a flag of each.
 // The counter needs a start, so the first meeting has flags -- any contents but this launch's mark mean "not yet" -- that CTA 0 alone
 // reads, and a word by which it lets the others go; it clears the counters of the later ones on the way.
-__device__ __forceinline__ bool meet_first(const MoeParams& p) {
+// `meanwhile` is done between a CTA's arrival and its wait.
+template <typename F>
+__device__ __forceinline__ bool meet_first(const MoeParams& p, F meanwhile) {
     bar_consumers();
     bool ok = true;
     if (threadIdx.x == 0) st_release(p.flags + blockIdx.x, p.mark);
+    meanwhile();
     if (blockIdx.x == 0) {
 #pragma unroll 1
         for (unsigned i = threadIdx.x; i < gridDim.x; i += kMoeThreads) ok = wait_word(p.flags + i, p.mark, true) && ok;
@@ -277,8 +280,7 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
             bar_consumers();
         }
     }
-    if (p.all_x) stage_x(p.T, [](int t) { return t; });
-    bool met1 = meet_first(p);
+    bool met1 = meet_first(p, [&]() { if (p.all_x) stage_x(p.T, [](int t) { return t; }); });
     if (threadIdx.x == 0) { shared[1] = met1; p.flags[cta] = 0; }        // (cleared for the next launch, which may be this one replayed)
     // top-k of a token: an expert's place is the number of those before it (a larger logit, or an equal one of a lower expert), a
     // thread an expert against all of them in shared memory.  Up to 8 tokens are worked out by every CTA for itself; of more, each

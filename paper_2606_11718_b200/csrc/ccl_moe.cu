@@ -116,20 +116,26 @@ __device__ __noinline__ bool wait_word(const unsigned long long* word, unsigned 
 __device__ __forceinline__ void st_release(unsigned long long* p, unsigned long long v) { asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(p), "l"(v) : "memory"); }
 // The grid's meetings (all consumer threads call; what a CTA wrote before is seen by all behind it).  Measured, 148 CTAs: 1.3 us
 // when every CTA adds to one counter and one thread of each reads it; 4.9 us when 148 threads of every CTA read a flag of each.
-// The counter needs a start, so the first meeting has flags -- any contents but this launch's mark mean "not yet" -- that CTA 0 alone
-// reads, and a word by which it lets the others go; it clears the counters of the later ones on the way.
-// `meanwhile` is done between a CTA's arrival and its wait.
+// The counter needs a start, so the first meeting -- which ends when the `writers`, the first CTAs of the grid, have their logits out
+// -- has flags (any contents but this launch's mark mean "not yet").  Up to 16 of them are read by every CTA (one token, 8 writers:
+// 1.2 us less than the other way); of more, CTA 0 alone reads them and lets the others go by a word.  CTA 0 clears the counters of
+// the later meetings on the way.  `meanwhile` is done between a CTA's arrival and its wait.
+constexpr int kMoeReaders = 16;
 template <typename F>
-__device__ __forceinline__ bool meet_first(const MoeParams& p, F meanwhile) {
+__device__ __forceinline__ bool meet_first(const MoeParams& p, int writers, F meanwhile) {
     bar_consumers();
     bool ok = true;
-    if (threadIdx.x == 0) st_release(p.flags + blockIdx.x, p.mark);
+    if (threadIdx.x == 0 && (int)blockIdx.x < writers) {
+        if (blockIdx.x == 0) p.gate[1] = p.gate[2] = 0;
+        st_release(p.flags + blockIdx.x, p.mark);
+    }
     meanwhile();
-    if (blockIdx.x == 0) {
+    const bool all = writers <= kMoeReaders;
+    if (all || blockIdx.x == 0) {
 #pragma unroll 1
-        for (unsigned i = threadIdx.x; i < gridDim.x; i += kMoeThreads) ok = wait_word(p.flags + i, p.mark, true) && ok;
+        for (int i = threadIdx.x; i < writers; i += kMoeThreads) ok = wait_word(p.flags + i, p.mark, true) && ok;
         ok = bar_consumers_and(ok);
-        if (threadIdx.x == 0 && ok) { p.gate[1] = p.gate[2] = 0; st_release(p.gate, p.mark); }
+        if (threadIdx.x == 0 && ok && !all) st_release(p.gate, p.mark);
     } else {
         if (threadIdx.x == 0) ok = wait_word(p.gate, p.mark, true);
         ok = bar_consumers_and(ok);
@@ -280,8 +286,8 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
             bar_consumers();
         }
     }
-    bool met1 = meet_first(p, [&]() { if (p.all_x) stage_x(p.T, [](int t) { return t; }); });
-    if (threadIdx.x == 0) { shared[1] = met1; p.flags[cta] = 0; }        // (cleared for the next launch, which may be this one replayed)
+    bool met1 = meet_first(p, min(ctas, (p.E + 15) / 16 * ((p.T + 7) / 8)), [&]() { if (p.all_x) stage_x(p.T, [](int t) { return t; }); });
+    if (threadIdx.x == 0) shared[1] = met1;
     // top-k of a token: an expert's place is the number of those before it (a larger logit, or an equal one of a lower expert), a
     // thread an expert against all of them in shared memory.  Up to 8 tokens are worked out by every CTA for itself; of more, each
     // by one CTA, and the grid meets once more: 64 tokens x 128 experts took 10 us the first way, a warp a token.
@@ -291,6 +297,7 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
         uint32_t* keys = reinterpret_cast<uint32_t*>(smem + p.at_red);           // [token][ep]
         float* vals = reinterpret_cast<float*>(keys + nt * ep);                  // [token][16]: the chosen logits, best first
         int* who = reinterpret_cast<int*>(vals + nt * kMoeMaxK);                 // ... and their experts
+#pragma unroll 4
         for (int i = threadIdx.x; i < nt * ep; i += kMoeThreads) {
             const int t = i / ep, e = i - t * ep;
             keys[i] = e < p.E ? order_key(__ldcg(p.logits + (int64_t)(first + t) * p.E + e)) : 0u;
@@ -589,7 +596,10 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
     }
     const bool met = meet_counted(p.gate + 1);
     if (threadIdx.x == 0) { shared[2] = met; mbar_arrive(met_bar); }
-    if (cta == 0 && threadIdx.x == 0) p.gate[0] = 0;      // (everyone is past the first meeting)
+    if (met && threadIdx.x == 0) {                        // everyone is past the first meeting: cleared for the next launch, which may be this one replayed
+        p.flags[cta] = 0;
+        if (cta == 0) p.gate[0] = 0;
+    }
 
     // ---- 3. down -------------------------------------------------------------------------------------------------------
     {

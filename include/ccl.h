@@ -288,7 +288,7 @@ ccl_status ccl_gemm_swiglu(const ccl_gemm_desc* d, const void* A_dev, const void
 /*
  * Synchronises `cuda_stream` (the one entry point that does), then reports and clears the status word of the
  * GEMMs and repacks finished on the current device: CCL_OK, or CCL_ERR_TIMEOUT with *detail = the raw device code
- * (1-6: a GEMM wait, 101: a repack wait), or CCL_ERR_SHAPE (detail 5) for bad offsets of a ragged batch.
+ * (1-6: a GEMM wait, 8-9: ccl_moe_tokens, 101: a repack wait), or CCL_ERR_SHAPE (detail 5) for bad offsets of a ragged batch.
  * detail may be NULL.  There is ONE status word per device, shared by every stream: with several streams in flight
  * the first caller after an expiry gets the report, whichever stream's kernel it was.
  */
@@ -402,8 +402,8 @@ ccl_status ccl_bias_act_grad(const ccl_mat* m, int32_t act, const void* dY_dev, 
  * Requirements: 1 <= T <= 64, 1 <= E <= 512, 1 <= topk <= min(E, 16), H in [8, 8192] and I in [8, 32768] multiples of 8, gu_strips a divisor of
  * I / 8 (else CCL_ERR_SHAPE / CCL_ERR_UNSUPPORTED); X, residual, Y, Wr, Wgu, Wd and the workspace 16-byte aligned, strides multiples of
  * 16 bytes (else CCL_ERR_ALIGN).
- * One cooperative launch of one CTA per SM, which meet at two grid-wide barriers; the waits are bounded and reported by
- * ccl_gemm_status (code 8).  A logit that is NaN is never chosen before a number; NaN inputs give NaN outputs for their token.
+ * One cooperative launch of one CTA per SM, which meet at two or three grid-wide barriers; every wait is bounded and reported by
+ * ccl_gemm_status (codes 8 and 9).  A logit that is NaN is never chosen before a number; NaN inputs give NaN outputs for their token.
  * Workspace: ccl_moe_tokens_workspace bytes, whatever they hold; calls that can overlap on the GPU must not share it.  The result does
  * not depend on the order in which CTAs run.
  */

@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(256) column_sum_finish_kernel(const float* par
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, n = blockIdx.x * 32 + lane;
     float s = 0.0f;
     if (n < N)
-#pragma unroll 4
+#pragma unroll 16                                        // (sixteen loads in flight: the time is a trip or two to the L2)
         for (int b = w; b < blocks; b += 8) s += partial[(int64_t)b * N + n];
     part[w][lane] = s;
     __syncthreads();

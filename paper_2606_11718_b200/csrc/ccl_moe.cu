@@ -4,8 +4,9 @@
 // Bound by memory: every chosen expert's weights are read once (3 H I elements each) and nothing else is of that order; with
 // m tokens an expert the arithmetic is 2 m flops per 2-byte weight, far below what the tensor cores take.  So the kernel is a
 // stream of weights through shared memory that stops for nothing it can avoid:
-//   1. router: the CTAs share the E x T dot products; first meeting of the grid; every CTA then works out the same top-k and the
-//      same lists of tokens per expert by itself
+//   1. router: the CTAs share the E x T dot products (16 experts x 8 tokens a matrix product); first meeting of the grid; top-k, by
+//      every CTA for itself for up to 8 tokens, by a CTA a token and with one more meeting for more; every CTA works out the same lists
+//      of tokens per expert
 //   2. gate and up: the (expert, 16 features) units are shared out evenly.  A unit is 32 weight rows -- 16 gate, 16 up -- times
 //      its expert's tokens (n = 8 columns): two m16n8k16 accumulators then hold the gate and the up value of a
 //      feature in the same lane, and silu(gate) * up needs no exchange.  h goes to the workspace; second meeting
@@ -14,9 +15,12 @@
 // The k range of a unit is dealt out in blocks of 64 (32 rows x 128 bytes) to the 8 consumer warps of the CTA in turn (phase 3: to
 // the 16 of the pair).  A ninth warp fetches the blocks, one TMA copy each, up to 32 of them ahead: it stops for nothing but a
 // full ring, runs ahead across units and from phase 2 into phase 3, so the weights of phase 3 arrive during the second meeting.
-// A tenth fetches the h that goes with phase 3's blocks, by cp.async: the TMA takes ~60 ns a block as it is (a 128-byte row every four
+// Four more fetch the h that goes with phase 3's blocks, by cp.async: the TMA takes ~60 ns a block as it is (a 128-byte row every four
 // cycles), and h by TMA as well had the products wait.  (Consumers that issued their own copies, or read h themselves, made loops
-// that were slower to run than the weights to come: phase 3 of 64 tokens x 128 experts of 2048 x 768 took 118 and 86 us.)
+// that were slower to run than the weights to come: phase 3 of 64 tokens x 128 experts of 2048 x 768 took 118 and 86 us, 66 now.)
+//
+// Measured (B200, 128 experts of 2048 x 768, 8 a token): 64 tokens 215 us, 5.5 TB/s over everything and above 6 while weights stream;
+// 16 tokens 136 us; one token 29.6 us, of which the weights take 12 and the rest is launch, router, top-k and two meetings.
 //
 // The matrix instructions are mma.sync: with n = 8 columns a tcgen05 tile would be 128 rows high and leave most SMs without
 // work for one token; they are nowhere near their limit here.  Weights and tokens are both K-contiguous, so a lane may take any 8
@@ -82,11 +86,6 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool o
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ unsigned long long ld_acquire_flag(const unsigned long long* p) {
-    unsigned long long v;
-    asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
-    return v;
 }
 // All consumer threads
 __device__ __forceinline__ void bar_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(kMoeThreads) : "memory"); }
@@ -243,7 +242,6 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
     // ---- 1. router --------------------------------------------------------------------------------------------------
     // an item is 16 experts' rows times up to 8 tokens, one matrix product; the warps split its k range
     if (warp < kMoeWarps) {
-    {
         float4* part = reinterpret_cast<float4*>(smem + p.at_red);
         const int g = lane >> 2, q = lane & 3, ne = (p.E + 15) / 16, ntb = (p.T + 7) / 8, steps = (p.H + 31) / 32;
 #pragma unroll 1
@@ -285,7 +283,6 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
             }
             bar_consumers();
         }
-    }
     bool met1 = meet_first(p, min(ctas, (p.E + 15) / 16 * ((p.T + 7) / 8)), [&]() { if (p.all_x) stage_x(p.T, [](int t) { return t; }); });
     if (threadIdx.x == 0) shared[1] = met1;
     // top-k of a token: an expert's place is the number of those before it (a larger logit, or an equal one of a lower expert), a
@@ -321,31 +318,29 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
         if (warp < nt) {
             const int t = first + warp;
             keys += warp * ep; vals += warp * kMoeMaxK; who += warp * kMoeMaxK;
-            {
-                const float top = vals[0];
-                float sum = 0.0f, w = 0.0f;
-                bool nan = false;
-                if (lane < p.topk) w = __expf(vals[lane] - top);
-                for (int e = lane; e < p.E; e += 32) {
-                    nan |= keys[e] == 1u;
-                    if (!p.norm) sum += __expf(key_value(keys[e]) - top);
-                }
-                if (p.norm) sum = w;
+            const float top = vals[0];
+            float sum = 0.0f, w = 0.0f;
+            bool nan = false;
+            if (lane < p.topk) w = __expf(vals[lane] - top);
+            for (int e = lane; e < p.E; e += 32) {
+                nan |= keys[e] == 1u;
+                if (!p.norm) sum += __expf(key_value(keys[e]) - top);
+            }
+            if (p.norm) sum = w;
 #pragma unroll
-                for (int m = 16; m >= 1; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-                nan = __any_sync(0xffffffffu, nan);
-                if (lane < p.topk) {
-                    const int at = t * p.topk + lane, e = who[lane];
-                    w = nan ? __int_as_float(0x7fffffff) : w / sum;
-                    if (every) {
-                        sel[at] = (uint16_t)e;
-                        selw[at] = w;
-                        atomicOr(reinterpret_cast<uint32_t*>(mask + e), 1u << t);    // (in whatever order the bits arrive; 64-bit ones are emulated)
-                    } else p.choice[at] = make_int2(e, __float_as_int(w));
-                    if (!every || cta == 0) {
-                        if (p.ids) p.ids[at] = e;
-                        if (p.weights) p.weights[at] = w;
-                    }
+            for (int m = 16; m >= 1; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+            nan = __any_sync(0xffffffffu, nan);
+            if (lane < p.topk) {
+                const int at = t * p.topk + lane, e = who[lane];
+                w = nan ? __int_as_float(0x7fffffff) : w / sum;
+                if (every) {
+                    sel[at] = (uint16_t)e;
+                    selw[at] = w;
+                    atomicOr(reinterpret_cast<uint32_t*>(mask + e), 1u << t);    // (in whatever order the bits arrive; 64-bit ones are emulated)
+                } else p.choice[at] = make_int2(e, __float_as_int(w));
+                if (!every || cta == 0) {
+                    if (p.ids) p.ids[at] = e;
+                    if (p.weights) p.weights[at] = w;
                 }
             }
         }
@@ -717,6 +712,7 @@ static ccl_status plan_moe(const ccl_moe_desc* d, int sms, MoePlan* plan) {
     plan->gu_stride = d->gu_stride_bytes ? d->gu_stride_bytes : gu; plan->d_stride = d->d_stride_bytes ? d->d_stride_bytes : dn;
     if (plan->gu_stride >= (INT64_C(1) << 40) || plan->d_stride >= (INT64_C(1) << 40)) return fail(CCL_ERR_UNSUPPORTED, "ccl_moe_tokens: an expert stride is too large for a tensor map");
     plan->ctas = sms & ~1;                               // CTA pairs
+    if (plan->ctas < d->T) return fail(CCL_ERR_UNSUPPORTED, "ccl_moe_tokens: %lld tokens need as many SMs (the device has %d)", (long long)d->T, sms);
     const int64_t pr = sms / 2, per = (d->H + pr * kMoeRows - 1) / (pr * kMoeRows);          // row blocks a pair takes
     p.rows_per_block = (int32_t)((d->H + pr * per - 1) / (pr * per));
     p.blocks = (int32_t)((d->H + p.rows_per_block - 1) / p.rows_per_block);

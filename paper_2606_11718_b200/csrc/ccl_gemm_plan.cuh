@@ -254,10 +254,12 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
                 const int64_t waves = (tiles * sp + units - 1) / units;
                 // (a last wave that leaves SMs idle streams a little slower: measured ~5 % between 96 and 128 busy SMs)
                 const double last = (double)(tiles * sp - (waves - 1) * units) / (double)units;
-                // an operator in the epilogue: ~6000 cycles a piece and warp (four pieces side by side), behind the next tile's
-                // product where the accumulator is double-buffered, in the open otherwise (measured, 4096 x 28672 x 8192: 1363 us
-                // with 256 x 256 pair tiles, 1469 with 256 x 512, which ccl_gemm prefers)
-                const double t_op = epi ? 6000.0 * ((b + 255) / 256) : 0.0;
+                // an operator in the epilogue: its pieces run side by side, and more of them get in each other's way (measured,
+                // 1 x 4360 x 72: 6.7 us with 128 columns, 8.5 with 256; 304 x 22912 x 96, two rounds of 256 columns or four of
+                // 128: 15.2 and 19.3), behind the next tile's product where the accumulator is double-buffered, in the open
+                // otherwise (measured, 4096 x 28672 x 8192: 1363 us with 256 x 256 pair tiles, 1469 with 256 x 512, which
+                // ccl_gemm prefers)
+                const double t_op = epi ? 2000.0 + 17.0 * b : 0.0;
                 const double per_tile = !epi || sp > 1 ? (double)kbps * t_kb + (sp > 1 ? 2.0 * t_drain : t_drain)
                                                        : (b <= 256 ? std::max((double)kbps * t_kb, t_op) + 500.0 : (double)kbps * t_kb + t_op + t_drain);
                 double cost = std::max((double)waves * per_tile + (epi && b <= 256 ? t_op : 0.0), stream_clk * (1.0 + 0.1 * (1.0 - last))) + 3000.0;
@@ -349,7 +351,9 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
                 if ((num_kb + kbps - 1) / kbps != k || kbps < 2) continue;           // every CTA of the cluster owns k blocks
                 // drain, the exchange (every CTA sends (k - 1) / k of its sums and adds up k sources: ~1000 cycles per CTA of
                 // the cluster, measured on 256 x 768 x 2048: 7.0 / 7.4 / 7.9 / 8.5 us with clusters of 4 / 3 / 6 / 8), launch
-                const double cost = (double)kbps * kblock_cycles(b, 1, bt, tiles * k) + 1500.0 + (1000.0 + 1000.0 * k) + 3000.0;
+                // (an operator's kernel exchanges with four times the warps: 17 x 192 x 1032 takes 5.8 us with clusters of 4,
+                // 7.3 with 2; and pays for width: 1 x 8192 x 2048 takes 11.3 us with 128 columns and clusters of 2, 14.0 with 256 and 4)
+                const double cost = (double)kbps * kblock_cycles(b, 1, bt, tiles * k) + 1500.0 + (1000.0 + (epi ? 600.0 : 1000.0) * k) + (epi ? 12.0 * b : 0.0) + 3000.0;
                 if (best_ks < 0 || cost < best_ks) { best_ks = cost; kb_ = b; kk = k; }
             }
         }

@@ -60,8 +60,6 @@ static ccl_status launch_variant(const GemmPlan& plan, const CUtensorMap* maps, 
         return plan.bn == 256 ? launch_epi<256, 1, true, 0, EPI>(plan, maps, em, st) : launch_epi<128, 1, true, 0, EPI>(plan, maps, em, st);
     }
     switch (plan.bn * 10 + plan.ctas) {
-        case 5122: return launch_epi<512, 2, false, 0, EPI>(plan, maps, em, st);
-        case 3842: return launch_epi<384, 2, false, 0, EPI>(plan, maps, em, st);
         case 2562: return launch_epi<256, 2, false, 0, EPI>(plan, maps, em, st);
         case 1922: return launch_epi<192, 2, false, 0, EPI>(plan, maps, em, st);
         case 1282: return launch_epi<128, 2, false, 0, EPI>(plan, maps, em, st);
@@ -236,7 +234,7 @@ ccl_status launch_with_maps(const GemmPlan& plan, const CUtensorMap* maps, cudaS
 
 ccl_status encode_maps(const GemmPlan& plan, const void* A, const void* B, void* C, CUtensorMap* m) {
     const GemmParams& p = plan.p;
-    const uint32_t bnh = plan.bn == 384 ? 64u : (uint32_t)(plan.subn / plan.ctas);   // B rows of one K-major box
+    const uint32_t bnh = (uint32_t)(plan.subn / plan.ctas);   // B rows of one K-major box
     struct { const MatView* v; const void* base; uint32_t inner, rows; } op[3] = {
         {&plan.va, A, p.a_mn ? 64u : (uint32_t)BK, p.a_mn ? (uint32_t)BK : (uint32_t)plan.a_box_rows},
         {&plan.vb, B, p.b_mn ? 64u : (uint32_t)BK, p.b_mn ? (uint32_t)BK : bnh},

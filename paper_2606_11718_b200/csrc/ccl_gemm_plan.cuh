@@ -228,7 +228,11 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
             if (c == 1 && b > 256) continue;
             if (c == 2 && b == 192 && !bt && il_b) continue;    // 96 columns per CTA of an N-contiguous B: a box and a half (see the kernel), not across chunks
             if (b == 192 && (c == 2 ? no_192_pair : no_192)) continue;
-            if (epi_full && b != 256 && b != 128) continue;
+            // an operator in the epilogue takes tiles whose accumulator is double-buffered: with 256 x 512 pair tiles it stands in
+            // the open (4096 x 28672 x 8192: 1363 us with 256 columns, 1469 with 512; 4096 x 8192 x 28672: 1262 and 1500, 384
+            // columns 1526; 2048 x 5120 x 13824: 252, 362 and 273)
+            if (epi && b > 256) continue;
+            if (epi_full && b == 192) continue;
             if (b == 384 && (cap > 0 || ragk)) continue;            // (no ragged-batch instantiation of the 256 + 128 tile)
             if (force_bn && atoi(force_bn) != b) continue;
             if (swiglu && !(c == 2 && b == 512)) continue;          // the gated activation pairs the two accumulators of the wide tile
@@ -248,6 +252,9 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
             for (int sp : {1, 2, 3, 4, 6, 8, 12, 16}) {
                 if (sp > 1 && (swiglu || cap > 0 || ragk || any_rag || num_kb / sp < 2)) continue;
                 if (force_split && atoi(force_split) != sp) continue;
+                // (an operator after a split is a kernel of its own over the partial sums: 2048 x 5120 x 13824, 160 tiles on 74
+                // pairs, takes 261 us whole and 346 in three parts)
+                if (epi && sp > 1 && tiles >= units && !force_split) continue;
                 const int64_t kbps = (num_kb + sp - 1) / sp;
                 const int64_t sp_eff = (num_kb + kbps - 1) / kbps;          // every split owns at least one k block
                 if (sp_eff != sp) continue;
@@ -256,13 +263,11 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
                 const double last = (double)(tiles * sp - (waves - 1) * units) / (double)units;
                 // an operator in the epilogue: its pieces run side by side, and more of them get in each other's way (measured,
                 // 1 x 4360 x 72: 6.7 us with 128 columns, 8.5 with 256; 304 x 22912 x 96, two rounds of 256 columns or four of
-                // 128: 15.2 and 19.3), behind the next tile's product where the accumulator is double-buffered, in the open
-                // otherwise (measured, 4096 x 28672 x 8192: 1363 us with 256 x 256 pair tiles, 1469 with 256 x 512, which
-                // ccl_gemm prefers)
+                // 128: 15.2 and 19.3), behind the next tile's product
                 const double t_op = epi ? 2000.0 + 17.0 * b : 0.0;
                 const double per_tile = !epi || sp > 1 ? (double)kbps * t_kb + (sp > 1 ? 2.0 * t_drain : t_drain)
-                                                       : (b <= 256 ? std::max((double)kbps * t_kb, t_op) + 500.0 : (double)kbps * t_kb + t_op + t_drain);
-                double cost = std::max((double)waves * per_tile + (epi && b <= 256 ? t_op : 0.0), stream_clk * (1.0 + 0.1 * (1.0 - last))) + 3000.0;
+                                                       : std::max((double)kbps * t_kb, t_op) + 500.0;
+                double cost = std::max((double)waves * per_tile + t_op, stream_clk * (1.0 + 0.1 * (1.0 - last))) + 3000.0;
                 // a problem that runs for long runs at the power cap, where the clock follows the energy a k block costs:
                 // measured, 256 x 256 pair tiles (a third more operand bytes per flop than 256 x 512) take 3-6 % longer on
                 // the Llama-size GEMMs although they need fewer cycles

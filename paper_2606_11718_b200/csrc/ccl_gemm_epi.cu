@@ -21,7 +21,7 @@ static ccl_status launch_epi(const GemmPlan& plan, const CUtensorMap* maps, cons
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(plan.grid, 1, 1);
-    cfg.blockDim = dim3(gemm_threads<EPI>, 1, 1);
+    cfg.blockDim = dim3(gemm_threads<EPI, KS>, 1, 1);
     cfg.dynamicSmemBytes = plan.smem_bytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];

@@ -27,21 +27,23 @@ constexpr int BK = 64;
 #endif
 constexpr int kEpiWarps = CCL_EPI_WARPS;        // 4, or 8: two warps per TMEM lane quadrant taking alternate 64-column pieces
 constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
-// The kernels with an operator in the epilogue (EPI != 0) drain with sixteen warps, one 64-column piece of a 256-wide tile each:
-// their arithmetic -- an exponential, a reciprocal and some twenty instructions a value -- has the time of the next tile's product,
-// and what eight warps lost was latency (4096 x 8192 x 2048 with gelu's slope: 140 us with eight, 94 for the plain product).
-constexpr int kEpiOpWarps = 16;
+// The kernels with an operator in the epilogue (EPI != 0) drain with eight warps, two 64-column pieces of a 256-wide tile each.
+// Their arithmetic has the time of the next tile's product; what it costs is the ring: pieces of the addend and of C that move
+// all at once hold up the operands behind them in the TMA unit, and every 4 KB buffer is taken from the ring.  4096 x 8192 x 2048,
+// no operator at all: 92 us with eight warps and six stages, 99 with sixteen and five, 106 with four stages; relu's slope 98 and
+// 107.  The cluster split drains once, from the exchanged sums, with sixteen (777 x 1544 x 1000: 14.2 us, 15.6 with eight).
+constexpr int kEpiOpWarps = 8, kEpiOpWarpsKs = 16;
 // (the cluster split exchanges its partial sums in the ring and stores from registers: no staging, a longer ring)
 template <int EPI, int KS> constexpr uint32_t staging_bytes = EPI ? (KS ? 0u : kEpiOpWarps * 32u * 128u) : 4u * 2 * 32 * 128;
-template <int EPI> constexpr int epi_warps = EPI ? kEpiOpWarps : kEpiWarps;
-template <int EPI> constexpr int gemm_threads = 64 + 32 * epi_warps<EPI>;
+template <int EPI, int KS> constexpr int epi_warps = EPI ? (KS ? kEpiOpWarpsKs : kEpiOpWarps) : kEpiWarps;
+template <int EPI, int KS> constexpr int gemm_threads = 64 + 32 * epi_warps<EPI, KS>;
 constexpr int kTmemCols = 512;
 constexpr uint32_t kSmemBudget = 192 * 1024;    // ring of operand stages
 constexpr int64_t kRaggedDense = 4096;         // problems of a ragged batch whose tile prefix is kept in shared memory
 constexpr uint32_t kEpiBytes = 4 * 2 * 32 * 128; // epilogue staging: per warp two buffers of 32 rows x 128 B
 constexpr uint32_t kSmemBudgetOpKs = 224 * 1024;
-constexpr uint32_t kSmemBudgetOp = 160 * 1024;  // EPI: a shorter ring,
-constexpr uint32_t kEpiBytesOp = kEpiOpWarps * 32 * 128;       // and a buffer for each of the sixteen warps, in which an addend's piece becomes C's
+constexpr uint32_t kSmemBudgetOp = 192 * 1024;
+constexpr uint32_t kEpiBytesOp = kEpiOpWarps * 32 * 128;       // EPI: a buffer for each warp, in which an addend's piece becomes C's
 
 static __device__ int g_gemm_status = 0;
 
@@ -577,7 +579,7 @@ struct Scheduler {
 // EPI: 1 = bias, activation and residual in the epilogue (ccl_gemm_epilogue), 2 = activation slope and column sums
 // (ccl_gemm_act_grad)
 template <int BN, int CTAS, bool SWIGLU = false, int RAG = 0, bool FULL = true, int KS = 0, int EPI = 0>
-__global__ void __launch_bounds__(gemm_threads<EPI>, 1)
+__global__ void __launch_bounds__(gemm_threads<EPI, KS>, 1)
 ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                 const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_a2,
                 const __grid_constant__ CUtensorMap map_b2, const __grid_constant__ CUtensorMap map_c2,
@@ -592,7 +594,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         static_assert(sizeof(GemmParams) % 4 == 0, "GemmParams is copied word by word");
         const uint32_t* src = reinterpret_cast<const uint32_t*>(&gp);
         uint32_t* dst = reinterpret_cast<uint32_t*>(&p);
-        for (int i = threadIdx.x; i < (int)(sizeof(GemmParams) / 4); i += gemm_threads<EPI>) dst[i] = src[i];
+        for (int i = threadIdx.x; i < (int)(sizeof(GemmParams) / 4); i += gemm_threads<EPI, KS>) dst[i] = src[i];
     }
     // A tile wider than 256 columns is computed as two sub-tiles (one MMA each per k step), the first 256 columns wide,
     // the second the rest (256 or 128), each with a 256-column half of TMEM; narrower tiles use the two halves as a
@@ -634,7 +636,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         prefetch_tmap(&map_b);
         prefetch_tmap(&map_c);
         for (int s = 0; s < gp.stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int a = 0; a < NACC; ++a) { mbar_init(&tmem_full[a], 1); mbar_init(&tmem_empty[a], epi_warps<EPI> * CTAS); }
+        for (int a = 0; a < NACC; ++a) { mbar_init(&tmem_full[a], 1); mbar_init(&tmem_empty[a], epi_warps<EPI, KS> * CTAS); }
         if constexpr (EPI != 0)
             for (int w = 0; w < kEpiOpWarps; ++w) mbar_init(&addend_full[w], 1);
         fence_barrier_init();
@@ -894,7 +896,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         // ------------------------------------------------------------------ epilogue (warps 2..5)
         if (RAG == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
         const int quad = warp & 3;                       // TMEM lane quadrant this warp may read
-        constexpr int EW = epi_warps<EPI> / 4;         // warps per quadrant
+        constexpr int EW = epi_warps<EPI, KS> / 4;         // warps per quadrant
         const int hf = (warp - 2) >> 2;                  // which of them this one is
         const uint32_t tmem_empty0 = CTAS == 2 ? map_to_cta(smem_u32(&tmem_empty[0]), 0) : smem_u32(&tmem_empty[0]);
         TileCoord t;

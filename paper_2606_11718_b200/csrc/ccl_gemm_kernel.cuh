@@ -295,6 +295,15 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
           "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(taddr) : "memory");
 }
+// 32 rows x 16 columns in the layout of a matrix fragment: lane l gets rows l / 4 + 0, 8 (r[0..7]) and 16, 24 (r[8..15]), columns
+// 2 (l % 4) + 0, 1 of each group of eight: r[8 half + 4 group + 2 (row / 8 % 2) + column].
+__device__ __forceinline__ void tmem_ld16_fragment(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr + (16u << 16)) : "memory");
+}
 // 16-byte global store under a predicate, without a branch: the epilogue's TMEM loads and waits are warp-wide
 // (.sync.aligned) and must never be reached by a warp that the compiler has split by a per-lane row test.
 __device__ __forceinline__ void st_global_v4_if(void* ptr, uint4 v, bool pred) {
@@ -1140,6 +1149,64 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 }
                 if (addend_ahead) { __syncwarp(); fetch_addend(); }
             };
+            // EPI 2, a whole 32 x 64 piece whose Z is in the buffer: the accumulator in fragments, so that a lane holds four rows of its
+            // columns and adds them up before anything crosses lanes -- 4 exchanges a 16-column step for the sums, not 16.  An
+            // exchange is a pass through the shared memory that feeds the tensor cores.
+            auto gradient_piece = [&](int c) {
+                const int n64 = nb + c * 64;
+                if (addend_ahead) {
+                    if (!mbar_wait_bounded(&addend_full[warp - 2], addend_phase) && lane == 0) atomicExch(&g_gemm_status, 4);
+                    addend_phase ^= 1;
+                    ap.out = false;
+                } else { if (lane == 0) tma_store_wait_read<0>(); __syncwarp(); }
+                int sm, jm;
+                p.fd_wm.divmod(t.m0, sm, jm);
+                const int64_t blk = ((int64_t)sm * p.tps_m + jm / (BM * CTAS)) * (4 * CTAS) + rank * 4 + quad;
+                const int g = lane >> 2, own = (lane >> 4) * 8 + (lane & 3) * 2 + ((lane >> 3) & 1);       // the column whose sum ends up here
+                unsigned char* cell = op_buf + g * 128 + (lane & 3) * 4;
+                uint32_t nx[16];
+                tmem_ld16_fragment(taddr + (uint32_t)(c * 64), nx);
+#pragma unroll 1
+                for (int q = 0; q < 4; ++q) {
+                    const int u[2] = {((2 * q) ^ g) << 4, ((2 * q + 1) ^ g) << 4};
+                    uint32_t z[8];
+                    if (addend_ahead)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) z[i] = *reinterpret_cast<const uint32_t*>(cell + ((i & 1) + 2 * (i >> 2)) * 1024 + u[(i >> 1) & 1]);
+                    tmem_ld_wait();
+                    tmem_regs_ready(nx);
+                    f32x2 v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = pair(__uint_as_float(nx[2 * i]), __uint_as_float(nx[2 * i + 1]));
+                    tmem_ld16_fragment(taddr + (uint32_t)(c * 64 + min(q + 1, 3) * 16), nx);
+                    if (addend_ahead) slope_pairs(p.act, v, z);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) *reinterpret_cast<uint32_t*>(cell + ((i & 1) + 2 * (i >> 2)) * 1024 + u[(i >> 1) & 1]) = bf16_pack(v[i]);
+                    if (p.colsum) {
+                        float f[4];
+                        split((v[0] + v[1]) + (v[4] + v[5]), f[0], f[1]);
+                        split((v[2] + v[3]) + (v[6] + v[7]), f[2], f[3]);
+                        const bool hi = lane & 16, odd = lane & 8;
+                        const float k0 = (hi ? f[2] : f[0]) + __shfl_xor_sync(0xffffffffu, hi ? f[0] : f[2], 16);
+                        const float k1 = (hi ? f[3] : f[1]) + __shfl_xor_sync(0xffffffffu, hi ? f[1] : f[3], 16);
+                        float s = (odd ? k1 : k0) + __shfl_xor_sync(0xffffffffu, odd ? k0 : k1, 8);
+                        s += __shfl_xor_sync(0xffffffffu, s, 4);
+                        if (!(lane & 4)) p.colsum[blk * p.N + n64 + q * 16 + own] = s;
+                    }
+                }
+                tmem_ld_wait();
+                tmem_regs_ready(nx);
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) {
+                    int cx = cx0 + c * 64, cy = cy0, cz = cz0, cu = cu0;
+                    if (c_chunked) to_coords<FULL>(p.c, row0, n64, cx, cy, cz, cu);
+                    tma_store_5d(mpc, op_buf, cx, cy, cz, cu, 0);
+                    tma_store_commit();
+                    if (addend_ahead) tma_store_wait_read<0>();
+                }
+                if (addend_ahead) { __syncwarp(); fetch_addend(); }
+            };
             // EPI: the fp32 partial sums of a piece of a K split
             auto partial_piece = [&](int c) {
                 float* wrow = p.ws + ((int64_t)t.split * p.M + min(m, t.m1 - 1)) * (int64_t)p.N;
@@ -1359,7 +1426,9 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             } else if constexpr (EPI != 0) {
 #pragma unroll 1
                 for (int c = hf; c < npieces; c += EW) {
-                    if (p.splits > 1) partial_piece(c); else epilogue_piece(c);
+                    if (p.splits > 1) partial_piece(c);
+                    else if (EPI == 2 && rows_full && nb + c * 64 + 64 <= t.n1 && !(FULL && p.c.il_mode == 3) && (addend_ahead || p.act == CCL_ACT_NONE)) gradient_piece(c);
+                    else epilogue_piece(c);
                 }
             } else if (EW > 1) {
 #pragma unroll 1

@@ -9,19 +9,19 @@
 
 namespace ccl {
 
-template <int BN, int CTAS, bool FULL, int KS, int EPI>
-static ccl_status launch_epi(const GemmPlan& plan, const CUtensorMap* maps, const EpiMaps<EPI>& em, cudaStream_t st) {
-    auto kernel = ccl_gemm_kernel<BN, CTAS, false, 0, FULL, KS, EPI>;
+template <int BN, int CTAS, bool FULL, int KS, int EPI, int OPW>
+static ccl_status launch_epi_warps(const GemmPlan& plan, const CUtensorMap* maps, const EpiMaps<EPI>& em, cudaStream_t st) {
+    auto kernel = ccl_gemm_kernel<BN, CTAS, false, 0, FULL, KS, EPI, OPW>;
     static std::atomic<uint64_t> configured{0};                 // bit per device: the shared-memory limit has been raised
     int dev = 0;
     CCL_CUDA_TRY(cudaGetDevice(&dev));
     if (dev >= 64 || !(configured.load() >> dev & 1)) {
-        CCL_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((KS ? kSmemBudgetOpKs : kSmemBudgetOp) + staging_bytes<EPI, KS> + 2048)));
+        CCL_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(smem_budget_op(KS, OPW) + staging_bytes<EPI, KS, OPW> + 2048)));
         if (dev < 64) configured.fetch_or(1ull << dev);
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(plan.grid, 1, 1);
-    cfg.blockDim = dim3(gemm_threads<EPI, KS>, 1, 1);
+    cfg.blockDim = dim3(gemm_threads<EPI, OPW>, 1, 1);
     cfg.dynamicSmemBytes = plan.smem_bytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -38,6 +38,13 @@ static ccl_status launch_epi(const GemmPlan& plan, const CUtensorMap* maps, cons
     CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], plan.p, em));
     count_launch();
     return CCL_OK;
+}
+
+template <int BN, int CTAS, bool FULL, int KS, int EPI>
+static ccl_status launch_epi(const GemmPlan& plan, const CUtensorMap* maps, const EpiMaps<EPI>& em, cudaStream_t st) {
+    if constexpr (KS != 0) return launch_epi_warps<BN, CTAS, FULL, KS, EPI, 16>(plan, maps, em, st);
+    else if constexpr (FULL) return launch_epi_warps<BN, CTAS, FULL, KS, EPI, 8>(plan, maps, em, st);
+    else return plan.opw == 16 ? launch_epi_warps<BN, CTAS, FULL, KS, EPI, 16>(plan, maps, em, st) : launch_epi_warps<BN, CTAS, FULL, KS, EPI, 8>(plan, maps, em, st);
 }
 
 template <int EPI>
@@ -78,6 +85,8 @@ static __global__ void __launch_bounds__(256) splitk_epilogue_kernel(const GemmP
     const int row = blockIdx.y * 32 + (threadIdx.x >> 3), n = blockIdx.x * 64 + (threadIdx.x & 7) * 8;
     const bool ok = row < p.M && n < p.N;
     const int r = min(row, p.M - 1), c = min(n, p.N - 8);
+    const int64_t off = c_offset(p, r, c);
+    const uint4 x8 = ld_global_v4_if(p.addend + off, ok && p.addend), b8 = ld_global_v4_if(p.bias + c, EPI == 1 && ok && p.bias);
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = 0.0f;
@@ -87,8 +96,7 @@ static __global__ void __launch_bounds__(256) splitk_epilogue_kernel(const GemmP
         v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
         v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
     }
-    const int64_t off = c_offset(p, r, c);
-    epilogue8<EPI>(p, v, off, c, ok);
+    epilogue8<EPI>(p, v, off, ok, x8, b8);
     st_global_v4_if(p.C + off, bf16x8_pack(v), ok);
     if (EPI == 2 && p.colsum) {
         __shared__ float part[32][64 + 4];

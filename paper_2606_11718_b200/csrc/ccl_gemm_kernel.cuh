@@ -27,23 +27,23 @@ constexpr int BK = 64;
 #endif
 constexpr int kEpiWarps = CCL_EPI_WARPS;        // 4, or 8: two warps per TMEM lane quadrant taking alternate 64-column pieces
 constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
-// The kernels with an operator in the epilogue (EPI != 0) drain with eight warps, two 64-column pieces of a 256-wide tile each.
-// Their arithmetic has the time of the next tile's product; what it costs is the ring: pieces of the addend and of C that move
-// all at once hold up the operands behind them in the TMA unit, and every 4 KB buffer is taken from the ring.  4096 x 8192 x 2048,
-// no operator at all: 92 us with eight warps and six stages, 99 with sixteen and five, 106 with four stages; relu's slope 98 and
-// 107.  The cluster split drains once, from the exchanged sums, with sixteen (777 x 1544 x 1000: 14.2 us, 15.6 with eight).
-constexpr int kEpiOpWarps = 8, kEpiOpWarpsKs = 16;
+// The kernels with an operator in the epilogue (EPI != 0) drain with OPW = 8 or 16 warps, two or one 64-column pieces of a 256-wide
+// tile each.  Where the next tile's product is long enough to hide the drain, what the drain costs is the ring: pieces of the
+// addend and of C that move all at once hold up the operands behind them in the TMA unit, and every 4 KB buffer is taken from the
+// ring.  4096 x 8192 x 2048, no operator at all: 92 us with eight warps and six stages, 99 with sixteen and five, 106 with four
+// stages; relu's slope 98 and 107.  The cluster split drains once, from the exchanged sums, with sixteen (777 x 1544 x 1000:
+// 14.2 us, 15.6 with eight).
 // (the cluster split exchanges its partial sums in the ring and stores from registers: no staging, a longer ring)
-template <int EPI, int KS> constexpr uint32_t staging_bytes = EPI ? (KS ? 0u : kEpiOpWarps * 32u * 128u) : 4u * 2 * 32 * 128;
-template <int EPI, int KS> constexpr int epi_warps = EPI ? (KS ? kEpiOpWarpsKs : kEpiOpWarps) : kEpiWarps;
-template <int EPI, int KS> constexpr int gemm_threads = 64 + 32 * epi_warps<EPI, KS>;
+template <int EPI, int KS, int OPW> constexpr uint32_t staging_bytes = EPI ? (KS ? 0u : OPW * 32u * 128u) : 4u * 2 * 32 * 128;
+template <int EPI, int OPW> constexpr int epi_warps = EPI ? OPW : kEpiWarps;
+template <int EPI, int OPW> constexpr int gemm_threads = 64 + 32 * epi_warps<EPI, OPW>;
 constexpr int kTmemCols = 512;
 constexpr uint32_t kSmemBudget = 192 * 1024;    // ring of operand stages
 constexpr int64_t kRaggedDense = 4096;         // problems of a ragged batch whose tile prefix is kept in shared memory
 constexpr uint32_t kEpiBytes = 4 * 2 * 32 * 128; // epilogue staging: per warp two buffers of 32 rows x 128 B
 constexpr uint32_t kSmemBudgetOpKs = 224 * 1024;
-constexpr uint32_t kSmemBudgetOp = 192 * 1024;
-constexpr uint32_t kEpiBytesOp = kEpiOpWarps * 32 * 128;       // EPI: a buffer for each warp, in which an addend's piece becomes C's
+// EPI: the ring beside the warps' buffers, in which an addend's piece becomes C's
+constexpr uint32_t smem_budget_op(int ks, int opw) { return ks ? kSmemBudgetOpKs : (224u * 1024 - (uint32_t)opw * 32 * 128); }
 
 static __device__ int g_gemm_status = 0;
 
@@ -390,26 +390,24 @@ __device__ __forceinline__ int64_t c_offset(const GemmParams& p, int64_t m, int6
 
 // One row's 8 columns from column n on, whose element offset in C's layout is `off`: fp32 accumulators -> what C gets (fp32,
 // before the rounding).  EPI 1: act(v + bias) + residual, the pre-activation stored on the way.  EPI 2: v * act'(z).
-// `ok` off: nothing is stored and, for EPI 2, v becomes zero (it goes into column sums).
+// x and b: the addend's and the bias's 8 values.  `ok` off: nothing is stored and, for EPI 2, v becomes zero (it goes into column
+// sums).
 template <int EPI>
-__device__ __forceinline__ void epilogue8(const GemmParams& p, float (&v)[8], int64_t off, int n, bool ok) {
+__device__ __forceinline__ void epilogue8(const GemmParams& p, float (&v)[8], int64_t off, bool ok, const uint4& x, const uint4& b) {
     f32x2 w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = pair(v[2 * i], v[2 * i + 1]);
     if (EPI == 1) {
         if (p.bias) {
-            const uint4 b = ld_global_v4_if(p.bias + n, ok);
             w[0] = w[0] + bf16_unpack(b.x); w[1] = w[1] + bf16_unpack(b.y); w[2] = w[2] + bf16_unpack(b.z); w[3] = w[3] + bf16_unpack(b.w);
         }
         if (p.preact) st_global_v4_if(p.preact + off, bf16x8_pack(w), ok);
         act_pairs(p.act, w);
         if (p.addend) {
-            const uint4 x = ld_global_v4_if(p.addend + off, ok);
             w[0] = w[0] + bf16_unpack(x.x); w[1] = w[1] + bf16_unpack(x.y); w[2] = w[2] + bf16_unpack(x.z); w[3] = w[3] + bf16_unpack(x.w);
         }
     }
     if (EPI == 2 && p.act != CCL_ACT_NONE) {
-        const uint4 x = ld_global_v4_if(p.addend + off, ok);
         const uint32_t z[4] = {x.x, x.y, x.z, x.w};
         slope_pairs(p.act, w, z);
     }
@@ -587,8 +585,8 @@ struct Scheduler {
 // KS > 0: cluster split along K (CTAS = 1): the KS CTAs of a cluster share one tile
 // EPI: 1 = bias, activation and residual in the epilogue (ccl_gemm_epilogue), 2 = activation slope and column sums
 // (ccl_gemm_act_grad)
-template <int BN, int CTAS, bool SWIGLU = false, int RAG = 0, bool FULL = true, int KS = 0, int EPI = 0>
-__global__ void __launch_bounds__(gemm_threads<EPI, KS>, 1)
+template <int BN, int CTAS, bool SWIGLU = false, int RAG = 0, bool FULL = true, int KS = 0, int EPI = 0, int OPW = 0>
+__global__ void __launch_bounds__(gemm_threads<EPI, OPW>, 1)
 ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                 const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_a2,
                 const __grid_constant__ CUtensorMap map_b2, const __grid_constant__ CUtensorMap map_c2,
@@ -603,7 +601,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         static_assert(sizeof(GemmParams) % 4 == 0, "GemmParams is copied word by word");
         const uint32_t* src = reinterpret_cast<const uint32_t*>(&gp);
         uint32_t* dst = reinterpret_cast<uint32_t*>(&p);
-        for (int i = threadIdx.x; i < (int)(sizeof(GemmParams) / 4); i += gemm_threads<EPI, KS>) dst[i] = src[i];
+        for (int i = threadIdx.x; i < (int)(sizeof(GemmParams) / 4); i += gemm_threads<EPI, OPW>) dst[i] = src[i];
     }
     // A tile wider than 256 columns is computed as two sub-tiles (one MMA each per k step), the first 256 columns wide,
     // the second the rest (256 or 128), each with a 256-column half of TMEM; narrower tiles use the two halves as a
@@ -626,13 +624,13 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     unsigned char* epi = smem + (size_t)gp.stages * gp.stage_bytes;     // 1024-byte aligned: stage sizes are multiples of 1 KB
-    uint64_t* bars = reinterpret_cast<uint64_t*>(epi + staging_bytes<EPI, KS>);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(epi + staging_bytes<EPI, KS, OPW>);
     uint64_t* full = bars;                           // used in the leader CTA only
     uint64_t* empty = bars + gp.stages;               // one set per CTA
     uint64_t* tmem_full = bars + 2 * gp.stages;       // one set per CTA
     uint64_t* tmem_empty = tmem_full + 4;            // used in the leader CTA only
     uint64_t* addend_full = tmem_empty + 4;          // EPI: one per epilogue warp
-    uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(addend_full + (EPI ? kEpiOpWarps : 0));
+    uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(addend_full + (EPI ? OPW : 0));
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0;
@@ -645,9 +643,9 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         prefetch_tmap(&map_b);
         prefetch_tmap(&map_c);
         for (int s = 0; s < gp.stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int a = 0; a < NACC; ++a) { mbar_init(&tmem_full[a], 1); mbar_init(&tmem_empty[a], epi_warps<EPI, KS> * CTAS); }
+        for (int a = 0; a < NACC; ++a) { mbar_init(&tmem_full[a], 1); mbar_init(&tmem_empty[a], epi_warps<EPI, OPW> * CTAS); }
         if constexpr (EPI != 0)
-            for (int w = 0; w < kEpiOpWarps; ++w) mbar_init(&addend_full[w], 1);
+            for (int w = 0; w < OPW; ++w) mbar_init(&addend_full[w], 1);
         fence_barrier_init();
     }
     if (warp == 1) tmem_alloc<CTAS>(tmem_ptr, kTmemCols);
@@ -905,7 +903,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         // ------------------------------------------------------------------ epilogue (warps 2..5)
         if (RAG == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
         const int quad = warp & 3;                       // TMEM lane quadrant this warp may read
-        constexpr int EW = epi_warps<EPI, KS> / 4;         // warps per quadrant
+        constexpr int EW = epi_warps<EPI, OPW> / 4;         // warps per quadrant
         const int hf = (warp - 2) >> 2;                  // which of them this one is
         const uint32_t tmem_empty0 = CTAS == 2 ? map_to_cta(smem_u32(&tmem_empty[0]), 0) : smem_u32(&tmem_empty[0]);
         TileCoord t;
@@ -1284,11 +1282,23 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                                      "r"(ra[4 * j + 2]), "r"(ra[4 * j + 3]) : "memory");
                     }
                 }
-                cluster_sync();
                 // (a tile lies inside one strip of C: the columns of a row follow each other from the tile's first column on)
                 const int row = t.m0 + quad * 32 + lane;
                 const int64_t coff = c_offset<FULL>(p, min(row, t.m1 - 1), nb) + (int)krank * JS * 4;
                 unsigned short* crow = p.C + coff;
+                // EPI 1: a warp has one piece at most; its residual and bias are on their way while the cluster meets (333 x 1000 x 1544:
+                // 9.9 -> 9.6 us; the gradient's Z stays where it is used, 777 x 1544 x 1000: 14.4 us, 15.2 fetched here)
+                static_assert(EPI == 0 || KS == 0 || EW * 64 >= BN, "one piece a warp");
+                [[maybe_unused]] uint4 xs[JS / 2], bs[JS / 2];
+                if constexpr (EPI == 1)
+#pragma unroll
+                    for (int i = 0; i < JS / 2; ++i) {
+                        const int col = nb + hf * 64 + ((int)krank * JS + 2 * i) * 4;
+                        const bool ok8 = hf < npieces && row < t.m1 && col < t.n1;
+                        xs[i] = ld_global_v4_if(p.addend + coff + hf * 64 + i * 8, ok8 && p.addend);
+                        bs[i] = ld_global_v4_if(p.bias + col, ok8 && p.bias);
+                    }
+                cluster_sync();
 #pragma unroll 1
                 for (int c = hf; c < npieces; c += EW)
 #pragma unroll
@@ -1305,7 +1315,8 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         if (EPI != 0) {
                             float v[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
                             const bool ok8 = row < t.m1 && col < t.n1;
-                            epilogue8<EPI>(p, v, coff + c * 64 + js * 4, col, ok8);
+                            if (EPI == 2) { xs[0] = ld_global_v4_if(p.addend + coff + c * 64 + js * 4, ok8 && p.addend); bs[0] = xs[0]; }
+                            epilogue8<EPI>(p, v, coff + c * 64 + js * 4, ok8, xs[EPI == 2 ? 0 : js / 2], bs[EPI == 2 ? 0 : js / 2]);
                             st_global_v4_if(crow + c * 64 + js * 4, bf16x8_pack(v), ok8);
                             if (EPI == 2 && p.colsum) {
                                 const float sum = column_sums8(v, lane);

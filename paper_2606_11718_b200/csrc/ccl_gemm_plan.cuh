@@ -22,6 +22,7 @@ struct GemmPlan {
     bool lean;                 // no optional feature in use (see FULL)
     unsigned grid;
     int ks;                    // cluster split along K: CTAs per cluster (0: none)
+    int opw;                   // an operator in the epilogue: warps that drain (8 or 16)
 };
 
 // How a page-interleaved operand is expressed as a rank-4 tensor map (OpMap::il_mode): 0 = not interleaved,
@@ -420,7 +421,13 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     const char* rag_env = std::getenv("CCL_GEMM_RAGGED_DENSE");
     const uint32_t rag_bytes = cap > 0 && batch <= kRaggedDense && !(rag_env && atoi(rag_env) == 0) ? (uint32_t)(4 * (kGemmThreads + batch + 1) + 1023) & ~1023u : 0;
     p.rag_dense = rag_bytes ? 1 : 0;
-    p.stages = (int32_t)(((epi ? (ks ? kSmemBudgetOpKs : kSmemBudgetOp) : kSmemBudget) - rag_bytes) / p.stage_bytes);
+    // the warps that drain an operator's tiles: eight and a long ring where a tile's product is longer than its drain, sixteen and a
+    // shorter one where the drain is what the tiles wait for; both grow with the tile's width, so K decides (4096 x 8192, gelu
+    // and a residual, eight / sixteen: K = 1024 88 / 74 us, 2048 107 / 108, 4096 197 / 203; gradient: K = 256 72 / 67, 1024 89 / 89,
+    // 2048 111 / 115, 4096 201 / 210).  The kernels with every layout exist with eight, the cluster split drains once, with sixteen.
+    const int opw = ks ? 16 : (epi_full || p.kb_per_split * BK >= 1536 ? 8 : 16);
+    plan->opw = opw;
+    p.stages = (int32_t)(((epi ? smem_budget_op(ks, opw) : kSmemBudget) - rag_bytes) / p.stage_bytes);
     if (p.stages > 8) p.stages = 8;
     int64_t ntiles = (int64_t)p.tiles_m * p.tiles_n * splits * batch;
     p.batch = (int32_t)batch;
@@ -483,7 +490,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     p.fd_upg = make_fastdiv(p.sch_upg); p.fd_groups = make_fastdiv(p.groups); p.fd_splits = make_fastdiv(p.splits);
     p.fd_per_panel = make_fastdiv((int64_t)p.panel * p.sch_gn); p.fd_panel = make_fastdiv(p.panel);
     p.fd_tps_m = make_fastdiv(p.tps_m); p.fd_tps_n = make_fastdiv(p.tps_n);
-    plan->smem_bytes = (uint32_t)p.stages * p.stage_bytes + (epi ? (ks ? 0u : kEpiBytesOp) + kEpiOpWarps * 8 : kEpiBytes) + 1024 + (2 * p.stages + 8) * 8 + 16 + rag_bytes;
+    plan->smem_bytes = (uint32_t)p.stages * p.stage_bytes + (epi ? (ks ? 0u : (uint32_t)opw * 32 * 128) + (uint32_t)opw * 8 : kEpiBytes) + 1024 + (2 * p.stages + 8) * 8 + 16 + rag_bytes;
     p.fd_tiles_n = make_fastdiv(p.tiles_n);
     return CCL_OK;
 }

@@ -167,6 +167,17 @@ def test_several_tiles_per_cta_and_a_grouped_raster():
             check_grad(M, N, K, "gelu_tanh", d, 0, 0, seed=2)
 
 
+# a product long enough to hide the drain is drained by eight warps, a shorter one by sixteen: both sides of the limit, whole and cut tiles
+@pytest.mark.parametrize("ctas,bn", [(1, 128), (1, 192), (1, 256), (2, 128), (2, 192), (2, 256)])
+@pytest.mark.parametrize("K", [1472, 1544])
+def test_both_sides_of_the_drain_limit(ctas, bn, K):
+    M, N = 1800, 2632                            # more tiles than the GPU takes at a time
+    with forced(ctas=ctas, bn=bn, splitk=1, clusterk=0):
+        d = gemm_desc(M, N, K, 1, ROW, 0, 0, 0, 0)
+        check_forward(M, N, K, "gelu_tanh", d, 0, 0, seed=7)
+        check_grad(M, N, K, "silu", d, 0, 0, seed=8)
+
+
 # page-interleaved operands, an operand split along K, strips of unequal size, a 2-D partition
 FULL = [
     dict(M=200, N=1024, K=256, P=4, lay=("row", "ileave", "ileave"), at=0, bt=0, op=2, align=4096),     # a chunk holds whole strip rows

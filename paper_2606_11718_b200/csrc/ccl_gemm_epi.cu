@@ -217,9 +217,14 @@ ccl_status shape_plan(const ccl_gemm_desc* d, int epi, GemmPlan* out) {
     return CCL_OK;
 }
 
-// Row blocks of the partial column sums: 32 rows each, of every tile row (whole tiles) or of the matrix (K split)
+// Row blocks of the partial column sums: 32 rows each, of every tile row that has rows (whole tiles) or of the matrix (K split).
+// Tile rows are numbered strip by strip, tps_m to a strip; a last strip that is lower than the others may have fewer, and the places
+// behind its last one, which are the last of all, are skipped by the kernel: their sums are never written.
 int64_t row_blocks(const GemmPlan& plan) {
-    return plan.p.splits > 1 ? ((int64_t)plan.p.M + 31) / 32 : (int64_t)plan.p.tiles_m * 4 * plan.ctas;
+    const GemmParams& p = plan.p;
+    if (p.splits > 1) return ((int64_t)p.M + 31) / 32;
+    const int64_t strips = ((int64_t)p.M + p.Wm - 1) / p.Wm, tile = (int64_t)BM * plan.ctas, last = (int64_t)p.M - (strips - 1) * p.Wm;
+    return ((strips - 1) * p.tps_m + (last + tile - 1) / tile) * 4 * plan.ctas;
 }
 size_t partial_sums_at(const GemmPlan& plan) { return (plan.ws_bytes + 255) & ~(size_t)255; }
 

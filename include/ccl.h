@@ -404,8 +404,9 @@ ccl_status ccl_bias_act_grad(const ccl_mat* m, int32_t act, const void* dY_dev, 
  * 16 bytes (else CCL_ERR_ALIGN).
  * One cooperative launch of one CTA per SM, which meet at two or three grid-wide barriers; every wait is bounded and reported by
  * ccl_gemm_status (codes 8 and 9).  A logit that is NaN is never chosen before a number; NaN inputs give NaN outputs for their token.
- * Workspace: ccl_moe_tokens_workspace bytes, whatever they hold; calls that can overlap on the GPU must not share it.  The result does
- * not depend on the order in which CTAs run.
+ * Workspace: ccl_moe_tokens_workspace bytes, whatever they hold; calls that can overlap on the GPU must not share it.  A launch leaves
+ * its meeting flags cleared, also when a wait ran out, so that a call recorded in a CUDA graph may be replayed on the same
+ * workspace.  The result does not depend on the order in which CTAs run.
  */
 typedef struct ccl_moe_desc {
     int64_t T, H, I;
@@ -540,6 +541,14 @@ ccl_status ccl_probe_l2_latency(const void* zero_buf_dev, int32_t nlines, int64_
  *              flight are drained before the CTA exits.  src_dev: 2048 readable bytes, 16-byte aligned (which = 1 only).
  */
 ccl_status ccl_selftest_wait_timeout(int32_t which, uint32_t limit_us, const void* src_dev, void* cuda_stream);
+/*
+ * The same for the meetings of ccl_moe_tokens: its kernel, on the operands of an ordinary call, with a meeting (1: the first, 2: the
+ * others) that waits for one CTA more than there are, for limit_us microseconds (1..100000) at most.  Y is not computed;
+ * ccl_gemm_status() returns CCL_ERR_TIMEOUT once (code 8 or 9).
+ */
+ccl_status ccl_selftest_moe_timeout(const ccl_moe_desc* d, const void* X_dev, const void* Wr_dev, const void* Wgu_dev, const void* Wd_dev,
+                                    void* Y_dev, void* ws_dev, size_t ws_bytes, int32_t meeting, uint32_t limit_us,
+                                    void* cuda_stream);
 
 /* Message for the last non-OK status returned on this thread ("" if none). Static storage. */
 const char* ccl_last_error(void);

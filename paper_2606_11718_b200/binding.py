@@ -21,7 +21,7 @@ ACT_NONE, ACT_RELU, ACT_GELU_TANH, ACT_GELU_ERF, ACT_SILU = 0, 1, 2, 3, 4
 ASSIGN_N_STRIPS, ASSIGN_M_STRIPS, ASSIGN_EXPLICIT, ASSIGN_2D = 0, 1, 2, 3
 
 EXPORTS = ["ccl_map_offset", "ccl_map_inverse", "ccl_buffer_bytes", "ccl_strip_stride", "ccl_repack", "ccl_repack_batched", "ccl_repack_transpose", "ccl_gemm_workspace",
-           "ccl_gemm", "ccl_gemm_batched_workspace", "ccl_gemm_batched", "ccl_gemm_grouped", "ccl_gemm_grouped_swiglu", "ccl_gemm_grouped_k", "ccl_gemm_axpby", "ccl_gemm_swiglu", "ccl_gemm_static_ws", "ccl_gemm_status", "ccl_selftest_wait_timeout", "ccl_gemm_epilogue_workspace", "ccl_gemm_epilogue",
+           "ccl_gemm", "ccl_gemm_batched_workspace", "ccl_gemm_batched", "ccl_gemm_grouped", "ccl_gemm_grouped_swiglu", "ccl_gemm_grouped_k", "ccl_gemm_axpby", "ccl_gemm_swiglu", "ccl_gemm_static_ws", "ccl_gemm_status", "ccl_selftest_wait_timeout", "ccl_selftest_moe_timeout", "ccl_gemm_epilogue_workspace", "ccl_gemm_epilogue",
            "ccl_gemm_act_grad_workspace", "ccl_gemm_act_grad", "ccl_bias_act_grad", "ccl_moe_tokens_workspace", "ccl_moe_tokens", "ccl_traffic_sizes", "ccl_traffic", "ccl_traffic_l2", "ccl_traffic_lru", "ccl_probe_l2_latency", "ccl_last_error", "ccl_launch_count", "ccl_version"]
 
 
@@ -120,6 +120,7 @@ def lib():
         l.ccl_bias_act_grad.argtypes = [C.POINTER(Mat), C.c_int32] + [C.c_void_p] * 5
         l.ccl_moe_tokens_workspace.argtypes = [C.POINTER(MoeDesc), C.POINTER(C.c_size_t)]
         l.ccl_moe_tokens.argtypes = [C.POINTER(MoeDesc)] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]
+        l.ccl_selftest_moe_timeout.argtypes = [C.POINTER(MoeDesc)] + [C.c_void_p] * 6 + [C.c_size_t, C.c_int32, C.c_uint32, C.c_void_p]
         l.ccl_traffic_sizes.argtypes = [C.POINTER(TrafficDesc), C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
         l.ccl_traffic.argtypes = [C.POINTER(TrafficDesc), C.c_void_p, C.c_void_p, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                   C.c_void_p, C.c_void_p]
@@ -390,6 +391,11 @@ def ccl_gemm_status():
 def ccl_selftest_wait_timeout(which, limit_us, src=None):
     """Test support: launches a CTA whose bounded wait runs out after limit_us (0: the GEMM's path, 1: the repack ring)."""
     _check(lib().ccl_selftest_wait_timeout(which, limit_us, _ptr(src), _stream()))
+
+
+def ccl_selftest_moe_timeout(d, X, Wr, Wgu, Wd, Y, ws, meeting, limit_us):
+    """Test support: ccl_moe_tokens with a meeting (1 or 2) of its CTAs that waits for one more than there are, for limit_us at most."""
+    _check(lib().ccl_selftest_moe_timeout(C.byref(d), _ptr(X), _ptr(Wr), _ptr(Wgu), _ptr(Wd), _ptr(Y), _ptr(ws), ws.nbytes, meeting, limit_us, _stream()))
 
 
 def ccl_traffic_sizes(d):

@@ -65,6 +65,9 @@ struct MoeParams {
     unsigned char* h;                       // workspace: [groups of 4 pairs][value, remainder][4][h_pitch bytes] bf16
     int64_t h_pitch;
     unsigned long long mark;                // this launch's mark in the flags
+    int32_t writers;                        // CTAs the first meeting waits for: the first of the grid, those with logits to write
+    int32_t quorum;                         // CTAs the others wait for: all
+    uint64_t wait_ns;                       // how long a CTA waits at a meeting
     int32_t group;                          // most tokens of an expert taken together (8 or 4)
     int32_t depth;                          // blocks in a warp's ring
     int32_t all_x;                          // 1: the rows of all tokens are staged once; 0: those of an expert's tokens when it comes up
@@ -103,13 +106,13 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity) {
     return done;
 }
 // One thread waits (bounded) until the word is `mark` (exact) or at least that.
-__device__ __noinline__ bool wait_word(const unsigned long long* word, unsigned long long mark, bool exact) {
+__device__ __noinline__ bool wait_word(const unsigned long long* word, unsigned long long mark, bool exact, uint64_t limit_ns) {
     const uint64_t t0 = global_timer_ns();
     for (;;) {
         unsigned long long v;
         asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(word) : "memory");
         if (exact ? v == mark : v >= mark) return true;
-        if (global_timer_ns() - t0 > kWaitLimitNs) return false;
+        if (global_timer_ns() - t0 > limit_ns) return false;
     }
 }
 __device__ __forceinline__ void st_release(unsigned long long* p, unsigned long long v) { asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(p), "l"(v) : "memory"); }
@@ -118,10 +121,12 @@ __device__ __forceinline__ void st_release(unsigned long long* p, unsigned long 
 // The counter needs a start, so the first meeting -- which ends when the `writers`, the first CTAs of the grid, have their logits out
 // -- has flags (any contents but this launch's mark mean "not yet").  Up to 16 of them are read by every CTA (one token, 8 writers:
 // 1.2 us less than the other way); of more, CTA 0 alone reads them and lets the others go by a word.  CTA 0 clears the counters of
-// the later meetings on the way.  `meanwhile` is done between a CTA's arrival and its wait.
+// the later meetings on the way.  `meanwhile` is done between a CTA's arrival and its wait.  A CTA that leaves the kernel, on whatever
+// way, clears its flag (leave_meetings): a replayed CUDA graph uses the same mark again, and must not take an old flag for a new one.
 constexpr int kMoeReaders = 16;
 template <typename F>
-__device__ __forceinline__ bool meet_first(const MoeParams& p, int writers, F meanwhile) {
+__device__ __forceinline__ bool meet_first(const MoeParams& p, F meanwhile) {
+    const int writers = p.writers;
     bar_consumers();
     bool ok = true;
     if (threadIdx.x == 0 && (int)blockIdx.x < writers) {
@@ -132,25 +137,31 @@ __device__ __forceinline__ bool meet_first(const MoeParams& p, int writers, F me
     const bool all = writers <= kMoeReaders;
     if (all || blockIdx.x == 0) {
 #pragma unroll 1
-        for (int i = threadIdx.x; i < writers; i += kMoeThreads) ok = wait_word(p.flags + i, p.mark, true) && ok;
+        for (int i = threadIdx.x; i < writers; i += kMoeThreads) ok = wait_word(p.flags + i, p.mark, true, p.wait_ns) && ok;
         ok = bar_consumers_and(ok);
         if (threadIdx.x == 0 && ok && !all) st_release(p.gate, p.mark);
     } else {
-        if (threadIdx.x == 0) ok = wait_word(p.gate, p.mark, true);
+        if (threadIdx.x == 0) ok = wait_word(p.gate, p.mark, true, p.wait_ns);
         ok = bar_consumers_and(ok);
     }
     if (!ok && threadIdx.x == 0) atomicExch(&g_moe_status, 8);
     return ok;
 }
-__device__ __forceinline__ bool meet_counted(unsigned long long* counter) {
+__device__ __forceinline__ bool meet_counted(const MoeParams& p, unsigned long long* counter) {
     bar_consumers();
     bool ok = true;
     if (threadIdx.x == 0) {
         asm volatile("red.release.gpu.global.add.u64 [%0], 1;" ::"l"(counter) : "memory");
-        ok = wait_word(counter, gridDim.x, false);
+        ok = wait_word(counter, (unsigned long long)p.quorum, false, p.wait_ns);
         if (!ok) atomicExch(&g_moe_status, 8);
     }
     return bar_consumers_and(ok);
+}
+// One thread of a CTA that goes to no meeting any more.  (Where all came about, everyone is past the first; where one did not, a CTA that
+// still waits for this flag runs into its limit as well.)
+__device__ __forceinline__ void leave_meetings(const MoeParams& p) {
+    p.flags[blockIdx.x] = 0;
+    if (blockIdx.x == 0) p.gate[0] = 0;
 }
 // All threads of the CTA pair
 __device__ __forceinline__ void pair_sync() {
@@ -283,7 +294,7 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
             }
             bar_consumers();
         }
-    bool met1 = meet_first(p, min(ctas, (p.E + 15) / 16 * ((p.T + 7) / 8)), [&]() { if (p.all_x) stage_x(p.T, [](int t) { return t; }); });
+    bool met1 = meet_first(p, [&]() { if (p.all_x) stage_x(p.T, [](int t) { return t; }); });
     if (threadIdx.x == 0) shared[1] = met1;
     // top-k of a token: an expert's place is the number of those before it (a larger logit, or an equal one of a lower expert), a
     // thread an expert against all of them in shared memory.  Up to 8 tokens are worked out by every CTA for itself; of more, each
@@ -345,7 +356,7 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
             }
         }
         if (!every) {
-            met1 = met1 && meet_counted(p.gate + 2);
+            met1 = met1 && meet_counted(p, p.gate + 2);
             if (threadIdx.x == 0) shared[1] = met1;
             for (int i = threadIdx.x; met1 && i < pairs; i += kMoeThreads) {
                 const int2 c = __ldcg(p.choice + i);
@@ -388,7 +399,11 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
     }
     }
     __syncthreads();
-    if (!shared[1]) { pair_sync(); return; }              // (the first meeting did not come about; nothing is in flight)
+    if (!shared[1]) {                                     // a meeting did not come about; nothing is in flight
+        if (threadIdx.x == 0) leave_meetings(p);
+        pair_sync();
+        return;
+    }
     const int ents = shared[0], units = ents * nfb;
     const int u0 = (int)((int64_t)units * cta / ctas), u1 = (int)((int64_t)units * (cta + 1) / ctas);
 
@@ -589,12 +604,8 @@ __global__ void __launch_bounds__(kMoeBlockThreads, 1) moe_tokens_kernel(const _
             if (++f == nfb) { f = 0; ++i; }
         }
     }
-    const bool met = meet_counted(p.gate + 1);
-    if (threadIdx.x == 0) { shared[2] = met; mbar_arrive(met_bar); }
-    if (met && threadIdx.x == 0) {                        // everyone is past the first meeting: cleared for the next launch, which may be this one replayed
-        p.flags[cta] = 0;
-        if (cta == 0) p.gate[0] = 0;
-    }
+    const bool met = meet_counted(p, p.gate + 1);
+    if (threadIdx.x == 0) { shared[2] = met; mbar_arrive(met_bar); leave_meetings(p); }
 
     // ---- 3. down -------------------------------------------------------------------------------------------------------
     {
@@ -810,9 +821,9 @@ extern "C" ccl_status ccl_moe_tokens_workspace(const ccl_moe_desc* d, size_t* by
     return CCL_OK;
 }
 
-extern "C" ccl_status ccl_moe_tokens(const ccl_moe_desc* d, const void* X_dev, const void* Wr_dev, const void* Wgu_dev, const void* Wd_dev,
-                                     const void* residual_dev, void* Y_dev, int32_t* ids_dev, float* weights_dev, void* ws_dev, size_t ws_bytes,
-                                     void* cuda_stream) {
+// `absent`: 0, or the number of the meeting (1, 2) that waits for a CTA more than there are, for `wait_ns` at most
+static ccl_status moe_impl(const ccl_moe_desc* d, const void* X_dev, const void* Wr_dev, const void* Wgu_dev, const void* Wd_dev, const void* residual_dev,
+                           void* Y_dev, int32_t* ids_dev, float* weights_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream, int absent, uint64_t wait_ns) {
     if (!X_dev || !Wr_dev || !Wgu_dev || !Wd_dev || !Y_dev) return fail(CCL_ERR_INVALID_ARG, "ccl_moe_tokens: NULL operand");
     MoePlan plan;
     ccl_status s = plan_moe(d, 148, &plan);              // validation first: no CUDA call on bad input
@@ -834,10 +845,13 @@ extern "C" ccl_status ccl_moe_tokens(const ccl_moe_desc* d, const void* X_dev, c
     p.gate = p.flags + plan.ctas + 16;                   // (in another line than the flags)
     p.choice = reinterpret_cast<int2*>(p.gate + 16);
     p.h = ws + up128((size_t)p.T * p.E * 4) + up128((size_t)(plan.ctas + 32 + p.T * p.topk) * 8);
-    // A mark that no workspace holds yet, whatever its contents.  A launch leaves the first meeting's flags and word cleared, so that a
-    // replayed CUDA graph may use its mark again.
+    // A mark that no workspace holds yet, whatever its contents.  A launch leaves the first meeting's flags and word cleared, whatever
+    // became of it, so that a replayed CUDA graph may use its mark again.
     static std::atomic<unsigned long long> next{(unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull};
     do p.mark = next.fetch_add(0x9E3779B97F4A7C15ull); while (p.mark == 0);
+    p.writers = absent == 1 ? plan.ctas + 1 : std::min(plan.ctas, (p.E + 15) / 16 * ((p.T + 7) / 8));
+    p.quorum = absent == 2 ? plan.ctas + 1 : plan.ctas;
+    p.wait_ns = wait_ns;
     // gate | up weights as {k, row of a strip's half, half of a strip, expert}: a block is the same 16 rows of a strip's gate and up
     // half.  Down weights as {k, row, expert}.  Rows and k past the end read as zero.
     CUtensorMap map_gu, map_d;
@@ -851,4 +865,17 @@ extern "C" ccl_status ccl_moe_tokens(const ccl_moe_desc* d, const void* X_dev, c
         if ((s = encode_tmap(&map_d, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, Wd_dev, ddims, dstrides, dbox, CU_TENSOR_MAP_SWIZZLE_128B))) return s;
     }
     return launch_moe(plan, map_gu, map_d, reinterpret_cast<cudaStream_t>(cuda_stream));
+}
+
+extern "C" ccl_status ccl_moe_tokens(const ccl_moe_desc* d, const void* X_dev, const void* Wr_dev, const void* Wgu_dev, const void* Wd_dev,
+                                     const void* residual_dev, void* Y_dev, int32_t* ids_dev, float* weights_dev, void* ws_dev, size_t ws_bytes,
+                                     void* cuda_stream) {
+    return moe_impl(d, X_dev, Wr_dev, Wgu_dev, Wd_dev, residual_dev, Y_dev, ids_dev, weights_dev, ws_dev, ws_bytes, cuda_stream, 0, kWaitLimitNs);
+}
+
+extern "C" ccl_status ccl_selftest_moe_timeout(const ccl_moe_desc* d, const void* X_dev, const void* Wr_dev, const void* Wgu_dev, const void* Wd_dev,
+                                               void* Y_dev, void* ws_dev, size_t ws_bytes, int32_t meeting, uint32_t limit_us, void* cuda_stream) {
+    if (meeting != 1 && meeting != 2) return fail(CCL_ERR_INVALID_ARG, "ccl_selftest_moe_timeout: meeting must be 1 or 2");
+    if (limit_us < 1 || limit_us > 100000) return fail(CCL_ERR_INVALID_ARG, "ccl_selftest_moe_timeout: limit_us must be in [1, 100000]");
+    return moe_impl(d, X_dev, Wr_dev, Wgu_dev, Wd_dev, nullptr, Y_dev, nullptr, nullptr, ws_dev, ws_bytes, cuda_stream, meeting, (uint64_t)limit_us * 1000ull);
 }

@@ -288,15 +288,34 @@ def ccl_gemm_swiglu(d, A, B, Cout):
 
 
 def _check_operands(what, *pairs):
-    """Every (tensor or None, bytes) pair: a contiguous CUDA tensor with at least that many bytes."""
+    """Every (tensor or None, bytes) pair: contiguous, on the current CUDA device, with at least that many bytes of bf16 or raw (integer)
+    storage.  Another floating type is refused: its bytes would be read as bf16.  Returns the device."""
+    device = None
     for t, nbytes in pairs:
-        if t is not None and (t.nbytes < nbytes or not t.is_cuda or not t.is_contiguous()):
-            raise ValueError(f"{what}: an operand must be a contiguous CUDA tensor that holds what the descriptor says")
+        if t is None:                                          # (the library says where it cannot do without)
+            continue
+        at, dtype = t.get_device(), t.dtype                    # (-1: not on a GPU)
+        if device is None and at >= 0 and at == torch.cuda.current_device():
+            device = at
+        if t.nbytes < nbytes or at != device or not t.is_contiguous():
+            raise ValueError(f"{what}: an operand must be a contiguous tensor on the current CUDA device that holds what the descriptor says")
+        if dtype is not torch.bfloat16 and dtype.is_floating_point:
+            raise ValueError(f"{what}: an operand is {dtype}, not bfloat16")
+    return device
 
 
-def _check_vector(t, n, what):
-    if t is not None and (t.dtype != torch.bfloat16 or t.nbytes < 2 * n or not t.is_cuda or not t.is_contiguous()):
-        raise ValueError(f"{what} must be a contiguous bfloat16 CUDA tensor with at least {n} entries")
+def _check_vector(t, n, what, device):
+    if t is not None and (t.dtype is not torch.bfloat16 or t.nbytes < 2 * n or t.get_device() != device or not t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous bfloat16 tensor with at least {n} entries beside the operands")
+
+
+def _check_workspace(t, what, device):
+    """Bytes of a workspace of any type (the library says whether they are enough)."""
+    if t is None:
+        return 0
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what}: the workspace must be contiguous and beside the operands")
+    return t.nbytes
 
 
 _gemm_bytes_cache = {}
@@ -324,10 +343,10 @@ def ccl_gemm_epilogue_workspace(d):
 def ccl_gemm_epilogue(d, A, B, Cout, ws=None, act=ACT_NONE, bias=None, residual=None, preact=None):
     """C = act(A*B + bias) + residual; preact receives A*B + bias.  bias: [N] bfloat16; residual (may be Cout) and preact in C's layout."""
     a_bytes, b_bytes, c_bytes = _gemm_bytes(d)
-    _check_operands("ccl_gemm_epilogue", (A, a_bytes), (B, b_bytes), (Cout, c_bytes), (residual, c_bytes), (preact, c_bytes))
-    _check_vector(bias, d.N, "ccl_gemm_epilogue: bias")
+    device = _check_operands("ccl_gemm_epilogue", (A, a_bytes), (B, b_bytes), (Cout, c_bytes), (residual, c_bytes), (preact, c_bytes))
+    _check_vector(bias, d.N, "ccl_gemm_epilogue: bias", device)
+    ws_bytes = _check_workspace(ws, "ccl_gemm_epilogue", device)
     e = Epilogue(act, _ptr(bias), _ptr(residual), _ptr(preact))
-    ws_bytes = ws.nbytes if ws is not None else 0
     _check(lib().ccl_gemm_epilogue(C.byref(d), C.byref(e), _ptr(A), _ptr(B), _ptr(Cout), _ptr(ws), ws_bytes, _stream()))
 
 
@@ -338,17 +357,17 @@ def ccl_gemm_act_grad_workspace(d):
 def ccl_gemm_act_grad(d, A, B, preact, dz, ws=None, act=ACT_NONE, dbias=None):
     """dz = (A*B) * act'(preact), dbias = its column sums.  preact and dz in C's layout; dbias: [N] bfloat16."""
     a_bytes, b_bytes, c_bytes = _gemm_bytes(d)
-    _check_operands("ccl_gemm_act_grad", (A, a_bytes), (B, b_bytes), (preact, c_bytes), (dz, c_bytes))
-    _check_vector(dbias, d.N, "ccl_gemm_act_grad: dbias")
-    ws_bytes = ws.nbytes if ws is not None else 0
+    device = _check_operands("ccl_gemm_act_grad", (A, a_bytes), (B, b_bytes), (preact, c_bytes), (dz, c_bytes))
+    _check_vector(dbias, d.N, "ccl_gemm_act_grad: dbias", device)
+    ws_bytes = _check_workspace(ws, "ccl_gemm_act_grad", device)
     _check(lib().ccl_gemm_act_grad(C.byref(d), act, _ptr(A), _ptr(B), _ptr(preact), _ptr(dz), _ptr(dbias), _ptr(ws), ws_bytes, _stream()))
 
 
 def ccl_bias_act_grad(m, dy, preact, dz, dbias=None, act=ACT_NONE):
     """dz = dy * act'(preact) (None: not wanted), dbias = its column sums; dy, preact and dz as `m` describes, dbias: [cols] bfloat16."""
     nbytes = ccl_buffer_bytes(m)
-    _check_operands("ccl_bias_act_grad", (dy, nbytes), (preact, nbytes), (dz, nbytes))
-    _check_vector(dbias, m.cols, "ccl_bias_act_grad: dbias")
+    device = _check_operands("ccl_bias_act_grad", (dy, nbytes), (preact, nbytes), (dz, nbytes))
+    _check_vector(dbias, m.cols, "ccl_bias_act_grad: dbias", device)
     _check(lib().ccl_bias_act_grad(C.byref(m), act, _ptr(dy), _ptr(preact), _ptr(dz), _ptr(dbias), _stream()))
 
 
@@ -356,15 +375,25 @@ def ccl_moe_tokens_workspace(d):
     return _size(lib().ccl_moe_tokens_workspace, d)
 
 
+def _check_moe(what, d, X, Wr, Wgu, Wd, residual, Y, ws):
+    """Returns the device and the workspace's bytes."""
+    th, gu, dn = 2 * d.T * d.H, 4 * d.I * d.H, 2 * d.I * d.H
+    device = _check_operands(what, (X, th), (Y, th), (residual, th), (Wr, 2 * d.E * d.H), (Wgu, (d.E - 1) * (d.gu_stride_bytes or gu) + gu),
+                             (Wd, (d.E - 1) * (d.d_stride_bytes or dn) + dn))
+    return device, _check_workspace(ws, what, device)
+
+
+def _check_choice(t, dtype, n, what, device):
+    if t is not None and (t.dtype is not dtype or t.numel() < n or t.get_device() != device or not t.is_contiguous()):
+        raise ValueError(f"ccl_moe_tokens: {what} must be a contiguous {dtype} tensor with at least {n} entries beside the operands")
+
+
 def ccl_moe_tokens(d, X, Wr, Wgu, Wd, Y, ws, residual=None, ids=None, weights=None):
     """A mixture-of-experts layer for d.T tokens: Y = residual + sum over each token's topk experts.  Wr [E x H], Wgu per expert
     [2I x H], Wd per expert [H x I]; ids int32 / weights float32 [T x topk] receive the choice if wanted."""
-    th, gu, dn = 2 * d.T * d.H, 4 * d.I * d.H, 2 * d.I * d.H
-    _check_operands("ccl_moe_tokens", (X, th), (Y, th), (residual, th), (Wr, 2 * d.E * d.H), (Wgu, (d.E - 1) * (d.gu_stride_bytes or gu) + gu),
-              (Wd, (d.E - 1) * (d.d_stride_bytes or dn) + dn), (ids, 4 * d.T * d.topk), (weights, 4 * d.T * d.topk))
-    if (ids is not None and ids.dtype != torch.int32) or (weights is not None and weights.dtype != torch.float32):
-        raise ValueError("ccl_moe_tokens: ids must be int32 and weights float32")
-    ws_bytes = ws.nbytes if ws is not None else 0
+    device, ws_bytes = _check_moe("ccl_moe_tokens", d, X, Wr, Wgu, Wd, residual, Y, ws)
+    _check_choice(ids, torch.int32, d.T * d.topk, "ids", device)
+    _check_choice(weights, torch.float32, d.T * d.topk, "weights", device)
     _check(lib().ccl_moe_tokens(C.byref(d), _ptr(X), _ptr(Wr), _ptr(Wgu), _ptr(Wd), _ptr(residual), _ptr(Y), _ptr(ids), _ptr(weights), _ptr(ws), ws_bytes,
                                 _stream()))
 
@@ -395,7 +424,8 @@ def ccl_selftest_wait_timeout(which, limit_us, src=None):
 
 def ccl_selftest_moe_timeout(d, X, Wr, Wgu, Wd, Y, ws, meeting, limit_us):
     """Test support: ccl_moe_tokens with a meeting (1 or 2) of its CTAs that waits for one more than there are, for limit_us at most."""
-    _check(lib().ccl_selftest_moe_timeout(C.byref(d), _ptr(X), _ptr(Wr), _ptr(Wgu), _ptr(Wd), _ptr(Y), _ptr(ws), ws.nbytes, meeting, limit_us, _stream()))
+    _, ws_bytes = _check_moe("ccl_selftest_moe_timeout", d, X, Wr, Wgu, Wd, None, Y, ws)
+    _check(lib().ccl_selftest_moe_timeout(C.byref(d), _ptr(X), _ptr(Wr), _ptr(Wgu), _ptr(Wd), _ptr(Y), _ptr(ws), ws_bytes, meeting, limit_us, _stream()))
 
 
 def ccl_traffic_sizes(d):

@@ -135,9 +135,16 @@ def _check(status):
         raise CclError(status, lib().ccl_last_error().decode())
 
 
+# torch.cuda.current_stream() builds an object around the handle, 3 us a call; these two do not, but are not part of torch's public
+# interface: a torch that lacks one of them gets the public call.
+_raw_stream, _raw_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream():
-    """Handle of torch's current stream (an int; torch.cuda.current_stream() builds an object around it, 3 us)."""
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    """Handle (an int) of torch's current stream on the current device."""
+    if _raw_stream is None or _raw_device is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(_raw_device())
 
 
 def _ptr(t):

@@ -326,13 +326,16 @@ def _check_workspace(t, what, device):
 
 
 _gemm_bytes_cache = {}
+GEMM_BYTES_ENTRIES = 1024
 
 
 def _gemm_bytes(d):
-    """Bytes of the buffers of A, B and C that a GEMM descriptor addresses (kept by the descriptor's contents)."""
+    """Bytes of the buffers of A, B and C that a GEMM descriptor addresses (kept by the descriptor's contents, for so many at most)."""
     key = bytes(d)
     v = _gemm_bytes_cache.get(key)
     if v is None:
+        if len(_gemm_bytes_cache) >= GEMM_BYTES_ENTRIES:
+            _gemm_bytes_cache.clear()
         v = _gemm_bytes_cache[key] = tuple(ccl_buffer_bytes(m) for m in (d.A, d.B, d.C))
     return v
 

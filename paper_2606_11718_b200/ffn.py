@@ -21,7 +21,8 @@ def _buffer(m):
 
 class Block:
     """y = x + act(x W1 + b1) W2 + b2 for `tokens` rows; W1 [H x I] and W2 [I x H] row-major bfloat16.  With strips > 1 W1, the inner
-    activation and its gradient are stored in that many column strips (I / strips a multiple of 64)."""
+    activation and its gradient are stored in that many column strips (I / strips a multiple of 64).  The inner activations of the last
+    forward pass and the workspace are kept in the object: its calls go to one stream, or wait for each other."""
 
     def __init__(self, w1, b1, w2, b2, tokens, act=ccl.ACT_GELU_TANH, strips=1):
         H, I = w1.shape
@@ -75,21 +76,23 @@ class Block:
 
 
 class MoeLayer:
-    """Decode steps through a mixture-of-experts layer: router [E x H], w_gu [E x 2I x H] (gate rows, then up rows), w_down [E x H x I]."""
+    """Decode steps through a mixture-of-experts layer: router [E x H], w_gu [E x 2I x H] (gate rows, then up rows), w_down [E x H x I].
+    Steps on different streams may overlap: each has a workspace of its own, from torch's allocator for its stream."""
 
     def __init__(self, router, w_gu, w_down, topk, norm_topk=True):
         self.weights = (router, w_gu, w_down)
         self.E, self.H = router.shape
         self.I, self.topk, self.norm = w_down.shape[2], topk, int(norm_topk)
-        self.plans = {}                                                               # tokens -> descriptor, workspace
+        self.plans = {}                                                               # tokens -> descriptor, bytes of workspace
 
     def step(self, x, out=None):
         """out = x + layer(x) for x [T x H], T <= 64; out may be x."""
         T = x.shape[0]
         if T not in self.plans:
             d = ccl.MoeDesc(T, self.E, self.topk, self.H, self.I, norm_topk=self.norm)
-            self.plans[T] = d, torch.empty(ccl.ccl_moe_tokens_workspace(d), dtype=torch.uint8, device="cuda")
-        d, ws = self.plans[T]
+            self.plans[T] = d, ccl.ccl_moe_tokens_workspace(d)
+        d, ws_bytes = self.plans[T]
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device="cuda")
         out = torch.empty_like(x) if out is None else out
         ccl.ccl_moe_tokens(d, x, *self.weights, out, ws, residual=x)
         return out

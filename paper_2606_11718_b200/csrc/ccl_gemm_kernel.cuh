@@ -612,7 +612,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     constexpr int SUBN1 = NSUB == 1 ? 0 : BN - 256;   // width of the second
     constexpr int ACC_COLS = 256;                     // TMEM columns between accumulators
     constexpr int NACC = 2;                           // accumulator barriers in use
-    static_assert(EPI == 0 || (!SWIGLU && RAG == 0), "the epilogue operators are plain calls");
+    static_assert(EPI == 0 || (!SWIGLU && RAG == 0 && NSUB == 1), "the epilogue operators are plain calls, their tiles have one accumulator");
     static_assert(!SWIGLU || BN == 512, "the gated activation pairs the two accumulators of a wide tile");
     constexpr int TILE_N = SWIGLU ? SUBN : BN;        // tile width in the columns the tile walk counts (output columns)
     constexpr int SUBH = SUBN / CTAS;                // B columns of the first sub-tile this CTA stages
@@ -917,19 +917,17 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         constexpr bool kOp = EPI != 0 && KS == 0;
         unsigned char* op_buf = epi + (size_t)(warp - 2) * (32 * 128);
         uint32_t addend_phase = 0;
-        [[maybe_unused]] struct { int it, h, c; bool ok, out; TileCoord t; } ap = {};       // out: a fetch is under way
+        [[maybe_unused]] struct { int it, c; bool ok, out; TileCoord t; } ap = {};          // out: a fetch is under way
         auto fetch_addend = [&]() {
             if constexpr (kOp) {
                 while (ap.ok) {                          // the next piece that exists
-                    const int n0 = ap.t.n0 + ap.h * SUBN;
-                    if (!ap.t.skip && ap.h < NSUB && ap.c < ((ap.h == 0 ? SUBN : SUBN1) / 64) && n0 + ap.c * 64 < ap.t.n1) break;
-                    if (!ap.t.skip && ap.h + 1 < NSUB) { ++ap.h; ap.c = hf; continue; }
-                    ap.h = 0; ap.c = hf;
+                    if (!ap.t.skip && ap.c < SUBN / 64 && ap.t.n0 + ap.c * 64 < ap.t.n1) break;
+                    ap.c = hf;
                     ap.ok = sched.template get<RAG, FULL>(++ap.it, ap.t);
                 }
                 if (!ap.ok) return;
                 if (lane == 0) {
-                    const int r = ap.t.m0 + (int)rank * BM + quad * 32, n = ap.t.n0 + ap.h * SUBN + ap.c * 64;
+                    const int r = ap.t.m0 + (int)rank * BM + quad * 32, n = ap.t.n0 + ap.c * 64;
                     int x, y, z, u;
                     to_coords<FULL>(p.c, r, n, x, y, z, u);
                     const CUtensorMap* map = &em.addend;
@@ -944,7 +942,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         const bool addend_ahead = kOp && p.addend && p.addend_tma && p.splits == 1;
         if constexpr (kOp)
             if (addend_ahead) {
-                ap.it = 0; ap.h = 0; ap.c = hf;
+                ap.it = 0; ap.c = hf;
                 ap.ok = sched.template get<RAG, FULL>(0, ap.t);
                 fetch_addend();
             }

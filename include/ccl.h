@@ -327,7 +327,8 @@ ccl_status ccl_gemm_static_ws(const ccl_gemm_desc* d, const void* A_dev, const v
  * What a feed-forward block does between its GEMMs, in their epilogues, and its gradients.  The paper has no counterpart:
  * like ccl_gemm_swiglu these keep activations in the layout the next GEMM reads (Sec. 3.3).  bf16 storage, fp32 arithmetic,
  * every output rounded once, to nearest even.  Activations are good to about 2^-19 of their value (their exponentials, of an
- * argument t, to |t| 2^-22 more), also where gelu and silu are small beside their argument.
+ * argument t, to |t| 2^-21 more), also where gelu and silu are small beside their argument, down to where the exponential leaves
+ * fp32's normal numbers and they become zero.
  */
 
 typedef enum {
@@ -393,6 +394,7 @@ ccl_status ccl_bias_act_grad(const ccl_mat* m, int32_t act, const void* dY_dev, 
  *   logits = X * Wr^T (fp32),  p = softmax(logits) over the E experts,  the topk largest p of each token (equal ones: the
  *   lowest expert first),  weight w = p, divided by the sum of the token's topk p when norm_topk is set,
  *   Y[t] = bf16( residual[t] + sum over the chosen experts e of w_te * Wd_e * ( silu(Wg_e x_t) .* (Wu_e x_t) ) )
+ * (fp32 sums; between the two products silu(Wg_e x) .* (Wu_e x) is held in 16 significant bits, a bf16 value and a bf16 remainder)
  *   X [T x H], residual [T x H] (or NULL; may be Y itself), Y [T x H]: bf16 row-major
  *   Wr        bf16 [E x H]
  *   Wgu       per expert bf16 [2I x H] (K along the rows): I gate rows, then I up rows; with gu_strips = S > 1 the rows form S

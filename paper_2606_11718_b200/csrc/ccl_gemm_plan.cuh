@@ -424,7 +424,8 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     // the warps that drain an operator's tiles: eight and a long ring where a tile's product is longer than its drain, sixteen and a
     // shorter one where the drain is what the tiles wait for; both grow with the tile's width, so K decides (4096 x 8192, gelu
     // and a residual, eight / sixteen: K = 1024 88 / 74 us, 2048 107 / 108, 4096 197 / 203; gradient: K = 256 72 / 67, 1024 89 / 89,
-    // 2048 111 / 115, 4096 201 / 210).  The kernels with every layout exist with eight, the cluster split drains once, with sixteen.
+    // 2048 111 / 115, 4096 201 / 210).  Those are problems of seven rounds of tiles; with one round, where no next tile hides the
+    // drain, the two have not been compared.  The kernels with every layout exist with eight, the cluster split drains once, with sixteen.
     const int opw = ks ? 16 : (epi_full || p.kb_per_split * BK >= 1536 ? 8 : 16);
     plan->opw = opw;
     p.stages = (int32_t)(((epi ? smem_budget_op(ks, opw) : kSmemBudget) - rag_bytes) / p.stage_bytes);

@@ -19,8 +19,8 @@
 // cycles), and h by TMA as well had the products wait.  (Consumers that issued their own copies, or read h themselves, made loops
 // that were slower to run than the weights to come: phase 3 of 64 tokens x 128 experts of 2048 x 768 took 118 and 86 us, 66 now.)
 //
-// Measured (B200, 128 experts of 2048 x 768, 8 a token): 64 tokens 215 us, 5.5 TB/s over everything and above 6 while weights stream;
-// 16 tokens 136 us; one token 29.6 us, of which the weights take 12 and the rest is launch, router, top-k and two meetings.
+// Measured (B200, 128 experts of 2048 x 768, 8 a token): 64 tokens 215-226 us, 5.3-5.5 TB/s over everything and above 6 while weights
+// stream; 16 tokens 134-136 us; one token 29.5-30.7 us, of which the weights take 12 and the rest is launch, router, top-k and two meetings.
 //
 // The matrix instructions are mma.sync: with n = 8 columns a tcgen05 tile would be 128 rows high and leave most SMs without
 // work for one token; they are nowhere near their limit here.  Weights and tokens are both K-contiguous, so a lane may take any 8

@@ -423,6 +423,82 @@ ccl_status ccl_moe_tokens(const ccl_moe_desc* d, const void* X_dev, const void* 
                           const void* residual_dev, void* Y_dev, int32_t* ids_dev, float* weights_dev, void* ws_dev,
                           size_t ws_bytes, void* cuda_stream);
 
+/* ---- around the feed-forward blocks of a training step ----------------------------------
+ *
+ * What stands before a block (the normalisation of the residual stream), behind the last one (the loss over a vocabulary) and after the
+ * backward pass (the parameters' update).  The paper has no counterpart.  Matrices bf16, arithmetic and statistics fp32, every output
+ * rounded once to nearest even.
+ */
+
+typedef enum { CCL_NORM_LAYER = 0, CCL_NORM_RMS = 1 } ccl_norm_kind;
+
+/*
+ * Every row of X [rows x cols, cols = H] normalised:
+ *   CCL_NORM_LAYER  mean = sum(x) / H,  rstd = 1 / sqrt(sum((x - mean)^2) / H + eps),  y = (x - mean) * rstd * gamma + beta
+ *   CCL_NORM_RMS    rstd = 1 / sqrt(sum(x^2) / H + eps),                                y = x * rstd * gamma
+ * X and Y are both stored as `m` describes (2-byte elements, any layout the map accepts, fewer than 2^31 columns; padding is not
+ * touched); Y_dev may be X_dev.  gamma, beta: bf16 [H], NULL: ones / zeros.  mean_dev, rstd_dev: fp32 [rows], what the gradient needs;
+ * NULL: not wanted.  beta_dev and mean_dev are NULL with CCL_NORM_RMS.  Bases 2-byte aligned (fp32 ones 4-byte); 16-byte aligned ones
+ * with column groups of 8 that are aligned pieces of the buffer take the fast path.  eps >= 0; a constant row with eps = 0 gives NaN.
+ */
+ccl_status ccl_norm(const ccl_mat* m, int32_t kind, float eps, const void* X_dev, const void* gamma_dev, const void* beta_dev, void* Y_dev,
+                    float* mean_dev, float* rstd_dev, void* cuda_stream);
+/*
+ * Its gradient, from X and the statistics that ccl_norm left (mean_dev is not read with CCL_NORM_RMS).  With h = (x - mean) * rstd, g = dy * gamma:
+ *   dX = bf16( rstd * (g - sum(g) / H - h * sum(g * h) / H) + addend )        (without the sum(g) term for CCL_NORM_RMS)
+ *   dgamma = bf16( sum over rows of dy * h ),  dbeta = bf16( sum over rows of dy )        (in a fixed order: the same bits on every run)
+ *   addend_dev  bf16, stored like X: the gradient that reaches X past the normalisation (the residual stream's); NULL: none
+ *   dX_dev, dgamma_dev, dbeta_dev: NULL: not wanted; dX_dev may be X_dev, dY_dev or addend_dev.  dbeta_dev is NULL with CCL_NORM_RMS.
+ * Workspace: ccl_norm_grad_workspace bytes, needed for dgamma / dbeta only; whatever they hold.  Calls that can overlap on the GPU must
+ * not share it.
+ */
+ccl_status ccl_norm_grad_workspace(const ccl_mat* m, size_t* bytes);
+ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* X_dev, const void* gamma_dev, const float* mean_dev, const float* rstd_dev,
+                         const void* dY_dev, const void* addend_dev, void* dX_dev, void* dgamma_dev, void* dbeta_dev, void* ws_dev, size_t ws_bytes,
+                         void* cuda_stream);
+
+/*
+ * One step of AdamW over `count` tensors.  Step t (from 1 on) of a parameter p with gradient g, moments m and v and r = sqrt(v):
+ *   g = g * grad_scale                                  (only with grad_scale_dev)
+ *   m = m * beta1 + g * (1 - beta1)
+ *   v = v * beta2 + (g * (1 - beta2)) * g
+ *   p = p * (1 - lr * weight_decay) - (m / (r * (1 / sqrt(1 - beta2^t)) + eps)) * (lr / (1 - beta1^t))
+ * The factors that hold no tensor are computed in 64 bits and rounded to fp32 once; every other operation is rounded to nearest in fp32,
+ * in the order written: the same bits on every run.
+ *   state_bits = 32: m and v are fp32 [n].
+ *   state_bits = 8:  m and v are e4m3 [n], m_scale and v_scale fp32 [ceil(n / 256)]: element i of m stands for m[i] * m_scale[i / 256],
+ *       element i of v for the ROOT r = v[i] * v_scale[i / 256].  A step decodes them, computes as above and keeps, of each 256 elements,
+ *       scale = top * (1 / 448) and e4m3(value * (448 / top)), top the largest magnitude; an r > 0 never becomes 0 but the least e4m3
+ *       value instead.  A block whose top is below 1e-30 is kept as zeros (scale 0); one with a NaN or an infinite value is NaN from then on.
+ *       All bytes and scales zero are the states before the first step.
+ * param fp32 [n]; param_bf16: receives bf16(p), the weights that the products read, NULL: not wanted; grad bf16 [n], or fp32 [n] with
+ * grad_fp32.  The operation is elementwise but for the blocks of 256: any layout of a matrix will do, the same for all of its buffers.
+ * Tensors with n = 0 are skipped.  No two buffers of a call may overlap.  Buffers are aligned to their types; tensors whose buffers allow
+ * 16-byte accesses four elements at a time take the fast path.
+ *   grad_scale_dev  fp32 [1] on the DEVICE (the factor that clips gradients or takes back a loss scale), NULL: none
+ *   step_dev        int64 [1] on the DEVICE: the step's number, read by the kernel, so that a captured call can be replayed; NULL: `step`
+ *   lr_dev          fp32 [1] on the DEVICE in place of lr, with step_dev only; NULL: `lr`
+ * The list itself is read before the call returns.  lr, weight_decay >= 0; beta1, beta2 in [0, 1); eps > 0.  One launch for every 400 tensors.
+ */
+typedef struct ccl_adamw_tensor {
+    int64_t n;
+    float* param;
+    void* param_bf16;
+    const void* grad;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    int32_t grad_fp32;
+} ccl_adamw_tensor;
+typedef struct ccl_adamw_desc {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;
+    int32_t state_bits;
+    const float* grad_scale_dev;
+    const float* lr_dev;
+    const int64_t* step_dev;
+} ccl_adamw_desc;
+ccl_status ccl_adamw(const ccl_adamw_desc* d, const ccl_adamw_tensor* tensors, int32_t count, void* cuda_stream);
+
 /* ---- remote-traffic counter (Sec. 4.1 metric, every touched byte counted: no L2 filter) */
 
 typedef enum { CCL_PLACE_RR = 0, CCL_PLACE_BLOCK = 1, CCL_PLACE_BEST = 2 } ccl_place;

@@ -18,11 +18,13 @@ ROWMAJOR, CCL, CCL_INTERLEAVED = 0, 1, 2
 PART_NONE, PART_ROWS, PART_COLS, PART_2D = 0, 1, 2, 3
 PLACE_RR, PLACE_BLOCK, PLACE_BEST = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_GELU_TANH, ACT_GELU_ERF, ACT_SILU = 0, 1, 2, 3, 4
+NORM_LAYER, NORM_RMS = 0, 1
 ASSIGN_N_STRIPS, ASSIGN_M_STRIPS, ASSIGN_EXPLICIT, ASSIGN_2D = 0, 1, 2, 3
 
 EXPORTS = ["ccl_map_offset", "ccl_map_inverse", "ccl_buffer_bytes", "ccl_strip_stride", "ccl_repack", "ccl_repack_batched", "ccl_repack_transpose", "ccl_gemm_workspace",
            "ccl_gemm", "ccl_gemm_batched_workspace", "ccl_gemm_batched", "ccl_gemm_grouped", "ccl_gemm_grouped_swiglu", "ccl_gemm_grouped_k", "ccl_gemm_axpby", "ccl_gemm_swiglu", "ccl_gemm_static_ws", "ccl_gemm_status", "ccl_selftest_wait_timeout", "ccl_selftest_moe_timeout", "ccl_gemm_epilogue_workspace", "ccl_gemm_epilogue",
-           "ccl_gemm_act_grad_workspace", "ccl_gemm_act_grad", "ccl_bias_act_grad", "ccl_moe_tokens_workspace", "ccl_moe_tokens", "ccl_traffic_sizes", "ccl_traffic", "ccl_traffic_l2", "ccl_traffic_lru", "ccl_probe_l2_latency", "ccl_last_error", "ccl_launch_count", "ccl_version"]
+           "ccl_gemm_act_grad_workspace", "ccl_gemm_act_grad", "ccl_bias_act_grad", "ccl_moe_tokens_workspace", "ccl_moe_tokens",
+           "ccl_norm", "ccl_norm_grad_workspace", "ccl_norm_grad", "ccl_adamw", "ccl_traffic_sizes", "ccl_traffic", "ccl_traffic_l2", "ccl_traffic_lru", "ccl_probe_l2_latency", "ccl_last_error", "ccl_launch_count", "ccl_version"]
 
 
 class CclError(RuntimeError):
@@ -59,6 +61,21 @@ class MoeDesc(C.Structure):
 
     def __init__(self, T=0, E=0, topk=0, H=0, I=0, norm_topk=1, gu_strips=1, gu_stride_bytes=0, d_stride_bytes=0):
         super().__init__(T, H, I, E, topk, norm_topk, gu_strips, gu_stride_bytes, d_stride_bytes)
+
+
+class AdamwTensor(C.Structure):
+    """ccl_adamw_tensor"""
+    _fields_ = [("n", C.c_int64), ("param", C.c_void_p), ("param_bf16", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("grad_fp32", C.c_int32)]
+
+
+class AdamwDesc(C.Structure):
+    """ccl_adamw_desc (the width of the states comes from the tensors, the device scalars from ccl_adamw's arguments)"""
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double), ("step", C.c_int64),
+                ("state_bits", C.c_int32), ("grad_scale_dev", C.c_void_p), ("lr_dev", C.c_void_p), ("step_dev", C.c_void_p)]
+
+    def __init__(self, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1):
+        super().__init__(lr, beta1, beta2, eps, weight_decay, step, 32, None, None, None)
 
 
 class TrafficDesc(C.Structure):
@@ -120,6 +137,10 @@ def lib():
         l.ccl_bias_act_grad.argtypes = [C.POINTER(Mat), C.c_int32] + [C.c_void_p] * 5
         l.ccl_moe_tokens_workspace.argtypes = [C.POINTER(MoeDesc), C.POINTER(C.c_size_t)]
         l.ccl_moe_tokens.argtypes = [C.POINTER(MoeDesc)] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]
+        l.ccl_norm.argtypes = [C.POINTER(Mat), C.c_int32, C.c_float] + [C.c_void_p] * 7
+        l.ccl_norm_grad_workspace.argtypes = [C.POINTER(Mat), C.POINTER(C.c_size_t)]
+        l.ccl_norm_grad.argtypes = [C.POINTER(Mat), C.c_int32] + [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]
+        l.ccl_adamw.argtypes = [C.POINTER(AdamwDesc), C.POINTER(AdamwTensor), C.c_int32, C.c_void_p]
         l.ccl_selftest_moe_timeout.argtypes = [C.POINTER(MoeDesc)] + [C.c_void_p] * 6 + [C.c_size_t, C.c_int32, C.c_uint32, C.c_void_p]
         l.ccl_traffic_sizes.argtypes = [C.POINTER(TrafficDesc), C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
         l.ccl_traffic.argtypes = [C.POINTER(TrafficDesc), C.c_void_p, C.c_void_p, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
@@ -316,6 +337,11 @@ def _check_vector(t, n, what, device):
         raise ValueError(f"{what} must be a contiguous bfloat16 tensor with at least {n} entries beside the operands")
 
 
+def _check_beside(t, dtype, n, what, device):
+    if t is not None and (t.dtype is not dtype or t.numel() < n or t.get_device() != device or not t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor with at least {n} entries beside the operands")
+
+
 def _check_workspace(t, what, device):
     """Bytes of a workspace of any type (the library says whether they are enough)."""
     if t is None:
@@ -406,6 +432,92 @@ def ccl_moe_tokens(d, X, Wr, Wgu, Wd, Y, ws, residual=None, ids=None, weights=No
     _check_choice(weights, torch.float32, d.T * d.topk, "weights", device)
     _check(lib().ccl_moe_tokens(C.byref(d), _ptr(X), _ptr(Wr), _ptr(Wgu), _ptr(Wd), _ptr(residual), _ptr(Y), _ptr(ids), _ptr(weights), _ptr(ws), ws_bytes,
                                 _stream()))
+
+
+def ccl_norm(m, X, gamma, beta, Y, kind=NORM_LAYER, eps=1e-5, mean=None, rstd=None):
+    """Y = (X - mean) * rstd * gamma + beta for every row (NORM_RMS: X * rstd * gamma); X and Y (may be X) as `m` describes, gamma and beta [cols]
+    bfloat16 or None, mean and rstd float32 [rows] receive the statistics if wanted."""
+    nbytes = ccl_buffer_bytes(m)
+    device = _check_operands("ccl_norm", (X, nbytes), (Y, nbytes))
+    _check_vector(gamma, m.cols, "ccl_norm: gamma", device)
+    _check_vector(beta, m.cols, "ccl_norm: beta", device)
+    _check_beside(mean, torch.float32, m.rows, "ccl_norm: mean", device)
+    _check_beside(rstd, torch.float32, m.rows, "ccl_norm: rstd", device)
+    _check(lib().ccl_norm(C.byref(m), kind, eps, _ptr(X), _ptr(gamma), _ptr(beta), _ptr(Y), _ptr(mean), _ptr(rstd), _stream()))
+
+
+def ccl_norm_grad_workspace(m):
+    return _size(lib().ccl_norm_grad_workspace, m)
+
+
+def ccl_norm_grad(m, X, gamma, mean, rstd, dy, dx, ws=None, kind=NORM_LAYER, addend=None, dgamma=None, dbeta=None):
+    """dx = gradient of ccl_norm's X (+ addend), dgamma / dbeta [cols] bfloat16 = those of its weights; None: not wanted.  ws: for the sums only."""
+    nbytes = ccl_buffer_bytes(m)
+    device = _check_operands("ccl_norm_grad", (X, nbytes), (dy, nbytes), (dx, nbytes), (addend, nbytes))
+    for t, what in ((gamma, "gamma"), (dgamma, "dgamma"), (dbeta, "dbeta")):
+        _check_vector(t, m.cols, "ccl_norm_grad: " + what, device)
+    _check_beside(mean, torch.float32, m.rows, "ccl_norm_grad: mean", device)
+    _check_beside(rstd, torch.float32, m.rows, "ccl_norm_grad: rstd", device)
+    ws_bytes = _check_workspace(ws, "ccl_norm_grad", device)
+    _check(lib().ccl_norm_grad(C.byref(m), kind, _ptr(X), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dy), _ptr(addend), _ptr(dx), _ptr(dgamma), _ptr(dbeta),
+                               _ptr(ws), ws_bytes, _stream()))
+
+
+def _current_device():
+    return torch.cuda.current_device() if torch.cuda.is_available() else None
+
+
+ADAMW_BLOCK = 256                                              # elements that share a scale of the 8-bit states
+
+
+class AdamwTensors:
+    """The tensors of an update, checked and laid out once: params float32, grads bfloat16 or float32 and the states m and v of the same sizes, all
+    float32, or (8 bits) float8_e4m3fn or uint8 with m_scales and v_scales float32 of ceil(n / 256); copies: bfloat16 or None, the weights that the
+    products read.  Lists of contiguous tensors on the current CUDA device, none overlapping another.  Kept alive by the object; what they hold may
+    change between steps, where they are may not."""
+
+    def __init__(self, params, grads, m, v, copies=None, m_scales=None, v_scales=None):
+        n = len(params)
+        copies = copies if copies is not None else [None] * n
+        eight = m_scales is not None or v_scales is not None
+        columns = [params, copies, grads, m, v] + ([m_scales or [], v_scales or []] if eight else [])
+        if any(len(c) != n for c in columns):
+            raise ValueError("AdamwTensors: lists of different lengths")
+        states = (torch.float8_e4m3fn, torch.uint8) if eight else (torch.float32,)
+        wanted = [(torch.float32,), (torch.bfloat16,), (torch.bfloat16, torch.float32), states, states, (torch.float32,), (torch.float32,)]
+        self.bits, self.count, self.tensors, self.device = (8 if eight else 32), n, columns, _current_device() if n else None
+        self.table = (AdamwTensor * max(n, 1))()
+        spans = []
+        for i in range(n):
+            size = params[i].numel()
+            for k, c in enumerate(columns):
+                t = c[i]
+                if t is None and k == 1:
+                    continue
+                if t is None or t.dtype not in wanted[k] or t.get_device() != self.device or not t.is_contiguous() or t.numel() != (size if k < 5 else -(-size // ADAMW_BLOCK)):
+                    raise ValueError(f"AdamwTensors: tensor {i}: a buffer has another type, size or device than its place asks for, or is not contiguous")
+                if t.numel():
+                    spans.append((t.data_ptr(), t.data_ptr() + t.nbytes, i))
+            scales = [_ptr(columns[5][i]), _ptr(columns[6][i])] if eight else [None, None]
+            self.table[i] = AdamwTensor(size, _ptr(params[i]), _ptr(copies[i]), _ptr(grads[i]), _ptr(m[i]), _ptr(v[i]), *scales, int(grads[i].dtype is torch.float32))
+        spans.sort()
+        for (_, end, i), (start, _, j) in zip(spans, spans[1:]):
+            if start < end:
+                raise ValueError(f"AdamwTensors: buffers of tensors {i} and {j} overlap")
+
+
+def ccl_adamw(d, tensors, grad_scale=None, step=None, lr=None):
+    """One step of AdamW over an AdamwTensors.  grad_scale: float32 CUDA tensor with the gradients' factor; step (int64) and lr (float32, with step):
+    CUDA tensors read when the kernel runs, in place of d.step and d.lr."""
+    device = tensors.device
+    if tensors.count and device != _current_device():
+        raise ValueError("ccl_adamw: the tensors are not on the current CUDA device")
+    _check_beside(grad_scale, torch.float32, 1, "ccl_adamw: grad_scale", device)
+    _check_beside(step, torch.int64, 1, "ccl_adamw: step", device)
+    _check_beside(lr, torch.float32, 1, "ccl_adamw: lr", device)
+    call = AdamwDesc.from_buffer_copy(d)
+    call.state_bits, call.grad_scale_dev, call.step_dev, call.lr_dev = tensors.bits, _ptr(grad_scale), _ptr(step), _ptr(lr)
+    _check(lib().ccl_adamw(C.byref(call), tensors.table, tensors.count, _stream()))
 
 
 GEMM_STATIC_WS_BYTES = 8 * 1024 * 1024

@@ -1,0 +1,624 @@
+// ccl_norm: y = (x - mean) / sqrt(var + eps) * gamma + beta of every row (or x / sqrt(mean of squares + eps) * gamma), and
+// ccl_norm_grad: the gradients of x, gamma and beta.
+//
+// Bound by memory: a row is read once into registers, its statistics are taken from there and the result is written from there.  The
+// variance is the mean square about a mean: about the warp's own one first, and the warps' moments are then joined with
+//   var = sum of var_w + n_w / H (mean_w - mean)^2          (var_w: a warp's share of the mean square about its own mean)
+// so that one meeting of a row's warps is enough and a mean far from zero costs no digits (a difference of E x^2 and (E x)^2 would).
+// CTAs are persistent and fetch their next row while the present one meets.  The gradients of gamma and beta are sums over the rows:
+// every thread keeps its columns' sums in registers, a CTA leaves one line of them in the workspace, and a second kernel, placed early,
+// adds the lines in a fixed order: no atomics, the same bits on every run.
+#include <algorithm>
+#include <atomic>
+
+#include "ccl_act.cuh"
+#include "ccl_tma.h"
+
+namespace ccl {
+
+bool device_units(int* sms, int* pairs);                 // ccl_gemm.cu
+
+struct NormParams {
+    MatView v;
+    const uint16_t *x, *dy, *addend, *gamma, *beta;
+    uint16_t* out;                  // y or dx (may be one of the inputs: an element is written by the thread that has read it)
+    float *mean, *rstd;             // written by ccl_norm, read by ccl_norm_grad
+    float* partial;                 // ccl_norm_grad: [CTAs][2][cols] sums for gamma and beta, or NULL
+    int32_t want_beta;
+    int32_t layer;                  // 1: about the row's mean, 0: about zero
+    float eps, inv_cols;
+    int32_t lanes;                  // threads of a row
+};
+
+template <int VEC>
+__device__ __forceinline__ void load_vec(const uint16_t* p, uint32_t (&v)[(VEC + 1) / 2]) {
+    if constexpr (VEC == 8) {
+        const uint4 w = *reinterpret_cast<const uint4*>(p);
+        v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+    } else v[0] = *p;
+}
+template <int VEC>
+__device__ __forceinline__ void load_weights(const uint16_t* p, int64_t col, float none, float (&f)[VEC]) {
+    if (!p) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) f[i] = none;
+        return;
+    }
+    if constexpr (VEC == 8) {
+        const uint4 w = __ldg(reinterpret_cast<const uint4*>(p + col));
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(u[i]); f[2 * i + 1] = bf16_hi(u[i]); }
+    } else f[0] = bf16_lo(__ldg(p + col));
+}
+template <int VEC>
+__device__ __forceinline__ void unpack(const uint32_t (&v)[(VEC + 1) / 2], float (&f)[VEC]) {
+#pragma unroll
+    for (int i = 0; i < (VEC + 1) / 2; ++i) {
+        f[2 * i] = bf16_lo(v[i]);
+        if (VEC > 1) f[2 * i + (VEC > 1)] = bf16_hi(v[i]);
+    }
+}
+template <int VEC>
+__device__ __forceinline__ void store_vec(uint16_t* p, const float (&f)[VEC]) {
+    if constexpr (VEC == 8) *reinterpret_cast<uint4*>(p) = make_uint4(bf16_pack(f[0], f[1]), bf16_pack(f[2], f[3]), bf16_pack(f[4], f[5]), bf16_pack(f[6], f[7]));
+    else *p = (uint16_t)bf16_pack(f[0], 0.0f);
+}
+// Sum over the `lanes` (a power of two, 32 at most) threads of a row that share a warp
+__device__ __forceinline__ float lanes_sum(float s, int lanes) {
+    for (int w = lanes >> 1; w >= 1; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
+    return s;
+}
+
+// A thread's NV groups of VEC columns: where they are in the row it works on and how far the next row is.  LINEAR: a column strip's rows
+// follow each other at one pitch (row-major and CCL split along the columns); otherwise every group is looked up in the address map.
+template <int VEC, int NV, bool LINEAR>
+struct RowCursor {
+    int64_t off[NV], step[NV];
+    int64_t row;
+    __device__ RowCursor(const NormParams& p, int lane, int64_t row0, int64_t stride) : row(row0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int64_t col = min(column(p, lane, i), p.v.cols - VEC);
+            off[i] = 0; step[i] = stride;
+            if (LINEAR) {
+                const int64_t pitch = p.v.split == 2 ? strip_w_of(p.v, col / p.v.w) : p.v.cols;
+                off[i] = map(p.v, 0, col) + row0 * pitch;
+                step[i] = stride * pitch;
+            }
+        }
+    }
+    __device__ static int64_t column(const NormParams& p, int lane, int i) { return ((int64_t)i * p.lanes + lane) * VEC; }
+    __device__ int64_t at(const NormParams& p, int lane, int i) const { return LINEAR ? off[i] : map(p.v, row, column(p, lane, i)); }
+    __device__ void next(int64_t stride) {
+        row += stride;
+        if (LINEAR)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) off[i] += step[i];
+    }
+};
+
+// ONE: a row's threads lie in one warp (several rows in a CTA side by side); otherwise the CTA has one row at a time
+template <int VEC, int NV, bool LINEAR, bool ONE>
+__global__ void __launch_bounds__(ONE ? 256 : 1024) norm_kernel(const __grid_constant__ NormParams p) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __shared__ float2 moments[2][32];
+    __shared__ float counts[32];
+    const int lanes = p.lanes, lane = ONE ? threadIdx.x & (lanes - 1) : threadIdx.x, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int64_t rows_at_once = ONE ? blockDim.x / lanes : 1, stride = gridDim.x * rows_at_once;
+    RowCursor<VEC, NV, LINEAR> cur(p, lane, blockIdx.x * rows_at_once + (ONE ? threadIdx.x / lanes : 0), stride);
+    bool mine[NV];
+    float n_warp = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        mine[i] = cur.column(p, lane, i) < p.v.cols;
+        n_warp += mine[i] ? (float)VEC : 0.0f;
+    }
+    if (!ONE) {
+        n_warp = lanes_sum(n_warp, 32);
+        if ((threadIdx.x & 31) == 0) counts[warp] = n_warp;
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    uint32_t nx[NV][(VEC + 1) / 2];
+    auto fetch = [&]() {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int j = 0; j < (VEC + 1) / 2; ++j) nx[i][j] = 0;
+            if (mine[i] && cur.row < p.v.rows) load_vec<VEC>(p.x + cur.at(p, lane, i), nx[i]);
+        }
+    };
+    fetch();
+    int turn = 0;
+    // (ONE: the rows of a warp end together, so that its shuffles stay whole)
+    for (int64_t first = blockIdx.x * rows_at_once; first < p.v.rows; first += stride, turn ^= 1) {
+        const int64_t row = cur.row;
+        int64_t to[NV];
+        float f[NV][VEC];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) { to[i] = row < p.v.rows && mine[i] ? cur.at(p, lane, i) : 0; unpack<VEC>(nx[i], f[i]); }
+        cur.next(stride);
+        fetch();
+        float s = 0.0f, mean = 0.0f, m2 = 0.0f;
+        if (p.layer) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) s += f[i][j];
+            s = lanes_sum(s, ONE ? lanes : 32);
+            mean = ONE ? s * p.inv_cols : (n_warp > 0.0f ? s / n_warp : 0.0f);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float d = mine[i] ? f[i][j] - mean : 0.0f;
+                m2 = fmaf(d * p.inv_cols, d, m2);        // (a mean as it grows: a sum of H squares could leave fp32 where their mean does not)
+            }
+        m2 = lanes_sum(m2, ONE ? lanes : 32);
+        if (!ONE) {
+            if ((threadIdx.x & 31) == 0) moments[turn][warp] = make_float2(mean, m2);
+            __syncthreads();
+            mean = 0.0f;
+            if (p.layer) {
+                for (int w = 0; w < warps; ++w) mean = fmaf(counts[w], moments[turn][w].x, mean);
+                mean *= p.inv_cols;
+            }
+            m2 = 0.0f;
+            for (int w = 0; w < warps; ++w) {
+                const float d = moments[turn][w].x - mean;
+                m2 += fmaf(counts[w] * p.inv_cols * d, d, moments[turn][w].y);
+            }
+        }
+        const float rstd = 1.0f / sqrtf(m2 + p.eps);
+        if (row < p.v.rows) {
+            if (lane == 0) {
+                if (p.mean) p.mean[row] = mean;
+                if (p.rstd) p.rstd[row] = rstd;
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (mine[i]) {
+                    float g[VEC], b[VEC];
+                    load_weights<VEC>(p.gamma, cur.column(p, lane, i), 1.0f, g);
+                    load_weights<VEC>(p.beta, cur.column(p, lane, i), 0.0f, b);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) f[i][j] = fmaf((f[i][j] - mean) * rstd, g[j], b[j]);
+                    store_vec<VEC>(p.out + to[i], f[i]);
+                }
+        }
+    }
+}
+
+template <int VEC, int NV, bool LINEAR, bool ONE>
+__global__ void __launch_bounds__(ONE ? 256 : 512) norm_grad_kernel(const __grid_constant__ NormParams p) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __shared__ float2 sums[2][32];
+    extern __shared__ float lines[];                     // ONE: the warps' sums for gamma and beta, [2][cols]
+    const int lanes = p.lanes, lane = ONE ? threadIdx.x & (lanes - 1) : threadIdx.x, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int64_t rows_at_once = ONE ? blockDim.x / lanes : 1, stride = gridDim.x * rows_at_once;
+    RowCursor<VEC, NV, LINEAR> cur(p, lane, blockIdx.x * rows_at_once + (ONE ? threadIdx.x / lanes : 0), stride);
+    bool mine[NV];
+    float dgamma[NV][VEC], dbeta[NV][VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        mine[i] = cur.column(p, lane, i) < p.v.cols;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) dgamma[i][j] = dbeta[i][j] = 0.0f;
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    constexpr int PR = (VEC + 1) / 2;
+    uint32_t nx[NV][PR], ny[NV][PR];
+    float n_mean = 0.0f, n_rstd = 0.0f;
+    auto fetch = [&]() {
+        const bool ok = cur.row < p.v.rows;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int j = 0; j < PR; ++j) nx[i][j] = ny[i][j] = 0;
+            if (mine[i] && ok) {
+                const int64_t at = cur.at(p, lane, i);
+                load_vec<VEC>(p.x + at, nx[i]);
+                load_vec<VEC>(p.dy + at, ny[i]);
+            }
+        }
+        n_rstd = ok ? p.rstd[cur.row] : 0.0f;
+        n_mean = ok && p.layer ? p.mean[cur.row] : 0.0f;
+    };
+    fetch();
+    int turn = 0;
+    for (int64_t first = blockIdx.x * rows_at_once; first < p.v.rows; first += stride, turn ^= 1) {
+        const int64_t row = cur.row;
+        const float mean = n_mean, rstd = n_rstd;
+        int64_t to[NV];
+        uint32_t ad[NV][PR], x[NV][PR], y[NV][PR];
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            to[i] = row < p.v.rows && mine[i] ? cur.at(p, lane, i) : 0;
+#pragma unroll
+            for (int j = 0; j < PR; ++j) { x[i][j] = nx[i][j]; y[i][j] = ny[i][j]; ad[i][j] = 0; }
+            if (p.addend && row < p.v.rows && mine[i]) load_vec<VEC>(p.addend + to[i], ad[i]);
+        }
+        cur.next(stride);
+        fetch();
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (mine[i]) {
+                float f[VEC], d[VEC], g[VEC];
+                unpack<VEC>(x[i], f);
+                unpack<VEC>(y[i], d);
+                load_weights<VEC>(p.gamma, cur.column(p, lane, i), 1.0f, g);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float h = (f[j] - mean) * rstd, gg = d[j] * g[j];
+                    s1 += gg;
+                    s2 = fmaf(gg, h, s2);
+                    dgamma[i][j] = fmaf(d[j], h, dgamma[i][j]);
+                    dbeta[i][j] += d[j];
+                }
+            }
+        s1 = lanes_sum(s1, ONE ? lanes : 32);
+        s2 = lanes_sum(s2, ONE ? lanes : 32);
+        if (!ONE) {
+            if ((threadIdx.x & 31) == 0) sums[turn][warp] = make_float2(s1, s2);
+            __syncthreads();
+            s1 = s2 = 0.0f;
+            for (int w = 0; w < warps; ++w) { const float2 q = sums[turn][w]; s1 += q.x; s2 += q.y; }
+        }
+        s1 = p.layer ? s1 * p.inv_cols : 0.0f;
+        s2 *= p.inv_cols;
+        if (p.out && row < p.v.rows)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (mine[i]) {
+                    float f[VEC], d[VEC], g[VEC], a[VEC];
+                    unpack<VEC>(x[i], f);
+                    unpack<VEC>(y[i], d);
+                    unpack<VEC>(ad[i], a);
+                    load_weights<VEC>(p.gamma, cur.column(p, lane, i), 1.0f, g);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const float h = (f[j] - mean) * rstd;
+                        f[j] = fmaf(rstd, fmaf(-h, s2, fmaf(d[j], g[j], -s1)), a[j]);
+                    }
+                    store_vec<VEC>(p.out + to[i], f);
+                }
+    }
+    if (!p.partial) return;
+    float* line = p.partial + (int64_t)blockIdx.x * 2 * p.v.cols;
+    if (!ONE) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (mine[i]) {
+                const int64_t col = cur.column(p, lane, i);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) { line[col + j] = dgamma[i][j]; line[p.v.cols + col + j] = dbeta[i][j]; }
+            }
+        return;
+    }
+    // the rows of a warp first (fixed exchanges), then the warps one after the other
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+            for (int w = lanes; w < 32; w <<= 1) {
+                dgamma[i][j] += __shfl_xor_sync(0xffffffffu, dgamma[i][j], w);
+                dbeta[i][j] += __shfl_xor_sync(0xffffffffu, dbeta[i][j], w);
+            }
+    const int cols = (int)p.v.cols;
+    for (int w = 0; w < warps; ++w) {
+        if (warp == w && (int)(threadIdx.x & 31) < lanes)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (mine[i]) {
+                    const int col = (int)cur.column(p, lane, i);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        lines[col + j] = (w ? lines[col + j] : 0.0f) + dgamma[i][j];
+                        lines[cols + col + j] = (w ? lines[cols + col + j] : 0.0f) + dbeta[i][j];
+                    }
+                }
+        __syncthreads();
+    }
+    for (int c = threadIdx.x; c < 2 * cols; c += blockDim.x) line[c] = lines[c];
+}
+
+// Rows longer than the registers of a CTA: the row is read once for every sum and once more for the result (from the L2, where it still
+// is), by any layout's address map.  GRAD: a CTA's line of sums is added up in the workspace, every column by one thread.
+template <int VEC, bool GRAD>
+__global__ void __launch_bounds__(512) norm_long_kernel(const __grid_constant__ NormParams p) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ float2 part[2][16];
+    const int warp = threadIdx.x >> 5;
+    constexpr int PR = (VEC + 1) / 2;
+    int turn = 0;
+    auto meet = [&](float& a, float& b) {                // sums over the CTA
+        a = lanes_sum(a, 32); b = lanes_sum(b, 32);
+        if ((threadIdx.x & 31) == 0) part[turn][warp] = make_float2(a, b);
+        __syncthreads();
+        a = b = 0.0f;
+        for (int w = 0; w < 16; ++w) { a += part[turn][w].x; b += part[turn][w].y; }
+        turn ^= 1;
+    };
+    float* line = GRAD && p.partial ? p.partial + (int64_t)blockIdx.x * 2 * p.v.cols : nullptr;
+    for (int64_t row = blockIdx.x; row < p.v.rows; row += gridDim.x) {
+        float mean = 0.0f, rstd = 0.0f, s1 = 0.0f, s2 = 0.0f;
+        uint32_t u[PR];
+        if (!GRAD) {
+            if (p.layer) {
+                float none = 0.0f;
+                for (int64_t c = (int64_t)threadIdx.x * VEC; c < p.v.cols; c += 512 * VEC) {
+                    float f[VEC];
+                    load_vec<VEC>(p.x + map(p.v, row, c), u);
+                    unpack<VEC>(u, f);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) mean += f[j];
+                }
+                meet(mean, none);
+                mean *= p.inv_cols;
+            }
+            for (int64_t c = (int64_t)threadIdx.x * VEC; c < p.v.cols; c += 512 * VEC) {
+                float f[VEC];
+                load_vec<VEC>(p.x + map(p.v, row, c), u);
+                unpack<VEC>(u, f);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) { s1 += f[j] - mean; s2 = fmaf((f[j] - mean) * p.inv_cols, f[j] - mean, s2); }
+            }
+            meet(s1, s2);
+            // (s1 is zero but for the mean's own rounding, which it takes out of the variance)
+            if (p.layer) s2 -= (s1 * p.inv_cols) * (s1 * p.inv_cols);
+            rstd = 1.0f / sqrtf((s2 < 0.0f ? 0.0f : s2) + p.eps);
+            if (threadIdx.x == 0) {
+                if (p.mean) p.mean[row] = mean;
+                if (p.rstd) p.rstd[row] = rstd;
+            }
+        } else {
+            mean = p.layer ? p.mean[row] : 0.0f;
+            rstd = p.rstd[row];
+            for (int64_t c = (int64_t)threadIdx.x * VEC; c < p.v.cols; c += 512 * VEC) {
+                float f[VEC], d[VEC], g[VEC];
+                const int64_t at = map(p.v, row, c);
+                load_vec<VEC>(p.x + at, u);
+                unpack<VEC>(u, f);
+                load_vec<VEC>(p.dy + at, u);
+                unpack<VEC>(u, d);
+                load_weights<VEC>(p.gamma, c, 1.0f, g);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) { s1 += d[j] * g[j]; s2 = fmaf(d[j] * g[j], (f[j] - mean) * rstd, s2); }
+            }
+            meet(s1, s2);
+            s1 = p.layer ? s1 * p.inv_cols : 0.0f;
+            s2 *= p.inv_cols;
+        }
+        for (int64_t c = (int64_t)threadIdx.x * VEC; c < p.v.cols; c += 512 * VEC) {
+            const int64_t at = map(p.v, row, c);
+            float f[VEC], g[VEC], o[VEC];
+            load_vec<VEC>(p.x + at, u);
+            unpack<VEC>(u, f);
+            load_weights<VEC>(p.gamma, c, 1.0f, g);
+            if (!GRAD) {
+                float b[VEC];
+                load_weights<VEC>(p.beta, c, 0.0f, b);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) o[j] = fmaf((f[j] - mean) * rstd, g[j], b[j]);
+                store_vec<VEC>(p.out + at, o);
+            } else {
+                float d[VEC], a[VEC];
+                load_vec<VEC>(p.dy + at, u);
+                unpack<VEC>(u, d);
+#pragma unroll
+                for (int j = 0; j < PR; ++j) u[j] = 0;
+                if (p.addend) load_vec<VEC>(p.addend + at, u);
+                unpack<VEC>(u, a);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float h = (f[j] - mean) * rstd;
+                    o[j] = fmaf(rstd, fmaf(-h, s2, fmaf(d[j], g[j], -s1)), a[j]);
+                    if (line) {
+                        const bool more = row != blockIdx.x;
+                        line[c + j] = fmaf(d[j], h, more ? line[c + j] : 0.0f);
+                        line[p.v.cols + c + j] = (more ? line[p.v.cols + c + j] : 0.0f) + d[j];
+                    }
+                }
+                if (p.out) store_vec<VEC>(p.out + at, o);
+            }
+        }
+    }
+}
+
+// dgamma and dbeta (blockIdx.y) from the CTAs' lines: 32 columns a block, eight warps over the lines, their sums added in a fixed order
+__global__ void __launch_bounds__(256) norm_grad_finish_kernel(const float* partial, int ctas, int64_t cols, uint16_t* dgamma, uint16_t* dbeta) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ float part[8][32];
+    uint16_t* out = blockIdx.y ? dbeta : dgamma;
+    if (!out) return;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int64_t n = (int64_t)blockIdx.x * 32 + lane;
+    float s = 0.0f;
+    if (n < cols)
+#pragma unroll 16
+        for (int b = w; b < ctas; b += 8) s += partial[((int64_t)b * 2 + blockIdx.y) * cols + n];
+    part[w][lane] = s;
+    __syncthreads();
+    if (w == 0 && n < cols) {
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += part[i][lane];
+        reinterpret_cast<__nv_bfloat16*>(out)[n] = __float2bfloat16_rn(s);
+    }
+}
+
+namespace {
+
+// How a problem is laid over threads
+struct NormPlan {
+    int vec, nv, lanes, threads;    // nv 0: the kernel for long rows
+    bool linear, one;
+    int64_t groups;                 // CTAs that would each have one row (or one set of rows side by side)
+};
+
+bool vectors(const MatView& v) {    // every group of eight columns is one aligned 16-byte piece of the buffer
+    return v.cols % 8 == 0 && (v.split != 2 || (v.w % 8 == 0 && v.wlast % 8 == 0)) && v.stride % 8 == 0 && v.ichunk % 8 == 0;
+}
+
+NormPlan plan_norm(const MatView& v, bool aligned, bool grad) {
+    NormPlan q = {};
+    q.vec = aligned && vectors(v) ? 8 : 1;
+    q.linear = !v.ichunk && v.split != 1;
+    const int64_t groups = (v.cols + q.vec - 1) / q.vec;            // column groups of a row
+    const int64_t most = grad ? 512 : 1024;
+    // (a thread's columns: few where there are few rows, so that a row is spread over more threads)
+    if (q.vec == 8) q.nv = groups <= 32 ? 1 : (groups <= 2 * most ? 2 : 4);
+    else q.nv = groups <= 64 ? 2 : 8;
+    const int64_t need = (groups + q.nv - 1) / q.nv;
+    if (need > most) { q.nv = 0; q.threads = 512; q.lanes = 512; q.groups = v.rows; return q; }
+    q.one = need <= 32;
+    if (q.one) {
+        q.lanes = 8;
+        while (q.lanes < need) q.lanes *= 2;
+        q.threads = 256;
+        q.groups = (v.rows + q.threads / q.lanes - 1) / (q.threads / q.lanes);
+    } else {
+        q.lanes = q.threads = (int)((need + 31) / 32 * 32);
+        q.groups = v.rows;
+    }
+    return q;
+}
+
+// CTAs a SM holds of the gradient's kernels: bounded by what its registers are compiled for; the lines of the workspace are counted with it
+int ctas_per_sm(const NormPlan& q) { return std::max(1, (q.nv == 0 ? 1024 : 1024) / q.threads); }
+int64_t grid_of(const NormPlan& q, int sms) { return std::min<int64_t>(q.groups, (int64_t)sms * ctas_per_sm(q)); }
+
+template <typename... Params, typename... Args>
+ccl_status launch_norm(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // placed early; the kernel waits for what runs before it
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
+    count_launch();
+    return CCL_OK;
+}
+
+template <bool GRAD, int VEC, int NV, bool LINEAR, bool ONE>
+ccl_status launch_shape(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
+    if constexpr (GRAD) return launch_norm(norm_grad_kernel<VEC, NV, LINEAR, ONE>, dim3(grid), q.threads, ONE ? (size_t)p.v.cols * 8 : 0, st, p);
+    else return launch_norm(norm_kernel<VEC, NV, LINEAR, ONE>, dim3(grid), q.threads, 0, st, p);
+}
+template <bool GRAD, int VEC, int NV, bool LINEAR>
+ccl_status launch_one(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
+    return q.one ? launch_shape<GRAD, VEC, NV, LINEAR, true>(p, q, grid, st) : launch_shape<GRAD, VEC, NV, LINEAR, false>(p, q, grid, st);
+}
+template <bool GRAD, int VEC, int NV>
+ccl_status launch_linear(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
+    return q.linear ? launch_one<GRAD, VEC, NV, true>(p, q, grid, st) : launch_one<GRAD, VEC, NV, false>(p, q, grid, st);
+}
+template <bool GRAD>
+ccl_status launch_plan(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
+    if (q.nv == 0) return launch_norm(q.vec == 8 ? norm_long_kernel<8, GRAD> : norm_long_kernel<1, GRAD>, dim3(grid), q.threads, 0, st, p);
+    switch (q.vec * 10 + q.nv) {
+        case 81: return launch_linear<GRAD, 8, 1>(p, q, grid, st);
+        case 82: return launch_linear<GRAD, 8, 2>(p, q, grid, st);
+        case 84: return launch_linear<GRAD, 8, 4>(p, q, grid, st);
+        case 12: return launch_linear<GRAD, 1, 2>(p, q, grid, st);
+        default: return launch_linear<GRAD, 1, 8>(p, q, grid, st);
+    }
+}
+
+ccl_status norm_view(const char* who, const ccl_mat* m, int32_t kind, MatView* v) {
+    ccl_status s = make_view(m, who, v);
+    if (s) return s;
+    if (kind != CCL_NORM_LAYER && kind != CCL_NORM_RMS) return fail(CCL_ERR_INVALID_ARG, "%s: unknown kind %d", who, kind);
+    if (v->e != 2) return fail(CCL_ERR_UNSUPPORTED, "%s: only 2-byte (bf16) elements are supported", who);
+    if (v->cols >= (INT64_C(1) << 31)) return fail(CCL_ERR_UNSUPPORTED, "%s: rows of %lld columns are too long", who, (long long)v->cols);
+    return CCL_OK;
+}
+uintptr_t bits(const void* p) { return reinterpret_cast<uintptr_t>(p); }
+const uint16_t* bf16(const void* p) { return static_cast<const uint16_t*>(p); }
+
+size_t grad_workspace(const MatView& v, int sms) {
+    // (the vector and the scalar plan may differ in their grids; buffers of either alignment find room)
+    const int64_t lines = std::max(grid_of(plan_norm(v, true, true), sms), grid_of(plan_norm(v, false, true), sms));
+    return (size_t)lines * 2 * (size_t)v.cols * 4;
+}
+
+}  // namespace
+}  // namespace ccl
+
+using namespace ccl;
+
+extern "C" ccl_status ccl_norm(const ccl_mat* m, int32_t kind, float eps, const void* X_dev, const void* gamma_dev, const void* beta_dev, void* Y_dev,
+                               float* mean_dev, float* rstd_dev, void* cuda_stream) {
+    NormParams p = {};
+    ccl_status s = norm_view("ccl_norm", m, kind, &p.v);
+    if (s) return s;
+    if (!(eps >= 0.0f && eps < 1e30f)) return fail(CCL_ERR_INVALID_ARG, "ccl_norm: eps must be a number >= 0");
+    if (!X_dev || !Y_dev) return fail(CCL_ERR_INVALID_ARG, "ccl_norm: NULL operand");
+    if (kind == CCL_NORM_RMS && (beta_dev || mean_dev)) return fail(CCL_ERR_INVALID_ARG, "ccl_norm: the root-mean-square form has neither beta nor means");
+    const uintptr_t any = bits(X_dev) | bits(Y_dev) | bits(gamma_dev) | bits(beta_dev);
+    if (any & 1) return fail(CCL_ERR_ALIGN, "ccl_norm: a base pointer is not 2-byte aligned");
+    if ((bits(mean_dev) | bits(rstd_dev)) & 3) return fail(CCL_ERR_ALIGN, "ccl_norm: mean / rstd is not 4-byte aligned");
+    p.x = bf16(X_dev); p.out = static_cast<uint16_t*>(Y_dev); p.gamma = bf16(gamma_dev); p.beta = bf16(beta_dev);
+    p.mean = mean_dev; p.rstd = rstd_dev;
+    p.layer = kind == CCL_NORM_LAYER; p.eps = eps; p.inv_cols = (float)(1.0 / (double)p.v.cols);
+    const NormPlan q = plan_norm(p.v, (any & 15) == 0, false);
+    p.lanes = q.lanes;
+    int sms, pairs;
+    device_units(&sms, &pairs);
+    return launch_plan<false>(p, q, (unsigned)std::min<int64_t>(q.groups, (int64_t)sms * std::max(1, 2048 / q.threads)), reinterpret_cast<cudaStream_t>(cuda_stream));
+}
+
+extern "C" ccl_status ccl_norm_grad_workspace(const ccl_mat* m, size_t* bytes) {
+    MatView v;
+    ccl_status s = norm_view("ccl_norm_grad_workspace", m, CCL_NORM_LAYER, &v);
+    if (s) return s;
+    if (!bytes) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad_workspace: NULL output");
+    int sms, pairs;
+    device_units(&sms, &pairs);
+    *bytes = grad_workspace(v, sms);
+    return CCL_OK;
+}
+
+extern "C" ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* X_dev, const void* gamma_dev, const float* mean_dev, const float* rstd_dev,
+                                    const void* dY_dev, const void* addend_dev, void* dX_dev, void* dgamma_dev, void* dbeta_dev, void* ws_dev,
+                                    size_t ws_bytes, void* cuda_stream) {
+    NormParams p = {};
+    ccl_status s = norm_view("ccl_norm_grad", m, kind, &p.v);
+    if (s) return s;
+    const bool layer = kind == CCL_NORM_LAYER;
+    if (!X_dev || !dY_dev || !rstd_dev || (layer && !mean_dev)) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: NULL operand");
+    if (!dX_dev && !dgamma_dev && !dbeta_dev) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: no output is wanted");
+    if (!layer && dbeta_dev) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: the root-mean-square form has no beta");
+    if (dX_dev && (dX_dev == gamma_dev)) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: dX needs a buffer of its own");
+    const uintptr_t any = bits(X_dev) | bits(dY_dev) | bits(addend_dev) | bits(dX_dev) | bits(gamma_dev);
+    if ((any | bits(dgamma_dev) | bits(dbeta_dev)) & 1) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: a base pointer is not 2-byte aligned");
+    if ((bits(mean_dev) | bits(rstd_dev)) & 3) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: mean / rstd is not 4-byte aligned");
+    int sms, pairs;
+    device_units(&sms, &pairs);
+    const bool sums = dgamma_dev || dbeta_dev;
+    if (sums) {
+        const size_t need = grad_workspace(p.v, sms);
+        if (!ws_dev || ws_bytes < need) return fail(CCL_ERR_WORKSPACE, "ccl_norm_grad: needs %zu bytes of workspace (got %zu)", need, ws_dev ? ws_bytes : (size_t)0);
+        if (bits(ws_dev) & 15) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: workspace is not 16-byte aligned");
+    }
+    p.x = bf16(X_dev); p.dy = bf16(dY_dev); p.addend = dX_dev ? bf16(addend_dev) : nullptr; p.out = static_cast<uint16_t*>(dX_dev); p.gamma = bf16(gamma_dev);
+    p.mean = const_cast<float*>(mean_dev); p.rstd = const_cast<float*>(rstd_dev);
+    p.layer = layer; p.inv_cols = (float)(1.0 / (double)p.v.cols);
+    p.partial = sums ? static_cast<float*>(ws_dev) : nullptr;
+    const NormPlan q = plan_norm(p.v, (any & 15) == 0, true);
+    p.lanes = q.lanes;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    const int64_t grid = grid_of(q, sms);
+    if ((s = launch_plan<true>(p, q, (unsigned)grid, st)) || !sums) return s;
+    return launch_norm(norm_grad_finish_kernel, dim3((unsigned)((p.v.cols + 31) / 32), 2), 256, 0, st, (const float*)p.partial, (int)grid, p.v.cols,
+                       static_cast<uint16_t*>(dgamma_dev), static_cast<uint16_t*>(dbeta_dev));
+}

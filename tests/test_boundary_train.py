@@ -1,0 +1,131 @@
+"""C-ABI boundary of the normalisation and of the AdamW step on the CPU: descriptors, workspace sizes and refusals before any launch.  No GPU."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2606_11718_b200 import binding as ccl
+from paper_2606_11718_b200 import build as ccl_build
+from test_boundary import expect
+from test_boundary_ffn import NULL, P1, P2, P3, P4, P5, P6, status
+
+P7, P8, P9 = (C.c_void_p(i << 12) for i in range(7, 10))
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    ccl_build.build()
+
+
+def test_struct_sizes_match_c_layout():
+    assert C.sizeof(ccl.AdamwTensor) == 9 * 8
+    assert C.sizeof(ccl.AdamwDesc) == 5 * 8 + 8 + 8 + 3 * 8
+
+
+def test_norm_refusals():
+    l, m = ccl.lib(), ccl.Mat(16, 24, 2)
+
+    def call(m=m, kind=0, eps=1e-5, x=P1, g=P2, b=P3, y=P4, mean=P5, rstd=P6):
+        return l.ccl_norm(C.byref(m) if m else None, kind, eps, x, g, b, y, mean, rstd, None)
+
+    status(ccl.ERR_INVALID_ARG, call(m=None))
+    status(ccl.ERR_INVALID_ARG, call(kind=2))
+    status(ccl.ERR_INVALID_ARG, call(x=NULL))
+    status(ccl.ERR_INVALID_ARG, call(y=NULL))
+    for eps in (-1e-9, float("nan"), float("inf")):
+        status(ccl.ERR_INVALID_ARG, call(eps=eps))
+    status(ccl.ERR_INVALID_ARG, call(kind=1, mean=NULL))                                 # beta
+    status(ccl.ERR_INVALID_ARG, call(kind=1, b=NULL))                                    # means
+    status(ccl.ERR_UNSUPPORTED, call(m=ccl.Mat(16, 24, 4)))
+    status(ccl.ERR_UNSUPPORTED, call(m=ccl.Mat(1, 1 << 31, 2)))
+    status(ccl.ERR_SHAPE, call(m=ccl.Mat(4, 9, 2, 4, ccl.PART_COLS, ccl.CCL)))
+    status(ccl.ERR_ALIGN, call(x=C.c_void_p(4097)))
+    status(ccl.ERR_ALIGN, call(g=C.c_void_p(4097)))
+    status(ccl.ERR_ALIGN, call(rstd=C.c_void_p(4098)))
+
+
+def test_norm_grad_refusals():
+    l, m = ccl.lib(), ccl.Mat(16, 24, 2)
+    need = ccl.ccl_norm_grad_workspace(m)
+    assert need >= 2 * 24 * 4
+
+    def call(m=m, kind=0, x=P1, g=P2, mean=P3, rstd=P4, dy=P5, add=P6, dx=P7, dg=P8, db=P9, ws=P1, n=1 << 30):
+        return l.ccl_norm_grad(C.byref(m) if m else None, kind, x, g, mean, rstd, dy, add, dx, dg, db, ws, n, None)
+
+    status(ccl.ERR_INVALID_ARG, call(m=None))
+    status(ccl.ERR_INVALID_ARG, call(kind=-1))
+    for k in ("x", "dy", "rstd", "mean"):
+        status(ccl.ERR_INVALID_ARG, call(**{k: NULL}))
+    status(ccl.ERR_INVALID_ARG, call(kind=1))                                            # dbeta
+    status(ccl.ERR_INVALID_ARG, call(dx=NULL, dg=NULL, db=NULL))
+    status(ccl.ERR_INVALID_ARG, call(dx=P2))                                             # in gamma
+    status(ccl.ERR_WORKSPACE, call(ws=NULL))
+    status(ccl.ERR_WORKSPACE, call(n=need - 1))
+    status(ccl.ERR_ALIGN, call(ws=C.c_void_p(4104)))
+    status(ccl.ERR_ALIGN, call(dg=C.c_void_p(4097)))
+    status(ccl.ERR_ALIGN, call(mean=C.c_void_p(4098)))
+    status(ccl.ERR_UNSUPPORTED, call(m=ccl.Mat(16, 24, 1)))
+    status(ccl.ERR_INVALID_ARG, l.ccl_norm_grad_workspace(C.byref(m), None))
+    expect(ccl.ERR_UNSUPPORTED, ccl.ccl_norm_grad_workspace, ccl.Mat(16, 24, 4))
+
+
+def test_norm_grad_workspace_is_bounded():
+    # a line of two sums a column for every CTA, of which there are a few for each SM at most
+    for rows in (1, 300, 1 << 20):
+        for cols in (1, 8, 520, 8192, 8191, 100000):
+            lines = ccl.ccl_norm_grad_workspace(ccl.Mat(rows, cols, 2)) / (8 * cols)
+            assert 1 <= lines <= min(rows, 148 * 16)
+
+
+def test_adamw_refusals():
+    l = ccl.lib()
+    base = dict(n=100, param=P1, param_bf16=P2, grad=P3, m=P4, v=P5, m_scale=P6, v_scale=P7, grad_fp32=0)
+
+    def call(tensors=1, bits=32, lr=1e-3, b1=0.9, b2=0.99, eps=1e-8, wd=0.1, step=1, gs=None, lr_dev=None, step_dev=None, desc=True, **kw):
+        d = ccl.AdamwDesc(lr, b1, b2, eps, wd, step)
+        d.state_bits, d.grad_scale_dev, d.lr_dev, d.step_dev = bits, gs, lr_dev, step_dev
+        t = ccl.AdamwTensor(**{k: (v.value if isinstance(v, C.c_void_p) else v) for k, v in {**base, **kw}.items()})
+        return l.ccl_adamw(C.byref(d) if desc else None, C.byref(t) if tensors else None, 1 if tensors >= 0 else -1, None)
+
+    status(ccl.ERR_INVALID_ARG, call(desc=False))
+    status(ccl.ERR_INVALID_ARG, call(tensors=0))
+    status(ccl.ERR_INVALID_ARG, call(tensors=-1))
+    status(ccl.ERR_UNSUPPORTED, call(bits=16))
+    for kw in (dict(lr=-1.0), dict(lr=float("nan")), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(eps=0.0), dict(eps=1e-60), dict(wd=-1.0), dict(wd=float("inf")),
+               dict(step=0), dict(step=-5), dict(lr_dev=4096)):
+        status(ccl.ERR_INVALID_ARG, call(**kw))
+    for kw in (dict(n=-1), dict(param=None), dict(grad=None), dict(m=None), dict(v=None), dict(bits=8, m_scale=None), dict(bits=8, v_scale=None)):
+        status(ccl.ERR_INVALID_ARG, call(**kw))
+    status(ccl.ERR_UNSUPPORTED, call(n=(1 << 40) + 1))
+    for kw in (dict(param=4098), dict(m=4098), dict(grad=4098, grad_fp32=1), dict(grad=4097), dict(param_bf16=4097), dict(bits=8, v_scale=4098), dict(gs=4098),
+               dict(step_dev=4100)):
+        status(ccl.ERR_ALIGN, call(**kw))
+    assert call(n=0, param=None) == ccl.OK                                               # nothing to do: nothing is launched
+    assert l.ccl_adamw(C.byref(ccl.AdamwDesc()), None, 0, None) == ccl.OK
+
+
+def test_adamw_tensor_list_refusals(monkeypatch):
+    monkeypatch.setattr(ccl, "_current_device", lambda: -1)                                # CPU tensors say -1: the other checks then run here
+    f, h = lambda n: torch.zeros(n), lambda n: torch.zeros(n, dtype=torch.bfloat16)       # noqa: E731
+    q = lambda n: torch.zeros(n, dtype=torch.float8_e4m3fn)                               # noqa: E731
+
+    def make(p=None, g=None, m=None, v=None, **kw):
+        return ccl.AdamwTensors(p or [f(300)], g or [h(300)], m or [f(300)], v or [f(300)], **kw)
+
+    assert make().count == 1 and make().bits == 32
+    assert make(m=[q(300)], v=[q(300)], m_scales=[f(2)], v_scales=[f(2)]).bits == 8
+    assert ccl.AdamwTensors([], [], [], []).count == 0
+    bad = [dict(p=[h(300)]), dict(g=[f(299)]), dict(m=[q(300)]), dict(v=[f(300), f(300)]), dict(copies=[f(300)]), dict(copies=[]), dict(m_scales=[f(2)], v_scales=[f(2)]),
+           dict(m=[q(300)], v=[q(300)], m_scales=[f(1)], v_scales=[f(2)]), dict(m=[q(300)], v=[q(300)], m_scales=[f(2)]), dict(g=[None]),
+           dict(p=[torch.zeros(20, 30).t()], g=[h(600)], m=[f(600)], v=[f(600)])]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            make(**kw)
+    x = f(600)
+    with pytest.raises(ValueError, match="overlap"):
+        make(p=[x[:300]], m=[x[299:599]])
+    with pytest.raises(ValueError, match="overlap"):
+        ccl.AdamwTensors([x[:300], x[:300]], [h(300)] * 2, [f(300), f(300)], [f(300), f(300)])
+    monkeypatch.undo()
+    with pytest.raises(ValueError):
+        make()                                                                           # not on a GPU

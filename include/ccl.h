@@ -288,7 +288,8 @@ ccl_status ccl_gemm_swiglu(const ccl_gemm_desc* d, const void* A_dev, const void
 /*
  * Synchronises `cuda_stream` (the one entry point that does), then reports and clears the status word of the
  * GEMMs and repacks finished on the current device: CCL_OK, or CCL_ERR_TIMEOUT with *detail = the raw device code
- * (1-6: a GEMM wait, 8-9: ccl_moe_tokens, 101: a repack wait), or CCL_ERR_SHAPE (detail 5) for bad offsets of a ragged batch.
+ * (1-6: a GEMM wait, 8-9: ccl_moe_tokens, 101: a repack wait), or CCL_ERR_SHAPE for bad offsets of a ragged batch (detail 5) or a bad
+ * target of ccl_linear_xent (detail 10).
  * detail may be NULL.  There is ONE status word per device, shared by every stream: with several streams in flight
  * the first caller after an expiry gets the report, whichever stream's kernel it was.
  */
@@ -456,6 +457,40 @@ ccl_status ccl_norm_grad_workspace(const ccl_mat* m, size_t* bytes);
 ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* X_dev, const void* gamma_dev, const float* mean_dev, const float* rstd_dev,
                          const void* dY_dev, const void* addend_dev, void* dX_dev, void* dgamma_dev, void* dbeta_dev, void* ws_dev, size_t ws_bytes,
                          void* cuda_stream);
+
+/*
+ * The cross entropy of the logits z = X * W^T over a vocabulary, without the logits being kept: with c = targets[t],
+ *   lse[t] = log sum over v of exp(z[t][v]),   loss[t] = lse[t] - z[t][c]
+ * and its gradients, for dloss[t] the gradient that reaches loss[t]:
+ *   dz[t][v] = dloss[t] * (exp(z[t][v] - lse[t]) - [v = c]),   dX = bf16(dz * W),   dW = bf16(dz^T * X)
+ *   X, dX     bf16 [T x H] row-major
+ *   W, dW     bf16, stored as d->W describes: with w_trans = 1 [V x H] row-major; with w_trans = 0 [H x V], row-major or in CCL split along its
+ *             columns into equal strips of a multiple of 8 columns (not page-interleaved)
+ *   targets   int32 [T]; a row whose target is ignore_index has loss 0 and takes no part in the gradients (its X must be finite all the
+ *             same).  Any other target outside [0, V) counts as ignored too, and ccl_gemm_status() then returns CCL_ERR_SHAPE (detail 10)
+ *             after ccl_linear_xent.
+ *   loss, lse fp32 [T], either NULL: not wanted; the gradient reads lse as ccl_linear_xent left it.   dloss fp32 [T].   dX, dW: either
+ *             NULL: not wanted.
+ * Logits, exponentials and their sums are fp32 (the exponentials good to 2^-21).  The gradient works through the vocabulary in pieces:
+ * it computes a piece's logits again, holds its dz as bf16 (the operand of two products; each value off by 2^-8 of itself at most) in the
+ * workspace, and sums dX over the pieces in fp32, always in the same order.  A piece's dz takes at most 512 MB, or T x 256 x 2 bytes
+ * where that is more, or that of one strip (of the whole matrix where a [H x V] is row-major).
+ * Any T >= 1 and V >= 1; H a multiple of 8 (else CCL_ERR_UNSUPPORTED); X, W, dX, dW and the workspace 16-byte aligned.  Workspace: the bytes that
+ * the _workspace calls say, whatever they hold; calls that can overlap on the GPU must not share it.  Bounded waits and asynchrony as for
+ * ccl_gemm.
+ */
+typedef struct ccl_xent_desc {
+    int64_t T, V, H;
+    ccl_mat W;
+    int32_t w_trans;
+    int32_t ignore_index;
+} ccl_xent_desc;
+ccl_status ccl_linear_xent_workspace(const ccl_xent_desc* d, size_t* bytes);
+ccl_status ccl_linear_xent(const ccl_xent_desc* d, const void* X_dev, const void* W_dev, const int32_t* targets_dev, float* loss_dev, float* lse_dev,
+                           void* ws_dev, size_t ws_bytes, void* cuda_stream);
+ccl_status ccl_linear_xent_grad_workspace(const ccl_xent_desc* d, size_t* bytes);
+ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X_dev, const void* W_dev, const int32_t* targets_dev, const float* lse_dev,
+                                const float* dloss_dev, void* dX_dev, void* dW_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream);
 
 /*
  * One step of AdamW over `count` tensors.  Step t (from 1 on) of a parameter p with gradient g, moments m and v and r = sqrt(v):

@@ -24,7 +24,7 @@ ASSIGN_N_STRIPS, ASSIGN_M_STRIPS, ASSIGN_EXPLICIT, ASSIGN_2D = 0, 1, 2, 3
 EXPORTS = ["ccl_map_offset", "ccl_map_inverse", "ccl_buffer_bytes", "ccl_strip_stride", "ccl_repack", "ccl_repack_batched", "ccl_repack_transpose", "ccl_gemm_workspace",
            "ccl_gemm", "ccl_gemm_batched_workspace", "ccl_gemm_batched", "ccl_gemm_grouped", "ccl_gemm_grouped_swiglu", "ccl_gemm_grouped_k", "ccl_gemm_axpby", "ccl_gemm_swiglu", "ccl_gemm_static_ws", "ccl_gemm_status", "ccl_selftest_wait_timeout", "ccl_selftest_moe_timeout", "ccl_gemm_epilogue_workspace", "ccl_gemm_epilogue",
            "ccl_gemm_act_grad_workspace", "ccl_gemm_act_grad", "ccl_bias_act_grad", "ccl_moe_tokens_workspace", "ccl_moe_tokens",
-           "ccl_norm", "ccl_norm_grad_workspace", "ccl_norm_grad", "ccl_adamw", "ccl_traffic_sizes", "ccl_traffic", "ccl_traffic_l2", "ccl_traffic_lru", "ccl_probe_l2_latency", "ccl_last_error", "ccl_launch_count", "ccl_version"]
+           "ccl_norm", "ccl_norm_grad_workspace", "ccl_norm_grad", "ccl_linear_xent_workspace", "ccl_linear_xent", "ccl_linear_xent_grad_workspace", "ccl_linear_xent_grad", "ccl_adamw", "ccl_traffic_sizes", "ccl_traffic", "ccl_traffic_l2", "ccl_traffic_lru", "ccl_probe_l2_latency", "ccl_last_error", "ccl_launch_count", "ccl_version"]
 
 
 class CclError(RuntimeError):
@@ -61,6 +61,14 @@ class MoeDesc(C.Structure):
 
     def __init__(self, T=0, E=0, topk=0, H=0, I=0, norm_topk=1, gu_strips=1, gu_stride_bytes=0, d_stride_bytes=0):
         super().__init__(T, H, I, E, topk, norm_topk, gu_strips, gu_stride_bytes, d_stride_bytes)
+
+
+class XentDesc(C.Structure):
+    """ccl_xent_desc"""
+    _fields_ = [("T", C.c_int64), ("V", C.c_int64), ("H", C.c_int64), ("W", Mat), ("w_trans", C.c_int32), ("ignore_index", C.c_int32)]
+
+    def __init__(self, T=0, V=0, H=0, W=None, w_trans=1, ignore_index=-100):
+        super().__init__(T, V, H, W if W is not None else Mat(V, H, 2), w_trans, ignore_index)
 
 
 class AdamwTensor(C.Structure):
@@ -140,6 +148,10 @@ def lib():
         l.ccl_norm.argtypes = [C.POINTER(Mat), C.c_int32, C.c_float] + [C.c_void_p] * 7
         l.ccl_norm_grad_workspace.argtypes = [C.POINTER(Mat), C.POINTER(C.c_size_t)]
         l.ccl_norm_grad.argtypes = [C.POINTER(Mat), C.c_int32] + [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]
+        l.ccl_linear_xent_workspace.argtypes = [C.POINTER(XentDesc), C.POINTER(C.c_size_t)]
+        l.ccl_linear_xent.argtypes = [C.POINTER(XentDesc)] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
+        l.ccl_linear_xent_grad_workspace.argtypes = [C.POINTER(XentDesc), C.POINTER(C.c_size_t)]
+        l.ccl_linear_xent_grad.argtypes = [C.POINTER(XentDesc)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]
         l.ccl_adamw.argtypes = [C.POINTER(AdamwDesc), C.POINTER(AdamwTensor), C.c_int32, C.c_void_p]
         l.ccl_selftest_moe_timeout.argtypes = [C.POINTER(MoeDesc)] + [C.c_void_p] * 6 + [C.c_size_t, C.c_int32, C.c_uint32, C.c_void_p]
         l.ccl_traffic_sizes.argtypes = [C.POINTER(TrafficDesc), C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
@@ -461,6 +473,35 @@ def ccl_norm_grad(m, X, gamma, mean, rstd, dy, dx, ws=None, kind=NORM_LAYER, add
     ws_bytes = _check_workspace(ws, "ccl_norm_grad", device)
     _check(lib().ccl_norm_grad(C.byref(m), kind, _ptr(X), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dy), _ptr(addend), _ptr(dx), _ptr(dgamma), _ptr(dbeta),
                                _ptr(ws), ws_bytes, _stream()))
+
+
+def ccl_linear_xent_workspace(d):
+    return _size(lib().ccl_linear_xent_workspace, d)
+
+
+def ccl_linear_xent(d, X, W, targets, loss, lse, ws):
+    """loss, lse (float32 [T], None: not wanted) of the logits X W^T: X [T x H], W as d.W describes, targets int32 [T]."""
+    device = _check_operands("ccl_linear_xent", (X, 2 * d.T * d.H), (W, ccl_buffer_bytes(d.W)))
+    _check_beside(targets, torch.int32, d.T, "ccl_linear_xent: targets", device)
+    _check_beside(loss, torch.float32, d.T, "ccl_linear_xent: loss", device)
+    _check_beside(lse, torch.float32, d.T, "ccl_linear_xent: lse", device)
+    ws_bytes = _check_workspace(ws, "ccl_linear_xent", device)
+    _check(lib().ccl_linear_xent(C.byref(d), _ptr(X), _ptr(W), _ptr(targets), _ptr(loss), _ptr(lse), _ptr(ws), ws_bytes, _stream()))
+
+
+def ccl_linear_xent_grad_workspace(d):
+    return _size(lib().ccl_linear_xent_grad_workspace, d)
+
+
+def ccl_linear_xent_grad(d, X, W, targets, lse, dloss, dX, dW, ws):
+    """dX [T x H] and dW (as d.W describes), None: not wanted, from ccl_linear_xent's lse and the gradient dloss (float32 [T]) of its loss."""
+    w_bytes = ccl_buffer_bytes(d.W)
+    device = _check_operands("ccl_linear_xent_grad", (X, 2 * d.T * d.H), (W, w_bytes), (dX, 2 * d.T * d.H), (dW, w_bytes))
+    _check_beside(targets, torch.int32, d.T, "ccl_linear_xent_grad: targets", device)
+    _check_beside(lse, torch.float32, d.T, "ccl_linear_xent_grad: lse", device)
+    _check_beside(dloss, torch.float32, d.T, "ccl_linear_xent_grad: dloss", device)
+    ws_bytes = _check_workspace(ws, "ccl_linear_xent_grad", device)
+    _check(lib().ccl_linear_xent_grad(C.byref(d), _ptr(X), _ptr(W), _ptr(targets), _ptr(lse), _ptr(dloss), _ptr(dX), _ptr(dW), _ptr(ws), ws_bytes, _stream()))
 
 
 def _current_device():

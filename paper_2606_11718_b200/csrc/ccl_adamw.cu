@@ -18,6 +18,7 @@
 #include <cuda_fp8.h>
 
 #include "ccl_act.cuh"
+#include "ccl_launch.cuh"
 #include "ccl_tma.h"
 
 namespace ccl {
@@ -272,22 +273,6 @@ namespace {
 
 uintptr_t bits(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 
-template <int N, bool EIGHT>
-ccl_status launch_adamw(const AdamParams<N>& a, int sms, cudaStream_t st) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)std::min(a.first[a.count], sms * 4));
-    cfg.blockDim = dim3(kAdamThreads, 1, 1);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // placed early; the kernel waits for what runs before it
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, adamw_kernel<N, EIGHT>, a));
-    count_launch();
-    return CCL_OK;
-}
-
 template <int N>
 ccl_status run_adamw(const ccl_adamw_desc* d, const ccl_adamw_tensor* tensors, int count, cudaStream_t st) {
     int sms, pairs;
@@ -318,7 +303,7 @@ ccl_status run_adamw(const ccl_adamw_desc* d, const ccl_adamw_tensor* tensors, i
         }
         if (!a.count) break;
         a.first[a.count] = (int32_t)pieces;
-        ccl_status s = eight ? launch_adamw<N, true>(a, sms, st) : launch_adamw<N, false>(a, sms, st);
+        ccl_status s = launch_early(eight ? adamw_kernel<N, true> : adamw_kernel<N, false>, dim3((unsigned)std::min(a.first[a.count], sms * 4)), kAdamThreads, 0, st, a);
         if (s) return s;
     }
     return CCL_OK;

@@ -159,6 +159,7 @@ ccl_status wave_barrier(GemmPlan& plan, bool plain, cudaStream_t st) {
 
 ccl_status epi_status_take(int* code);      // ccl_gemm_epi.cu
 ccl_status moe_status_take(int* code);      // ccl_moe.cu
+ccl_status xent_status_take(int* code);     // ccl_xent.cu
 ccl_status repack_status_take(int* code);   // ccl_repack.cu
 ccl_status repack_selftest_launch(const void* src_dev, uint64_t limit_ns, cudaStream_t st);   // ccl_repack.cu
 
@@ -275,9 +276,11 @@ ccl_status static_ws_address(void** out) {
 
 // strides[X]: bytes between the buffers of operand X (A, B, C) of consecutive problems; 0 = shared (A and B only)
 // m_offs / cap: ragged batch (ccl_gemm_grouped), else nullptr / 0
+// rows_c, rows_b: not 0 where the buffer of C / B ends before the descriptor's last rows (fewer than 64 of them): those are not written / are
+// read as zeros
 static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, const int64_t* strides, const void* A_dev, const void* B_dev, void* C_dev,
                             void* ws_dev, size_t ws_bytes, void* cuda_stream, float alpha = 1.0f, float beta = 0.0f, const int32_t* m_offs = nullptr,
-                            int64_t cap = 0, const int32_t* k_offs = nullptr, bool static_ws = false) {
+                            int64_t cap = 0, const int32_t* k_offs = nullptr, bool static_ws = false, int64_t rows_c = 0, int64_t rows_b = 0) {
     if (!A_dev || !B_dev || !C_dev) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: NULL operand");
     if (!d) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: NULL descriptor");
     if (batch < 1 || batch > kMaxBatch) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: batch must be in [1, %lld]", (long long)kMaxBatch);
@@ -292,6 +295,7 @@ static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     // ws_bytes; the scratch array for ccl_gemm_static_ws).  A caller that passes none gets whole-tile plans, as before.
     const size_t max_ws = static_ws ? (size_t)CCL_GEMM_STATIC_WS_BYTES : (ws_dev ? ws_bytes : 0);
     key.f[38] = (int64_t)max_ws;
+    key.f[39] = rows_c | rows_b << 32;
     Prepared prep;
     bool hit = false;
     {
@@ -320,10 +324,12 @@ static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
         CCL_CUDA_TRY(cudaDeviceGetAttribute(&prep.sms, cudaDevAttrMultiProcessorCount, dev));
         if (dev != key.dev) {
             make_key(d, batch4, A_dev, B_dev, C_dev, &key);
-            key.mode = (swiglu ? 1 : 0) | (static_ws ? 2 : 0); key.alpha = alpha; key.beta = beta; key.f[38] = (int64_t)max_ws;
+            key.mode = (swiglu ? 1 : 0) | (static_ws ? 2 : 0); key.alpha = alpha; key.beta = beta; key.f[38] = (int64_t)max_ws; key.f[39] = rows_c | rows_b << 32;
             key.f[36] = (int64_t)reinterpret_cast<uintptr_t>(m_offs) ^ ((int64_t)reinterpret_cast<uintptr_t>(k_offs) << 1); key.f[37] = cap + (k_offs ? (INT64_C(1) << 62) : 0);
         }
         if ((s = make_plan(d, batch, swiglu, A_dev, B_dev, C_dev, prep.sms, resident_pairs(), &plan, cap, k_offs != nullptr, max_ws, true))) return s;
+        if (rows_c) { plan.p.M = plan.p.Wm = (int32_t)rows_c; plan.vc.rows = rows_c; }
+        if (rows_b) plan.vb.rows = rows_b;
         plan.p.C = static_cast<uint16_t*>(C_dev);
         plan.p.a.batched = batch4[1] != 0; plan.p.b.batched = batch4[2] != 0; plan.p.c.batched = m_offs ? 0 : 1;
         plan.p.m_offs = m_offs;
@@ -439,6 +445,14 @@ extern "C" ccl_status ccl_gemm(const ccl_gemm_desc* d, const void* A_dev, const 
     return gemm_impl(d, 1, false, none, A_dev, B_dev, C_dev, ws_dev, ws_bytes, cuda_stream);
 }
 
+namespace ccl {
+// ccl_gemm for a row-major C (B) that has fewer rows than the descriptor says (see gemm_impl)
+ccl_status gemm_cut(const ccl_gemm_desc* d, int64_t rows_c, int64_t rows_b, const void* A, const void* B, void* C, void* ws, size_t ws_bytes, void* stream) {
+    const int64_t none[3] = {0, 0, 0};
+    return gemm_impl(d, 1, false, none, A, B, C, ws, ws_bytes, stream, 1.0f, 0.0f, nullptr, 0, nullptr, false, rows_c, rows_b);
+}
+}  // namespace ccl
+
 extern "C" ccl_status ccl_gemm_batched(const ccl_gemm_desc* d, int32_t batch, const void* A_dev, int64_t a_stride_bytes, const void* B_dev,
                                        int64_t b_stride_bytes, void* C_dev, int64_t c_stride_bytes, void* ws_dev, size_t ws_bytes,
                                        void* cuda_stream) {
@@ -498,11 +512,12 @@ extern "C" ccl_status ccl_gemm_status(void* cuda_stream, int32_t* detail) {
     if (v) CCL_CUDA_TRY(cudaMemcpyToSymbol(g_gemm_status, &z, sizeof(int)));
     ccl_status s = repack_status_take(&rv);
     if (s) return s;
-    int ev = 0, mv = 0;
-    if ((s = epi_status_take(&ev)) || (s = moe_status_take(&mv))) return s;
-    if (!v) v = ev ? ev : mv;
+    int ev = 0, mv = 0, xv = 0;
+    if ((s = epi_status_take(&ev)) || (s = moe_status_take(&mv)) || (s = xent_status_take(&xv))) return s;
+    if (!v) v = ev ? ev : (mv ? mv : xv);
     if (detail) *detail = v ? v : (rv ? 100 + rv : 0);
     if (v == 5) return fail(CCL_ERR_SHAPE, "ccl_gemm_grouped: row offsets outside [0, M] or a problem with more rows than max_rows (such problems were not computed)");
+    if (v == 10) return fail(CCL_ERR_SHAPE, "ccl_linear_xent: a target outside [0, V) that is not ignore_index (its row was ignored)");
     if (v || rv) return fail(CCL_ERR_TIMEOUT, "a bounded device-side wait expired (code %d)", v ? v : 100 + rv);
     return CCL_OK;
 }

@@ -165,6 +165,19 @@ struct GemmParams {
 // Tensor maps of the epilogue operators: the addend (residual / Z), boxes as C's, and its last strip where that differs
 template <int EPI> struct EpiMaps { CUtensorMap addend, addend2; };
 template <> struct EpiMaps<0> {};
+// The logits of a linear cross entropy (EPI 3: each row's largest and sum of exponentials, EPI 4: the gradient of the logits), columns
+// being classes: column n of the product is class v0 + n, columns from `classes` on do not exist.
+struct LogitArgs {
+    const int32_t* targets;         // [M]
+    int32_t ignore, v0, classes, all;   // all: classes of the whole problem (a target outside [0, all) is taken as ignored)
+    float2* part;                   // EPI 3: [tile column x drain warps of a quadrant][M]: log2 of the scale, sum of 2^(z log2 e - it)
+    float* at_target;               // EPI 3: [M] the target's logit
+    const float *lse, *dloss;       // EPI 4: [M]
+};
+template <> struct EpiMaps<3> { LogitArgs logits; };
+template <> struct EpiMaps<4> { LogitArgs logits; };
+// EPI 5: sums kept in fp32 over several products, [splits][M][N]; the first `have` of them hold the sums of earlier ones
+template <> struct EpiMaps<5> { float* acc; int32_t have; };
 
 // ---- PTX wrappers ---------------------------------------------------------------------------
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -303,6 +316,10 @@ __device__ __forceinline__ void tmem_ld16_fragment(uint32_t taddr, uint32_t (&r)
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(taddr + (16u << 16)) : "memory");
+}
+__device__ __forceinline__ void tmem_regs_ready(uint32_t (&r)[32]) {
+    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+    asm volatile("" : "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
 }
 // 16-byte global store under a predicate, without a branch: the epilogue's TMEM loads and waits are warp-wide
 // (.sync.aligned) and must never be reached by a warp that the compiler has split by a per-lane row test.
@@ -584,7 +601,7 @@ struct Scheduler {
 // walk and the k loops of all other calls stay as they are (the extra branches cost 1-1.5 us on a 15-30 us GEMM)
 // KS > 0: cluster split along K (CTAS = 1): the KS CTAs of a cluster share one tile
 // EPI: 1 = bias, activation and residual in the epilogue (ccl_gemm_epilogue), 2 = activation slope and column sums
-// (ccl_gemm_act_grad)
+// (ccl_gemm_act_grad), 3 and 4 = rows' statistics and gradients of logits, 5 = sums kept in fp32 (ccl_linear_xent and its gradient)
 template <int BN, int CTAS, bool SWIGLU = false, int RAG = 0, bool FULL = true, int KS = 0, int EPI = 0, int OPW = 0>
 __global__ void __launch_bounds__(gemm_threads<EPI, OPW>, 1)
 ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -914,7 +931,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         int npend = 0;
         // EPI: the addend's part of this warp's next piece (32 rows x 64 columns) is fetched into the warp's buffer as soon as the
         // piece before has been stored from it; the cursor `ap` runs one piece ahead, into the next tile.
-        constexpr bool kOp = EPI != 0 && KS == 0;
+        constexpr bool kOp = (EPI == 1 || EPI == 2) && KS == 0;
         unsigned char* op_buf = epi + (size_t)(warp - 2) * (32 * 128);
         uint32_t addend_phase = 0;
         [[maybe_unused]] struct { int it, c; bool ok, out; TileCoord t; } ap = {};          // out: a fetch is under way
@@ -950,6 +967,17 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           if (t.skip) continue;
           const int tile_no = done++;
           int m = t.m0 + (int)rank * BM + quad * 32 + lane;
+          // EPI 3, 4: this lane's row of the logits, fetched while the tile's product is under way
+          [[maybe_unused]] int target = -1;              // column of the row's target (any value outside the tile: not here)
+          [[maybe_unused]] float row_lse2 = 0.0f, row_scale = 0.0f;
+          [[maybe_unused]] bool row_live = false;
+          if constexpr (EPI == 3 || EPI == 4) {
+              const LogitArgs& la = em.logits;
+              const int cls = m < t.m1 ? la.targets[m] : la.ignore;
+              row_live = cls != la.ignore && (unsigned)cls < (unsigned)la.all;
+              target = row_live ? cls - la.v0 : -1;
+              if (EPI == 4 && row_live) { row_lse2 = la.lse[m] * kLog2e; row_scale = la.dloss[m]; }
+          }
 #pragma unroll 1                                         // one copy of the (large) drain code: a short GEMM pays for every instruction-cache miss
           for (int h = 0; h < (SWIGLU ? 1 : NSUB); ++h) {
             const int acc = NSUB == 1 ? (tile_no & 1) : h;
@@ -1431,6 +1459,119 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         npend = 0;
                         if (!alive) break;
                     }
+                }
+            } else if constexpr (EPI >= 3) {
+                // This warp's columns of the tile, 32 at a time: the next 32 accumulators are on their way while these are worked on.
+                const int steps = npieces > hf ? 2 * ((npieces - hf + EW - 1) / EW) : 0;
+                auto offset = [&](int k) { return (hf + (k >> 1) * EW) * 64 + (k & 1) * 32; };
+                // log2 of the scale of the sum (finite, below every logit, so that no difference is undefined) and the sum
+                [[maybe_unused]] float top2 = -1e30f, sum = 0.0f;
+                uint32_t nx[32];
+                if (steps > 0) tmem_ld32(taddr + (uint32_t)offset(0), nx);
+#pragma unroll 1
+                for (int k = 0; k < steps; ++k) {
+                    const int n32 = nb + offset(k);
+                    [[maybe_unused]] uint4 old[8];
+                    [[maybe_unused]] float* at = nullptr;
+                    if constexpr (EPI == 5) {            // (what is there already, while the accumulators arrive)
+                        at = em.acc + ((int64_t)t.split * p.M + min(m, t.m1 - 1)) * (int64_t)p.N + n32;
+                        const bool add = t.split < em.have && m < t.m1;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) old[j] = ld_global_v4_if(at + 4 * j, add && n32 + 4 * j < t.n1);
+                    }
+                    tmem_ld_wait();
+                    tmem_regs_ready(nx);
+                    f32x2 v[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = pair(__uint_as_float(nx[2 * i]), __uint_as_float(nx[2 * i + 1]));
+                    tmem_ld32(taddr + (uint32_t)offset(min(k + 1, steps - 1)), nx);       // (the last ones again: no branch around a warp-wide load)
+                    if constexpr (EPI == 5) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            float a, b, c, d;
+                            split(v[2 * j] + pair(__uint_as_float(old[j].x), __uint_as_float(old[j].y)), a, b);
+                            split(v[2 * j + 1] + pair(__uint_as_float(old[j].z), __uint_as_float(old[j].w)), c, d);
+                            st_global_v4_if(at + 4 * j, make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)), m < t.m1 && n32 + 4 * j < t.n1);
+                        }
+                    } else {
+                        const LogitArgs& la = em.logits;
+                        const int last = min(t.n1, la.classes) - n32;          // columns of these that exist (the same for the whole warp)
+                        const int off = target - n32;                          // (a tile may reach past its strip: the next one's classes are not here)
+                        const unsigned place = off < last ? (unsigned)off : 32u;
+                        const bool here = __any_sync(0xffffffffu, place < 32u);
+                        if constexpr (EPI == 3) {
+                            float f[32];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) split(v[i], f[2 * i], f[2 * i + 1]);
+                            if (here) {
+                                float z = 0.0f;
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) z = place == (unsigned)i ? f[i] : z;
+                                if (place < 32u) la.at_target[m] = z;
+                                __syncwarp();            // (whole again before the next warp-wide load)
+                            }
+                            if (last < 32) {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) f[i] = i < last ? f[i] : -INFINITY;
+                            }
+                            float top[4] = {f[0], f[1], f[2], f[3]};
+#pragma unroll
+                            for (int i = 4; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], f[i]);
+                            const float t2 = fmaxf(top2, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * kLog2e);
+                            f32x2 s[2] = {both(0.0f), both(0.0f)};
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[i & 1] = s[i & 1] + exp2_fast(fma2(pair(f[2 * i], f[2 * i + 1]), both(kLog2e), both(-t2)));
+                            float a, b;
+                            split(s[0] + s[1], a, b);
+                            sum = fmaf(sum, exp2_fast(top2 - t2), a + b);
+                            top2 = t2;
+                        } else {
+                            const bool full = rows_full && (n32 & ~63) + 64 <= t.n1;
+                            if (full && !(k & 1)) { if (lane == 0) tma_store_wait_read<0>(); __syncwarp(); }       // the buffer's last piece has been stored
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) v[i] = exp2_fast(fma2(v[i], both(kLog2e), both(-row_lse2))) * both(row_scale);
+                            if (here) {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    const float lo = place == 2u * i ? -row_scale : 0.0f, hi = place == 2u * i + 1 ? -row_scale : 0.0f;
+                                    v[i] = v[i] + pair(lo, hi);
+                                }
+                            }
+                            uint32_t w[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) w[i] = row_live ? bf16_pack(v[i]) : 0u;
+                            if (last < 32) {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) w[i] = 2 * i + 1 < last ? w[i] : (2 * i < last ? w[i] & 0xFFFFu : 0u);
+                            }
+                            if (full) {
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    *reinterpret_cast<uint4*>(op_buf + lane * 128 + ((((k & 1) * 4 + j) ^ (lane & 7)) << 4)) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+                                if (k & 1) {
+                                    fence_proxy_async();
+                                    __syncwarp();
+                                    if (lane == 0) {
+                                        tma_store_5d(mpc, op_buf, cx0 + (n32 - 32 - nb), cy0, cz0, cu0, 0);
+                                        tma_store_commit();
+                                    }
+                                }
+                            } else {
+                                unsigned short* dst = p.C + c_offset<FULL>(p, min(m, t.m1 - 1), n32);
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    st_global_v4_if(dst + 8 * j, make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]), m < t.m1 && n32 + 8 * j < t.n1);
+                            }
+                        }
+                    }
+                }
+                tmem_ld_wait();
+                tmem_regs_ready(nx);
+                if constexpr (EPI == 3) {
+                    int sn, jn;
+                    p.fd_wn.divmod(t.n0, sn, jn);
+                    const int64_t line = ((int64_t)sn * p.tps_n + jn / BN) * EW + hf;
+                    if (m < t.m1) em.logits.part[line * p.M + m] = make_float2(top2, sum);
                 }
             } else if constexpr (EPI != 0) {
 #pragma unroll 1

@@ -112,7 +112,8 @@ static double kblock_cycles(int b, int c, bool b_kmajor, int64_t active) {
 }
 
 // have_device: the unit counts come from the current device (else the figures of a B200)
-// epi: 1 / 2 = a plan for ccl_gemm_epilogue / ccl_gemm_act_grad
+// epi: 1 / 2 = a plan for ccl_gemm_epilogue / ccl_gemm_act_grad, 3 / 4 / 5 = for the logits' statistics, the logits' gradient and fp32 sums of
+// ccl_linear_xent and its gradient (tiles of 128 and 256 columns; a row's logits are whole sums: K is split by the sums alone)
 static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, const void* A, const void* B, const void* C, int sms, int pairs, GemmPlan* plan,
                             int64_t cap = 0, bool ragk = false, size_t max_ws = ~(size_t)0, bool have_device = false, int epi = 0) {
     if (!d) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: NULL descriptor");
@@ -233,7 +234,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
             // the open (4096 x 28672 x 8192: 1363 us with 256 columns, 1469 with 512; 4096 x 8192 x 28672: 1262 and 1500, 384
             // columns 1526; 2048 x 5120 x 13824: 252, 362 and 273)
             if (epi && b > 256) continue;
-            if (epi_full && b == 192) continue;
+            if ((epi_full || epi >= 3) && b == 192) continue;
             if (b == 384 && (cap > 0 || ragk)) continue;            // (no ragged-batch instantiation of the 256 + 128 tile)
             if (force_bn && atoi(force_bn) != b) continue;
             if (swiglu && !(c == 2 && b == 512)) continue;          // the gated activation pairs the two accumulators of the wide tile
@@ -251,7 +252,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
             const double stream_clk = tiles_m_all == 1 ? (double)tiles * (double)num_kb * (double)b * (BK * 2) / (sms * 29.0) *
                                                              (b <= 128 ? 1.10 : (b <= 192 ? 1.04 : 1.0)) : 0.0;
             for (int sp : {1, 2, 3, 4, 6, 8, 12, 16}) {
-                if (sp > 1 && (swiglu || cap > 0 || ragk || any_rag || num_kb / sp < 2)) continue;
+                if (sp > 1 && (swiglu || epi == 3 || epi == 4 || cap > 0 || ragk || any_rag || num_kb / sp < 2)) continue;
                 if (force_split && atoi(force_split) != sp) continue;
                 // (an operator after a split is a kernel of its own over the partial sums: 2048 x 5120 x 13824, 160 tiles on 74
                 // pairs, takes 261 us whole and 346 in three parts)
@@ -342,7 +343,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
         const char* force_ks = std::getenv("CCL_GEMM_CLUSTERK");
         const int want_ks = force_ks ? atoi(force_ks) : -1;
         const bool can = want_ks != 0 && batch == 1 && !swiglu && cap == 0 && !ragk && !any_rag && !il_a && !il_b && !il_c && !ka && !kb &&
-                         !(force_split && atoi(force_split) > 1) && !balanced && !(force_ctas && atoi(force_ctas) != 1) && d->out_part != CCL_PART_2D;
+                         !(force_split && atoi(force_split) > 1) && !balanced && epi < 3 && !(force_ctas && atoi(force_ctas) != 1) && d->out_part != CCL_PART_2D;
         double best_ks = -1.0;
         int kb_ = 0, kk = 0;
         for (int b : {256, 192, 128}) {
@@ -426,7 +427,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     // and a residual, eight / sixteen: K = 1024 88 / 74 us, 2048 107 / 108, 4096 197 / 203; gradient: K = 256 72 / 67, 1024 89 / 89,
     // 2048 111 / 115, 4096 201 / 210).  Those are problems of seven rounds of tiles; with one round, where no next tile hides the
     // drain, the two have not been compared.  The kernels with every layout exist with eight, the cluster split drains once, with sixteen.
-    const int opw = ks ? 16 : (epi_full || p.kb_per_split * BK >= 1536 ? 8 : 16);
+    const int opw = ks ? 16 : (epi_full || epi == 5 || p.kb_per_split * BK >= 1536 ? 8 : 16);
     plan->opw = opw;
     p.stages = (int32_t)(((epi ? smem_budget_op(ks, opw) : kSmemBudget) - rag_bytes) / p.stage_bytes);
     if (p.stages > 8) p.stages = 8;

@@ -12,6 +12,7 @@
 #include <atomic>
 
 #include "ccl_act.cuh"
+#include "ccl_launch.cuh"
 #include "ccl_tma.h"
 
 namespace ccl {
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(ONE ? 256 : 512) norm_grad_kernel(const __grid
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < VEC; ++j)
-            for (int w = lanes; w < 32; w <<= 1) {
+            for (int w = lanes; ONE && w < 32; w <<= 1) {
                 dgamma[i][j] += __shfl_xor_sync(0xffffffffu, dgamma[i][j], w);
                 dbeta[i][j] += __shfl_xor_sync(0xffffffffu, dbeta[i][j], w);
             }
@@ -492,27 +493,10 @@ NormPlan plan_norm(const MatView& v, bool aligned, bool grad) {
 int ctas_per_sm(const NormPlan& q) { return std::max(1, (q.nv == 0 ? 1024 : 1024) / q.threads); }
 int64_t grid_of(const NormPlan& q, int sms) { return std::min<int64_t>(q.groups, (int64_t)sms * ctas_per_sm(q)); }
 
-template <typename... Params, typename... Args>
-ccl_status launch_norm(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3((unsigned)threads, 1, 1);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // placed early; the kernel waits for what runs before it
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    CCL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
-    count_launch();
-    return CCL_OK;
-}
-
 template <bool GRAD, int VEC, int NV, bool LINEAR, bool ONE>
 ccl_status launch_shape(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
-    if constexpr (GRAD) return launch_norm(norm_grad_kernel<VEC, NV, LINEAR, ONE>, dim3(grid), q.threads, ONE ? (size_t)p.v.cols * 8 : 0, st, p);
-    else return launch_norm(norm_kernel<VEC, NV, LINEAR, ONE>, dim3(grid), q.threads, 0, st, p);
+    if constexpr (GRAD) return launch_early(norm_grad_kernel<VEC, NV, LINEAR, ONE>, dim3(grid), q.threads, ONE ? (size_t)p.v.cols * 8 : 0, st, p);
+    else return launch_early(norm_kernel<VEC, NV, LINEAR, ONE>, dim3(grid), q.threads, 0, st, p);
 }
 template <bool GRAD, int VEC, int NV, bool LINEAR>
 ccl_status launch_one(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
@@ -524,7 +508,7 @@ ccl_status launch_linear(const NormParams& p, const NormPlan& q, unsigned grid, 
 }
 template <bool GRAD>
 ccl_status launch_plan(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
-    if (q.nv == 0) return launch_norm(q.vec == 8 ? norm_long_kernel<8, GRAD> : norm_long_kernel<1, GRAD>, dim3(grid), q.threads, 0, st, p);
+    if (q.nv == 0) return launch_early(q.vec == 8 ? norm_long_kernel<8, GRAD> : norm_long_kernel<1, GRAD>, dim3(grid), q.threads, 0, st, p);
     switch (q.vec * 10 + q.nv) {
         case 81: return launch_linear<GRAD, 8, 1>(p, q, grid, st);
         case 82: return launch_linear<GRAD, 8, 2>(p, q, grid, st);
@@ -619,6 +603,6 @@ extern "C" ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* 
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     const int64_t grid = grid_of(q, sms);
     if ((s = launch_plan<true>(p, q, (unsigned)grid, st)) || !sums) return s;
-    return launch_norm(norm_grad_finish_kernel, dim3((unsigned)((p.v.cols + 31) / 32), 2), 256, 0, st, (const float*)p.partial, (int)grid, p.v.cols,
+    return launch_early(norm_grad_finish_kernel, dim3((unsigned)((p.v.cols + 31) / 32), 2), 256, 0, st, (const float*)p.partial, (int)grid, p.v.cols,
                        static_cast<uint16_t*>(dgamma_dev), static_cast<uint16_t*>(dbeta_dev));
 }

@@ -1,0 +1,340 @@
+// ccl_linear_xent: the cross entropy of z = X W^T over a large vocabulary, and ccl_linear_xent_grad: its gradients with respect to X and W.
+// The logits z are never stored.
+//
+// Forward.  The GEMM of ccl_gemm (ccl_gemm_kernel.cuh, EPI = 3) with another drain: a lane has a row of the tile's accumulators and leaves,
+// of its columns, the largest and the sum of exponentials about it (two numbers for every 64 to 128 logits; the target's logit where it
+// passes by), and a second kernel joins a row's numbers:  lse = max + log(sum of s_i exp(m_i - max)).  Powers of two throughout: one
+// multiply-add and one hardware exponential a logit, behind the next tile's product.
+//
+// Gradient.  dz = dloss (exp(z - lse) - [target]), piece by piece of the vocabulary: the logits' product again, its drain turning z into dz
+// (EPI = 4), rounded to bf16 because it is the operand of the two products that follow; dW of the piece = dz^T X, a whole sum over the
+// tokens, and dX += dz W, which is kept in fp32 from piece to piece (EPI = 5) and rounded once at the end.  A piece's dz is at most kPieceBytes
+// unless 256 columns (or a strip) are more.  Recomputing the logits costs a quarter of the gradient's products; keeping them would
+// cost T x V x 4 bytes.
+//
+// Bound by the tensor cores: 2 T V H and 6 T V H operations.
+#include "ccl_gemm_epi.cuh"
+
+namespace ccl {
+
+ccl_status gemm_cut(const ccl_gemm_desc* d, int64_t rows_c, int64_t rows_b, const void* A, const void* B, void* C, void* ws, size_t ws_bytes, void* stream);   // ccl_gemm.cu
+
+constexpr int64_t kPieceBytes = INT64_C(1) << 29;
+
+template <int EPI, int BN, int CTAS>
+static ccl_status launch_logits_warps(const GemmPlan& plan, const CUtensorMap* maps, const EpiMaps<EPI>& em, cudaStream_t st) {
+    if constexpr (EPI != 5)
+        if (plan.opw == 16) return launch_epi_warps<BN, CTAS, false, 0, EPI, 16>(plan, maps, em, st);
+    return launch_epi_warps<BN, CTAS, false, 0, EPI, 8>(plan, maps, em, st);
+}
+
+// A product over part of the vocabulary.  rows_b: rows of B that exist (0: all that the descriptor says); the rest reads as zeros.
+template <int EPI>
+static ccl_status run_logits(GemmPlan& plan, const EpiMaps<EPI>& em, int64_t rows_b, const void* A, const void* B, void* C, cudaStream_t st) {
+    if (!plan.lean) return fail(CCL_ERR_UNSUPPORTED, "ccl_linear_xent: this layout of W is not supported");
+    if (rows_b) plan.vb.rows = rows_b;
+    CUtensorMap maps[6];
+    ccl_status s = encode_maps(plan, A, B, C, maps);
+    if (s) return s;
+    plan.p.C = static_cast<uint16_t*>(C);
+    plan.p.alpha = 1.0f;
+    if ((s = wave_barrier(plan, true, st))) return s;
+    switch (plan.bn * 10 + plan.ctas) {
+        case 2562: return launch_logits_warps<EPI, 256, 2>(plan, maps, em, st);
+        case 1282: return launch_logits_warps<EPI, 128, 2>(plan, maps, em, st);
+        case 2561: return launch_logits_warps<EPI, 256, 1>(plan, maps, em, st);
+        default: return launch_logits_warps<EPI, 128, 1>(plan, maps, em, st);
+    }
+}
+
+// Joins `lines` pairs (log2 of a scale, sum about it) of each row: `lanes` rows side by side in a block, the other threads along the lines,
+// always in the same order.  The last steps, a few per row, are taken in 64 bits.
+__global__ void __launch_bounds__(256) xent_finish_kernel(const float2* part, int lines, int M, int lanes, const int32_t* targets, int32_t ignore, int32_t classes,
+                                                          const float* at_target, float* loss, float* lse) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ float2 both_[256];
+    const int across = 256 / lanes, lx = threadIdx.x & (lanes - 1), ly = threadIdx.x / lanes;
+    const int64_t row = (int64_t)blockIdx.x * lanes + lx;
+    float t = -1e30f, s = 0.0f;
+    auto join = [&](float2 o) {
+        const float top = fmaxf(t, o.x);
+        s = fmaf(s, exp2_fast(t - top), o.y * exp2_fast(o.x - top));
+        t = top;
+    };
+    if (row < M) {
+        int b = ly;
+        for (; b + 7 * across < lines; b += 8 * across) {            // (eight loads in flight)
+            float2 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = part[(int64_t)(b + i * across) * M + row];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) join(v[i]);
+        }
+        for (; b < lines; b += across) join(part[(int64_t)b * M + row]);
+    }
+    both_[threadIdx.x] = make_float2(t, s);
+    for (int w = across >> 1; w >= 1; w >>= 1) {
+        __syncthreads();
+        if (ly < w) {
+            join(both_[threadIdx.x + w * lanes]);
+            both_[threadIdx.x] = make_float2(t, s);
+        }
+    }
+    if (ly != 0 || row >= M) return;
+    const double l = ((double)t + log2((double)s)) * 0.6931471805599453;
+    if (lse) lse[row] = (float)l;
+    const int cls = targets[row];
+    const bool live = cls != ignore && (unsigned)cls < (unsigned)classes;
+    if (!live && cls != ignore) atomicExch(&g_gemm_status, 10);
+    if (loss) loss[row] = live ? (float)(l - (double)at_target[row]) : 0.0f;
+}
+
+// dX = bf16(sum of the `parts` fp32 sums), eight values a thread
+__global__ void __launch_bounds__(256) xent_dx_kernel(const float* acc, int parts, int64_t n, uint16_t* dx) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 256 * 8) {
+        f32x2 v[4] = {both(0.0f), both(0.0f), both(0.0f), both(0.0f)};
+        for (int k = 0; k < parts; ++k) {
+            const float4 a = *reinterpret_cast<const float4*>(acc + k * n + i), b = *reinterpret_cast<const float4*>(acc + k * n + i + 4);
+            v[0] = v[0] + pair(a.x, a.y); v[1] = v[1] + pair(a.z, a.w);
+            v[2] = v[2] + pair(b.x, b.y); v[3] = v[3] + pair(b.z, b.w);
+        }
+        *reinterpret_cast<uint4*>(dx + i) = bf16x8_pack(v);
+    }
+}
+
+namespace {
+
+ccl_mat matrix(int64_t rows, int64_t cols) { return ccl_mat{rows, cols, 2, 1, CCL_PART_NONE, CCL_ROWMAJOR, 0}; }
+ccl_gemm_desc product(int64_t M, int64_t N, int64_t K, const ccl_mat& A, int a_trans, const ccl_mat& B, int b_trans, const ccl_mat& C) {
+    ccl_gemm_desc d = {};
+    d.M = M; d.N = N; d.K = K; d.A = A; d.B = B; d.C = C;
+    d.a_trans = a_trans; d.b_trans = b_trans; d.out_part = CCL_PART_NONE; d.P = 1;
+    return d;
+}
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+struct Vocabulary {
+    int64_t T, V, H;
+    bool trans;                     // W stored [V x H]; otherwise [H x V] in strips
+    ccl_mat W;
+    int64_t strip, strips, stride;  // columns of a strip, their number, elements between them
+};
+
+ccl_status check_vocabulary(const char* who, const ccl_xent_desc* d, Vocabulary* v) {
+    if (!d) return fail(CCL_ERR_INVALID_ARG, "%s: NULL descriptor", who);
+    if (d->T <= 0 || d->V <= 0 || d->H <= 0) return fail(CCL_ERR_INVALID_ARG, "%s: T, V and H must be positive", who);
+    if (d->T >= (INT64_C(1) << 31) - 256 || d->V >= (INT64_C(1) << 31) - 256 || d->H >= (INT64_C(1) << 31) - 256) return fail(CCL_ERR_UNSUPPORTED, "%s: dimension too large", who);
+    if (d->H % 8) return fail(CCL_ERR_UNSUPPORTED, "%s: H (%lld) is not a multiple of 8", who, (long long)d->H);
+    MatView w;
+    ccl_status s = make_view(&d->W, who, &w);
+    if (s) return s;
+    if (w.rows != (d->w_trans ? d->V : d->H) || w.cols != (d->w_trans ? d->H : d->V)) return fail(CCL_ERR_SHAPE, "%s: W is not %s", who, d->w_trans ? "[V x H]" : "[H x V]");
+    if (w.e != 2) return fail(CCL_ERR_UNSUPPORTED, "%s: only 2-byte (bf16) elements are supported", who);
+    if (d->w_trans ? w.split != 0 : (w.split == 1 || w.ichunk || ragged(w) || w.w % 8 || w.stride % 8))
+        return fail(CCL_ERR_UNSUPPORTED, "%s: W must be [V x H] row-major, or [H x V] in equal strips of a multiple of 8 columns", who);
+    v->T = d->T; v->V = d->V; v->H = d->H; v->trans = d->w_trans != 0; v->W = d->W;
+    v->strip = w.w; v->strips = w.nstrips; v->stride = w.stride;
+    return CCL_OK;
+}
+
+// The logits of `real` classes from one piece (all: of the whole of W); a row-major W is padded to whole 64s with classes that read as zeros
+ccl_gemm_desc logits(const Vocabulary& v, int64_t real, bool all) {
+    const int64_t n = v.trans ? up(real, 64) : real;
+    return product(v.T, n, v.H, matrix(v.T, v.H), 0, v.trans ? matrix(n, v.H) : (all ? v.W : matrix(v.H, n)), v.trans, matrix(v.T, n));
+}
+
+int forward_lines(const GemmPlan& plan) { return plan.p.tiles_n * (plan.opw / 4); }
+
+// The gradient's pieces of the vocabulary and the layout of its workspace
+struct GradPlan {
+    int64_t pieces, width;          // classes of a piece but the last
+    bool all;                       // one piece that is the whole of W
+    int parts;                      // fp32 sums of dX (0: one piece, no sum is kept)
+    size_t acc_at, gemm_at, gemm_bytes, bytes;
+};
+
+int64_t piece_real(const Vocabulary& v, const GradPlan& g, int64_t i) { return std::min(g.width, v.V - i * g.width); }
+ccl_gemm_desc dx_product(const Vocabulary& v, const GradPlan& g, int64_t real) {
+    const int64_t n = v.trans ? up(real, 64) : real;
+    return product(v.T, v.H, n, matrix(v.T, n), 0, v.trans ? matrix(n, v.H) : (g.all ? v.W : matrix(v.H, n)), v.trans ? 0 : 1, matrix(v.T, v.H));
+}
+ccl_gemm_desc dw_product(const Vocabulary& v, const GradPlan& g, int64_t real) {
+    if (v.trans) {
+        const int64_t n = up(real, 64);
+        return product(n, v.H, v.T, matrix(v.T, n), 1, matrix(v.T, v.H), 0, matrix(n, v.H));
+    }
+    return product(v.H, real, v.T, matrix(v.T, v.H), 1, matrix(v.T, real), 0, g.all ? v.W : matrix(v.H, real));
+}
+
+ccl_status plan_grad(const Vocabulary& v, GradPlan* g) {
+    if (v.trans) {
+        const int64_t most = std::max<int64_t>(256, kPieceBytes / (2 * v.T) / 256 * 256);
+        g->pieces = (v.V + most - 1) / most;
+        g->width = g->pieces == 1 ? v.V : up((v.V + g->pieces - 1) / g->pieces, 256);
+        g->pieces = (v.V + g->width - 1) / g->width;
+        g->all = g->pieces == 1;
+    } else {
+        // (all strips at once need them along the K of dX's product, in whole blocks of it)
+        g->all = v.strips == 1 || (2 * v.T * v.V <= kPieceBytes && v.strip % BK == 0);
+        g->pieces = g->all ? 1 : v.strips;
+        g->width = g->all ? v.V : v.strip;
+    }
+    g->parts = 0;
+    g->gemm_bytes = 0;
+    ccl_status s;
+    size_t n;
+    const int64_t ends[2] = {piece_real(v, *g, 0), piece_real(v, *g, g->pieces - 1)};
+    for (int64_t real : ends) {
+        ccl_gemm_desc d = dw_product(v, *g, real);
+        if ((s = ccl_gemm_workspace(&d, &n))) return s;
+        g->gemm_bytes = std::max(g->gemm_bytes, n);
+        d = dx_product(v, *g, real);
+        if (g->pieces == 1) {
+            if ((s = ccl_gemm_workspace(&d, &n))) return s;
+            g->gemm_bytes = std::max(g->gemm_bytes, n);
+        } else {
+            GemmPlan plan;
+            if ((s = shape_plan(&d, 5, &plan))) return s;
+            g->parts = std::max(g->parts, (int)plan.p.splits);
+        }
+    }
+    const size_t dz = up256((size_t)v.T * (size_t)(v.trans ? up(g->width, 64) : g->width) * 2);
+    g->acc_at = dz;
+    g->gemm_at = up256(dz + (size_t)g->parts * (size_t)v.T * (size_t)v.H * 4);
+    g->bytes = g->gemm_at + g->gemm_bytes;
+    return CCL_OK;
+}
+
+ccl_status check_common(const char* who, const ccl_xent_desc* d, Vocabulary* v, const void* X, const void* W, const int32_t* targets) {
+    ccl_status s = check_vocabulary(who, d, v);
+    if (s) return s;
+    if (!X || !W || !targets) return fail(CCL_ERR_INVALID_ARG, "%s: NULL operand", who);
+    if (misaligned(X) || misaligned(W)) return fail(CCL_ERR_ALIGN, "%s: X / W is not 16-byte aligned", who);
+    if (reinterpret_cast<uintptr_t>(targets) & 3) return fail(CCL_ERR_ALIGN, "%s: targets are not 4-byte aligned", who);
+    return CCL_OK;
+}
+ccl_status check_workspace(const char* who, size_t need, const void* ws, size_t ws_bytes) {
+    if (!ws || ws_bytes < need) return fail(CCL_ERR_WORKSPACE, "%s: needs %zu bytes of workspace (got %zu)", who, need, ws ? ws_bytes : (size_t)0);
+    return misaligned(ws) ? fail(CCL_ERR_ALIGN, "%s: workspace is not 16-byte aligned", who) : CCL_OK;
+}
+
+}  // namespace
+
+// The status word of this file's kernels, read and cleared (ccl_gemm_status)
+ccl_status xent_status_take(int* code) {
+    int zero = 0;
+    CCL_CUDA_TRY(cudaMemcpyFromSymbol(code, g_gemm_status, sizeof(int)));
+    if (*code) CCL_CUDA_TRY(cudaMemcpyToSymbol(g_gemm_status, &zero, sizeof(int)));
+    return CCL_OK;
+}
+
+}  // namespace ccl
+
+using namespace ccl;
+
+static size_t forward_bytes(const GemmPlan& plan, int64_t T) { return up256((size_t)forward_lines(plan) * (size_t)T * 8) + (size_t)T * 4; }
+
+extern "C" ccl_status ccl_linear_xent_workspace(const ccl_xent_desc* d, size_t* bytes) {
+    Vocabulary v = {};
+    ccl_status s = check_vocabulary("ccl_linear_xent_workspace", d, &v);
+    if (s) return s;
+    if (!bytes) return fail(CCL_ERR_INVALID_ARG, "ccl_linear_xent_workspace: NULL output");
+    const ccl_gemm_desc g = logits(v, v.V, true);
+    GemmPlan plan;
+    if ((s = shape_plan(&g, 3, &plan))) return s;
+    *bytes = forward_bytes(plan, v.T);
+    return CCL_OK;
+}
+
+extern "C" ccl_status ccl_linear_xent(const ccl_xent_desc* d, const void* X_dev, const void* W_dev, const int32_t* targets_dev, float* loss_dev, float* lse_dev,
+                                      void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+    const char* who = "ccl_linear_xent";
+    Vocabulary v = {};
+    ccl_status s = check_common(who, d, &v, X_dev, W_dev, targets_dev);
+    if (s) return s;
+    if (!loss_dev && !lse_dev) return fail(CCL_ERR_INVALID_ARG, "%s: no output is wanted", who);
+    if ((reinterpret_cast<uintptr_t>(loss_dev) | reinterpret_cast<uintptr_t>(lse_dev)) & 3) return fail(CCL_ERR_ALIGN, "%s: loss / lse is not 4-byte aligned", who);
+    const ccl_gemm_desc g = logits(v, v.V, true);
+    GemmPlan plan;
+    if ((s = shape_plan(&g, 3, &plan))) return s;
+    if ((s = check_workspace(who, forward_bytes(plan, v.T), ws_dev, ws_bytes))) return s;
+    EpiMaps<3> em = {};
+    LogitArgs& la = em.logits;
+    const int lines = forward_lines(plan);
+    la.targets = targets_dev; la.ignore = d->ignore_index; la.classes = la.all = (int32_t)v.V;
+    la.part = static_cast<float2*>(ws_dev);
+    la.at_target = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + up256((size_t)lines * (size_t)v.T * 8));
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    if ((s = run_logits<3>(plan, em, v.trans ? v.V : 0, X_dev, W_dev, nullptr, st))) return s;
+    int lanes = 1;
+    while (lanes < 32 && lanes < v.T) lanes *= 2;
+    return launch_early(xent_finish_kernel, dim3((unsigned)((v.T + lanes - 1) / lanes)), 256, 0, st, (const float2*)la.part, lines, (int)v.T, lanes, targets_dev,
+                        la.ignore, la.classes, (const float*)la.at_target, loss_dev, lse_dev);
+}
+
+extern "C" ccl_status ccl_linear_xent_grad_workspace(const ccl_xent_desc* d, size_t* bytes) {
+    Vocabulary v = {};
+    ccl_status s = check_vocabulary("ccl_linear_xent_grad_workspace", d, &v);
+    if (s) return s;
+    if (!bytes) return fail(CCL_ERR_INVALID_ARG, "ccl_linear_xent_grad_workspace: NULL output");
+    GradPlan g;
+    if ((s = plan_grad(v, &g))) return s;
+    *bytes = g.bytes;
+    return CCL_OK;
+}
+
+extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X_dev, const void* W_dev, const int32_t* targets_dev, const float* lse_dev,
+                                           const float* dloss_dev, void* dX_dev, void* dW_dev, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+    const char* who = "ccl_linear_xent_grad";
+    Vocabulary v = {};
+    ccl_status s = check_common(who, d, &v, X_dev, W_dev, targets_dev);
+    if (s) return s;
+    if (!lse_dev || !dloss_dev) return fail(CCL_ERR_INVALID_ARG, "%s: NULL operand", who);
+    if (!dX_dev && !dW_dev) return fail(CCL_ERR_INVALID_ARG, "%s: no output is wanted", who);
+    if (dX_dev == X_dev || dW_dev == W_dev) return fail(CCL_ERR_INVALID_ARG, "%s: a gradient needs a buffer of its own", who);
+    if (misaligned(dX_dev) || misaligned(dW_dev)) return fail(CCL_ERR_ALIGN, "%s: dX / dW is not 16-byte aligned", who);
+    if ((reinterpret_cast<uintptr_t>(lse_dev) | reinterpret_cast<uintptr_t>(dloss_dev)) & 3) return fail(CCL_ERR_ALIGN, "%s: lse / dloss is not 4-byte aligned", who);
+    GradPlan g;
+    if ((s = plan_grad(v, &g))) return s;
+    if ((s = check_workspace(who, g.bytes, ws_dev, ws_bytes))) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    char* ws = static_cast<char*>(ws_dev);
+    void *dz = ws, *gemm_ws = g.gemm_bytes ? ws + g.gemm_at : nullptr;
+    float* acc = reinterpret_cast<float*>(ws + g.acc_at);
+    int have = 0;                                            // sums of dX that earlier pieces have begun
+    for (int64_t i = 0; i < g.pieces; ++i) {
+        const int64_t real = piece_real(v, g, i), rows = v.trans ? real : 0;
+        const int64_t at = v.trans ? i * g.width * v.H : i * v.stride;
+        const uint16_t* W = static_cast<const uint16_t*>(W_dev) + at;
+        GemmPlan plan;
+        ccl_gemm_desc p = logits(v, real, g.all);
+        if ((s = shape_plan(&p, 4, &plan))) return s;
+        EpiMaps<4> em = {};
+        LogitArgs& la = em.logits;
+        la.targets = targets_dev; la.ignore = d->ignore_index; la.v0 = (int32_t)(i * g.width); la.classes = (int32_t)real; la.all = (int32_t)v.V;
+        la.lse = lse_dev; la.dloss = dloss_dev;
+        if ((s = run_logits<4>(plan, em, rows, X_dev, W, dz, st))) return s;
+        if (dX_dev) {
+            p = dx_product(v, g, real);
+            if (g.pieces == 1) {
+                if ((s = gemm_cut(&p, 0, rows, dz, W, dX_dev, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
+            } else {
+                if ((s = shape_plan(&p, 5, &plan))) return s;
+                EpiMaps<5> sums = {acc, have};
+                if ((s = run_logits<5>(plan, sums, rows, dz, W, nullptr, st))) return s;
+                have = std::max(have, (int)plan.p.splits);
+            }
+        }
+        if (dW_dev) {
+            p = dw_product(v, g, real);
+            if ((s = gemm_cut(&p, rows, 0, v.trans ? dz : X_dev, v.trans ? X_dev : dz, static_cast<uint16_t*>(dW_dev) + at, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
+        }
+    }
+    if (!dX_dev || g.pieces == 1) return CCL_OK;
+    const int64_t n = v.T * v.H;
+    return launch_early(xent_dx_kernel, dim3((unsigned)std::min<int64_t>((n / 8 + 255) / 256, 148 * 8)), 256, 0, st, (const float*)acc, have, n, static_cast<uint16_t*>(dX_dev));
+}

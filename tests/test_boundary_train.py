@@ -129,3 +129,58 @@ def test_adamw_tensor_list_refusals(monkeypatch):
     monkeypatch.undo()
     with pytest.raises(ValueError):
         make()                                                                           # not on a GPU
+
+
+def test_xent_refusals():
+    l = ccl.lib()
+
+    def desc(T=16, V=100, H=64, W=None, trans=1):
+        return ccl.XentDesc(T, V, H, W if W is not None else (ccl.Mat(V, H, 2) if trans else ccl.Mat(H, V, 2)), trans)
+
+    def fwd(d, X=P1, W=P2, t=P3, loss=P4, lse=P5, ws=P6, n=1 << 40):
+        return l.ccl_linear_xent(C.byref(d) if d else None, X, W, t, loss, lse, ws, n, None)
+
+    def grad(d, X=P1, W=P2, t=P3, lse=P4, dl=P5, dx=P6, dw=P7, ws=P8, n=1 << 40):
+        return l.ccl_linear_xent_grad(C.byref(d) if d else None, X, W, t, lse, dl, dx, dw, ws, n, None)
+
+    strips = ccl.Mat(64, 96, 2, 4, ccl.PART_COLS, ccl.CCL)
+    for call, size in ((fwd, ccl.ccl_linear_xent_workspace), (grad, ccl.ccl_linear_xent_grad_workspace)):
+        status(ccl.ERR_INVALID_ARG, call(None))
+        for kw in (dict(T=0), dict(V=0), dict(H=-8)):
+            status(ccl.ERR_INVALID_ARG, call(desc(**kw, W=ccl.Mat(100, 64, 2))))
+        status(ccl.ERR_SHAPE, call(desc(W=ccl.Mat(101, 64, 2))))
+        status(ccl.ERR_SHAPE, call(desc(W=ccl.Mat(64, 100, 2))))
+        for d in (desc(H=60), desc(T=1 << 31), desc(W=ccl.Mat(100, 64, 4)), desc(W=ccl.Mat(100, 64, 2, 4, ccl.PART_ROWS, ccl.CCL)), desc(V=100, trans=0),
+                  desc(V=96, W=ccl.Mat(64, 96, 2, 8, ccl.PART_COLS, ccl.CCL), trans=0), desc(V=96, W=ccl.Mat(64, 96, 2, 4, ccl.PART_COLS, ccl.CCL_INTERLEAVED, 48), trans=0),
+                  desc(V=96, W=ccl.Mat(64, 96, 2, 4, ccl.PART_ROWS, ccl.CCL), trans=0), desc(V=100, W=ccl.Mat(64, 100, 2, 3, ccl.PART_COLS, ccl.CCL), trans=0),
+                  desc(V=96, W=ccl.Mat(64, 96, 2, 4, ccl.PART_COLS, ccl.CCL, 3082), trans=0)):
+            status(ccl.ERR_UNSUPPORTED, call(d))
+        for k in ("X", "W", "t"):
+            status(ccl.ERR_INVALID_ARG, call(desc(), **{k: NULL}))
+        for k, v in (("X", 4104), ("W", 4104), ("t", 4098), ("lse", 4098), ("ws", 4104)):
+            status(ccl.ERR_ALIGN, call(desc(), **{k: C.c_void_p(v)}))
+        for d in (desc(), desc(V=96, W=strips, trans=0)):
+            need = size(d)
+            assert need > 0
+            status(ccl.ERR_WORKSPACE, call(d, n=need - 1))
+            status(ccl.ERR_WORKSPACE, call(d, ws=NULL))
+        expect(ccl.ERR_UNSUPPORTED, size, desc(H=60))
+    status(ccl.ERR_INVALID_ARG, fwd(desc(), loss=NULL, lse=NULL))
+    status(ccl.ERR_ALIGN, fwd(desc(), loss=C.c_void_p(4098)))
+    status(ccl.ERR_INVALID_ARG, grad(desc(), lse=NULL))
+    status(ccl.ERR_INVALID_ARG, grad(desc(), dl=NULL))
+    status(ccl.ERR_INVALID_ARG, grad(desc(), dx=NULL, dw=NULL))
+    status(ccl.ERR_INVALID_ARG, grad(desc(), dx=P1))
+    status(ccl.ERR_INVALID_ARG, grad(desc(), dw=P2))
+    status(ccl.ERR_ALIGN, grad(desc(), dw=C.c_void_p(4104)))
+    assert C.sizeof(ccl.XentDesc) == 3 * 8 + C.sizeof(ccl.Mat) + 8
+
+
+def test_xent_workspace_is_bounded():
+    # the gradient's piece is 512 MB at most, or 256 columns, and dX's fp32 sums come beside it
+    for T in (1, 100, 8192, 1 << 20):
+        for V in (1, 1000, 131072, 131071):
+            for H in (64, 4096):
+                d = ccl.XentDesc(T, V, H)
+                assert ccl.ccl_linear_xent_workspace(d) <= T * (V // 128 + 2) * 8 * 4 + T * 4 + 512
+                assert ccl.ccl_linear_xent_grad_workspace(d) <= max(1 << 29, T * 512) + 16 * T * H * 4 * 2 + 16 * 64 * max(T, V) * H + 4096

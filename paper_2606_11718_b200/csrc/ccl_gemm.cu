@@ -160,6 +160,7 @@ ccl_status wave_barrier(GemmPlan& plan, bool plain, cudaStream_t st) {
 ccl_status epi_status_take(int* code);      // ccl_gemm_epi.cu
 ccl_status moe_status_take(int* code);      // ccl_moe.cu
 ccl_status xent_status_take(int* code);     // ccl_xent.cu
+ccl_status norm_status_take(int* code);     // ccl_norm.cu
 ccl_status repack_status_take(int* code);   // ccl_repack.cu
 ccl_status repack_selftest_launch(const void* src_dev, uint64_t limit_ns, cudaStream_t st);   // ccl_repack.cu
 
@@ -512,9 +513,9 @@ extern "C" ccl_status ccl_gemm_status(void* cuda_stream, int32_t* detail) {
     if (v) CCL_CUDA_TRY(cudaMemcpyToSymbol(g_gemm_status, &z, sizeof(int)));
     ccl_status s = repack_status_take(&rv);
     if (s) return s;
-    int ev = 0, mv = 0, xv = 0;
-    if ((s = epi_status_take(&ev)) || (s = moe_status_take(&mv)) || (s = xent_status_take(&xv))) return s;
-    if (!v) v = ev ? ev : (mv ? mv : xv);
+    int ev = 0, mv = 0, xv = 0, nv = 0;
+    if ((s = epi_status_take(&ev)) || (s = moe_status_take(&mv)) || (s = xent_status_take(&xv)) || (s = norm_status_take(&nv))) return s;
+    if (!v) v = ev ? ev : (mv ? mv : (xv ? xv : nv));
     if (detail) *detail = v ? v : (rv ? 100 + rv : 0);
     if (v == 5) return fail(CCL_ERR_SHAPE, "ccl_gemm_grouped: row offsets outside [0, M] or a problem with more rows than max_rows (such problems were not computed)");
     if (v == 10) return fail(CCL_ERR_SHAPE, "ccl_linear_xent: a target outside [0, V) that is not ignore_index (its row was ignored)");

@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(ONE ? 256 : 512) norm_grad_kernel(const __grid
     }
     if (!p.partial) return;
     float* line = p.partial + (int64_t)blockIdx.x * 2 * p.v.cols;
-    if (!ONE) {
+    if constexpr (!ONE) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (mine[i]) {
@@ -296,14 +296,13 @@ __global__ void __launch_bounds__(ONE ? 256 : 512) norm_grad_kernel(const __grid
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) { line[col + j] = dgamma[i][j]; line[p.v.cols + col + j] = dbeta[i][j]; }
             }
-        return;
-    }
+    } else {
     // the rows of a warp first (fixed exchanges), then the warps one after the other
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < VEC; ++j)
-            for (int w = lanes; ONE && w < 32; w <<= 1) {
+            for (int w = lanes; w < 32; w <<= 1) {
                 dgamma[i][j] += __shfl_xor_sync(0xffffffffu, dgamma[i][j], w);
                 dbeta[i][j] += __shfl_xor_sync(0xffffffffu, dbeta[i][j], w);
             }
@@ -323,6 +322,322 @@ __global__ void __launch_bounds__(ONE ? 256 : 512) norm_grad_kernel(const __grid
         __syncthreads();
     }
     for (int c = threadIdx.x; c < 2 * cols; c += blockDim.x) line[c] = lines[c];
+    }
+}
+
+// ---- many rows whose column groups are aligned 16-byte pieces (row-major and CCL split along the columns) -------------------
+//
+// Loads are bulk copies into shared memory, under way whatever the warps are doing, one copy for each strip of a set of rows.
+
+static __device__ int g_norm_status = 0;
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void group_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ uint4 shared16(const void* p) { return *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ void parts(const uint4& w, f32x2 (&f)[4]) { f[0] = bf16_unpack(w.x); f[1] = bf16_unpack(w.y); f[2] = bf16_unpack(w.z); f[3] = bf16_unpack(w.w); }
+__device__ __forceinline__ float warp_total(f32x2 a) { float lo, hi; split(a, lo, hi); return lanes_sum(lo + hi, 32); }
+
+constexpr uint32_t kOnes = 0x3F803F80u;                  // two ones in bf16
+
+struct StreamParams {
+    NormParams n;
+    int32_t groups, slots, arrays, set_rows;
+    uint32_t slot_bytes, array_bytes;
+};
+
+// Forward.  A warp has a row to itself and nothing to wait for but its own loads: no CTA-wide meeting, eight to sixteen rows in different
+// phases side by side.  A warp owns `slots` slots of `set_rows` consecutive rows and refills one as soon as it is done with it.  The row is
+// read from its slot twice: first and second moment, then the result; gamma and beta lie behind the slots.
+//   The moments are taken about the mean of the row's first 256 values (all lanes' first eight).  That is off by a^2 <= (H / 256 - 1) var at
+// most, so the difference E d^2 - a^2 loses log2(H / 256) bits in the worst case, six at 16384 columns.
+template <bool LAYER>
+__global__ void __launch_bounds__(512, 1) norm_rows_kernel(const __grid_constant__ StreamParams q) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ uint64_t full[64];
+    const NormParams& p = q.n;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, cols = (int)p.v.cols;
+    uint16_t* weights = reinterpret_cast<uint16_t*>(smem + (size_t)warps * q.slots * q.slot_bytes);
+    if ((int)threadIdx.x < warps * q.slots) { mbar_init(&full[threadIdx.x], 1); fence_barrier_init(); }
+    const uint4 ones = make_uint4(kOnes, kOnes, kOnes, kOnes), zeros = make_uint4(0u, 0u, 0u, 0u);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int c = threadIdx.x * 8; c < cols; c += blockDim.x * 8) {
+        *reinterpret_cast<uint4*>(weights + c) = p.gamma ? __ldg(reinterpret_cast<const uint4*>(p.gamma + c)) : ones;
+        *reinterpret_cast<uint4*>(weights + cols + c) = p.beta ? __ldg(reinterpret_cast<const uint4*>(p.beta + c)) : zeros;
+    }
+    __syncthreads();
+    const int64_t rows = p.v.rows, stride = (int64_t)gridDim.x * warps * q.set_rows, begin = ((int64_t)blockIdx.x * warps + warp) * q.set_rows;
+    unsigned char* mine = smem + (size_t)warp * q.slots * q.slot_bytes;
+    uint64_t* bars = full + warp * q.slots;
+    int64_t next = begin;                                // (of lane 0: the first row of the next set to be loaded)
+    auto fill = [&](int slot) {
+        if (next >= rows) return;
+        const int64_t n = min((int64_t)q.set_rows, rows - next);
+        mbar_expect_tx(&bars[slot], (uint32_t)(n * cols * 2));
+        for (int64_t s = 0; s < p.v.nstrips; ++s) {
+            const int64_t w = strip_w_of(p.v, s);
+            bulk_load(mine + (size_t)slot * q.slot_bytes + s * q.set_rows * p.v.w * 2, p.x + s * p.v.stride + next * w, (uint32_t)(n * w * 2), &bars[slot]);
+        }
+        next += stride;
+    };
+    if (lane == 0)
+        for (int s = 0; s < q.slots; ++s) fill(s);
+    const int n_first = min(cols, 256);
+    const float inv_first = 1.0f / (float)n_first;
+    int slot = 0;
+    uint32_t phase = 0;
+    for (int64_t r0 = begin; r0 < rows; r0 += stride) {
+        const bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars[slot], phase));
+        if (!ok) {                                       // (the copies under way land before the CTA ends)
+            if (lane == 0) {
+                atomicExch(&g_norm_status, 11);
+                for (int s = 0; s < q.slots; ++s)
+                    if (r0 + s * stride < next) mbar_wait_bounded(&bars[(slot + s) % q.slots], slot + s < q.slots ? phase : phase ^ 1);
+            }
+            break;
+        }
+        const uint16_t* set = reinterpret_cast<const uint16_t*>(mine + (size_t)slot * q.slot_bytes);
+        const int n = (int)min((int64_t)q.set_rows, rows - r0);
+        for (int r = 0; r < n; ++r) {
+            const int64_t row = r0 + r;
+            // every strip's columns of the row: f(place in the slot, first column, groups of eight)
+            auto strips = [&](auto f) {
+                for (int64_t s = 0; s < p.v.nstrips; ++s) {
+                    const int w = (int)strip_w_of(p.v, s);
+                    f(set + s * q.set_rows * p.v.w + r * w, (int)(s * p.v.w), w >> 3, p.out + s * p.v.stride + row * w);
+                }
+            };
+            f32x2 f[4];
+            float pivot = 0.0f;
+            if (LAYER) {
+                const int c = lane * 8;
+                const int64_t s = c / p.v.w;             // (strips may be narrower than the first 256 columns)
+                parts(c < n_first ? shared16(set + s * q.set_rows * p.v.w + r * strip_w_of(p.v, s) + (c - s * p.v.w)) : zeros, f);
+                pivot = warp_total((f[0] + f[1]) + (f[2] + f[3])) * inv_first;
+            }
+            f32x2 m1[2] = {both(0.0f), both(0.0f)}, m2[2] = {both(0.0f), both(0.0f)};
+            strips([&](const uint16_t* x, int, int groups, uint16_t*) {
+#pragma unroll 4
+                for (int i = lane; i < groups; i += 32) {
+                    parts(shared16(x + i * 8), f);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x2 d = LAYER ? f[j] + both(-pivot) : f[j];
+                        if (LAYER) m1[j & 1] = m1[j & 1] + d;
+                        m2[j & 1] = fma2(d, d, m2[j & 1]);
+                    }
+                }
+            });
+            // (means from here on: a sum of H squares could leave fp32 where their mean does not)
+            const float a = LAYER ? warp_total(m1[0] + m1[1]) * p.inv_cols : 0.0f;
+            float var = warp_total((m2[0] + m2[1]) * both(p.inv_cols));
+            if (LAYER) { var = fmaf(-a, a, var); var = var < 0.0f ? 0.0f : var; }
+            const float mean = pivot + a, rstd = rsqrtf(var + p.eps);
+            if (lane == 0) {
+                if (p.mean) p.mean[row] = mean;
+                if (p.rstd) p.rstd[row] = rstd;
+            }
+            strips([&](const uint16_t* x, int col, int groups, uint16_t* to) {
+#pragma unroll 4
+                for (int i = lane; i < groups; i += 32) {
+                    f32x2 g[4], b[4];
+                    parts(shared16(x + i * 8), f);
+                    parts(shared16(weights + col + i * 8), g);
+                    if (LAYER) parts(shared16(weights + cols + col + i * 8), b);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) f[j] = LAYER ? fma2(f[j] + both(-mean), g[j] * both(rstd), b[j]) : f[j] * (g[j] * both(rstd));
+                    *reinterpret_cast<uint4*>(to + i * 8) = bf16x8_pack(f);
+                }
+            });
+        }
+        __syncwarp();
+        if (lane == 0) fill(slot);
+        if (++slot == q.slots) { slot = 0; phase ^= 1; }
+    }
+}
+
+// Back.  The sums for gamma and beta want a thread to keep its columns, so a row is spread over a group of `lanes` threads, R rows at a time
+// (two chains of sums that do not wait for each other, gamma unpacked once for both); `groups` groups side by side have the next rows.  A
+// stage of the ring is set_rows = groups x R rows of all inputs; thread 0 refills it when all warps are done with it.  One CTA an SM.
+constexpr int kGradThreads = 512;
+
+template <int NV, int R>
+__global__ void __launch_bounds__(kGradThreads, 1) norm_grad_stream_kernel(const __grid_constant__ StreamParams q) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ uint64_t full[8], empty[8];
+    __shared__ float2 sums[2][R][kGradThreads / 32];
+    __shared__ int gone[2][kGradThreads / 32];           // a wait of a group ran out
+    const NormParams& p = q.n;
+    const int L = p.lanes, G = q.groups, warp = threadIdx.x >> 5, wl = threadIdx.x & 31, cols = (int)p.v.cols;
+    const int64_t rows = p.v.rows, set_rows = q.set_rows, stride = gridDim.x * set_rows, begin = blockIdx.x * set_rows;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < q.slots; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], L * G / 32); }
+        fence_barrier_init();
+    }
+    if (threadIdx.x < kGradThreads / 32) gone[0][threadIdx.x] = gone[1][threadIdx.x] = 0;
+    uint16_t* weights = reinterpret_cast<uint16_t*>(ring + (size_t)q.slots * q.slot_bytes);
+    const uint4 ones = make_uint4(kOnes, kOnes, kOnes, kOnes), zeros = make_uint4(0u, 0u, 0u, 0u);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int c = threadIdx.x * 8; c < cols; c += blockDim.x * 8) *reinterpret_cast<uint4*>(weights + c) = p.gamma ? __ldg(reinterpret_cast<const uint4*>(p.gamma + c)) : ones;
+    __syncthreads();
+    int64_t next = begin;                                // (of thread 0: the first row of the next set to be loaded)
+    auto fill = [&](int slot) {
+        if (next >= rows) return;
+        const int64_t n = min(set_rows, rows - next);
+        mbar_expect_tx(&full[slot], (uint32_t)(n * cols * 2) * q.arrays);
+        unsigned char* to = ring + (size_t)slot * q.slot_bytes;
+        for (int64_t s = 0; s < p.v.nstrips; ++s) {
+            const int64_t w = strip_w_of(p.v, s), from = s * p.v.stride + next * w, at = s * set_rows * p.v.w * 2;
+            bulk_load(to + at, p.x + from, (uint32_t)(n * w * 2), &full[slot]);
+            bulk_load(to + q.array_bytes + at, p.dy + from, (uint32_t)(n * w * 2), &full[slot]);
+            if (q.arrays == 3) bulk_load(to + 2 * q.array_bytes + at, p.addend + from, (uint32_t)(n * w * 2), &full[slot]);
+        }
+        next += stride;
+    };
+    if (threadIdx.x == 0)
+        for (int s = 0; s < q.slots; ++s) fill(s);
+    const int group = threadIdx.x / L, lane = threadIdx.x - group * L, warp0 = group * (L / 32), warps = L / 32;
+    bool mine[NV];
+    int col[NV], spot[NV], pitch[NV];                    // column, its place among a stage's elements, elements to the next row
+    uint16_t* out[NV];                                   // this thread's columns in the output's row 0
+    f32x2 dgamma[NV][4], dbeta[NV][4];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        col[i] = (i * L + lane) * 8;
+        mine[i] = col[i] < cols;
+        const int64_t c = mine[i] ? col[i] : 0, s = c / p.v.w;
+        pitch[i] = (int)strip_w_of(p.v, s);
+        spot[i] = (int)(s * set_rows * p.v.w + group * R * pitch[i] + (c - s * p.v.w));
+        out[i] = p.out + s * p.v.stride + (c - s * p.v.w);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dgamma[i][j] = dbeta[i][j] = both(0.0f);
+    }
+    int slot = 0, turn = 0;
+    uint32_t phase = 0;
+    float n_mean[R], n_rstd[R];
+    auto statistics = [&](int64_t row) {                 // (of the rows after these, ahead)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            n_rstd[r] = row + r < rows ? p.rstd[row + r] : 0.0f;
+            n_mean[r] = row + r < rows && p.layer ? p.mean[row + r] : 0.0f;
+        }
+    };
+    auto weight = [&](int i, f32x2 (&w)[4]) { parts(shared16(weights + col[i]), w); };
+    statistics(begin + group * R);
+    for (int64_t r0 = begin; r0 < rows; r0 += stride, turn ^= 1) {
+        const int64_t row = r0 + group * R;
+        bool lost = !mbar_wait_bounded(&full[slot], phase);
+        const unsigned char* st = ring + (size_t)slot * q.slot_bytes;
+        auto at = [&](int array, int r, int i) { return shared16(st + array * q.array_bytes + (spot[i] + r * pitch[i]) * 2); };
+        if (threadIdx.x == 0 && r0 != begin && next < rows) {
+            // refill the stage of the rows before these once all warps are done with it
+            const int before = slot ? slot - 1 : q.slots - 1;
+            if (mbar_wait_bounded(&empty[before], slot ? phase : phase ^ 1)) fill(before); else lost = true;
+        }
+        if (lost) { atomicExch(&g_norm_status, 11); *(volatile int*)&gone[turn][group] = 1; }
+        float mean[R], rstd[R], s1[R], s2[R];
+        f32x2 a[R], b[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) { mean[r] = n_mean[r]; rstd[r] = n_rstd[r]; a[r] = b[r] = both(0.0f); }
+        statistics(row + stride);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (mine[i]) {
+                f32x2 w[4];
+                weight(i, w);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    if (row + r < rows) {
+                        f32x2 f[4], d[4];
+                        parts(at(0, r, i), f); parts(at(1, r, i), d);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const f32x2 h = (f[j] + both(-mean[r])) * both(rstd[r]), g = d[j] * w[j];
+                            a[r] = a[r] + g;
+                            b[r] = fma2(g, h, b[r]);
+                            dgamma[i][j] = fma2(d[j], h, dgamma[i][j]);
+                            dbeta[i][j] = dbeta[i][j] + d[j];
+                        }
+                    }
+            }
+#pragma unroll
+        for (int r = 0; r < R; ++r) { s1[r] = warp_total(a[r]); s2[r] = warp_total(b[r]); }
+        if (warps > 1) {                                 // (at most eight groups of two warps or more: named barriers 1 to 8)
+            if (wl == 0)
+#pragma unroll
+                for (int r = 0; r < R; ++r) sums[turn][r][warp] = make_float2(s1[r], s2[r]);
+            group_sync(1 + group, L);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {                // a lane a warp, 16 warps at most
+                const float2 o = wl < warps ? sums[turn][r][warp0 + wl] : make_float2(0.0f, 0.0f);
+                s1[r] = __shfl_sync(0xffffffffu, lanes_sum(o.x, 16), 0);
+                s2[r] = __shfl_sync(0xffffffffu, lanes_sum(o.y, 16), 0);
+            }
+        } else __syncwarp();
+        // (the same for every thread of the group: written before its meeting, and the other one of the two is written before the next)
+        if (*(volatile int*)&gone[turn][group]) break;
+#pragma unroll
+        for (int r = 0; r < R; ++r) { s1[r] = p.layer ? s1[r] * p.inv_cols : 0.0f; s2[r] *= p.inv_cols; }
+        if (p.out)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (mine[i]) {
+                    f32x2 w[4];
+                    weight(i, w);
+                    uint16_t* to = out[i] + row * pitch[i];
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+                        if (row + r < rows) {
+                            f32x2 f[4], d[4], o[4];
+                            parts(at(0, r, i), f); parts(at(1, r, i), d); parts(q.arrays == 3 ? at(2, r, i) : zeros, o);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const f32x2 h = (f[j] + both(-mean[r])) * both(rstd[r]);
+                                o[j] = fma2(both(rstd[r]), fma2(h, both(-s2[r]), fma2(d[j], w[j], both(-s1[r]))), o[j]);
+                            }
+                            *reinterpret_cast<uint4*>(to + r * pitch[i]) = bf16x8_pack(o);
+                        }
+                }
+        __syncwarp();
+        if (wl == 0) mbar_arrive(&empty[slot]);
+        if (++slot == q.slots) { slot = 0; phase ^= 1; }
+    }
+    // (left early: the copies under way land before the CTA ends)
+    if (threadIdx.x == 0 && (gone[0][0] || gone[1][0])) {
+        const int64_t fills = (next - begin) / stride;
+        for (int s = 0; s < q.slots && s < fills; ++s) mbar_wait_bounded(&full[s], (uint32_t)((fills - 1 - s) / q.slots) & 1);
+    }
+    __syncthreads();
+    if (!p.partial) return;
+    // the groups' sums one after the other, by way of the ring's memory
+    float* line = p.partial + (int64_t)blockIdx.x * 2 * cols;
+    float* lines = reinterpret_cast<float*>(ring);
+    for (int g = 0; g < G; ++g) {
+        if (group == g)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (mine[i])
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        float f[8];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) split(k ? dbeta[i][j] : dgamma[i][j], f[2 * j], f[2 * j + 1]);
+                        float4* t = reinterpret_cast<float4*>(lines + k * cols + col[i]);
+                        float4 u = make_float4(f[0], f[1], f[2], f[3]), v = make_float4(f[4], f[5], f[6], f[7]);
+                        if (g) {
+                            const float4 a = t[0], b = t[1];
+                            u.x += a.x; u.y += a.y; u.z += a.z; u.w += a.w;
+                            v.x += b.x; v.y += b.y; v.z += b.z; v.w += b.w;
+                        }
+                        if (g == G - 1) t = reinterpret_cast<float4*>(line + k * cols + col[i]);
+                        t[0] = u; t[1] = v;
+                    }
+        if (g < G - 1) __syncthreads();
+    }
 }
 
 // Rows longer than the registers of a CTA: the row is read once for every sum and once more for the result (from the L2, where it still
@@ -454,22 +769,51 @@ __global__ void __launch_bounds__(256) norm_grad_finish_kernel(const float* part
 
 namespace {
 
+constexpr int64_t kRing = 192 * 1024;                    // bytes of the gradient's ring: two stages of the longest rows (32 KB) with three inputs
+constexpr int64_t kSlots = 216 * 1024;                   // bytes of the forward pass's slots with gamma and beta
+constexpr int64_t kStreamCols = 16384;
+
 // How a problem is laid over threads
 struct NormPlan {
     int vec, nv, lanes, threads;    // nv 0: the kernel for long rows
     bool linear, one;
     int64_t groups;                 // CTAs that would each have one row (or one set of rows side by side)
+    int stream, slots, arrays;      // norm_rows_kernel: warps, norm_grad_stream_kernel: groups side by side (0: neither is taken)
+    int64_t set_rows;
 };
 
 bool vectors(const MatView& v) {    // every group of eight columns is one aligned 16-byte piece of the buffer
     return v.cols % 8 == 0 && (v.split != 2 || (v.w % 8 == 0 && v.wlast % 8 == 0)) && v.stride % 8 == 0 && v.ichunk % 8 == 0;
 }
 
-NormPlan plan_norm(const MatView& v, bool aligned, bool grad) {
+// arrays: inputs of the shape of a row (1 forward; 2 or 3 back)
+NormPlan plan_norm(const MatView& v, bool aligned, bool grad, int arrays, int sms) {
     NormPlan q = {};
     q.vec = aligned && vectors(v) ? 8 : 1;
     q.linear = !v.ichunk && v.split != 1;
     const int64_t groups = (v.cols + q.vec - 1) / q.vec;            // column groups of a row
+    if (q.vec == 8 && q.linear && v.nstrips <= 16 && v.cols >= 256 && v.cols <= kStreamCols) {
+        q.arrays = arrays;
+        if (grad) {
+            q.nv = groups < 64 ? 1 : (groups <= 2 * kGradThreads ? 2 : 4);
+            q.lanes = (int)((groups + q.nv - 1) / q.nv + 31) / 32 * 32;
+            q.stream = kGradThreads / q.lanes;
+            q.threads = q.stream * q.lanes;
+            q.set_rows = q.stream * (q.nv == 4 ? 1 : 2);
+            q.slots = (int)std::min<int64_t>(8, kRing / (q.set_rows * v.cols * 2 * arrays));         // (two at least)
+            q.groups = (v.rows + q.set_rows - 1) / q.set_rows;
+        } else {
+            const int64_t room = kSlots - v.cols * 4;                // (gamma and beta)
+            q.set_rows = std::max<int64_t>(1, 2048 / v.cols);        // 4 KB of a row or more
+            const int64_t all = room / (q.set_rows * v.cols * 2);    // slots of a CTA
+            q.stream = (int)std::min<int64_t>(16, all);              // a warp each
+            q.slots = (int)std::min<int64_t>(4, all / q.stream);
+            q.threads = q.stream * 32;
+            q.groups = (v.rows + q.stream * q.set_rows - 1) / (q.stream * q.set_rows);
+        }
+        if (v.rows >= 2 * sms * (grad ? q.set_rows : 4)) return q;
+        q.stream = 0;
+    }
     const int64_t most = grad ? 512 : 1024;
     // (a thread's columns: few where there are few rows, so that a row is spread over more threads)
     if (q.vec == 8) q.nv = groups <= 32 ? 1 : (groups <= 2 * most ? 2 : 4);
@@ -490,7 +834,7 @@ NormPlan plan_norm(const MatView& v, bool aligned, bool grad) {
 }
 
 // CTAs a SM holds of the gradient's kernels: bounded by what its registers are compiled for; the lines of the workspace are counted with it
-int ctas_per_sm(const NormPlan& q) { return std::max(1, (q.nv == 0 ? 1024 : 1024) / q.threads); }
+int ctas_per_sm(const NormPlan& q) { return q.stream ? 1 : std::max(1, 1024 / q.threads); }
 int64_t grid_of(const NormPlan& q, int sms) { return std::min<int64_t>(q.groups, (int64_t)sms * ctas_per_sm(q)); }
 
 template <bool GRAD, int VEC, int NV, bool LINEAR, bool ONE>
@@ -506,8 +850,28 @@ template <bool GRAD, int VEC, int NV>
 ccl_status launch_linear(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
     return q.linear ? launch_one<GRAD, VEC, NV, true>(p, q, grid, st) : launch_one<GRAD, VEC, NV, false>(p, q, grid, st);
 }
+template <int WHICH>
+ccl_status launch_stream(void (*kernel)(const StreamParams), const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
+    static std::atomic<uint64_t> configured{0};          // bit per device: the shared-memory limit has been raised
+    int dev = 0;
+    CCL_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev >= 64 || !(configured.load() >> dev & 1)) {
+        CCL_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(WHICH < 2 ? kSlots : kRing + kStreamCols * 2)));
+        if (dev < 64) configured.fetch_or(1ull << dev);
+    }
+    StreamParams sp;
+    sp.n = p;
+    sp.groups = q.stream; sp.slots = q.slots; sp.arrays = q.arrays; sp.set_rows = (int32_t)q.set_rows;
+    sp.array_bytes = (uint32_t)(q.set_rows * p.v.cols * 2);
+    sp.slot_bytes = sp.array_bytes * (uint32_t)q.arrays;
+    const size_t smem = (size_t)sp.slot_bytes * q.slots * (WHICH < 2 ? q.stream : 1) + (size_t)p.v.cols * (WHICH < 2 ? 4 : 2);
+    return launch_early(kernel, dim3(grid), q.threads, smem, st, sp);
+}
 template <bool GRAD>
 ccl_status launch_plan(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
+    if (q.stream && !GRAD) return p.layer ? launch_stream<0>(norm_rows_kernel<true>, p, q, grid, st) : launch_stream<1>(norm_rows_kernel<false>, p, q, grid, st);
+    if (q.stream) return q.nv == 1 ? launch_stream<2>(norm_grad_stream_kernel<1, 2>, p, q, grid, st)
+                                   : (q.nv == 2 ? launch_stream<3>(norm_grad_stream_kernel<2, 2>, p, q, grid, st) : launch_stream<4>(norm_grad_stream_kernel<4, 1>, p, q, grid, st));
     if (q.nv == 0) return launch_early(q.vec == 8 ? norm_long_kernel<8, GRAD> : norm_long_kernel<1, GRAD>, dim3(grid), q.threads, 0, st, p);
     switch (q.vec * 10 + q.nv) {
         case 81: return launch_linear<GRAD, 8, 1>(p, q, grid, st);
@@ -531,11 +895,21 @@ const uint16_t* bf16(const void* p) { return static_cast<const uint16_t*>(p); }
 
 size_t grad_workspace(const MatView& v, int sms) {
     // (the vector and the scalar plan may differ in their grids; buffers of either alignment find room)
-    const int64_t lines = std::max(grid_of(plan_norm(v, true, true), sms), grid_of(plan_norm(v, false, true), sms));
+    int64_t lines = grid_of(plan_norm(v, false, true, 3, sms), sms);
+    for (int arrays : {2, 3}) lines = std::max(lines, grid_of(plan_norm(v, true, true, arrays, sms), sms));
     return (size_t)lines * 2 * (size_t)v.cols * 4;
 }
 
 }  // namespace
+
+// The status word of this file's kernels, read and cleared (ccl_gemm_status)
+ccl_status norm_status_take(int* code) {
+    int zero = 0;
+    CCL_CUDA_TRY(cudaMemcpyFromSymbol(code, g_norm_status, sizeof(int)));
+    if (*code) CCL_CUDA_TRY(cudaMemcpyToSymbol(g_norm_status, &zero, sizeof(int)));
+    return CCL_OK;
+}
+
 }  // namespace ccl
 
 using namespace ccl;
@@ -554,11 +928,12 @@ extern "C" ccl_status ccl_norm(const ccl_mat* m, int32_t kind, float eps, const 
     p.x = bf16(X_dev); p.out = static_cast<uint16_t*>(Y_dev); p.gamma = bf16(gamma_dev); p.beta = bf16(beta_dev);
     p.mean = mean_dev; p.rstd = rstd_dev;
     p.layer = kind == CCL_NORM_LAYER; p.eps = eps; p.inv_cols = (float)(1.0 / (double)p.v.cols);
-    const NormPlan q = plan_norm(p.v, (any & 15) == 0, false);
-    p.lanes = q.lanes;
     int sms, pairs;
     device_units(&sms, &pairs);
-    return launch_plan<false>(p, q, (unsigned)std::min<int64_t>(q.groups, (int64_t)sms * std::max(1, 2048 / q.threads)), reinterpret_cast<cudaStream_t>(cuda_stream));
+    const NormPlan q = plan_norm(p.v, (any & 15) == 0, false, 1, sms);
+    p.lanes = q.lanes;
+    const int64_t grid = std::min<int64_t>(q.groups, (int64_t)sms * (q.stream ? 1 : std::max(1, 2048 / q.threads)));
+    return launch_plan<false>(p, q, (unsigned)grid, reinterpret_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" ccl_status ccl_norm_grad_workspace(const ccl_mat* m, size_t* bytes) {
@@ -598,7 +973,7 @@ extern "C" ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* 
     p.mean = const_cast<float*>(mean_dev); p.rstd = const_cast<float*>(rstd_dev);
     p.layer = layer; p.inv_cols = (float)(1.0 / (double)p.v.cols);
     p.partial = sums ? static_cast<float*>(ws_dev) : nullptr;
-    const NormPlan q = plan_norm(p.v, (any & 15) == 0, true);
+    const NormPlan q = plan_norm(p.v, (any & 15) == 0, true, p.addend ? 3 : 2, sms);
     p.lanes = q.lanes;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     const int64_t grid = grid_of(q, sms);

@@ -130,10 +130,27 @@ def test_grad_row_major(T, H):
     check_grad(m, dx=False, seed=9)
 
 
-@pytest.mark.parametrize("T,H", [(5000, 96), (3000, 256), (2500, 2048), (1300, 5000)])
+@pytest.mark.parametrize("T,H", [(5000, 96), (9481, 256), (9500, 264), (5003, 512), (4999, 520), (3000, 1024), (2501, 2048), (1301, 4104), (1300, 5000), (1250, 8192), (1203, 9000),
+                                 (1200, 16384)])
 def test_many_rows(T, H):
-    check_forward(ccl.Mat(T, H, 2), seed=11)
-    check_grad(ccl.Mat(T, H, 2), seed=12)
+    m = ccl.Mat(T, H, 2)
+    check_forward(m, seed=11)
+    check_forward(m, layer=False, inplace=True, seed=12)
+    check_grad(m, seed=13)
+    check_grad(m, layer=False, addend=False, inplace="dy", seed=14)
+    check_grad(m, inplace="addend", weights=False, seed=15)
+    check_grad(m, dx=False, seed=16)
+
+
+@pytest.mark.parametrize("m", [ccl.Mat(1500, 1536, 2, 4, ccl.PART_COLS, ccl.CCL, 0), ccl.Mat(1300, 4096, 2, 2, ccl.PART_COLS, ccl.CCL, 4096),
+                               ccl.Mat(9600, 312, 2, 13, ccl.PART_COLS, ccl.CCL, 0), ccl.Mat(1400, 2040, 2, 9, ccl.PART_COLS, ccl.CCL, 0),
+                               ccl.Mat(1300, 768, 2, 32, ccl.PART_COLS, ccl.CCL, 0), ccl.Mat(1200, 8192, 2, 4, ccl.PART_ROWS, ccl.CCL, 0)],
+                         ids=lambda m: f"{m.rows}x{m.cols}-P{m.P}-part{m.part}-{m.strip_align_bytes}")
+def test_many_rows_in_strips(m):
+    check_forward(m, seed=21)
+    check_forward(m, layer=False, inplace=True, seed=22)
+    check_grad(m, seed=23)
+    check_grad(m, layer=False, addend=False, seed=24)
 
 
 LAYOUTS = [
@@ -163,10 +180,26 @@ def test_padding_is_left_alone():
     assert int((y == 1.0).sum()) == 150 and int((y == 7.0).sum()) == n - 150
 
 
-@pytest.mark.parametrize("H", [520, 4096, 40000])
-def test_mean_far_from_zero(H):
+@pytest.mark.parametrize("T,H", [(17, 520), (17, 4096), (17, 40000), (1300, 4096), (1300, 520)])
+def test_mean_far_from_zero(T, H):
     # values about 100 with a spread of 1: E x^2 - (E x)^2 in fp32 would lose half of its digits
-    check_forward(ccl.Mat(17, H, 2), offset=100.0, seed=21)
+    check_forward(ccl.Mat(T, H, 2), offset=100.0, seed=21)
+
+
+@pytest.mark.parametrize("column", [0, 3, 255, 256, 4095])
+@pytest.mark.parametrize("T", [17, 1300])
+def test_one_column_far_out(T, column):
+    # a column hundreds of deviations away from the others, as residual streams have them
+    m = ccl.Mat(T, 4096, 2)
+    X = normal(T, 4096, 1.0, 31)
+    X[:, column] = 1500.0
+    y, mean, rstd = torch.empty(T, 4096, dtype=torch.bfloat16, device="cuda"), torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    ccl.ccl_norm(m, X.cuda(), None, None, y, mean=mean, rstd=rstd)
+    mu, var, rs = stats64(X.double().cuda(), True, 1e-5)
+    # (the bounds above; the mean's error is of the mean magnitude, here that of the one column spread over the row)
+    d = depth(4096) * E * X.double().cuda().abs().mean(1, keepdim=True)
+    assert_within(mean[:, None], mu, d + E * mu.abs(), "mean")
+    assert_within(rstd[:, None], rs, rs * (0.5 * ((depth(4096) + 8) * E * var + 4 * d * d + 2 * d * var.sqrt() * (depth(4096) + 8) * E) / var + 3 * E), "rstd")
 
 
 def test_constant_rows_and_extremes():

@@ -450,8 +450,8 @@ ccl_status ccl_norm(const ccl_mat* m, int32_t kind, float eps, const void* X_dev
  *   dgamma = bf16( sum over rows of dy * h ),  dbeta = bf16( sum over rows of dy )        (in a fixed order: the same bits on every run)
  *   addend_dev  bf16, stored like X: the gradient that reaches X past the normalisation (the residual stream's); NULL: none
  *   dX_dev, dgamma_dev, dbeta_dev: NULL: not wanted; dX_dev may be X_dev, dY_dev or addend_dev.  dbeta_dev is NULL with CCL_NORM_RMS.
- * Workspace: ccl_norm_grad_workspace bytes, needed for dgamma / dbeta only; whatever they hold.  Calls that can overlap on the GPU must
- * not share it.
+ * Workspace: ccl_norm_grad_workspace bytes (0 for few rows and for odd widths), needed for dgamma / dbeta only; whatever they hold.
+ * Calls that can overlap on the GPU must not share it.
  */
 ccl_status ccl_norm_grad_workspace(const ccl_mat* m, size_t* bytes);
 ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* X_dev, const void* gamma_dev, const float* mean_dev, const float* rstd_dev,

@@ -5,9 +5,11 @@
 // variance is the mean square about a mean: about the warp's own one first, and the warps' moments are then joined with
 //   var = sum of var_w + n_w / H (mean_w - mean)^2          (var_w: a warp's share of the mean square about its own mean)
 // so that one meeting of a row's warps is enough and a mean far from zero costs no digits (a difference of E x^2 and (E x)^2 would).
-// CTAs are persistent and fetch their next row while the present one meets.  The gradients of gamma and beta are sums over the rows:
-// every thread keeps its columns' sums in registers, a CTA leaves one line of them in the workspace, and a second kernel, placed early,
-// adds the lines in a fixed order: no atomics, the same bits on every run.
+// The gradients of gamma and beta are sums over the rows, in a fixed order, without atomics: the same bits on every run.
+//
+// Three ways, by size and alignment (plan_norm).  Many rows in aligned 16-byte pieces: bulk copies into shared memory keep the loads under way
+// (norm_rows_kernel, norm_grad_stream_kernel).  Few rows, odd widths, other layouts: rows through registers.  Rows longer than a CTA's
+// registers hold: read again from the L2.
 #include <algorithm>
 #include <atomic>
 
@@ -24,8 +26,7 @@ struct NormParams {
     const uint16_t *x, *dy, *addend, *gamma, *beta;
     uint16_t* out;                  // y or dx (may be one of the inputs: an element is written by the thread that has read it)
     float *mean, *rstd;             // written by ccl_norm, read by ccl_norm_grad
-    float* partial;                 // ccl_norm_grad: [CTAs][2][cols] sums for gamma and beta, or NULL
-    int32_t want_beta;
+    float* partial;                 // norm_grad_stream_kernel: [CTAs][2][cols] sums for gamma and beta, or NULL
     int32_t layer;                  // 1: about the row's mean, 0: about zero
     float eps, inv_cols;
     int32_t lanes;                  // threads of a row
@@ -105,7 +106,7 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024) norm_kernel(const __grid_con
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ float2 moments[2][32];
     __shared__ float counts[32];
-    const int lanes = p.lanes, lane = ONE ? threadIdx.x & (lanes - 1) : threadIdx.x, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int lanes = p.lanes, lane = ONE ? threadIdx.x & (lanes - 1) : threadIdx.x, warp = threadIdx.x >> 5, wl = threadIdx.x & 31, warps = blockDim.x >> 5;
     const int64_t rows_at_once = ONE ? blockDim.x / lanes : 1, stride = gridDim.x * rows_at_once;
     RowCursor<VEC, NV, LINEAR> cur(p, lane, blockIdx.x * rows_at_once + (ONE ? threadIdx.x / lanes : 0), stride);
     bool mine[NV];
@@ -157,21 +158,15 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024) norm_kernel(const __grid_con
                 m2 = fmaf(d * p.inv_cols, d, m2);        // (a mean as it grows: a sum of H squares could leave fp32 where their mean does not)
             }
         m2 = lanes_sum(m2, ONE ? lanes : 32);
-        if (!ONE) {
-            if ((threadIdx.x & 31) == 0) moments[turn][warp] = make_float2(mean, m2);
+        if (!ONE) {                                      // (a lane a warp: its mean, its share of the variance, its share of the values)
+            if (wl == 0) moments[turn][warp] = make_float2(mean, m2);
             __syncthreads();
-            mean = 0.0f;
-            if (p.layer) {
-                for (int w = 0; w < warps; ++w) mean = fmaf(counts[w], moments[turn][w].x, mean);
-                mean *= p.inv_cols;
-            }
-            m2 = 0.0f;
-            for (int w = 0; w < warps; ++w) {
-                const float d = moments[turn][w].x - mean;
-                m2 += fmaf(counts[w] * p.inv_cols * d, d, moments[turn][w].y);
-            }
+            const float2 o = wl < warps ? moments[turn][wl] : make_float2(0.0f, 0.0f);
+            const float n = wl < warps ? counts[wl] * p.inv_cols : 0.0f;
+            mean = p.layer ? lanes_sum(n * o.x, 32) : 0.0f;
+            m2 = lanes_sum(fmaf(n * (o.x - mean), o.x - mean, o.y), 32);
         }
-        const float rstd = 1.0f / sqrtf(m2 + p.eps);
+        const float rstd = rsqrtf(m2 + p.eps);
         if (row < p.v.rows) {
             if (lane == 0) {
                 if (p.mean) p.mean[row] = mean;
@@ -192,57 +187,37 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024) norm_kernel(const __grid_con
 }
 
 template <int VEC, int NV, bool LINEAR, bool ONE>
-__global__ void __launch_bounds__(ONE ? 256 : 512) norm_grad_kernel(const __grid_constant__ NormParams p) {
+__global__ void __launch_bounds__(ONE ? 256 : 1024) norm_grad_kernel(const __grid_constant__ NormParams p) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ float2 sums[2][32];
-    extern __shared__ float lines[];                     // ONE: the warps' sums for gamma and beta, [2][cols]
-    const int lanes = p.lanes, lane = ONE ? threadIdx.x & (lanes - 1) : threadIdx.x, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int lanes = p.lanes, lane = ONE ? threadIdx.x & (lanes - 1) : threadIdx.x, warp = threadIdx.x >> 5, wl = threadIdx.x & 31, warps = blockDim.x >> 5;
     const int64_t rows_at_once = ONE ? blockDim.x / lanes : 1, stride = gridDim.x * rows_at_once;
     RowCursor<VEC, NV, LINEAR> cur(p, lane, blockIdx.x * rows_at_once + (ONE ? threadIdx.x / lanes : 0), stride);
     bool mine[NV];
-    float dgamma[NV][VEC], dbeta[NV][VEC];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        mine[i] = cur.column(p, lane, i) < p.v.cols;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) dgamma[i][j] = dbeta[i][j] = 0.0f;
-    }
+    for (int i = 0; i < NV; ++i) mine[i] = cur.column(p, lane, i) < p.v.cols;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int PR = (VEC + 1) / 2;
-    uint32_t nx[NV][PR], ny[NV][PR];
-    float n_mean = 0.0f, n_rstd = 0.0f;
-    auto fetch = [&]() {
-        const bool ok = cur.row < p.v.rows;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-#pragma unroll
-            for (int j = 0; j < PR; ++j) nx[i][j] = ny[i][j] = 0;
-            if (mine[i] && ok) {
-                const int64_t at = cur.at(p, lane, i);
-                load_vec<VEC>(p.x + at, nx[i]);
-                load_vec<VEC>(p.dy + at, ny[i]);
-            }
-        }
-        n_rstd = ok ? p.rstd[cur.row] : 0.0f;
-        n_mean = ok && p.layer ? p.mean[cur.row] : 0.0f;
-    };
-    fetch();
     int turn = 0;
     for (int64_t first = blockIdx.x * rows_at_once; first < p.v.rows; first += stride, turn ^= 1) {
         const int64_t row = cur.row;
-        const float mean = n_mean, rstd = n_rstd;
+        const bool live = row < p.v.rows;
+        const float rstd = live ? p.rstd[row] : 0.0f, mean = live && p.layer ? p.mean[row] : 0.0f;
         int64_t to[NV];
         uint32_t ad[NV][PR], x[NV][PR], y[NV][PR];
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            to[i] = row < p.v.rows && mine[i] ? cur.at(p, lane, i) : 0;
+            to[i] = live && mine[i] ? cur.at(p, lane, i) : 0;
 #pragma unroll
-            for (int j = 0; j < PR; ++j) { x[i][j] = nx[i][j]; y[i][j] = ny[i][j]; ad[i][j] = 0; }
-            if (p.addend && row < p.v.rows && mine[i]) load_vec<VEC>(p.addend + to[i], ad[i]);
+            for (int j = 0; j < PR; ++j) x[i][j] = y[i][j] = ad[i][j] = 0;
+            if (live && mine[i]) {
+                load_vec<VEC>(p.x + to[i], x[i]);
+                load_vec<VEC>(p.dy + to[i], y[i]);
+                if (p.addend) load_vec<VEC>(p.addend + to[i], ad[i]);
+            }
         }
         cur.next(stride);
-        fetch();
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (mine[i]) {
@@ -252,24 +227,22 @@ __global__ void __launch_bounds__(ONE ? 256 : 512) norm_grad_kernel(const __grid
                 load_weights<VEC>(p.gamma, cur.column(p, lane, i), 1.0f, g);
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
-                    const float h = (f[j] - mean) * rstd, gg = d[j] * g[j];
-                    s1 += gg;
-                    s2 = fmaf(gg, h, s2);
-                    dgamma[i][j] = fmaf(d[j], h, dgamma[i][j]);
-                    dbeta[i][j] += d[j];
+                    s1 = fmaf(d[j], g[j], s1);
+                    s2 = fmaf(d[j] * g[j], (f[j] - mean) * rstd, s2);
                 }
             }
         s1 = lanes_sum(s1, ONE ? lanes : 32);
         s2 = lanes_sum(s2, ONE ? lanes : 32);
         if (!ONE) {
-            if ((threadIdx.x & 31) == 0) sums[turn][warp] = make_float2(s1, s2);
+            if (wl == 0) sums[turn][warp] = make_float2(s1, s2);
             __syncthreads();
-            s1 = s2 = 0.0f;
-            for (int w = 0; w < warps; ++w) { const float2 q = sums[turn][w]; s1 += q.x; s2 += q.y; }
+            const float2 o = wl < warps ? sums[turn][wl] : make_float2(0.0f, 0.0f);
+            s1 = lanes_sum(o.x, 32);
+            s2 = lanes_sum(o.y, 32);
         }
         s1 = p.layer ? s1 * p.inv_cols : 0.0f;
         s2 *= p.inv_cols;
-        if (p.out && row < p.v.rows)
+        if (live)
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (mine[i]) {
@@ -286,43 +259,82 @@ __global__ void __launch_bounds__(ONE ? 256 : 512) norm_grad_kernel(const __grid
                     store_vec<VEC>(p.out + to[i], f);
                 }
     }
-    if (!p.partial) return;
-    float* line = p.partial + (int64_t)blockIdx.x * 2 * p.v.cols;
-    if constexpr (!ONE) {
+}
+
+// dgamma and dbeta where the rows' kernel leaves them (few rows, rows of odd widths or layouts): a cluster of up to eight CTAs owns a strip of
+// columns and shares its rows; a thread keeps the sums of its (eight) columns, the CTA's row lanes meet in shared memory and the cluster's
+// CTAs in distributed shared memory, in a fixed order.  x and dy are read once more, from the L2 where they fit it.
+template <int VEC, bool LINEAR>
+__global__ void __launch_bounds__(256) norm_sums_kernel(const __grid_constant__ NormParams p, uint16_t* dgamma, uint16_t* dbeta, int64_t rows_per_cta) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __shared__ float part[2][256 * VEC];
+    uint32_t rank, ctas;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
+    const int L = p.lanes, R = 256 / L, lx = threadIdx.x & (L - 1), ly = threadIdx.x / L;
+    const int64_t tile = blockIdx.x / ctas, col = (tile * L + lx) * VEC;
+    const bool col_ok = col < p.v.cols;
+    float dg[VEC], db[VEC];
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (mine[i]) {
-                const int64_t col = cur.column(p, lane, i);
+    for (int i = 0; i < VEC; ++i) dg[i] = db[i] = 0.0f;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (col_ok) {
+        const int64_t r1 = min(p.v.rows, (int64_t)(rank + 1) * rows_per_cta);
+        const int64_t base = LINEAR ? map(p.v, 0, col) : 0, pitch = p.v.split == 2 ? strip_w_of(p.v, col / p.v.w) : p.v.cols;
+        constexpr int U = VEC == 8 ? 2 : 8;              // rows whose loads are all in flight before the first is used
+        for (int64_t r = (int64_t)rank * rows_per_cta + ly; r < r1; r += (int64_t)U * R) {
+            uint32_t x[U][(VEC + 1) / 2], y[U][(VEC + 1) / 2];
+            float mean[U], rstd[U];
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) { line[col + j] = dgamma[i][j]; line[p.v.cols + col + j] = dbeta[i][j]; }
+            for (int u = 0; u < U; ++u) {
+                const int64_t row = min(r + (int64_t)u * R, r1 - 1), at = LINEAR ? base + row * pitch : map(p.v, row, col);
+                load_vec<VEC>(p.x + at, x[u]);
+                load_vec<VEC>(p.dy + at, y[u]);
+                rstd[u] = p.rstd[row];
+                mean[u] = p.layer ? p.mean[row] : 0.0f;
             }
-    } else {
-    // the rows of a warp first (fixed exchanges), then the warps one after the other
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+            for (int u = 0; u < U; ++u) {
+                if (r + (int64_t)u * R >= r1) break;
+                float f[VEC], d[VEC];
+                unpack<VEC>(x[u], f);
+                unpack<VEC>(y[u], d);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j)
-            for (int w = lanes; w < 32; w <<= 1) {
-                dgamma[i][j] += __shfl_xor_sync(0xffffffffu, dgamma[i][j], w);
-                dbeta[i][j] += __shfl_xor_sync(0xffffffffu, dbeta[i][j], w);
-            }
-    const int cols = (int)p.v.cols;
-    for (int w = 0; w < warps; ++w) {
-        if (warp == w && (int)(threadIdx.x & 31) < lanes)
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (mine[i]) {
-                    const int col = (int)cur.column(p, lane, i);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        lines[col + j] = (w ? lines[col + j] : 0.0f) + dgamma[i][j];
-                        lines[cols + col + j] = (w ? lines[cols + col + j] : 0.0f) + dbeta[i][j];
-                    }
+                for (int i = 0; i < VEC; ++i) {
+                    dg[i] = fmaf(d[i], (f[i] - mean[u]) * rstd[u], dg[i]);
+                    db[i] += d[i];
                 }
-        __syncthreads();
+            }
+        }
     }
-    for (int c = threadIdx.x; c < 2 * cols; c += blockDim.x) line[c] = lines[c];
+    const int cols = L * VEC;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) { part[0][ly * cols + lx * VEC + i] = dg[i]; part[1][ly * cols + lx * VEC + i] = db[i]; }
+    __syncthreads();
+    float s[2] = {0.0f, 0.0f};
+    if ((int)threadIdx.x < cols)
+        for (int y = 0; y < R; ++y) { s[0] += part[0][y * cols + threadIdx.x]; s[1] += part[1][y * cols + threadIdx.x]; }
+    __syncthreads();
+    if ((int)threadIdx.x < cols) { part[0][threadIdx.x] = s[0]; part[1][threadIdx.x] = s[1]; }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (rank == 0 && (int)threadIdx.x < cols) {
+        const int64_t n = tile * cols + threadIdx.x;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            uint16_t* out = k ? dbeta : dgamma;
+            for (uint32_t c = 1; c < ctas; ++c) {
+                uint32_t remote;
+                float x;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_u32(&part[k][threadIdx.x])), "r"(c));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(remote) : "memory");
+                s[k] += x;
+            }
+            if (out && n < p.v.cols) reinterpret_cast<__nv_bfloat16*>(out)[n] = __float2bfloat16_rn(s[k]);
+        }
     }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // the sums of a CTA stay until CTA 0 has read them
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // ---- many rows whose column groups are aligned 16-byte pieces (row-major and CCL split along the columns) -------------------
@@ -641,7 +653,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_stream_kernel(const
 }
 
 // Rows longer than the registers of a CTA: the row is read once for every sum and once more for the result (from the L2, where it still
-// is), by any layout's address map.  GRAD: a CTA's line of sums is added up in the workspace, every column by one thread.
+// is), by any layout's address map.
 template <int VEC, bool GRAD>
 __global__ void __launch_bounds__(512) norm_long_kernel(const __grid_constant__ NormParams p) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -658,7 +670,6 @@ __global__ void __launch_bounds__(512) norm_long_kernel(const __grid_constant__ 
         for (int w = 0; w < 16; ++w) { a += part[turn][w].x; b += part[turn][w].y; }
         turn ^= 1;
     };
-    float* line = GRAD && p.partial ? p.partial + (int64_t)blockIdx.x * 2 * p.v.cols : nullptr;
     for (int64_t row = blockIdx.x; row < p.v.rows; row += gridDim.x) {
         float mean = 0.0f, rstd = 0.0f, s1 = 0.0f, s2 = 0.0f;
         uint32_t u[PR];
@@ -685,7 +696,7 @@ __global__ void __launch_bounds__(512) norm_long_kernel(const __grid_constant__ 
             meet(s1, s2);
             // (s1 is zero but for the mean's own rounding, which it takes out of the variance)
             if (p.layer) s2 -= (s1 * p.inv_cols) * (s1 * p.inv_cols);
-            rstd = 1.0f / sqrtf((s2 < 0.0f ? 0.0f : s2) + p.eps);
+            rstd = rsqrtf((s2 < 0.0f ? 0.0f : s2) + p.eps);
             if (threadIdx.x == 0) {
                 if (p.mean) p.mean[row] = mean;
                 if (p.rstd) p.rstd[row] = rstd;
@@ -732,13 +743,8 @@ __global__ void __launch_bounds__(512) norm_long_kernel(const __grid_constant__ 
                 for (int j = 0; j < VEC; ++j) {
                     const float h = (f[j] - mean) * rstd;
                     o[j] = fmaf(rstd, fmaf(-h, s2, fmaf(d[j], g[j], -s1)), a[j]);
-                    if (line) {
-                        const bool more = row != blockIdx.x;
-                        line[c + j] = fmaf(d[j], h, more ? line[c + j] : 0.0f);
-                        line[p.v.cols + c + j] = (more ? line[p.v.cols + c + j] : 0.0f) + d[j];
-                    }
                 }
-                if (p.out) store_vec<VEC>(p.out + at, o);
+                store_vec<VEC>(p.out + at, o);
             }
         }
     }
@@ -811,11 +817,10 @@ NormPlan plan_norm(const MatView& v, bool aligned, bool grad, int arrays, int sm
             q.threads = q.stream * 32;
             q.groups = (v.rows + q.stream * q.set_rows - 1) / (q.stream * q.set_rows);
         }
-        if (v.rows >= 2 * sms * (grad ? q.set_rows : 4)) return q;
+        if (v.rows >= (grad ? sms * q.set_rows : 8 * sms)) return q;
         q.stream = 0;
     }
-    const int64_t most = grad ? 512 : 1024;
-    // (a thread's columns: few where there are few rows, so that a row is spread over more threads)
+    const int64_t most = 1024;
     if (q.vec == 8) q.nv = groups <= 32 ? 1 : (groups <= 2 * most ? 2 : 4);
     else q.nv = groups <= 64 ? 2 : 8;
     const int64_t need = (groups + q.nv - 1) / q.nv;
@@ -833,22 +838,12 @@ NormPlan plan_norm(const MatView& v, bool aligned, bool grad, int arrays, int sm
     return q;
 }
 
-// CTAs a SM holds of the gradient's kernels: bounded by what its registers are compiled for; the lines of the workspace are counted with it
-int ctas_per_sm(const NormPlan& q) { return q.stream ? 1 : std::max(1, 1024 / q.threads); }
-int64_t grid_of(const NormPlan& q, int sms) { return std::min<int64_t>(q.groups, (int64_t)sms * ctas_per_sm(q)); }
+unsigned grid_of(const NormPlan& q, int sms) { return (unsigned)std::min<int64_t>(q.groups, (int64_t)sms * (q.stream ? 1 : std::max(1, 2048 / q.threads))); }
 
-template <bool GRAD, int VEC, int NV, bool LINEAR, bool ONE>
+template <bool GRAD, int VEC, int NV, bool ONE>
 ccl_status launch_shape(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
-    if constexpr (GRAD) return launch_early(norm_grad_kernel<VEC, NV, LINEAR, ONE>, dim3(grid), q.threads, ONE ? (size_t)p.v.cols * 8 : 0, st, p);
-    else return launch_early(norm_kernel<VEC, NV, LINEAR, ONE>, dim3(grid), q.threads, 0, st, p);
-}
-template <bool GRAD, int VEC, int NV, bool LINEAR>
-ccl_status launch_one(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
-    return q.one ? launch_shape<GRAD, VEC, NV, LINEAR, true>(p, q, grid, st) : launch_shape<GRAD, VEC, NV, LINEAR, false>(p, q, grid, st);
-}
-template <bool GRAD, int VEC, int NV>
-ccl_status launch_linear(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
-    return q.linear ? launch_one<GRAD, VEC, NV, true>(p, q, grid, st) : launch_one<GRAD, VEC, NV, false>(p, q, grid, st);
+    if constexpr (GRAD) return launch_early(q.linear ? norm_grad_kernel<VEC, NV, true, ONE> : norm_grad_kernel<VEC, NV, false, ONE>, dim3(grid), q.threads, 0, st, p);
+    else return launch_early(q.linear ? norm_kernel<VEC, NV, true, ONE> : norm_kernel<VEC, NV, false, ONE>, dim3(grid), q.threads, 0, st, p);
 }
 template <int WHICH>
 ccl_status launch_stream(void (*kernel)(const StreamParams), const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
@@ -873,13 +868,12 @@ ccl_status launch_plan(const NormParams& p, const NormPlan& q, unsigned grid, cu
     if (q.stream) return q.nv == 1 ? launch_stream<2>(norm_grad_stream_kernel<1, 2>, p, q, grid, st)
                                    : (q.nv == 2 ? launch_stream<3>(norm_grad_stream_kernel<2, 2>, p, q, grid, st) : launch_stream<4>(norm_grad_stream_kernel<4, 1>, p, q, grid, st));
     if (q.nv == 0) return launch_early(q.vec == 8 ? norm_long_kernel<8, GRAD> : norm_long_kernel<1, GRAD>, dim3(grid), q.threads, 0, st, p);
-    switch (q.vec * 10 + q.nv) {
-        case 81: return launch_linear<GRAD, 8, 1>(p, q, grid, st);
-        case 82: return launch_linear<GRAD, 8, 2>(p, q, grid, st);
-        case 84: return launch_linear<GRAD, 8, 4>(p, q, grid, st);
-        case 12: return launch_linear<GRAD, 1, 2>(p, q, grid, st);
-        default: return launch_linear<GRAD, 1, 8>(p, q, grid, st);
+    if (q.vec == 8) {
+        if (q.one) return q.nv == 1 ? launch_shape<GRAD, 8, 1, true>(p, q, grid, st) : launch_shape<GRAD, 8, 2, true>(p, q, grid, st);
+        return q.nv == 2 ? launch_shape<GRAD, 8, 2, false>(p, q, grid, st) : launch_shape<GRAD, 8, 4, false>(p, q, grid, st);
     }
+    if (q.one) return q.nv == 2 ? launch_shape<GRAD, 1, 2, true>(p, q, grid, st) : launch_shape<GRAD, 1, 8, true>(p, q, grid, st);
+    return launch_shape<GRAD, 1, 8, false>(p, q, grid, st);
 }
 
 ccl_status norm_view(const char* who, const ccl_mat* m, int32_t kind, MatView* v) {
@@ -893,11 +887,27 @@ ccl_status norm_view(const char* who, const ccl_mat* m, int32_t kind, MatView* v
 uintptr_t bits(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 const uint16_t* bf16(const void* p) { return static_cast<const uint16_t*>(p); }
 
+// Lines of sums that the gradient's kernel leaves (0: it leaves them to norm_sums_kernel), whatever the buffers' alignment and the addend
 size_t grad_workspace(const MatView& v, int sms) {
-    // (the vector and the scalar plan may differ in their grids; buffers of either alignment find room)
-    int64_t lines = grid_of(plan_norm(v, false, true, 3, sms), sms);
-    for (int arrays : {2, 3}) lines = std::max(lines, grid_of(plan_norm(v, true, true, arrays, sms), sms));
-    return (size_t)lines * 2 * (size_t)v.cols * 4;
+    size_t lines = 0;
+    for (int arrays : {2, 3}) {
+        const NormPlan q = plan_norm(v, true, true, arrays, sms);
+        if (q.stream) lines = std::max<size_t>(lines, grid_of(q, sms));
+    }
+    return lines * 2 * (size_t)v.cols * 4;
+}
+
+ccl_status launch_sums(NormParams p, const NormPlan& q, uint16_t* dgamma, uint16_t* dbeta, cudaStream_t st) {
+    // as many threads along a row as leave every SM a few CTAs; eight CTAs at most share the rows
+    const int64_t groups = (p.v.cols + q.vec - 1) / q.vec;
+    int lanes = 32, ctas = 8;
+    while (ctas > 1 && p.v.rows < (int64_t)ctas * 32) ctas /= 2;
+    while (lanes > 2 && (groups + lanes - 1) / lanes * ctas < 148 * 3) lanes /= 2;
+    const int64_t tiles = (groups + lanes - 1) / lanes;
+    if (tiles * ctas >= (INT64_C(1) << 31)) return fail(CCL_ERR_UNSUPPORTED, "ccl_norm_grad: too many columns");
+    p.lanes = lanes;
+    auto kernel = q.vec == 8 ? (q.linear ? norm_sums_kernel<8, true> : norm_sums_kernel<8, false>) : (q.linear ? norm_sums_kernel<1, true> : norm_sums_kernel<1, false>);
+    return launch_early_clusters(kernel, dim3((unsigned)(tiles * ctas)), 256, ctas, st, p, dgamma, dbeta, (p.v.rows + ctas - 1) / ctas);
 }
 
 }  // namespace
@@ -932,8 +942,7 @@ extern "C" ccl_status ccl_norm(const ccl_mat* m, int32_t kind, float eps, const 
     device_units(&sms, &pairs);
     const NormPlan q = plan_norm(p.v, (any & 15) == 0, false, 1, sms);
     p.lanes = q.lanes;
-    const int64_t grid = std::min<int64_t>(q.groups, (int64_t)sms * (q.stream ? 1 : std::max(1, 2048 / q.threads)));
-    return launch_plan<false>(p, q, (unsigned)grid, reinterpret_cast<cudaStream_t>(cuda_stream));
+    return launch_plan<false>(p, q, grid_of(q, sms), reinterpret_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" ccl_status ccl_norm_grad_workspace(const ccl_mat* m, size_t* bytes) {
@@ -963,21 +972,25 @@ extern "C" ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* 
     if ((bits(mean_dev) | bits(rstd_dev)) & 3) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: mean / rstd is not 4-byte aligned");
     int sms, pairs;
     device_units(&sms, &pairs);
-    const bool sums = dgamma_dev || dbeta_dev;
-    if (sums) {
-        const size_t need = grad_workspace(p.v, sms);
-        if (!ws_dev || ws_bytes < need) return fail(CCL_ERR_WORKSPACE, "ccl_norm_grad: needs %zu bytes of workspace (got %zu)", need, ws_dev ? ws_bytes : (size_t)0);
-        if (bits(ws_dev) & 15) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: workspace is not 16-byte aligned");
-    }
     p.x = bf16(X_dev); p.dy = bf16(dY_dev); p.addend = dX_dev ? bf16(addend_dev) : nullptr; p.out = static_cast<uint16_t*>(dX_dev); p.gamma = bf16(gamma_dev);
     p.mean = const_cast<float*>(mean_dev); p.rstd = const_cast<float*>(rstd_dev);
     p.layer = layer; p.inv_cols = (float)(1.0 / (double)p.v.cols);
-    p.partial = sums ? static_cast<float*>(ws_dev) : nullptr;
+    uint16_t *dgamma = static_cast<uint16_t*>(dgamma_dev), *dbeta = static_cast<uint16_t*>(dbeta_dev);
+    const bool sums = dgamma || dbeta;
+    if (sums) {
+        const size_t need = grad_workspace(p.v, sms);
+        if (need && (!ws_dev || ws_bytes < need)) return fail(CCL_ERR_WORKSPACE, "ccl_norm_grad: needs %zu bytes of workspace (got %zu)", need, ws_dev ? ws_bytes : (size_t)0);
+        if (bits(ws_dev) & 15) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: workspace is not 16-byte aligned");
+    }
     const NormPlan q = plan_norm(p.v, (any & 15) == 0, true, p.addend ? 3 : 2, sms);
     p.lanes = q.lanes;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-    const int64_t grid = grid_of(q, sms);
-    if ((s = launch_plan<true>(p, q, (unsigned)grid, st)) || !sums) return s;
-    return launch_early(norm_grad_finish_kernel, dim3((unsigned)((p.v.cols + 31) / 32), 2), 256, 0, st, (const float*)p.partial, (int)grid, p.v.cols,
-                       static_cast<uint16_t*>(dgamma_dev), static_cast<uint16_t*>(dbeta_dev));
+    const unsigned grid = grid_of(q, sms);
+    if (q.stream && sums) {
+        p.partial = static_cast<float*>(ws_dev);
+        if ((s = launch_plan<true>(p, q, grid, st))) return s;
+        return launch_early(norm_grad_finish_kernel, dim3((unsigned)((p.v.cols + 31) / 32), 2), 256, 0, st, (const float*)p.partial, (int)grid, p.v.cols, dgamma, dbeta);
+    }
+    if (sums && (s = launch_sums(p, q, dgamma, dbeta, st))) return s;        // (first: dX may take the place of X or dY)
+    return p.out ? launch_plan<true>(p, q, grid, st) : CCL_OK;
 }

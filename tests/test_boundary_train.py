@@ -45,9 +45,9 @@ def test_norm_refusals():
 
 
 def test_norm_grad_refusals():
-    l, m = ccl.lib(), ccl.Mat(16, 24, 2)
+    l, m = ccl.lib(), ccl.Mat(8192, 2048, 2)
     need = ccl.ccl_norm_grad_workspace(m)
-    assert need >= 2 * 24 * 4
+    assert need >= 2 * 2048 * 4
 
     def call(m=m, kind=0, x=P1, g=P2, mean=P3, rstd=P4, dy=P5, add=P6, dx=P7, dg=P8, db=P9, ws=P1, n=1 << 30):
         return l.ccl_norm_grad(C.byref(m) if m else None, kind, x, g, mean, rstd, dy, add, dx, dg, db, ws, n, None)
@@ -70,11 +70,10 @@ def test_norm_grad_refusals():
 
 
 def test_norm_grad_workspace_is_bounded():
-    # a line of two sums a column for every CTA, of which there are a few for each SM at most
+    # a line of two sums a column for every CTA, one an SM, or none
     for rows in (1, 300, 1 << 20):
         for cols in (1, 8, 520, 8192, 8191, 100000):
-            lines = ccl.ccl_norm_grad_workspace(ccl.Mat(rows, cols, 2)) / (8 * cols)
-            assert 1 <= lines <= min(rows, 148 * 16)
+            assert ccl.ccl_norm_grad_workspace(ccl.Mat(rows, cols, 2)) / (8 * cols) <= min(rows, 148)
 
 
 def test_adamw_refusals():

@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024) norm_grad_kernel(const __gri
 template <int VEC, bool LINEAR>
 __global__ void __launch_bounds__(256) norm_sums_kernel(const __grid_constant__ NormParams p, uint16_t* dgamma, uint16_t* dbeta, int64_t rows_per_cta) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    __shared__ float part[2][256 * VEC];
+    __shared__ float part[2][256 * VEC];                 // [warp][column]
     uint32_t rank, ctas;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
@@ -307,13 +307,22 @@ __global__ void __launch_bounds__(256) norm_sums_kernel(const __grid_constant__ 
             }
         }
     }
-    const int cols = L * VEC;
+    // the row lanes of a warp by exchanges, the eight warps in shared memory, the cluster's CTAs in distributed shared memory
+    for (int w = L; w < 32; w <<= 1)
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) { part[0][ly * cols + lx * VEC + i] = dg[i]; part[1][ly * cols + lx * VEC + i] = db[i]; }
+        for (int i = 0; i < VEC; ++i) {
+            dg[i] += __shfl_xor_sync(0xffffffffu, dg[i], w);
+            db[i] += __shfl_xor_sync(0xffffffffu, db[i], w);
+        }
+    const int cols = L * VEC, warp = threadIdx.x >> 5;
+    if ((int)(threadIdx.x & 31) < L)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) { part[0][warp * cols + lx * VEC + i] = dg[i]; part[1][warp * cols + lx * VEC + i] = db[i]; }
     __syncthreads();
     float s[2] = {0.0f, 0.0f};
     if ((int)threadIdx.x < cols)
-        for (int y = 0; y < R; ++y) { s[0] += part[0][y * cols + threadIdx.x]; s[1] += part[1][y * cols + threadIdx.x]; }
+#pragma unroll
+        for (int y = 0; y < 8; ++y) { s[0] += part[0][y * cols + threadIdx.x]; s[1] += part[1][y * cols + threadIdx.x]; }
     __syncthreads();
     if ((int)threadIdx.x < cols) { part[0][threadIdx.x] = s[0]; part[1][threadIdx.x] = s[1]; }
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -323,13 +332,15 @@ __global__ void __launch_bounds__(256) norm_sums_kernel(const __grid_constant__ 
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             uint16_t* out = k ? dbeta : dgamma;
-            for (uint32_t c = 1; c < ctas; ++c) {
+            float x[7];
+#pragma unroll
+            for (uint32_t c = 1; c < 8; ++c) {           // (all on their way before the first is added)
                 uint32_t remote;
-                float x;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_u32(&part[k][threadIdx.x])), "r"(c));
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(remote) : "memory");
-                s[k] += x;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_u32(&part[k][threadIdx.x])), "r"(c < ctas ? c : 0u));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x[c - 1]) : "r"(remote));
             }
+#pragma unroll
+            for (uint32_t c = 1; c < 8; ++c) s[k] += c < ctas ? x[c - 1] : 0.0f;
             if (out && n < p.v.cols) reinterpret_cast<__nv_bfloat16*>(out)[n] = __float2bfloat16_rn(s[k]);
         }
     }
@@ -352,82 +363,153 @@ __device__ __forceinline__ uint4 shared16(const void* p) { return *reinterpret_c
 __device__ __forceinline__ void parts(const uint4& w, f32x2 (&f)[4]) { f[0] = bf16_unpack(w.x); f[1] = bf16_unpack(w.y); f[2] = bf16_unpack(w.z); f[3] = bf16_unpack(w.w); }
 __device__ __forceinline__ float warp_total(f32x2 a) { float lo, hi; split(a, lo, hi); return lanes_sum(lo + hi, 32); }
 
-constexpr uint32_t kOnes = 0x3F803F80u;                  // two ones in bf16
+constexpr uint16_t kOne = 0x3F80;                        // 1 in bf16
 
+// PHASED: rows of a row-major matrix whose width is no multiple of 8.  A row then starts anywhere in a 16-byte piece, but rows `period` apart start
+// at the same place, and a CTA takes only such rows (blockIdx mod period, and every period-th from there on): with its `phase` as a constant every
+// thread keeps its columns, whole 16-byte pieces are moved, and only a row's first and last piece are looked at element by element.
 struct StreamParams {
     NormParams n;
-    int32_t groups, slots, arrays, set_rows;
+    int32_t groups, slots, arrays, set_rows, period, pieces;        // pieces: of 8 elements, room for a row
     uint32_t slot_bytes, array_bytes;
 };
+
+// A row of a PHASED set: its pieces to shared memory; what lies in the buffer's last, incomplete piece element by element.  Returns the bytes of
+// the bulk copy (the caller announces them; the single elements are written before it does).
+__device__ __forceinline__ uint32_t phased_bytes(const MatView& v, int64_t row, int phase, int pieces) {
+    const int64_t whole = (v.rows * v.cols >> 3) - ((row * v.cols - phase) >> 3);
+    return (uint32_t)min((int64_t)pieces, whole) * 16;
+}
+__device__ __forceinline__ void phased_tail(const MatView& v, const uint16_t* src, int64_t row, int phase, int pieces, uint16_t* to) {
+    const int64_t at = row * v.cols - phase, total = v.rows * v.cols;
+    for (int64_t k = total & ~INT64_C(7); k < total && k < at + pieces * 8; ++k) to[k - at] = src[k];
+}
+// Elements of piece i that belong to a row of `cols` columns: [first, last) of 0..8
+__device__ __forceinline__ bool phased_edge(int i, int phase, int cols, int& first, int& last) {
+    first = phase - i * 8;
+    last = phase + cols - i * 8;
+    return first > 0 || last < 8;
+}
+// Eight results to an aligned place; of a row's first and last piece the row's own elements alone
+__device__ __forceinline__ void store_piece(uint16_t* to, const uint4& w, bool edge, int i, int phase, int cols) {
+    int first, last;
+    if (!edge || !phased_edge(i, phase, cols, first, last)) { *reinterpret_cast<uint4*>(to) = w; return; }
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j >= first && j < last) to[j] = (uint16_t)(u[j >> 1] >> (16 * (j & 1)));
+}
+// gamma or beta behind the slots, from `phase` on
+__device__ __forceinline__ void stage_weights(uint16_t* to, const uint16_t* w, uint16_t none, int phase, int cols, int pieces) {
+    const bool wide = w && !(reinterpret_cast<uintptr_t>(w) & 15);
+    if (wide)
+        for (int c = threadIdx.x * 8; c + 8 <= cols; c += blockDim.x * 8) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(w + c));
+            if (phase == 0) { *reinterpret_cast<uint4*>(to + c) = v; continue; }
+            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) to[phase + c + j] = (uint16_t)(u[j >> 1] >> (16 * (j & 1)));
+        }
+    // what is left: all of them where they are not aligned, else the last few; and the places that no column has
+    const int begin = wide ? cols & ~7 : 0;
+    for (int c = begin + threadIdx.x; c < cols; c += blockDim.x) to[phase + c] = w ? __ldg(w + c) : none;
+    if ((int)threadIdx.x < phase) to[threadIdx.x] = none;
+    const int end = phase + cols + threadIdx.x;
+    if (end < pieces * 8) to[end] = none;                // (fewer than eight)
+}
 
 // Forward.  A warp has a row to itself and nothing to wait for but its own loads: no CTA-wide meeting, eight to sixteen rows in different
 // phases side by side.  A warp owns `slots` slots of `set_rows` consecutive rows and refills one as soon as it is done with it.  The row is
 // read from its slot twice: first and second moment, then the result; gamma and beta lie behind the slots.
 //   The moments are taken about the mean of the row's first 256 values (all lanes' first eight).  That is off by a^2 <= (H / 256 - 1) var at
 // most, so the difference E d^2 - a^2 loses log2(H / 256) bits in the worst case, six at 16384 columns.
-template <bool LAYER>
+template <bool LAYER, bool PHASED>
 __global__ void __launch_bounds__(512, 1) norm_rows_kernel(const __grid_constant__ StreamParams q) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t full[64];
     const NormParams& p = q.n;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, cols = (int)p.v.cols;
-    uint16_t* weights = reinterpret_cast<uint16_t*>(smem + (size_t)warps * q.slots * q.slot_bytes);
+    const int period = PHASED ? q.period : 1, first_row = PHASED ? blockIdx.x % period : 0, phase = PHASED ? (int)((int64_t)first_row * cols & 7) : 0;
+    const int pieces = PHASED ? (phase + cols + 7) >> 3 : cols >> 3;
+    uint16_t *weights = reinterpret_cast<uint16_t*>(smem + (size_t)warps * q.slots * q.slot_bytes), *shifts = weights + q.pieces * 8;
     if ((int)threadIdx.x < warps * q.slots) { mbar_init(&full[threadIdx.x], 1); fence_barrier_init(); }
-    const uint4 ones = make_uint4(kOnes, kOnes, kOnes, kOnes), zeros = make_uint4(0u, 0u, 0u, 0u);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    for (int c = threadIdx.x * 8; c < cols; c += blockDim.x * 8) {
-        *reinterpret_cast<uint4*>(weights + c) = p.gamma ? __ldg(reinterpret_cast<const uint4*>(p.gamma + c)) : ones;
-        *reinterpret_cast<uint4*>(weights + cols + c) = p.beta ? __ldg(reinterpret_cast<const uint4*>(p.beta + c)) : zeros;
-    }
-    __syncthreads();
-    const int64_t rows = p.v.rows, stride = (int64_t)gridDim.x * warps * q.set_rows, begin = ((int64_t)blockIdx.x * warps + warp) * q.set_rows;
+    // sets of `set_rows` rows (one where PHASED), the next one of this warp `stride` further
+    const int64_t rows = p.v.rows, step = (int64_t)warps * q.set_rows * period, stride = step * (PHASED ? (gridDim.x - first_row + period - 1) / period : gridDim.x);
+    const int64_t begin = first_row + (int64_t)(blockIdx.x / period) * step + (int64_t)warp * q.set_rows * period;
     unsigned char* mine = smem + (size_t)warp * q.slots * q.slot_bytes;
     uint64_t* bars = full + warp * q.slots;
     int64_t next = begin;                                // (of lane 0: the first row of the next set to be loaded)
     auto fill = [&](int slot) {
         if (next >= rows) return;
-        const int64_t n = min((int64_t)q.set_rows, rows - next);
-        mbar_expect_tx(&bars[slot], (uint32_t)(n * cols * 2));
-        for (int64_t s = 0; s < p.v.nstrips; ++s) {
-            const int64_t w = strip_w_of(p.v, s);
-            bulk_load(mine + (size_t)slot * q.slot_bytes + s * q.set_rows * p.v.w * 2, p.x + s * p.v.stride + next * w, (uint32_t)(n * w * 2), &bars[slot]);
+        unsigned char* to = mine + (size_t)slot * q.slot_bytes;
+        if (PHASED) {
+            const uint32_t bytes = phased_bytes(p.v, next, phase, pieces);
+            phased_tail(p.v, p.x, next, phase, pieces, reinterpret_cast<uint16_t*>(to));
+            mbar_expect_tx(&bars[slot], bytes);
+            if (bytes) bulk_load(to, p.x + next * cols - phase, bytes, &bars[slot]);
+        } else {
+            const int64_t n = min((int64_t)q.set_rows, rows - next);
+            mbar_expect_tx(&bars[slot], (uint32_t)(n * cols * 2));
+            for (int64_t s = 0; s < p.v.nstrips; ++s) {
+                const int64_t w = strip_w_of(p.v, s);
+                bulk_load(to + s * q.set_rows * p.v.w * 2, p.x + s * p.v.stride + next * w, (uint32_t)(n * w * 2), &bars[slot]);
+            }
         }
         next += stride;
     };
+    // (gamma and beta first: behind a CTA's slots full of rows they would arrive 2.5 us later)
+    stage_weights(weights, p.gamma, kOne, phase, cols, pieces);
+    if (LAYER) stage_weights(shifts, p.beta, 0, phase, cols, pieces);
+    __syncthreads();
     if (lane == 0)
         for (int s = 0; s < q.slots; ++s) fill(s);
-    const int n_first = min(cols, 256);
+    const int n_first = min(cols, 256 - phase);
     const float inv_first = 1.0f / (float)n_first;
     int slot = 0;
-    uint32_t phase = 0;
+    uint32_t parity = 0;
     for (int64_t r0 = begin; r0 < rows; r0 += stride) {
-        const bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars[slot], phase));
+        const bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars[slot], parity));
         if (!ok) {                                       // (the copies under way land before the CTA ends)
             if (lane == 0) {
                 atomicExch(&g_norm_status, 11);
                 for (int s = 0; s < q.slots; ++s)
-                    if (r0 + s * stride < next) mbar_wait_bounded(&bars[(slot + s) % q.slots], slot + s < q.slots ? phase : phase ^ 1);
+                    if (r0 + s * stride < next) mbar_wait_bounded(&bars[(slot + s) % q.slots], slot + s < q.slots ? parity : parity ^ 1);
             }
             break;
         }
         const uint16_t* set = reinterpret_cast<const uint16_t*>(mine + (size_t)slot * q.slot_bytes);
-        const int n = (int)min((int64_t)q.set_rows, rows - r0);
+        const int n = PHASED ? 1 : (int)min((int64_t)q.set_rows, rows - r0);
         for (int r = 0; r < n; ++r) {
             const int64_t row = r0 + r;
-            // every strip's columns of the row: f(place in the slot, first column, groups of eight)
+            // every strip's columns of the row: f(place in the slot, first column, pieces, place in the output)
             auto strips = [&](auto f) {
-                for (int64_t s = 0; s < p.v.nstrips; ++s) {
-                    const int w = (int)strip_w_of(p.v, s);
-                    f(set + s * q.set_rows * p.v.w + r * w, (int)(s * p.v.w), w >> 3, p.out + s * p.v.stride + row * w);
-                }
+                if (PHASED) f(set, 0, pieces, p.out + row * cols - phase);
+                else
+                    for (int64_t s = 0; s < p.v.nstrips; ++s) {
+                        const int w = (int)strip_w_of(p.v, s);
+                        f(set + s * q.set_rows * p.v.w + r * w, (int)(s * p.v.w), w >> 3, p.out + s * p.v.stride + row * w);
+                    }
+            };
+            // elements of a row's first or last piece that are not the row's: `instead`
+            auto mask = [&](int i, f32x2 (&f)[4], float instead) {
+                int first, last;
+                if (PHASED && (i == 0 || i == pieces - 1) && phased_edge(i, phase, cols, first, last))
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float lo, hi;
+                        split(f[j], lo, hi);
+                        f[j] = pair(2 * j >= first && 2 * j < last ? lo : instead, 2 * j + 1 >= first && 2 * j + 1 < last ? hi : instead);
+                    }
             };
             f32x2 f[4];
             float pivot = 0.0f;
             if (LAYER) {
                 const int c = lane * 8;
-                const int64_t s = c / p.v.w;             // (strips may be narrower than the first 256 columns)
-                parts(c < n_first ? shared16(set + s * q.set_rows * p.v.w + r * strip_w_of(p.v, s) + (c - s * p.v.w)) : zeros, f);
+                const int64_t s = PHASED ? 0 : c / p.v.w;            // (strips may be narrower than the first 256 columns)
+                parts(lane < pieces ? shared16(PHASED ? set + c : set + s * q.set_rows * p.v.w + r * strip_w_of(p.v, s) + (c - s * p.v.w)) : make_uint4(0u, 0u, 0u, 0u), f);
+                mask(lane, f, 0.0f);
                 pivot = warp_total((f[0] + f[1]) + (f[2] + f[3])) * inv_first;
             }
             f32x2 m1[2] = {both(0.0f), both(0.0f)}, m2[2] = {both(0.0f), both(0.0f)};
@@ -435,6 +517,7 @@ __global__ void __launch_bounds__(512, 1) norm_rows_kernel(const __grid_constant
 #pragma unroll 4
                 for (int i = lane; i < groups; i += 32) {
                     parts(shared16(x + i * 8), f);
+                    mask(i, f, pivot);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const f32x2 d = LAYER ? f[j] + both(-pivot) : f[j];
@@ -458,25 +541,25 @@ __global__ void __launch_bounds__(512, 1) norm_rows_kernel(const __grid_constant
                     f32x2 g[4], b[4];
                     parts(shared16(x + i * 8), f);
                     parts(shared16(weights + col + i * 8), g);
-                    if (LAYER) parts(shared16(weights + cols + col + i * 8), b);
+                    if (LAYER) parts(shared16(shifts + col + i * 8), b);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) f[j] = LAYER ? fma2(f[j] + both(-mean), g[j] * both(rstd), b[j]) : f[j] * (g[j] * both(rstd));
-                    *reinterpret_cast<uint4*>(to + i * 8) = bf16x8_pack(f);
+                    store_piece(to + i * 8, bf16x8_pack(f), PHASED && (i == 0 || i == pieces - 1), i, phase, cols);
                 }
             });
         }
         __syncwarp();
         if (lane == 0) fill(slot);
-        if (++slot == q.slots) { slot = 0; phase ^= 1; }
+        if (++slot == q.slots) { slot = 0; parity ^= 1; }
     }
 }
 
 // Back.  The sums for gamma and beta want a thread to keep its columns, so a row is spread over a group of `lanes` threads, R rows at a time
 // (two chains of sums that do not wait for each other, gamma unpacked once for both); `groups` groups side by side have the next rows.  A
-// stage of the ring is set_rows = groups x R rows of all inputs; thread 0 refills it when all warps are done with it.  One CTA an SM.
+// stage of the ring is set_rows = groups x R rows of all inputs; warp 0 refills it when all warps are done with it.  One CTA an SM.
 constexpr int kGradThreads = 512;
 
-template <int NV, int R>
+template <int NV, int R, bool PHASED>
 __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_stream_kernel(const __grid_constant__ StreamParams q) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     extern __shared__ __align__(128) unsigned char ring[];
@@ -485,70 +568,110 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_stream_kernel(const
     __shared__ int gone[2][kGradThreads / 32];           // a wait of a group ran out
     const NormParams& p = q.n;
     const int L = p.lanes, G = q.groups, warp = threadIdx.x >> 5, wl = threadIdx.x & 31, cols = (int)p.v.cols;
-    const int64_t rows = p.v.rows, set_rows = q.set_rows, stride = gridDim.x * set_rows, begin = blockIdx.x * set_rows;
+    const int period = PHASED ? q.period : 1, first_row = PHASED ? blockIdx.x % period : 0, phase = PHASED ? (int)((int64_t)first_row * cols & 7) : 0;
+    const int pieces = PHASED ? (phase + cols + 7) >> 3 : cols >> 3;
+    // sets of set_rows rows, `period` apart; the next one of this CTA `stride` further
+    const int64_t rows = p.v.rows, set_rows = q.set_rows, step = set_rows * period;
+    const int64_t stride = step * (PHASED ? (gridDim.x - first_row + period - 1) / period : gridDim.x), begin = first_row + (int64_t)(blockIdx.x / period) * step;
     if (threadIdx.x == 0) {
         for (int s = 0; s < q.slots; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], L * G / 32); }
         fence_barrier_init();
     }
     if (threadIdx.x < kGradThreads / 32) gone[0][threadIdx.x] = gone[1][threadIdx.x] = 0;
     uint16_t* weights = reinterpret_cast<uint16_t*>(ring + (size_t)q.slots * q.slot_bytes);
-    const uint4 ones = make_uint4(kOnes, kOnes, kOnes, kOnes), zeros = make_uint4(0u, 0u, 0u, 0u);
+    const uint4 zeros = make_uint4(0u, 0u, 0u, 0u);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    for (int c = threadIdx.x * 8; c < cols; c += blockDim.x * 8) *reinterpret_cast<uint4*>(weights + c) = p.gamma ? __ldg(reinterpret_cast<const uint4*>(p.gamma + c)) : ones;
-    __syncthreads();
-    int64_t next = begin;                                // (of thread 0: the first row of the next set to be loaded)
-    auto fill = [&](int slot) {
+    int64_t next = begin;                                // (of warp 0: the first row of the next set to be loaded)
+    auto fill = [&](int slot) {                          // (a lane for each row or strip)
         if (next >= rows) return;
-        const int64_t n = min(set_rows, rows - next);
-        mbar_expect_tx(&full[slot], (uint32_t)(n * cols * 2) * q.arrays);
         unsigned char* to = ring + (size_t)slot * q.slot_bytes;
-        for (int64_t s = 0; s < p.v.nstrips; ++s) {
-            const int64_t w = strip_w_of(p.v, s), from = s * p.v.stride + next * w, at = s * set_rows * p.v.w * 2;
-            bulk_load(to + at, p.x + from, (uint32_t)(n * w * 2), &full[slot]);
-            bulk_load(to + q.array_bytes + at, p.dy + from, (uint32_t)(n * w * 2), &full[slot]);
-            if (q.arrays == 3) bulk_load(to + 2 * q.array_bytes + at, p.addend + from, (uint32_t)(n * w * 2), &full[slot]);
+        if (PHASED) {
+            const int64_t row = next + wl * period;
+            uint32_t bytes = 0;
+            if (wl < q.set_rows && row < rows) {
+                bytes = phased_bytes(p.v, row, phase, pieces);
+                const int64_t from = row * cols - phase;
+                unsigned char* at = to + wl * q.pieces * 16;
+                const uint16_t* src[3] = {p.x, p.dy, p.addend};
+#pragma unroll
+                for (int a = 0; a < 3; ++a)
+                    if (a < q.arrays) {
+                        phased_tail(p.v, src[a], row, phase, pieces, reinterpret_cast<uint16_t*>(at + a * q.array_bytes));
+                        if (bytes) bulk_load(at + a * q.array_bytes, src[a] + from, bytes, &full[slot]);
+                    }
+            }
+            bytes = __reduce_add_sync(0xffffffffu, bytes) * q.arrays;
+            __syncwarp();                                // (the single elements are written before lane 0 arrives; it may announce the bytes after they have landed)
+            if (wl == 0) mbar_expect_tx(&full[slot], bytes);
+        } else {
+            const int64_t n = min(set_rows, rows - next);
+            if (wl == 0) mbar_expect_tx(&full[slot], (uint32_t)(n * cols * 2) * q.arrays);
+            if (wl < p.v.nstrips) {
+                const int64_t w = strip_w_of(p.v, wl), from = wl * p.v.stride + next * w, at = wl * set_rows * p.v.w * 2;
+                bulk_load(to + at, p.x + from, (uint32_t)(n * w * 2), &full[slot]);
+                bulk_load(to + q.array_bytes + at, p.dy + from, (uint32_t)(n * w * 2), &full[slot]);
+                if (q.arrays == 3) bulk_load(to + 2 * q.array_bytes + at, p.addend + from, (uint32_t)(n * w * 2), &full[slot]);
+            }
         }
         next += stride;
     };
-    if (threadIdx.x == 0)
+    stage_weights(weights, p.gamma, kOne, phase, cols, pieces);      // (first, as in norm_rows_kernel)
+    __syncthreads();
+    if (warp == 0)
         for (int s = 0; s < q.slots; ++s) fill(s);
     const int group = threadIdx.x / L, lane = threadIdx.x - group * L, warp0 = group * (L / 32), warps = L / 32;
-    bool mine[NV];
-    int col[NV], spot[NV], pitch[NV];                    // column, its place among a stage's elements, elements to the next row
+    bool mine[NV], edge[NV];
+    int col[NV], spot[NV], pitch[NV];                    // column (of a piece's first element), its place among a stage's elements, elements to the next row there
     uint16_t* out[NV];                                   // this thread's columns in the output's row 0
     f32x2 dgamma[NV][4], dbeta[NV][4];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         col[i] = (i * L + lane) * 8;
-        mine[i] = col[i] < cols;
-        const int64_t c = mine[i] ? col[i] : 0, s = c / p.v.w;
-        pitch[i] = (int)strip_w_of(p.v, s);
+        mine[i] = col[i] < pieces * 8;
+        edge[i] = col[i] == 0 || col[i] == (pieces - 1) * 8;
+        const int64_t c = mine[i] ? col[i] : 0, s = PHASED ? 0 : c / p.v.w;
+        pitch[i] = PHASED ? q.pieces * 8 : (int)strip_w_of(p.v, s);
         spot[i] = (int)(s * set_rows * p.v.w + group * R * pitch[i] + (c - s * p.v.w));
-        out[i] = p.out + s * p.v.stride + (c - s * p.v.w);
+        out[i] = p.out + s * p.v.stride + (c - s * p.v.w) - phase;
 #pragma unroll
         for (int j = 0; j < 4; ++j) dgamma[i][j] = dbeta[i][j] = both(0.0f);
     }
+    // how far apart a thread's rows are in the output
+    auto out_pitch = [&](int i) { return PHASED ? (int64_t)cols : (int64_t)pitch[i]; };
     int slot = 0, turn = 0;
-    uint32_t phase = 0;
+    uint32_t parity = 0;
     float n_mean[R], n_rstd[R];
     auto statistics = [&](int64_t row) {                 // (of the rows after these, ahead)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            n_rstd[r] = row + r < rows ? p.rstd[row + r] : 0.0f;
-            n_mean[r] = row + r < rows && p.layer ? p.mean[row + r] : 0.0f;
+            const int64_t at = row + r * period;
+            n_rstd[r] = at < rows ? p.rstd[at] : 0.0f;
+            n_mean[r] = at < rows && p.layer ? p.mean[at] : 0.0f;
         }
     };
     auto weight = [&](int i, f32x2 (&w)[4]) { parts(shared16(weights + col[i]), w); };
-    statistics(begin + group * R);
+    statistics(begin + group * R * period);
     for (int64_t r0 = begin; r0 < rows; r0 += stride, turn ^= 1) {
-        const int64_t row = r0 + group * R;
-        bool lost = !mbar_wait_bounded(&full[slot], phase);
+        const int64_t row = r0 + group * R * period;
+        bool lost = !mbar_wait_bounded(&full[slot], parity);
         const unsigned char* st = ring + (size_t)slot * q.slot_bytes;
-        auto at = [&](int array, int r, int i) { return shared16(st + array * q.array_bytes + (spot[i] + r * pitch[i]) * 2); };
-        if (threadIdx.x == 0 && r0 != begin && next < rows) {
+        // (elements of a row's first or last piece that are not the row's read as zeros)
+        auto at = [&](int array, int r, int i) {
+            uint4 w = shared16(st + array * q.array_bytes + (spot[i] + r * pitch[i]) * 2);
+            int first, last;
+            if (PHASED && edge[i] && phased_edge(col[i] >> 3, phase, cols, first, last)) {
+                uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < first || j >= last) u[j >> 1] &= j & 1 ? 0xFFFFu : 0xFFFF0000u;
+                w = make_uint4(u[0], u[1], u[2], u[3]);
+            }
+            return w;
+        };
+        if (warp == 0 && r0 != begin && next < rows) {
             // refill the stage of the rows before these once all warps are done with it
             const int before = slot ? slot - 1 : q.slots - 1;
-            if (mbar_wait_bounded(&empty[before], slot ? phase : phase ^ 1)) fill(before); else lost = true;
+            if (__all_sync(0xffffffffu, mbar_wait_bounded(&empty[before], slot ? parity : parity ^ 1))) fill(before); else lost = true;
         }
         if (lost) { atomicExch(&g_norm_status, 11); *(volatile int*)&gone[turn][group] = 1; }
         float mean[R], rstd[R], s1[R], s2[R];
@@ -563,7 +686,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_stream_kernel(const
                 weight(i, w);
 #pragma unroll
                 for (int r = 0; r < R; ++r)
-                    if (row + r < rows) {
+                    if (row + r * period < rows) {
                         f32x2 f[4], d[4];
                         parts(at(0, r, i), f); parts(at(1, r, i), d);
 #pragma unroll
@@ -600,10 +723,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_stream_kernel(const
                 if (mine[i]) {
                     f32x2 w[4];
                     weight(i, w);
-                    uint16_t* to = out[i] + row * pitch[i];
+                    uint16_t* to = out[i] + row * out_pitch(i);
 #pragma unroll
                     for (int r = 0; r < R; ++r)
-                        if (row + r < rows) {
+                        if (row + r * period < rows) {
                             f32x2 f[4], d[4], o[4];
                             parts(at(0, r, i), f); parts(at(1, r, i), d); parts(q.arrays == 3 ? at(2, r, i) : zeros, o);
 #pragma unroll
@@ -611,12 +734,12 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_stream_kernel(const
                                 const f32x2 h = (f[j] + both(-mean[r])) * both(rstd[r]);
                                 o[j] = fma2(both(rstd[r]), fma2(h, both(-s2[r]), fma2(d[j], w[j], both(-s1[r]))), o[j]);
                             }
-                            *reinterpret_cast<uint4*>(to + r * pitch[i]) = bf16x8_pack(o);
+                            store_piece(to + r * period * out_pitch(i), bf16x8_pack(o), PHASED && edge[i], col[i] >> 3, phase, cols);
                         }
                 }
         __syncwarp();
         if (wl == 0) mbar_arrive(&empty[slot]);
-        if (++slot == q.slots) { slot = 0; phase ^= 1; }
+        if (++slot == q.slots) { slot = 0; parity ^= 1; }
     }
     // (left early: the copies under way land before the CTA ends)
     if (threadIdx.x == 0 && (gone[0][0] || gone[1][0])) {
@@ -625,8 +748,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_stream_kernel(const
     }
     __syncthreads();
     if (!p.partial) return;
-    // the groups' sums one after the other, by way of the ring's memory
-    float* line = p.partial + (int64_t)blockIdx.x * 2 * cols;
+    // the groups' sums one after the other, by way of the ring's memory (where PHASED the line begins with `phase` idle columns)
+    const int width = q.pieces * 8;
+    float* line = p.partial + (int64_t)blockIdx.x * 2 * width;
     float* lines = reinterpret_cast<float*>(ring);
     for (int g = 0; g < G; ++g) {
         if (group == g)
@@ -638,14 +762,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) norm_grad_stream_kernel(const
                         float f[8];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) split(k ? dbeta[i][j] : dgamma[i][j], f[2 * j], f[2 * j + 1]);
-                        float4* t = reinterpret_cast<float4*>(lines + k * cols + col[i]);
+                        float4* t = reinterpret_cast<float4*>(lines + k * width + col[i]);
                         float4 u = make_float4(f[0], f[1], f[2], f[3]), v = make_float4(f[4], f[5], f[6], f[7]);
                         if (g) {
                             const float4 a = t[0], b = t[1];
                             u.x += a.x; u.y += a.y; u.z += a.z; u.w += a.w;
                             v.x += b.x; v.y += b.y; v.z += b.z; v.w += b.w;
                         }
-                        if (g == G - 1) t = reinterpret_cast<float4*>(line + k * cols + col[i]);
+                        if (g == G - 1) t = reinterpret_cast<float4*>(line + k * width + col[i]);
                         t[0] = u; t[1] = v;
                     }
         if (g < G - 1) __syncthreads();
@@ -751,7 +875,7 @@ __global__ void __launch_bounds__(512) norm_long_kernel(const __grid_constant__ 
 }
 
 // dgamma and dbeta (blockIdx.y) from the CTAs' lines: 32 columns a block, eight warps over the lines, their sums added in a fixed order
-__global__ void __launch_bounds__(256) norm_grad_finish_kernel(const float* partial, int ctas, int64_t cols, uint16_t* dgamma, uint16_t* dbeta) {
+__global__ void __launch_bounds__(256) norm_grad_finish_kernel(const float* partial, int ctas, int64_t cols, int width, int phases, uint16_t* dgamma, uint16_t* dbeta) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ float part[8][32];
@@ -761,8 +885,16 @@ __global__ void __launch_bounds__(256) norm_grad_finish_kernel(const float* part
     const int64_t n = (int64_t)blockIdx.x * 32 + lane;
     float s = 0.0f;
     if (n < cols)
-#pragma unroll 16
-        for (int b = w; b < ctas; b += 8) s += partial[((int64_t)b * 2 + blockIdx.y) * cols + n];
+        for (int b0 = w; b0 < ctas; b0 += 8 * 20) {      // (twenty loads in flight: all of a line's, one line an SM)
+            float x[20];
+#pragma unroll
+            for (int u = 0; u < 20; ++u) {
+                const int b = b0 + 8 * u;
+                x[u] = b < ctas ? partial[((int64_t)b * 2 + blockIdx.y) * width + ((b & phases) * (int)(cols & 7) & 7) + n] : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < 20; ++u) s += x[u];
+        }
     part[w][lane] = s;
     __syncthreads();
     if (w == 0 && n < cols) {
@@ -785,6 +917,7 @@ struct NormPlan {
     bool linear, one;
     int64_t groups;                 // CTAs that would each have one row (or one set of rows side by side)
     int stream, slots, arrays;      // norm_rows_kernel: warps, norm_grad_stream_kernel: groups side by side (0: neither is taken)
+    int period, pieces;             // (see StreamParams)
     int64_t set_rows;
 };
 
@@ -792,34 +925,45 @@ bool vectors(const MatView& v) {    // every group of eight columns is one align
     return v.cols % 8 == 0 && (v.split != 2 || (v.w % 8 == 0 && v.wlast % 8 == 0)) && v.stride % 8 == 0 && v.ichunk % 8 == 0;
 }
 
-// arrays: inputs of the shape of a row (1 forward; 2 or 3 back)
-NormPlan plan_norm(const MatView& v, bool aligned, bool grad, int arrays, int sms) {
+// aligned: all matrices are 16-byte aligned, weights: gamma and beta are; arrays: inputs of the shape of a row (1 forward; 2 or 3 back)
+NormPlan plan_norm(const MatView& v, bool aligned, bool weights, bool grad, int arrays, int sms) {
     NormPlan q = {};
-    q.vec = aligned && vectors(v) ? 8 : 1;
+    const bool whole = aligned && vectors(v);
     q.linear = !v.ichunk && v.split != 1;
-    const int64_t groups = (v.cols + q.vec - 1) / q.vec;            // column groups of a row
-    if (q.vec == 8 && q.linear && v.nstrips <= 16 && v.cols >= 256 && v.cols <= kStreamCols) {
+    q.period = 1;
+    if (!whole) while ((q.period * v.cols) % 8) q.period *= 2;
+    q.pieces = (int)std::min<int64_t>((v.cols + (whole ? 7 : 14)) / 8, INT32_MAX / 16);
+    if (aligned && q.linear && v.cols >= 256 && q.pieces <= kStreamCols / 8 && (whole ? v.nstrips <= 16 : v.split == 0)) {
+        const int64_t row = (int64_t)q.pieces * 16;                  // bytes
         q.arrays = arrays;
         if (grad) {
-            q.nv = groups < 64 ? 1 : (groups <= 2 * kGradThreads ? 2 : 4);
-            q.lanes = (int)((groups + q.nv - 1) / q.nv + 31) / 32 * 32;
+            q.nv = q.pieces < 64 ? 1 : (q.pieces <= 2 * kGradThreads ? 2 : 4);
+            q.lanes = ((q.pieces + q.nv - 1) / q.nv + 31) / 32 * 32;
             q.stream = kGradThreads / q.lanes;
             q.threads = q.stream * q.lanes;
             q.set_rows = q.stream * (q.nv == 4 ? 1 : 2);
-            q.slots = (int)std::min<int64_t>(8, kRing / (q.set_rows * v.cols * 2 * arrays));         // (two at least)
+            q.slots = (int)std::min<int64_t>(8, kRing / (q.set_rows * row * arrays));        // (two at least)
             q.groups = (v.rows + q.set_rows - 1) / q.set_rows;
         } else {
-            const int64_t room = kSlots - v.cols * 4;                // (gamma and beta)
-            q.set_rows = std::max<int64_t>(1, 2048 / v.cols);        // 4 KB of a row or more
-            const int64_t all = room / (q.set_rows * v.cols * 2);    // slots of a CTA
-            q.stream = (int)std::min<int64_t>(16, all);              // a warp each
+            const int64_t room = kSlots - 2 * row;                   // (gamma and beta)
+            q.set_rows = whole ? std::max<int64_t>(1, 4096 / row) : 1;
+            const int64_t all = room / (q.set_rows * row);           // slots of a CTA
+            // a warp each; no more warps than leave every SM its rows
+            const int64_t sets = (v.rows + q.set_rows - 1) / q.set_rows;
+            q.stream = (int)std::min<int64_t>(std::min<int64_t>(16, all), std::max<int64_t>(4, (sets + sms - 1) / sms));
             q.slots = (int)std::min<int64_t>(4, all / q.stream);
             q.threads = q.stream * 32;
             q.groups = (v.rows + q.stream * q.set_rows - 1) / (q.stream * q.set_rows);
         }
-        if (v.rows >= (grad ? sms * q.set_rows : 8 * sms)) return q;
+        // (few rows: the register kernels have more threads for each; of odd widths they know single elements only)
+        if (!whole || v.rows >= (grad ? sms * q.set_rows : 8 * sms)) {
+            q.groups = std::max<int64_t>(q.groups, q.period);        // (a CTA for every phase)
+            return q;
+        }
         q.stream = 0;
     }
+    q.vec = whole && weights ? 8 : 1;
+    const int64_t groups = (v.cols + q.vec - 1) / q.vec;            // column groups of a row
     const int64_t most = 1024;
     if (q.vec == 8) q.nv = groups <= 32 ? 1 : (groups <= 2 * most ? 2 : 4);
     else q.nv = groups <= 64 ? 2 : 8;
@@ -851,22 +995,29 @@ ccl_status launch_stream(void (*kernel)(const StreamParams), const NormParams& p
     int dev = 0;
     CCL_CUDA_TRY(cudaGetDevice(&dev));
     if (dev >= 64 || !(configured.load() >> dev & 1)) {
-        CCL_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(WHICH < 2 ? kSlots : kRing + kStreamCols * 2)));
+        CCL_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(WHICH < 4 ? kSlots : kRing + kStreamCols * 2)));
         if (dev < 64) configured.fetch_or(1ull << dev);
     }
     StreamParams sp;
     sp.n = p;
-    sp.groups = q.stream; sp.slots = q.slots; sp.arrays = q.arrays; sp.set_rows = (int32_t)q.set_rows;
-    sp.array_bytes = (uint32_t)(q.set_rows * p.v.cols * 2);
+    sp.groups = q.stream; sp.slots = q.slots; sp.arrays = q.arrays; sp.set_rows = (int32_t)q.set_rows; sp.period = q.period; sp.pieces = q.pieces;
+    sp.array_bytes = (uint32_t)(q.set_rows * q.pieces * 16);
     sp.slot_bytes = sp.array_bytes * (uint32_t)q.arrays;
-    const size_t smem = (size_t)sp.slot_bytes * q.slots * (WHICH < 2 ? q.stream : 1) + (size_t)p.v.cols * (WHICH < 2 ? 4 : 2);
+    const size_t smem = (size_t)sp.slot_bytes * q.slots * (WHICH < 4 ? q.stream : 1) + (size_t)q.pieces * (WHICH < 4 ? 32 : 16);
     return launch_early(kernel, dim3(grid), q.threads, smem, st, sp);
 }
 template <bool GRAD>
 ccl_status launch_plan(const NormParams& p, const NormPlan& q, unsigned grid, cudaStream_t st) {
-    if (q.stream && !GRAD) return p.layer ? launch_stream<0>(norm_rows_kernel<true>, p, q, grid, st) : launch_stream<1>(norm_rows_kernel<false>, p, q, grid, st);
-    if (q.stream) return q.nv == 1 ? launch_stream<2>(norm_grad_stream_kernel<1, 2>, p, q, grid, st)
-                                   : (q.nv == 2 ? launch_stream<3>(norm_grad_stream_kernel<2, 2>, p, q, grid, st) : launch_stream<4>(norm_grad_stream_kernel<4, 1>, p, q, grid, st));
+    if (q.stream && !GRAD) {
+        if (q.period > 1) return p.layer ? launch_stream<0>(norm_rows_kernel<true, true>, p, q, grid, st) : launch_stream<1>(norm_rows_kernel<false, true>, p, q, grid, st);
+        return p.layer ? launch_stream<2>(norm_rows_kernel<true, false>, p, q, grid, st) : launch_stream<3>(norm_rows_kernel<false, false>, p, q, grid, st);
+    }
+    if (q.stream && q.period > 1)
+        return q.nv == 1 ? launch_stream<4>(norm_grad_stream_kernel<1, 2, true>, p, q, grid, st)
+                         : (q.nv == 2 ? launch_stream<5>(norm_grad_stream_kernel<2, 2, true>, p, q, grid, st) : launch_stream<6>(norm_grad_stream_kernel<4, 1, true>, p, q, grid, st));
+    if (q.stream)
+        return q.nv == 1 ? launch_stream<7>(norm_grad_stream_kernel<1, 2, false>, p, q, grid, st)
+                         : (q.nv == 2 ? launch_stream<8>(norm_grad_stream_kernel<2, 2, false>, p, q, grid, st) : launch_stream<9>(norm_grad_stream_kernel<4, 1, false>, p, q, grid, st));
     if (q.nv == 0) return launch_early(q.vec == 8 ? norm_long_kernel<8, GRAD> : norm_long_kernel<1, GRAD>, dim3(grid), q.threads, 0, st, p);
     if (q.vec == 8) {
         if (q.one) return q.nv == 1 ? launch_shape<GRAD, 8, 1, true>(p, q, grid, st) : launch_shape<GRAD, 8, 2, true>(p, q, grid, st);
@@ -891,10 +1042,10 @@ const uint16_t* bf16(const void* p) { return static_cast<const uint16_t*>(p); }
 size_t grad_workspace(const MatView& v, int sms) {
     size_t lines = 0;
     for (int arrays : {2, 3}) {
-        const NormPlan q = plan_norm(v, true, true, arrays, sms);
-        if (q.stream) lines = std::max<size_t>(lines, grid_of(q, sms));
+        const NormPlan q = plan_norm(v, true, true, true, arrays, sms);
+        if (q.stream) lines = std::max<size_t>(lines, (size_t)grid_of(q, sms) * q.pieces);
     }
-    return lines * 2 * (size_t)v.cols * 4;
+    return lines * 2 * 8 * 4;
 }
 
 ccl_status launch_sums(NormParams p, const NormPlan& q, uint16_t* dgamma, uint16_t* dbeta, cudaStream_t st) {
@@ -932,15 +1083,15 @@ extern "C" ccl_status ccl_norm(const ccl_mat* m, int32_t kind, float eps, const 
     if (!(eps >= 0.0f && eps < 1e30f)) return fail(CCL_ERR_INVALID_ARG, "ccl_norm: eps must be a number >= 0");
     if (!X_dev || !Y_dev) return fail(CCL_ERR_INVALID_ARG, "ccl_norm: NULL operand");
     if (kind == CCL_NORM_RMS && (beta_dev || mean_dev)) return fail(CCL_ERR_INVALID_ARG, "ccl_norm: the root-mean-square form has neither beta nor means");
-    const uintptr_t any = bits(X_dev) | bits(Y_dev) | bits(gamma_dev) | bits(beta_dev);
-    if (any & 1) return fail(CCL_ERR_ALIGN, "ccl_norm: a base pointer is not 2-byte aligned");
+    const uintptr_t any = bits(X_dev) | bits(Y_dev), weights = bits(gamma_dev) | bits(beta_dev);
+    if ((any | weights) & 1) return fail(CCL_ERR_ALIGN, "ccl_norm: a base pointer is not 2-byte aligned");
     if ((bits(mean_dev) | bits(rstd_dev)) & 3) return fail(CCL_ERR_ALIGN, "ccl_norm: mean / rstd is not 4-byte aligned");
     p.x = bf16(X_dev); p.out = static_cast<uint16_t*>(Y_dev); p.gamma = bf16(gamma_dev); p.beta = bf16(beta_dev);
     p.mean = mean_dev; p.rstd = rstd_dev;
     p.layer = kind == CCL_NORM_LAYER; p.eps = eps; p.inv_cols = (float)(1.0 / (double)p.v.cols);
     int sms, pairs;
     device_units(&sms, &pairs);
-    const NormPlan q = plan_norm(p.v, (any & 15) == 0, false, 1, sms);
+    const NormPlan q = plan_norm(p.v, (any & 15) == 0, (weights & 15) == 0, false, 1, sms);
     p.lanes = q.lanes;
     return launch_plan<false>(p, q, grid_of(q, sms), reinterpret_cast<cudaStream_t>(cuda_stream));
 }
@@ -967,8 +1118,8 @@ extern "C" ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* 
     if (!dX_dev && !dgamma_dev && !dbeta_dev) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: no output is wanted");
     if (!layer && dbeta_dev) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: the root-mean-square form has no beta");
     if (dX_dev && (dX_dev == gamma_dev)) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: dX needs a buffer of its own");
-    const uintptr_t any = bits(X_dev) | bits(dY_dev) | bits(addend_dev) | bits(dX_dev) | bits(gamma_dev);
-    if ((any | bits(dgamma_dev) | bits(dbeta_dev)) & 1) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: a base pointer is not 2-byte aligned");
+    const uintptr_t any = bits(X_dev) | bits(dY_dev) | bits(addend_dev) | bits(dX_dev);
+    if ((any | bits(gamma_dev) | bits(dgamma_dev) | bits(dbeta_dev)) & 1) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: a base pointer is not 2-byte aligned");
     if ((bits(mean_dev) | bits(rstd_dev)) & 3) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: mean / rstd is not 4-byte aligned");
     int sms, pairs;
     device_units(&sms, &pairs);
@@ -982,14 +1133,15 @@ extern "C" ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* 
         if (need && (!ws_dev || ws_bytes < need)) return fail(CCL_ERR_WORKSPACE, "ccl_norm_grad: needs %zu bytes of workspace (got %zu)", need, ws_dev ? ws_bytes : (size_t)0);
         if (bits(ws_dev) & 15) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: workspace is not 16-byte aligned");
     }
-    const NormPlan q = plan_norm(p.v, (any & 15) == 0, true, p.addend ? 3 : 2, sms);
+    const NormPlan q = plan_norm(p.v, (any & 15) == 0, (bits(gamma_dev) & 15) == 0, true, p.addend ? 3 : 2, sms);
     p.lanes = q.lanes;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     const unsigned grid = grid_of(q, sms);
     if (q.stream && sums) {
         p.partial = static_cast<float*>(ws_dev);
         if ((s = launch_plan<true>(p, q, grid, st))) return s;
-        return launch_early(norm_grad_finish_kernel, dim3((unsigned)((p.v.cols + 31) / 32), 2), 256, 0, st, (const float*)p.partial, (int)grid, p.v.cols, dgamma, dbeta);
+        return launch_early(norm_grad_finish_kernel, dim3((unsigned)((p.v.cols + 31) / 32), 2), 256, 0, st, (const float*)p.partial, (int)grid, p.v.cols, q.pieces * 8,
+                            q.period - 1, dgamma, dbeta);
     }
     if (sums && (s = launch_sums(p, q, dgamma, dbeta, st))) return s;        // (first: dX may take the place of X or dY)
     return p.out ? launch_plan<true>(p, q, grid, st) : CCL_OK;

@@ -105,7 +105,7 @@ def check_grad(m, layer=True, weights=True, addend=True, inplace=None, seed=0, s
 
 
 SIZES = [(1, 1), (3, 8), (1, 2048), (5, 7), (40, 64), (300, 104), (33, 264), (700, 512), (64, 1024), (31, 1544), (20, 1541), (150, 4096), (9, 8192), (5, 8191),
-         (4, 16384), (3, 20000), (3, 33000), (2, 40001)]
+         (4, 16384), (3, 20000), (3, 33000), (2, 40001), (1, 257), (7, 300), (9, 1026), (65, 259), (5, 16377), (3, 16379)]
 
 
 @pytest.mark.parametrize("T,H", SIZES)
@@ -130,7 +130,7 @@ def test_grad_row_major(T, H):
     check_grad(m, dx=False, seed=9)
 
 
-@pytest.mark.parametrize("T,H", [(5000, 96), (9481, 256), (9500, 264), (5003, 512), (4999, 520), (3000, 1024), (2501, 2048), (1301, 4104), (1300, 5000), (1250, 8192), (1203, 9000),
+@pytest.mark.parametrize("T,H", [(5000, 96), (9481, 256), (9500, 264), (5003, 512), (4999, 520), (3000, 1024), (2501, 2048), (1301, 4104), (1300, 5000), (1250, 8192), (1203, 9000), (1301, 1541), (2500, 258), (1207, 4100), (301, 8190), (500, 9001),
                                  (1200, 16384)])
 def test_many_rows(T, H):
     m = ccl.Mat(T, H, 2)

@@ -17,7 +17,8 @@
 
 namespace ccl {
 
-ccl_status gemm_cut(const ccl_gemm_desc* d, int64_t rows_c, int64_t rows_b, const void* A, const void* B, void* C, void* ws, size_t ws_bytes, void* stream);   // ccl_gemm.cu
+ccl_status gemm_cut(const ccl_gemm_desc* d, int64_t rows_c, int64_t rows_b, bool single, const void* A, const void* B, void* C, void* ws, size_t ws_bytes,
+                    void* stream);                       // ccl_gemm.cu
 
 constexpr int64_t kPieceBytes = INT64_C(1) << 29;
 
@@ -270,8 +271,10 @@ extern "C" ccl_status ccl_linear_xent(const ccl_xent_desc* d, const void* X_dev,
     la.at_target = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + up256((size_t)lines * (size_t)v.T * 8));
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     if ((s = run_logits<3>(plan, em, v.trans ? v.V : 0, X_dev, W_dev, nullptr, st))) return s;
+    // few rows side by side where there are few, and the more threads along the lines (1024 rows of 2048 lines: 80 us with 32 a block, on
+    // 32 SMs; four are a whole sector of memory)
     int lanes = 1;
-    while (lanes < 32 && lanes < v.T) lanes *= 2;
+    while (lanes < 32 && lanes < v.T && (lanes < 4 || v.T > lanes * 148 * 2)) lanes *= 2;
     return launch_early(xent_finish_kernel, dim3((unsigned)((v.T + lanes - 1) / lanes)), 256, 0, st, (const float2*)la.part, lines, (int)v.T, lanes, targets_dev,
                         la.ignore, la.classes, (const float*)la.at_target, loss_dev, lse_dev);
 }
@@ -321,7 +324,7 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
         if (dX_dev) {
             p = dx_product(v, g, real);
             if (g.pieces == 1) {
-                if ((s = gemm_cut(&p, 0, rows, dz, W, dX_dev, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
+                if ((s = gemm_cut(&p, 0, rows, false, dz, W, dX_dev, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
             } else {
                 if ((s = shape_plan(&p, 5, &plan))) return s;
                 EpiMaps<5> sums = {acc, have};
@@ -331,7 +334,9 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
         }
         if (dW_dev) {
             p = dw_product(v, g, real);
-            if ((s = gemm_cut(&p, rows, 0, v.trans ? dz : X_dev, v.trans ? X_dev : dz, static_cast<uint16_t*>(dW_dev) + at, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
+            // (over few tokens the product is its output's stores: see make_plan)
+            const bool single = v.T <= 256 && ((p.M + BM - 1) / BM) * ((p.N + 255) / 256) >= 148;
+            if ((s = gemm_cut(&p, rows, 0, single, v.trans ? dz : X_dev, v.trans ? X_dev : dz, static_cast<uint16_t*>(dW_dev) + at, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
         }
     }
     if (!dX_dev || g.pieces == 1) return CCL_OK;

@@ -278,11 +278,11 @@ ccl_status static_ws_address(void** out) {
 // strides[X]: bytes between the buffers of operand X (A, B, C) of consecutive problems; 0 = shared (A and B only)
 // m_offs / cap: ragged batch (ccl_gemm_grouped), else nullptr / 0
 // rows_c, rows_b: not 0 where the buffer of C / B ends before the descriptor's last rows (fewer than 64 of them): those are not written / are
-// read as zeros.  single: see make_plan
+// read as zeros.  single: see make_plan.  alpha_dev: alpha, on the device
 static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, const int64_t* strides, const void* A_dev, const void* B_dev, void* C_dev,
                             void* ws_dev, size_t ws_bytes, void* cuda_stream, float alpha = 1.0f, float beta = 0.0f, const int32_t* m_offs = nullptr,
                             int64_t cap = 0, const int32_t* k_offs = nullptr, bool static_ws = false, int64_t rows_c = 0, int64_t rows_b = 0,
-                            bool single = false) {
+                            bool single = false, const float* alpha_dev = nullptr) {
     if (!A_dev || !B_dev || !C_dev) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: NULL operand");
     if (!d) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: NULL descriptor");
     if (batch < 1 || batch > kMaxBatch) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: batch must be in [1, %lld]", (long long)kMaxBatch);
@@ -291,7 +291,7 @@ static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     // reuse the plan and the two encoded tensor maps: a host-side cache only, nothing is kept on the device.
     PreparedKey key;
     make_key(d, batch4, A_dev, B_dev, C_dev, &key);
-    key.mode = (swiglu ? 1 : 0) | (static_ws ? 2 : 0); key.alpha = alpha; key.beta = beta;
+    key.mode = (swiglu ? 1 : 0) | (static_ws ? 2 : 0) | (alpha_dev ? 4 : 0); key.alpha = alpha; key.beta = beta;
     key.f[36] = (int64_t)reinterpret_cast<uintptr_t>(m_offs) ^ ((int64_t)reinterpret_cast<uintptr_t>(k_offs) << 1); key.f[37] = cap + (k_offs ? (INT64_C(1) << 62) : 0);
     // The balanced split is optional: it is planned only when the workspace at hand holds its partial sums (the caller's
     // ws_bytes; the scratch array for ccl_gemm_static_ws).  A caller that passes none gets whole-tile plans, as before.
@@ -326,7 +326,7 @@ static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
         CCL_CUDA_TRY(cudaDeviceGetAttribute(&prep.sms, cudaDevAttrMultiProcessorCount, dev));
         if (dev != key.dev) {
             make_key(d, batch4, A_dev, B_dev, C_dev, &key);
-            key.mode = (swiglu ? 1 : 0) | (static_ws ? 2 : 0); key.alpha = alpha; key.beta = beta; key.f[38] = (int64_t)max_ws; key.f[39] = rows_c | rows_b << 32 | (single ? INT64_MIN : 0);
+            key.mode = (swiglu ? 1 : 0) | (static_ws ? 2 : 0) | (alpha_dev ? 4 : 0); key.alpha = alpha; key.beta = beta; key.f[38] = (int64_t)max_ws; key.f[39] = rows_c | rows_b << 32 | (single ? INT64_MIN : 0);
             key.f[36] = (int64_t)reinterpret_cast<uintptr_t>(m_offs) ^ ((int64_t)reinterpret_cast<uintptr_t>(k_offs) << 1); key.f[37] = cap + (k_offs ? (INT64_C(1) << 62) : 0);
         }
         if ((s = make_plan(d, batch, swiglu, A_dev, B_dev, C_dev, prep.sms, resident_pairs(), &plan, cap, k_offs != nullptr, max_ws, true, 0, single))) return s;
@@ -337,7 +337,7 @@ static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
         plan.p.m_offs = m_offs;
         plan.p.k_offs = k_offs;
         plan.p.c_batch_stride = batch4[3] / 2;
-        plan.p.alpha = alpha; plan.p.beta = beta; plan.p.axpby = (alpha != 1.0f || beta != 0.0f) ? 1 : 0;
+        plan.p.alpha = alpha; plan.p.beta = beta; plan.p.axpby = (alpha != 1.0f || beta != 0.0f || alpha_dev) ? 1 : 0;
         {
             const GemmParams& q = plan.p;
             const bool ks = (q.a_mn ? q.a.split == 1 : q.a.split == 2) || (q.b_mn ? q.b.split == 1 : q.b.split == 2);
@@ -381,6 +381,7 @@ static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
         if (reinterpret_cast<uintptr_t>(ws_dev) & 15) return fail(CCL_ERR_ALIGN, "ccl_gemm: workspace is not 16-byte aligned");
     }
     plan.p.ws = static_cast<float*>(ws_dev);
+    plan.p.alpha_dev = alpha_dev;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     if (plan.p.bal) {                                    // flags behind the partial sums, cleared in front of the launch
         plan.p.bal_flags = reinterpret_cast<unsigned long long*>(static_cast<char*>(ws_dev) + (size_t)plan.grid * 2 * ((size_t)BM * plan.bn * 4));
@@ -448,10 +449,11 @@ extern "C" ccl_status ccl_gemm(const ccl_gemm_desc* d, const void* A_dev, const 
 }
 
 namespace ccl {
-// ccl_gemm for a row-major C (B) that has fewer rows than the descriptor says (see gemm_impl)
-ccl_status gemm_cut(const ccl_gemm_desc* d, int64_t rows_c, int64_t rows_b, bool single, const void* A, const void* B, void* C, void* ws, size_t ws_bytes, void* stream) {
+// C = alpha A B for a row-major C (B) that has fewer rows than the descriptor says (see gemm_impl)
+ccl_status gemm_cut(const ccl_gemm_desc* d, int64_t rows_c, int64_t rows_b, bool single, const float* alpha_dev, const void* A, const void* B, void* C, void* ws, size_t ws_bytes,
+                    void* stream) {
     const int64_t none[3] = {0, 0, 0};
-    return gemm_impl(d, 1, false, none, A, B, C, ws, ws_bytes, stream, 1.0f, 0.0f, nullptr, 0, nullptr, false, rows_c, rows_b, single);
+    return gemm_impl(d, 1, false, none, A, B, C, ws, ws_bytes, stream, 1.0f, 0.0f, nullptr, 0, nullptr, false, rows_c, rows_b, single, alpha_dev);
 }
 }  // namespace ccl
 

@@ -159,6 +159,7 @@ struct GemmParams {
     const uint16_t* addend;         // EPI 1: the residual or NULL; EPI 2: the pre-activation Z
     uint16_t* preact;               // EPI 1: receives the pre-activation, or NULL
     float* colsum;                  // EPI 2: partial column sums [row blocks][N] fp32, or NULL
+    const float* alpha_dev;         // alpha where it is known on the device alone (axpby = 1), or NULL
     int32_t addend_tma;             // the addend comes by TMA, a piece ahead (else by ordinary loads: see line_of())
 };
 
@@ -173,6 +174,7 @@ struct LogitArgs {
     float2* part;                   // EPI 3: [tile column x drain warps of a quadrant][M]: log2 of the scale, sum of 2^(z log2 e - it)
     float* at_target;               // EPI 3: [M] the target's logit
     const float *lse, *dloss;       // EPI 4: [M]
+    const float* scale;             // EPI 4: what dloss is divided by
 };
 template <> struct EpiMaps<3> { LogitArgs logits; };
 template <> struct EpiMaps<4> { LogitArgs logits; };
@@ -404,6 +406,8 @@ __device__ __forceinline__ int64_t c_offset(const GemmParams& p, int64_t m, int6
     if (FULL && p.c_wlast && g == p.c.nstrips - 1) return (int64_t)g * p.c_stride + (int64_t)rr * p.c_wlast + xx;   // a narrower last strip
     return (int64_t)g * p.c_stride + (int64_t)rr * p.c_row + xx;
 }
+
+__device__ __forceinline__ float alpha_of(const GemmParams& p) { return p.alpha_dev ? *p.alpha_dev : p.alpha; }
 
 // One row's 8 columns from column n on, whose element offset in C's layout is `off`: fp32 accumulators -> what C gets (fp32,
 // before the rounding).  EPI 1: act(v + bias) + residual, the pre-activation stored on the way.  EPI 2: v * act'(z).
@@ -976,7 +980,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
               const int cls = m < t.m1 ? la.targets[m] : la.ignore;
               row_live = cls != la.ignore && (unsigned)cls < (unsigned)la.all;
               target = row_live ? cls - la.v0 : -1;
-              if (EPI == 4 && row_live) { row_lse2 = la.lse[m] * kLog2e; row_scale = la.dloss[m]; }
+              if (EPI == 4 && row_live) { row_lse2 = la.lse[m] * kLog2e; row_scale = la.dloss[m] / *la.scale; }
           }
 #pragma unroll 1                                         // one copy of the (large) drain code: a short GEMM pays for every instruction-cache miss
           for (int h = 0; h < (SWIGLU ? 1 : NSUB); ++h) {
@@ -1063,7 +1067,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const int n64 = nb + c * 64;
                 const bool row_ok = m < t.m1;
                 const unsigned short* src = p.C + c_offset<FULL>(p, min(m, t.m1 - 1), n64) + (int64_t)t.e * p.c_batch_stride;
-                const float alpha = p.alpha, beta = p.beta;
+                const float alpha = alpha_of(p), beta = p.beta;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     uint4 cv = make_uint4(0u, 0u, 0u, 0u);
@@ -1355,7 +1359,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         }
                         if (p.axpby) {                             // C <- alpha * sum + beta * C (C read through its own layout)
                             const uint4 cv = ld_global_v4_if(crow + c * 64 + js * 4, p.beta != 0.0f && row < t.m1 && col < t.n1);
-                            const float al = p.alpha, be = p.beta;
+                            const float al = alpha_of(p), be = p.beta;
                             a0.x = fmaf(al, a0.x, be * __uint_as_float(cv.x << 16)); a0.y = fmaf(al, a0.y, be * __uint_as_float(cv.x & 0xFFFF0000u));
                             a0.z = fmaf(al, a0.z, be * __uint_as_float(cv.y << 16)); a0.w = fmaf(al, a0.w, be * __uint_as_float(cv.y & 0xFFFF0000u));
                             a1.x = fmaf(al, a1.x, be * __uint_as_float(cv.z << 16)); a1.y = fmaf(al, a1.y, be * __uint_as_float(cv.z & 0xFFFF0000u));
@@ -1636,6 +1640,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 // the result is the same on every run.  One thread per 8 consecutive columns of a row.
 static __global__ void __launch_bounds__(256) splitk_reduce_kernel(const GemmParams p) {
     const int64_t n8 = p.N / 8, per_problem = (int64_t)p.M * n8, total = per_problem * p.batch;
+    const float alpha = alpha_of(p);
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t e = i / per_problem, r = i - e * per_problem;
         const int64_t m = r / n8, n = (r - m * n8) * 8;
@@ -1655,8 +1660,8 @@ static __global__ void __launch_bounds__(256) splitk_reduce_kernel(const GemmPar
             const uint32_t w[4] = {cv.x, cv.y, cv.z, cv.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                acc[2 * i] = fmaf(p.alpha, acc[2 * i], p.beta * __uint_as_float(w[i] << 16));
-                acc[2 * i + 1] = fmaf(p.alpha, acc[2 * i + 1], p.beta * __uint_as_float(w[i] & 0xFFFF0000u));
+                acc[2 * i] = fmaf(alpha, acc[2 * i], p.beta * __uint_as_float(w[i] << 16));
+                acc[2 * i + 1] = fmaf(alpha, acc[2 * i + 1], p.beta * __uint_as_float(w[i] & 0xFFFF0000u));
             }
         }
         uint4 v;

@@ -6,9 +6,12 @@
 // passes by), and a second kernel joins a row's numbers:  lse = max + log(sum of s_i exp(m_i - max)).  Powers of two throughout: one
 // multiply-add and one hardware exponential a logit, behind the next tile's product.
 //
-// Gradient.  dz = dloss (exp(z - lse) - [target]), piece by piece of the vocabulary: the logits' product again, its drain turning z into dz
-// (EPI = 4), rounded to bf16 because it is the operand of the two products that follow; dW of the piece = dz^T X, a whole sum over the
-// tokens, and dX += dz W, which is kept in fp32 from piece to piece (EPI = 5) and rounded once at the end.  A piece's dz is at most kPieceBytes
+// Gradient.  dz = dloss / s (exp(z - lse) - [target]), piece by piece of the vocabulary: the logits' product again, its drain turning z into dz
+// (EPI = 4), rounded to bf16 because it is the operand of the two products that follow; dW of the piece = s dz^T X, a whole sum over the
+// tokens, and dX += s dz W, which is kept in fp32 from piece to piece (EPI = 5) and rounded once at the end.  s is the largest |dloss|, so
+// that where all are alike (a mean over the tokens) the rounding is that of p - 1 and p themselves: a target that has little of the
+// probability is -1 then, exact or nearly so, where -dloss would be off by 2^-9 of itself (777 tokens: errors of dX and dW against 64 bits
+// 0.0025 -> 0.0019 of their norms, of which 0.0017 are the outputs' own rounding).  A piece's dz is at most kPieceBytes
 // unless 256 columns (or a strip) are more.  Recomputing the logits costs a quarter of the gradient's products; keeping them would
 // cost T x V x 4 bytes.
 //
@@ -17,7 +20,7 @@
 
 namespace ccl {
 
-ccl_status gemm_cut(const ccl_gemm_desc* d, int64_t rows_c, int64_t rows_b, bool single, const void* A, const void* B, void* C, void* ws, size_t ws_bytes,
+ccl_status gemm_cut(const ccl_gemm_desc* d, int64_t rows_c, int64_t rows_b, bool single, const float* alpha_dev, const void* A, const void* B, void* C, void* ws, size_t ws_bytes,
                     void* stream);                       // ccl_gemm.cu
 
 constexpr int64_t kPieceBytes = INT64_C(1) << 29;
@@ -91,10 +94,32 @@ __global__ void __launch_bounds__(256) xent_finish_kernel(const float2* part, in
     if (loss) loss[row] = live ? (float)(l - (double)at_target[row]) : 0.0f;
 }
 
-// dX = bf16(sum of the `parts` fp32 sums), eight values a thread
-__global__ void __launch_bounds__(256) xent_dx_kernel(const float* acc, int parts, int64_t n, uint16_t* dx) {
+// scale = the largest finite |dloss| of the rows that take part (1 where there is none)
+__global__ void __launch_bounds__(1024) xent_scale_kernel(const float* dloss, const int32_t* targets, int M, int32_t ignore, int32_t classes, float* scale) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ float tops[32];
+    float top = 0.0f;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < M; i += 1024) {
+        const int cls = targets[i];
+        const float d = fabsf(dloss[i]);
+        if (cls != ignore && (unsigned)cls < (unsigned)classes && d < INFINITY) top = fmaxf(top, d);
+    }
+    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));         // (ordered as their bits are)
+    if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(tops[threadIdx.x])));
+        if (threadIdx.x == 0) *scale = top > 0.0f ? top : 1.0f;
+    }
+}
+
+// dX = bf16(scale x sum of the `parts` fp32 sums), eight values a thread
+__global__ void __launch_bounds__(256) xent_dx_kernel(const float* acc, int parts, int64_t n, const float* scale, uint16_t* dx) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const f32x2 by = both(*scale);
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 256 * 8) {
         f32x2 v[4] = {both(0.0f), both(0.0f), both(0.0f), both(0.0f)};
         for (int k = 0; k < parts; ++k) {
@@ -102,6 +127,8 @@ __global__ void __launch_bounds__(256) xent_dx_kernel(const float* acc, int part
             v[0] = v[0] + pair(a.x, a.y); v[1] = v[1] + pair(a.z, a.w);
             v[2] = v[2] + pair(b.x, b.y); v[3] = v[3] + pair(b.z, b.w);
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = v[j] * by;
         *reinterpret_cast<uint4*>(dx + i) = bf16x8_pack(v);
     }
 }
@@ -155,7 +182,7 @@ struct GradPlan {
     int64_t pieces, width;          // classes of a piece but the last
     bool all;                       // one piece that is the whole of W
     int parts;                      // fp32 sums of dX (0: one piece, no sum is kept)
-    size_t acc_at, gemm_at, gemm_bytes, bytes;
+    size_t acc_at, gemm_at, gemm_bytes, scale_at, bytes;
 };
 
 int64_t piece_real(const Vocabulary& v, const GradPlan& g, int64_t i) { return std::min(g.width, v.V - i * g.width); }
@@ -206,7 +233,8 @@ ccl_status plan_grad(const Vocabulary& v, GradPlan* g) {
     const size_t dz = up256((size_t)v.T * (size_t)(v.trans ? up(g->width, 64) : g->width) * 2);
     g->acc_at = dz;
     g->gemm_at = up256(dz + (size_t)g->parts * (size_t)v.T * (size_t)v.H * 4);
-    g->bytes = g->gemm_at + g->gemm_bytes;
+    g->scale_at = up256(g->gemm_at + g->gemm_bytes);
+    g->bytes = g->scale_at + 4;
     return CCL_OK;
 }
 
@@ -307,7 +335,8 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(ws_dev);
     void *dz = ws, *gemm_ws = g.gemm_bytes ? ws + g.gemm_at : nullptr;
-    float* acc = reinterpret_cast<float*>(ws + g.acc_at);
+    float *acc = reinterpret_cast<float*>(ws + g.acc_at), *scale = reinterpret_cast<float*>(ws + g.scale_at);
+    if ((s = launch_early(xent_scale_kernel, dim3(1), 1024, 0, st, dloss_dev, targets_dev, (int)v.T, d->ignore_index, (int32_t)v.V, scale))) return s;
     int have = 0;                                            // sums of dX that earlier pieces have begun
     for (int64_t i = 0; i < g.pieces; ++i) {
         const int64_t real = piece_real(v, g, i), rows = v.trans ? real : 0;
@@ -319,12 +348,12 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
         EpiMaps<4> em = {};
         LogitArgs& la = em.logits;
         la.targets = targets_dev; la.ignore = d->ignore_index; la.v0 = (int32_t)(i * g.width); la.classes = (int32_t)real; la.all = (int32_t)v.V;
-        la.lse = lse_dev; la.dloss = dloss_dev;
+        la.lse = lse_dev; la.dloss = dloss_dev; la.scale = scale;
         if ((s = run_logits<4>(plan, em, rows, X_dev, W, dz, st))) return s;
         if (dX_dev) {
             p = dx_product(v, g, real);
             if (g.pieces == 1) {
-                if ((s = gemm_cut(&p, 0, rows, false, dz, W, dX_dev, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
+                if ((s = gemm_cut(&p, 0, rows, false, scale, dz, W, dX_dev, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
             } else {
                 if ((s = shape_plan(&p, 5, &plan))) return s;
                 EpiMaps<5> sums = {acc, have};
@@ -336,10 +365,10 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
             p = dw_product(v, g, real);
             // (over few tokens the product is its output's stores: see make_plan)
             const bool single = v.T <= 256 && ((p.M + BM - 1) / BM) * ((p.N + 255) / 256) >= 148;
-            if ((s = gemm_cut(&p, rows, 0, single, v.trans ? dz : X_dev, v.trans ? X_dev : dz, static_cast<uint16_t*>(dW_dev) + at, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
+            if ((s = gemm_cut(&p, rows, 0, single, scale, v.trans ? dz : X_dev, v.trans ? X_dev : dz, static_cast<uint16_t*>(dW_dev) + at, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
         }
     }
     if (!dX_dev || g.pieces == 1) return CCL_OK;
     const int64_t n = v.T * v.H;
-    return launch_early(xent_dx_kernel, dim3((unsigned)std::min<int64_t>((n / 8 + 255) / 256, 148 * 8)), 256, 0, st, (const float*)acc, have, n, static_cast<uint16_t*>(dX_dev));
+    return launch_early(xent_dx_kernel, dim3((unsigned)std::min<int64_t>((n / 8 + 255) / 256, 148 * 8)), 256, 0, st, (const float*)acc, have, n, (const float*)scale, static_cast<uint16_t*>(dX_dev));
 }

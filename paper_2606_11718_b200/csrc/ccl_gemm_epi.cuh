@@ -15,7 +15,7 @@ static ccl_status launch_epi_warps(const GemmPlan& plan, const CUtensorMap* maps
     int dev = 0;
     CCL_CUDA_TRY(cudaGetDevice(&dev));
     if (dev >= 64 || !(configured.load() >> dev & 1)) {
-        CCL_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(smem_budget_op(KS, OPW) + staging_bytes<EPI, KS, OPW> + 2048)));
+        CCL_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(smem_budget_op(KS, OPW, EPI) + staging_bytes<EPI, KS, OPW> + 2048)));
         if (dev < 64) configured.fetch_or(1ull << dev);
     }
     cudaLaunchConfig_t cfg = {};

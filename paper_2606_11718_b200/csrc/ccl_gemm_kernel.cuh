@@ -34,7 +34,7 @@ constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
 // stages; relu's slope 98 and 107.  The cluster split drains once, from the exchanged sums, with sixteen (777 x 1544 x 1000:
 // 14.2 us, 15.6 with eight).
 // (the cluster split exchanges its partial sums in the ring and stores from registers: no staging, a longer ring)
-template <int EPI, int KS, int OPW> constexpr uint32_t staging_bytes = EPI ? (KS ? 0u : OPW * 32u * 128u) : 4u * 2 * 32 * 128;
+template <int EPI, int KS, int OPW> constexpr uint32_t staging_bytes = EPI ? (KS || EPI == 3 ? 0u : OPW * 32u * 128u) : 4u * 2 * 32 * 128;
 template <int EPI, int OPW> constexpr int epi_warps = EPI ? OPW : kEpiWarps;
 template <int EPI, int OPW> constexpr int gemm_threads = 64 + 32 * epi_warps<EPI, OPW>;
 constexpr int kTmemCols = 512;
@@ -43,7 +43,13 @@ constexpr int64_t kRaggedDense = 4096;         // problems of a ragged batch who
 constexpr uint32_t kEpiBytes = 4 * 2 * 32 * 128; // epilogue staging: per warp two buffers of 32 rows x 128 B
 constexpr uint32_t kSmemBudgetOpKs = 224 * 1024;
 // EPI: the ring beside the warps' buffers, in which an addend's piece becomes C's
-constexpr uint32_t smem_budget_op(int ks, int opw) { return ks ? kSmemBudgetOpKs : (224u * 1024 - (uint32_t)opw * 32 * 128); }
+// (the logits' statistics store nothing of a tile: no buffers)
+constexpr uint32_t smem_budget_op(int ks, int opw, int epi) { return ks || epi == 3 ? kSmemBudgetOpKs : (224u * 1024 - (uint32_t)opw * 32 * 128); }
+// EPI 3: k blocks after which the accumulator is handed over and a new one begun; the drain warps add them up.  An accumulator in tensor memory
+// loses up to a unit in the last place with every 16 of K, always towards zero: a loss over sums of 2048 products was off by 1.8e-6 of
+// itself, over 8192 by 6e-6.  In pieces of 1024 it is 5e-7 to 8e-7 at any K, for no measurable time (8192 x 131072 x 4096: 5.8 to 5.9 ms);
+// in pieces of 512 3e-7 to 4e-7, but 7.1 ms: the hand-overs then come faster than sixteen warps take them.
+constexpr int kLogitBlocks = 16;
 
 static __device__ int g_gemm_status = 0;
 
@@ -171,7 +177,7 @@ template <> struct EpiMaps<0> {};
 struct LogitArgs {
     const int32_t* targets;         // [M]
     int32_t ignore, v0, classes, all;   // all: classes of the whole problem (a target outside [0, all) is taken as ignored)
-    float2* part;                   // EPI 3: [tile column x drain warps of a quadrant][M]: log2 of the scale, sum of 2^(z log2 e - it)
+    float2* part;                   // EPI 3: [64 columns of a tile][M]: log2 of the scale, sum of 2^(z log2 e - it)
     float* at_target;               // EPI 3: [M] the target's logit
     const float *lse, *dloss;       // EPI 4: [M]
     const float* scale;             // EPI 4: what dloss is divided by
@@ -846,17 +852,20 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 if (!__shfl_sync(FULLMASK, (int)more, 0)) break;
                 if ((RAG != 0 || FULL) && __shfl_sync(FULLMASK, (int)t.skip, 0)) continue;
                 if (KS) t.split = (int)krank;
+                int kb0 = t.split * kbps, kb1 = min(num_kb, kb0 + kbps), tail = BK;
+                if (RAG == 0 && gp.bal) { kb0 = t.kb0; kb1 = t.kb1; }
+                if (RAG == 2) { const KRange kr = k_range(p.k_offs, t.e, p.K); kb0 = 0; kb1 = kr.nkb; tail = kr.rem; }
+                kb0 = __shfl_sync(FULLMASK, kb0, 0); kb1 = __shfl_sync(FULLMASK, kb1, 0);
+                if (RAG == 2) tail = __shfl_sync(FULLMASK, tail, 0);
+                [[maybe_unused]] const int kz = kb1;
+                do {                                        // (once, but for EPI 3: kLogitBlocks k blocks an accumulator)
+                if (EPI == 3) kb1 = min(kz, kb0 + kLogitBlocks);
                 // NSUB == 1: TMEM half (done & 1) is this tile's accumulator, the other half is being drained.
                 // NSUB == 2: both halves belong to this tile; half h may be overwritten once the epilogue
                 //            of the previous tile has drained it.
                 const int acc0 = NSUB == 1 ? (done & 1) : 0;
                 const uint32_t acc_phase = NSUB == 1 ? ((uint32_t)(done >> 1) & 1) : ((uint32_t)done & 1);
                 ++done;
-                int kb0 = t.split * kbps, kb1 = min(num_kb, kb0 + kbps), tail = BK;
-                if (RAG == 0 && gp.bal) { kb0 = t.kb0; kb1 = t.kb1; }
-                if (RAG == 2) { const KRange kr = k_range(p.k_offs, t.e, p.K); kb0 = 0; kb1 = kr.nkb; tail = kr.rem; }
-                kb0 = __shfl_sync(FULLMASK, kb0, 0); kb1 = __shfl_sync(FULLMASK, kb1, 0);
-                if (RAG == 2) tail = __shfl_sync(FULLMASK, tail, 0);
                 for (int kb = kb0; ok && kb < kb1; ++kb) {
                     // (the copies' completion on the barrier orders the operand bytes before the MMAs that read them;
                     // tcgen05 fences are only needed around the accumulator hand-over below)
@@ -917,6 +926,8 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     a_lo = n_a_lo; b_lo = n_b_lo; fbar = n_fbar; ebar = n_ebar; phase = n_phase;
                 }
                 if (ok) umma_commit_addr<CTAS>(smem_u32(&tmem_full[acc0]));   // accumulator(s) complete (both CTAs); the sub-tiles of a wide tile finish together
+                kb0 = kb1;
+                } while (EPI == 3 && ok && kb0 < kz);
             }
         }
         if (KS) { __syncwarp(); cluster_sync(); cluster_sync(); }
@@ -969,7 +980,6 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             }
         for (int it = 0; alive && sched.template get<RAG, FULL>(it, t); ++it) {
           if (t.skip) continue;
-          const int tile_no = done++;
           int m = t.m0 + (int)rank * BM + quad * 32 + lane;
           // EPI 3, 4: this lane's row of the logits, fetched while the tile's product is under way
           [[maybe_unused]] int target = -1;              // column of the row's target (any value outside the tile: not here)
@@ -982,6 +992,82 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
               target = row_live ? cls - la.v0 : -1;
               if (EPI == 4 && row_live) { row_lse2 = la.lse[m] * kLog2e; row_scale = la.dloss[m] / *la.scale; }
           }
+          if constexpr (EPI == 3) {
+              // A warp has 64 of the tile's columns: their logits are added up here from the accumulators as these come, then the largest and
+              // the sum of exponentials about it are taken.
+              static_assert(EW * 64 >= BN, "one piece a warp");
+              const int n64 = t.n0 + hf * 64;
+              const bool mine = n64 < t.n1;                // (the same for the whole warp)
+              f32x2 z[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) z[i] = both(0.0f);
+#pragma unroll 1
+              for (int kb = 0; kb < p.num_kb; kb += kLogitBlocks) {
+                  const int acc = done & 1;
+                  const bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&tmem_full[acc], (uint32_t)(done >> 1) & 1));
+                  ++done;
+                  if (!ok) { if (lane == 0) atomicExch(&g_gemm_status, 4); alive = false; break; }
+                  tc_fence_after();
+                  if (mine) {
+                      const uint32_t at = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * ACC_COLS + hf * 64);
+#pragma unroll
+                      for (int part = 0; part < 4; ++part) {
+                          uint32_t r[16];
+                          tmem_ld16(at + part * 16, r);
+                          tmem_ld_wait();
+                          tmem_regs_ready(r);
+#pragma unroll
+                          for (int i = 0; i < 8; ++i) z[part * 8 + i] = z[part * 8 + i] + pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+                      }
+                  }
+                  tc_fence_before();
+                  __syncwarp();
+                  if (lane == 0) {
+                      if (CTAS == 2) mbar_arrive_cluster(tmem_empty0 + (uint32_t)acc * 8u);
+                      else mbar_arrive(&tmem_empty[acc]);
+                  }
+              }
+              if (!alive) break;
+              // log2 of the scale of the sum (finite, below every logit, so that no difference is undefined) and the sum
+              const LogitArgs& la = em.logits;
+              const int last = min(t.n1, la.classes) - n64;                // columns that exist
+              float top2 = -1e30f, sum = 0.0f;
+              if (mine && last > 0) {
+                  float f[64];
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) split(z[i], f[2 * i], f[2 * i + 1]);
+                  const int off = target - n64;            // (a tile may reach past its strip: the next one's classes are not here)
+                  const unsigned place = off < last ? (unsigned)off : 64u;
+                  if (__any_sync(0xffffffffu, place < 64u)) {
+                      float at = 0.0f;
+#pragma unroll
+                      for (int i = 0; i < 64; ++i) at = place == (unsigned)i ? f[i] : at;
+                      if (place < 64u) la.at_target[m] = at;
+                      __syncwarp();
+                  }
+                  if (last < 64) {
+#pragma unroll
+                      for (int i = 0; i < 64; ++i) f[i] = i < last ? f[i] : -INFINITY;
+                  }
+                  float top[4] = {f[0], f[1], f[2], f[3]};
+#pragma unroll
+                  for (int i = 4; i < 64; ++i) top[i & 3] = fmaxf(top[i & 3], f[i]);
+                  top2 = fmaxf(top2, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * kLog2e);
+                  f32x2 s[4] = {both(0.0f), both(0.0f), both(0.0f), both(0.0f)};
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) s[i & 3] = s[i & 3] + exp2_fast(fma2(pair(f[2 * i], f[2 * i + 1]), both(kLog2e), both(-top2)));
+                  float a, b;
+                  split((s[0] + s[1]) + (s[2] + s[3]), a, b);
+                  sum = a + b;
+              }
+              int sn, jn;
+              p.fd_wn.divmod(t.n0, sn, jn);
+              const int64_t line = ((int64_t)sn * p.tps_n + jn / BN) * EW + hf;
+              if (m < t.m1) la.part[line * p.M + m] = make_float2(top2, sum);
+              __syncwarp();
+              continue;
+          }
+          const int tile_no = done++;
 #pragma unroll 1                                         // one copy of the (large) drain code: a short GEMM pays for every instruction-cache miss
           for (int h = 0; h < (SWIGLU ? 1 : NSUB); ++h) {
             const int acc = NSUB == 1 ? (tile_no & 1) : h;
@@ -1464,12 +1550,10 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         if (!alive) break;
                     }
                 }
-            } else if constexpr (EPI >= 3) {
+            } else if constexpr (EPI >= 4) {
                 // This warp's columns of the tile, 32 at a time: the next 32 accumulators are on their way while these are worked on.
                 const int steps = npieces > hf ? 2 * ((npieces - hf + EW - 1) / EW) : 0;
                 auto offset = [&](int k) { return (hf + (k >> 1) * EW) * 64 + (k & 1) * 32; };
-                // log2 of the scale of the sum (finite, below every logit, so that no difference is undefined) and the sum
-                [[maybe_unused]] float top2 = -1e30f, sum = 0.0f;
                 uint32_t nx[32];
                 if (steps > 0) tmem_ld32(taddr + (uint32_t)offset(0), nx);
 #pragma unroll 1
@@ -1503,33 +1587,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         const int off = target - n32;                          // (a tile may reach past its strip: the next one's classes are not here)
                         const unsigned place = off < last ? (unsigned)off : 32u;
                         const bool here = __any_sync(0xffffffffu, place < 32u);
-                        if constexpr (EPI == 3) {
-                            float f[32];
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) split(v[i], f[2 * i], f[2 * i + 1]);
-                            if (here) {
-                                float z = 0.0f;
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) z = place == (unsigned)i ? f[i] : z;
-                                if (place < 32u) la.at_target[m] = z;
-                                __syncwarp();            // (whole again before the next warp-wide load)
-                            }
-                            if (last < 32) {
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) f[i] = i < last ? f[i] : -INFINITY;
-                            }
-                            float top[4] = {f[0], f[1], f[2], f[3]};
-#pragma unroll
-                            for (int i = 4; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], f[i]);
-                            const float t2 = fmaxf(top2, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * kLog2e);
-                            f32x2 s[2] = {both(0.0f), both(0.0f)};
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) s[i & 1] = s[i & 1] + exp2_fast(fma2(pair(f[2 * i], f[2 * i + 1]), both(kLog2e), both(-t2)));
-                            float a, b;
-                            split(s[0] + s[1], a, b);
-                            sum = fmaf(sum, exp2_fast(top2 - t2), a + b);
-                            top2 = t2;
-                        } else {
+                        {
                             const bool full = rows_full && (n32 & ~63) + 64 <= t.n1;
                             if (full && !(k & 1)) { if (lane == 0) tma_store_wait_read<0>(); __syncwarp(); }       // the buffer's last piece has been stored
 #pragma unroll
@@ -1571,12 +1629,6 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 }
                 tmem_ld_wait();
                 tmem_regs_ready(nx);
-                if constexpr (EPI == 3) {
-                    int sn, jn;
-                    p.fd_wn.divmod(t.n0, sn, jn);
-                    const int64_t line = ((int64_t)sn * p.tps_n + jn / BN) * EW + hf;
-                    if (m < t.m1) em.logits.part[line * p.M + m] = make_float2(top2, sum);
-                }
             } else if constexpr (EPI != 0) {
 #pragma unroll 1
                 for (int c = hf; c < npieces; c += EW) {

@@ -433,9 +433,9 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     // and a residual, eight / sixteen: K = 1024 88 / 74 us, 2048 107 / 108, 4096 197 / 203; gradient: K = 256 72 / 67, 1024 89 / 89,
     // 2048 111 / 115, 4096 201 / 210).  Those are problems of seven rounds of tiles; with one round, where no next tile hides the
     // drain, the two have not been compared.  The kernels with every layout exist with eight, the cluster split drains once, with sixteen.
-    const int opw = ks ? 16 : (epi_full || epi == 5 || p.kb_per_split * BK >= 1536 ? 8 : 16);
+    const int opw = ks || epi == 3 ? 16 : (epi_full || epi == 5 || p.kb_per_split * BK >= 1536 ? 8 : 16);
     plan->opw = opw;
-    p.stages = (int32_t)(((epi ? smem_budget_op(ks, opw) : kSmemBudget) - rag_bytes) / p.stage_bytes);
+    p.stages = (int32_t)(((epi ? smem_budget_op(ks, opw, epi) : kSmemBudget) - rag_bytes) / p.stage_bytes);
     if (p.stages > 8) p.stages = 8;
     int64_t ntiles = (int64_t)p.tiles_m * p.tiles_n * splits * batch;
     p.batch = (int32_t)batch;
@@ -498,7 +498,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     p.fd_upg = make_fastdiv(p.sch_upg); p.fd_groups = make_fastdiv(p.groups); p.fd_splits = make_fastdiv(p.splits);
     p.fd_per_panel = make_fastdiv((int64_t)p.panel * p.sch_gn); p.fd_panel = make_fastdiv(p.panel);
     p.fd_tps_m = make_fastdiv(p.tps_m); p.fd_tps_n = make_fastdiv(p.tps_n);
-    plan->smem_bytes = (uint32_t)p.stages * p.stage_bytes + (epi ? (ks ? 0u : (uint32_t)opw * 32 * 128) + (uint32_t)opw * 8 : kEpiBytes) + 1024 + (2 * p.stages + 8) * 8 + 16 + rag_bytes;
+    plan->smem_bytes = (uint32_t)p.stages * p.stage_bytes + (epi ? (ks || epi == 3 ? 0u : (uint32_t)opw * 32 * 128) + (uint32_t)opw * 8 : kEpiBytes) + 1024 + (2 * p.stages + 8) * 8 + 16 + rag_bytes;
     p.fd_tiles_n = make_fastdiv(p.tiles_n);
     return CCL_OK;
 }

@@ -1,9 +1,9 @@
 // ccl_linear_xent: the cross entropy of z = X W^T over a large vocabulary, and ccl_linear_xent_grad: its gradients with respect to X and W.
 // The logits z are never stored.
 //
-// Forward.  The GEMM of ccl_gemm (ccl_gemm_kernel.cuh, EPI = 3) with another drain: a lane has a row of the tile's accumulators and leaves,
-// of its columns, the largest and the sum of exponentials about it (two numbers for every 64 to 128 logits; the target's logit where it
-// passes by), and a second kernel joins a row's numbers:  lse = max + log(sum of s_i exp(m_i - max)).  Powers of two throughout: one
+// Forward.  The GEMM of ccl_gemm (ccl_gemm_kernel.cuh, EPI = 3) with another drain: a lane has a row of 64 of the tile's columns, adds their
+// logits up in fp32 from accumulators of 1024 of K each, and leaves the largest and the sum of exponentials about it (the target's logit
+// where it passes by), and a second kernel joins a row's numbers:  lse = max + log(sum of s_i exp(m_i - max)).  Powers of two throughout: one
 // multiply-add and one hardware exponential a logit, behind the next tile's product.
 //
 // Gradient.  dz = dloss / s (exp(z - lse) - [target]), piece by piece of the vocabulary: the logits' product again, its drain turning z into dz
@@ -27,9 +27,10 @@ constexpr int64_t kPieceBytes = INT64_C(1) << 29;
 
 template <int EPI, int BN, int CTAS>
 static ccl_status launch_logits_warps(const GemmPlan& plan, const CUtensorMap* maps, const EpiMaps<EPI>& em, cudaStream_t st) {
-    if constexpr (EPI != 5)
+    if constexpr (EPI == 3) return launch_epi_warps<BN, CTAS, false, 0, EPI, 16>(plan, maps, em, st);
+    if constexpr (EPI == 4)
         if (plan.opw == 16) return launch_epi_warps<BN, CTAS, false, 0, EPI, 16>(plan, maps, em, st);
-    return launch_epi_warps<BN, CTAS, false, 0, EPI, 8>(plan, maps, em, st);
+    if constexpr (EPI != 3) return launch_epi_warps<BN, CTAS, false, 0, EPI, 8>(plan, maps, em, st);
 }
 
 // A product over part of the vocabulary.  rows_b: rows of B that exist (0: all that the descriptor says); the rest reads as zeros.

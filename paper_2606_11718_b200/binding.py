@@ -5,6 +5,7 @@ torch CUDA tensors used as plain device buffers; the stream is torch's current s
 There is no CPU fallback: if libccl.so is missing the import of this module's functions
 raises, and device entry points fail without a CUDA device.
 """
+import array
 import ctypes as C
 import os
 
@@ -349,11 +350,6 @@ def _check_vector(t, n, what, device):
         raise ValueError(f"{what} must be a contiguous bfloat16 tensor with at least {n} entries beside the operands")
 
 
-def _check_beside(t, dtype, n, what, device):
-    if t is not None and (t.dtype is not dtype or t.numel() < n or t.get_device() != device or not t.is_contiguous()):
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor with at least {n} entries beside the operands")
-
-
 def _check_workspace(t, what, device):
     """Bytes of a workspace of any type (the library says whether they are enough)."""
     if t is None:
@@ -446,16 +442,49 @@ def ccl_moe_tokens(d, X, Wr, Wgu, Wd, Y, ws, residual=None, ids=None, weights=No
                                 _stream()))
 
 
+_BF16, _FP32, _INT32 = torch.bfloat16, torch.float32, torch.int32
+
+
+def _current_device():
+    return torch.cuda.current_device() if torch.cuda.is_available() else None
+
+
+def _device_of(t, what):
+    """The current CUDA device, which the first operand has to be on."""
+    at = t.get_device() if t is not None else -1
+    if at < 0 or at != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
+        raise ValueError(f"{what}: an operand must be a tensor on the current CUDA device")
+    return at
+
+
+def _operand(t, nbytes, device, what):
+    """Address of an operand (None: NULL; the library says where it cannot do without): contiguous, on that device, with at least that many
+    bytes of bf16 or raw (integer) storage."""
+    if t is None:
+        return None
+    dtype = t.dtype
+    if t.nbytes < nbytes or t.get_device() != device or not t.is_contiguous() or (dtype is not _BF16 and dtype.is_floating_point):
+        raise ValueError(f"{what}: an operand must be a contiguous tensor on the current CUDA device that holds what the descriptor says, as bfloat16")
+    return t.data_ptr()
+
+
+def _vector(t, dtype, n, device, what):
+    """Address of a vector of at least n entries of that type beside the operands (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < n or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor with at least {n} entries beside the operands")
+    return t.data_ptr()
+
+
 def ccl_norm(m, X, gamma, beta, Y, kind=NORM_LAYER, eps=1e-5, mean=None, rstd=None):
     """Y = (X - mean) * rstd * gamma + beta for every row (NORM_RMS: X * rstd * gamma); X and Y (may be X) as `m` describes, gamma and beta [cols]
     bfloat16 or None, mean and rstd float32 [rows] receive the statistics if wanted."""
-    nbytes = ccl_buffer_bytes(m)
-    device = _check_operands("ccl_norm", (X, nbytes), (Y, nbytes))
-    _check_vector(gamma, m.cols, "ccl_norm: gamma", device)
-    _check_vector(beta, m.cols, "ccl_norm: beta", device)
-    _check_beside(mean, torch.float32, m.rows, "ccl_norm: mean", device)
-    _check_beside(rstd, torch.float32, m.rows, "ccl_norm: rstd", device)
-    _check(lib().ccl_norm(C.byref(m), kind, eps, _ptr(X), _ptr(gamma), _ptr(beta), _ptr(Y), _ptr(mean), _ptr(rstd), _stream()))
+    nbytes, rows, cols = ccl_buffer_bytes(m), m.rows, m.cols
+    device = _device_of(X, "ccl_norm")
+    _check(lib().ccl_norm(C.byref(m), kind, eps, _operand(X, nbytes, device, "ccl_norm"), _vector(gamma, _BF16, cols, device, "ccl_norm: gamma"),
+                          _vector(beta, _BF16, cols, device, "ccl_norm: beta"), _operand(Y, nbytes, device, "ccl_norm"),
+                          _vector(mean, _FP32, rows, device, "ccl_norm: mean"), _vector(rstd, _FP32, rows, device, "ccl_norm: rstd"), _stream()))
 
 
 def ccl_norm_grad_workspace(m):
@@ -464,14 +493,13 @@ def ccl_norm_grad_workspace(m):
 
 def ccl_norm_grad(m, X, gamma, mean, rstd, dy, dx, ws=None, kind=NORM_LAYER, addend=None, dgamma=None, dbeta=None):
     """dx = gradient of ccl_norm's X (+ addend), dgamma / dbeta [cols] bfloat16 = those of its weights; None: not wanted.  ws: for the sums only."""
-    nbytes = ccl_buffer_bytes(m)
-    device = _check_operands("ccl_norm_grad", (X, nbytes), (dy, nbytes), (dx, nbytes), (addend, nbytes))
-    for t, what in ((gamma, "gamma"), (dgamma, "dgamma"), (dbeta, "dbeta")):
-        _check_vector(t, m.cols, "ccl_norm_grad: " + what, device)
-    _check_beside(mean, torch.float32, m.rows, "ccl_norm_grad: mean", device)
-    _check_beside(rstd, torch.float32, m.rows, "ccl_norm_grad: rstd", device)
-    ws_bytes = _check_workspace(ws, "ccl_norm_grad", device)
-    _check(lib().ccl_norm_grad(C.byref(m), kind, _ptr(X), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dy), _ptr(addend), _ptr(dx), _ptr(dgamma), _ptr(dbeta),
+    nbytes, rows, cols, who = ccl_buffer_bytes(m), m.rows, m.cols, "ccl_norm_grad"
+    device = _device_of(X, who)
+    ws_bytes = _check_workspace(ws, who, device)
+    _check(lib().ccl_norm_grad(C.byref(m), kind, _operand(X, nbytes, device, who), _vector(gamma, _BF16, cols, device, "ccl_norm_grad: gamma"),
+                               _vector(mean, _FP32, rows, device, "ccl_norm_grad: mean"), _vector(rstd, _FP32, rows, device, "ccl_norm_grad: rstd"),
+                               _operand(dy, nbytes, device, who), _operand(addend, nbytes, device, who), _operand(dx, nbytes, device, who),
+                               _vector(dgamma, _BF16, cols, device, "ccl_norm_grad: dgamma"), _vector(dbeta, _BF16, cols, device, "ccl_norm_grad: dbeta"),
                                _ptr(ws), ws_bytes, _stream()))
 
 
@@ -481,12 +509,12 @@ def ccl_linear_xent_workspace(d):
 
 def ccl_linear_xent(d, X, W, targets, loss, lse, ws):
     """loss, lse (float32 [T], None: not wanted) of the logits X W^T: X [T x H], W as d.W describes, targets int32 [T]."""
-    device = _check_operands("ccl_linear_xent", (X, 2 * d.T * d.H), (W, ccl_buffer_bytes(d.W)))
-    _check_beside(targets, torch.int32, d.T, "ccl_linear_xent: targets", device)
-    _check_beside(loss, torch.float32, d.T, "ccl_linear_xent: loss", device)
-    _check_beside(lse, torch.float32, d.T, "ccl_linear_xent: lse", device)
-    ws_bytes = _check_workspace(ws, "ccl_linear_xent", device)
-    _check(lib().ccl_linear_xent(C.byref(d), _ptr(X), _ptr(W), _ptr(targets), _ptr(loss), _ptr(lse), _ptr(ws), ws_bytes, _stream()))
+    who, T = "ccl_linear_xent", d.T
+    device = _device_of(X, who)
+    ws_bytes = _check_workspace(ws, who, device)
+    _check(lib().ccl_linear_xent(C.byref(d), _operand(X, 2 * T * d.H, device, who), _operand(W, ccl_buffer_bytes(d.W), device, who),
+                                 _vector(targets, _INT32, T, device, "ccl_linear_xent: targets"), _vector(loss, _FP32, T, device, "ccl_linear_xent: loss"),
+                                 _vector(lse, _FP32, T, device, "ccl_linear_xent: lse"), _ptr(ws), ws_bytes, _stream()))
 
 
 def ccl_linear_xent_grad_workspace(d):
@@ -495,17 +523,14 @@ def ccl_linear_xent_grad_workspace(d):
 
 def ccl_linear_xent_grad(d, X, W, targets, lse, dloss, dX, dW, ws):
     """dX [T x H] and dW (as d.W describes), None: not wanted, from ccl_linear_xent's lse and the gradient dloss (float32 [T]) of its loss."""
-    w_bytes = ccl_buffer_bytes(d.W)
-    device = _check_operands("ccl_linear_xent_grad", (X, 2 * d.T * d.H), (W, w_bytes), (dX, 2 * d.T * d.H), (dW, w_bytes))
-    _check_beside(targets, torch.int32, d.T, "ccl_linear_xent_grad: targets", device)
-    _check_beside(lse, torch.float32, d.T, "ccl_linear_xent_grad: lse", device)
-    _check_beside(dloss, torch.float32, d.T, "ccl_linear_xent_grad: dloss", device)
-    ws_bytes = _check_workspace(ws, "ccl_linear_xent_grad", device)
-    _check(lib().ccl_linear_xent_grad(C.byref(d), _ptr(X), _ptr(W), _ptr(targets), _ptr(lse), _ptr(dloss), _ptr(dX), _ptr(dW), _ptr(ws), ws_bytes, _stream()))
-
-
-def _current_device():
-    return torch.cuda.current_device() if torch.cuda.is_available() else None
+    who, T = "ccl_linear_xent_grad", d.T
+    x_bytes, w_bytes = 2 * T * d.H, ccl_buffer_bytes(d.W)
+    device = _device_of(X, who)
+    ws_bytes = _check_workspace(ws, who, device)
+    _check(lib().ccl_linear_xent_grad(C.byref(d), _operand(X, x_bytes, device, who), _operand(W, w_bytes, device, who),
+                                      _vector(targets, _INT32, T, device, "ccl_linear_xent_grad: targets"),
+                                      _vector(lse, _FP32, T, device, "ccl_linear_xent_grad: lse"), _vector(dloss, _FP32, T, device, "ccl_linear_xent_grad: dloss"),
+                                      _operand(dX, x_bytes, device, who), _operand(dW, w_bytes, device, who), _ptr(ws), ws_bytes, _stream()))
 
 
 ADAMW_BLOCK = 256                                              # elements that share a scale of the 8-bit states
@@ -518,33 +543,38 @@ class AdamwTensors:
     change between steps, where they are may not."""
 
     def __init__(self, params, grads, m, v, copies=None, m_scales=None, v_scales=None):
-        n = len(params)
-        copies = copies if copies is not None else [None] * n
-        eight = m_scales is not None or v_scales is not None
-        columns = [params, copies, grads, m, v] + ([m_scales or [], v_scales or []] if eight else [])
+        n, eight = len(params), m_scales is not None or v_scales is not None
+        columns = [params, copies if copies is not None else [None] * n, grads, m, v] + ([m_scales or [], v_scales or []] if eight else [])
         if any(len(c) != n for c in columns):
             raise ValueError("AdamwTensors: lists of different lengths")
-        states = (torch.float8_e4m3fn, torch.uint8) if eight else (torch.float32,)
-        wanted = [(torch.float32,), (torch.bfloat16,), (torch.bfloat16, torch.float32), states, states, (torch.float32,), (torch.float32,)]
-        self.bits, self.count, self.tensors, self.device = (8 if eight else 32), n, columns, _current_device() if n else None
-        self.table = (AdamwTensor * max(n, 1))()
-        spans = []
-        for i in range(n):
-            size = params[i].numel()
-            for k, c in enumerate(columns):
-                t = c[i]
+        self.bits, self.count, self.tensors, self.device = (8 if eight else 32), n, [list(c) for c in columns], _current_device() if n else None
+        state = (torch.float8_e4m3fn, torch.uint8) if eight else (_FP32,)
+        wanted = [(_FP32,), (_BF16,), (_BF16, _FP32), state, state, (_FP32,), (_FP32,)]
+        sizes = [p.numel() for p in params]
+        blocks = [-(-k // ADAMW_BLOCK) for k in sizes]
+        device, places, spans = self.device, [], []
+        for k, column in enumerate(columns):
+            place = []
+            for i, (t, size) in enumerate(zip(column, sizes if k < 5 else blocks)):
                 if t is None and k == 1:
+                    place.append(0)
                     continue
-                if t is None or t.dtype not in wanted[k] or t.get_device() != self.device or not t.is_contiguous() or t.numel() != (size if k < 5 else -(-size // ADAMW_BLOCK)):
+                if t is None or t.dtype not in wanted[k] or t.get_device() != device or not t.is_contiguous() or t.numel() != size:
                     raise ValueError(f"AdamwTensors: tensor {i}: a buffer has another type, size or device than its place asks for, or is not contiguous")
-                if t.numel():
-                    spans.append((t.data_ptr(), t.data_ptr() + t.nbytes, i))
-            scales = [_ptr(columns[5][i]), _ptr(columns[6][i])] if eight else [None, None]
-            self.table[i] = AdamwTensor(size, _ptr(params[i]), _ptr(copies[i]), _ptr(grads[i]), _ptr(m[i]), _ptr(v[i]), *scales, int(grads[i].dtype is torch.float32))
+                at = t.data_ptr()
+                place.append(at)
+                if size:
+                    spans.append((at, at + t.nbytes, i))
+            places.append(place)
         spans.sort()
         for (_, end, i), (start, _, j) in zip(spans, spans[1:]):
             if start < end:
                 raise ValueError(f"AdamwTensors: buffers of tensors {i} and {j} overlap")
+        places += [[0] * n] * (7 - len(places))
+        wide = [int(g.dtype is _FP32) for g in grads]
+        rows = zip(sizes, places[0], places[1], places[2], places[3], places[4], places[5], places[6], wide)
+        self.words = array.array("q", [word for row in rows for word in row] or [0] * 9)           # a tensor's nine words, as ccl_adamw_tensor has them
+        self.table = (AdamwTensor * max(n, 1)).from_buffer(self.words)
 
 
 def ccl_adamw(d, tensors, grad_scale=None, step=None, lr=None):
@@ -553,11 +583,9 @@ def ccl_adamw(d, tensors, grad_scale=None, step=None, lr=None):
     device = tensors.device
     if tensors.count and device != _current_device():
         raise ValueError("ccl_adamw: the tensors are not on the current CUDA device")
-    _check_beside(grad_scale, torch.float32, 1, "ccl_adamw: grad_scale", device)
-    _check_beside(step, torch.int64, 1, "ccl_adamw: step", device)
-    _check_beside(lr, torch.float32, 1, "ccl_adamw: lr", device)
     call = AdamwDesc.from_buffer_copy(d)
-    call.state_bits, call.grad_scale_dev, call.step_dev, call.lr_dev = tensors.bits, _ptr(grad_scale), _ptr(step), _ptr(lr)
+    call.state_bits, call.grad_scale_dev = tensors.bits, _vector(grad_scale, _FP32, 1, device, "ccl_adamw: grad_scale")
+    call.step_dev, call.lr_dev = _vector(step, torch.int64, 1, device, "ccl_adamw: step"), _vector(lr, _FP32, 1, device, "ccl_adamw: lr")
     _check(lib().ccl_adamw(C.byref(call), tensors.table, tensors.count, _stream()))
 
 

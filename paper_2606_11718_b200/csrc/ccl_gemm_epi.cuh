@@ -74,6 +74,17 @@ static ShapePlan g_shapes[kShapeSlots];
 static int g_shapes_next = 0;
 static std::mutex g_shapes_mutex;
 
+// What else a plan depends on: the device and the planner's switches (`env` comes cleared)
+static void key_surroundings(int* dev, char* env, size_t size) {
+    *dev = -1;
+    if (cudaGetDevice(dev) != cudaSuccess) (void)cudaGetLastError();
+    size_t pos = 0;
+    for (const char* name : {"CCL_GEMM_CTAS", "CCL_GEMM_BN", "CCL_GEMM_SPLITK", "CCL_GEMM_CLUSTERK"}) {
+        const char* v = std::getenv(name);
+        for (const char* c = v ? v : ""; *c && pos + 2 < size; ++c) env[pos++] = *c;
+        if (pos + 1 < size) env[pos++] = ';';
+    }
+}
 static void shape_key(const ccl_gemm_desc* d, int epi, ShapeKey* k) {
     std::memset(k, 0, sizeof(*k));
     int64_t* f = k->f;
@@ -86,14 +97,7 @@ static void shape_key(const ccl_gemm_desc* d, int epi, ShapeKey* k) {
     f[24] = d->a_trans; f[25] = d->b_trans; f[26] = d->out_part; f[27] = d->P; f[28] = d->grouped_raster;
     f[29] = d->out_part == CCL_PART_2D ? d->part_m : 0;
     k->epi = epi;
-    k->dev = -1;
-    if (cudaGetDevice(&k->dev) != cudaSuccess) (void)cudaGetLastError();
-    size_t pos = 0;
-    for (const char* name : {"CCL_GEMM_CTAS", "CCL_GEMM_BN", "CCL_GEMM_SPLITK", "CCL_GEMM_CLUSTERK"}) {
-        const char* v = std::getenv(name);
-        for (const char* c = v ? v : ""; *c && pos + 2 < sizeof(k->env); ++c) k->env[pos++] = *c;
-        if (pos + 1 < sizeof(k->env)) k->env[pos++] = ';';
-    }
+    key_surroundings(&k->dev, k->env, sizeof(k->env));
 }
 
 // Validates the descriptor and finds or makes its plan (a B200's unit counts when no device can be asked).

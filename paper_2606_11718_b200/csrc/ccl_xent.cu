@@ -199,7 +199,7 @@ ccl_gemm_desc dw_product(const Vocabulary& v, const GradPlan& g, int64_t real) {
     return product(v.H, real, v.T, matrix(v.T, v.H), 1, matrix(v.T, real), 0, g.all ? v.W : matrix(v.H, real));
 }
 
-ccl_status plan_grad(const Vocabulary& v, GradPlan* g) {
+ccl_status make_grad_plan(const Vocabulary& v, GradPlan* g) {
     if (v.trans) {
         const int64_t most = std::max<int64_t>(256, kPieceBytes / (2 * v.T) / 256 * 256);
         g->pieces = (v.V + most - 1) / most;
@@ -236,6 +236,42 @@ ccl_status plan_grad(const Vocabulary& v, GradPlan* g) {
     g->gemm_at = up256(dz + (size_t)g->parts * (size_t)v.T * (size_t)v.H * 4);
     g->scale_at = up256(g->gemm_at + g->gemm_bytes);
     g->bytes = g->scale_at + 4;
+    return CCL_OK;
+}
+
+// Plans of the gradient, by shape (four products planned cost 20 us)
+struct GradKey {
+    int64_t f[9];
+    int dev;
+    char env[60];
+};
+struct GradSlot {
+    GradKey key;
+    GradPlan plan;
+    bool valid = false;
+};
+GradSlot g_grads[16];
+int g_grads_next = 0;
+std::mutex g_grads_mutex;
+
+ccl_status plan_grad(const Vocabulary& v, GradPlan* g) {
+    GradKey key;
+    std::memset(&key, 0, sizeof(key));
+    const int64_t f[9] = {v.T, v.V, v.H, v.trans, v.W.P, v.W.part, v.W.layout, v.W.strip_align_bytes, v.strips};
+    std::memcpy(key.f, f, sizeof(f));
+    key_surroundings(&key.dev, key.env, sizeof(key.env));
+    {
+        std::lock_guard<std::mutex> lock(g_grads_mutex);
+        for (const GradSlot& s : g_grads)
+            if (s.valid && std::memcmp(&s.key, &key, sizeof(key)) == 0) { *g = s.plan; return CCL_OK; }
+    }
+    ccl_status s = make_grad_plan(v, g);
+    if (s) return s;
+    std::lock_guard<std::mutex> lock(g_grads_mutex);
+    g_grads[g_grads_next].key = key;
+    g_grads[g_grads_next].plan = *g;
+    g_grads[g_grads_next].valid = true;
+    g_grads_next = (g_grads_next + 1) % 16;
     return CCL_OK;
 }
 

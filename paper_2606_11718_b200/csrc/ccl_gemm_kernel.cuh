@@ -944,6 +944,11 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         int done = 0;                                    // tiles drained so far
         TileCoord pend[2];                               // balanced split: shares written but not yet reduced
         int npend = 0;
+        // alpha, fetched once: from global memory it would hold up every piece (128 x 256 tiles of one k block: 8 us each, 2 with it here)
+        [[maybe_unused]] float alpha = 1.0f;
+        if constexpr (FULL || KS != 0) alpha = alpha_of(p);
+        [[maybe_unused]] float by_scale = 1.0f;
+        if constexpr (EPI == 4) by_scale = 1.0f / *em.logits.scale;
         // EPI: the addend's part of this warp's next piece (32 rows x 64 columns) is fetched into the warp's buffer as soon as the
         // piece before has been stored from it; the cursor `ap` runs one piece ahead, into the next tile.
         constexpr bool kOp = (EPI == 1 || EPI == 2) && KS == 0;
@@ -987,10 +992,10 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           [[maybe_unused]] bool row_live = false;
           if constexpr (EPI == 3 || EPI == 4) {
               const LogitArgs& la = em.logits;
-              const int cls = m < t.m1 ? la.targets[m] : la.ignore;
-              row_live = cls != la.ignore && (unsigned)cls < (unsigned)la.all;
+              const int row = min(m, t.m1 - 1), cls = la.targets[row];
+              if (EPI == 4) { row_lse2 = la.lse[row] * kLog2e; row_scale = la.dloss[row] * by_scale; }     // (all three under way together)
+              row_live = m < t.m1 && cls != la.ignore && (unsigned)cls < (unsigned)la.all;
               target = row_live ? cls - la.v0 : -1;
-              if (EPI == 4 && row_live) { row_lse2 = la.lse[m] * kLog2e; row_scale = la.dloss[m] / *la.scale; }
           }
           if constexpr (EPI == 3) {
               // A warp has 64 of the tile's columns: their logits are added up here from the accumulators as these come, then the largest and
@@ -1153,11 +1158,16 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const int n64 = nb + c * 64;
                 const bool row_ok = m < t.m1;
                 const unsigned short* src = p.C + c_offset<FULL>(p, min(m, t.m1 - 1), n64) + (int64_t)t.e * p.c_batch_stride;
-                const float alpha = alpha_of(p), beta = p.beta;
+                const float beta = p.beta;
+                if (beta == 0.0f) {                      // (nothing of C is read)
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) r[i] = __float_as_uint(fmaf(alpha, __uint_as_float(r[i]), beta * 0.0f));
+                    return;
+                }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     uint4 cv = make_uint4(0u, 0u, 0u, 0u);
-                    if (beta != 0.0f && n64 + j * 8 < t.n1) cv = ld_global_v4_if(src + j * 8, row_ok);
+                    if (n64 + j * 8 < t.n1) cv = ld_global_v4_if(src + j * 8, row_ok);
                     const uint32_t w[4] = {cv.x, cv.y, cv.z, cv.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {                       // bf16 -> fp32 is a shift
@@ -1445,7 +1455,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         }
                         if (p.axpby) {                             // C <- alpha * sum + beta * C (C read through its own layout)
                             const uint4 cv = ld_global_v4_if(crow + c * 64 + js * 4, p.beta != 0.0f && row < t.m1 && col < t.n1);
-                            const float al = alpha_of(p), be = p.beta;
+                            const float al = alpha, be = p.beta;
                             a0.x = fmaf(al, a0.x, be * __uint_as_float(cv.x << 16)); a0.y = fmaf(al, a0.y, be * __uint_as_float(cv.x & 0xFFFF0000u));
                             a0.z = fmaf(al, a0.z, be * __uint_as_float(cv.y << 16)); a0.w = fmaf(al, a0.w, be * __uint_as_float(cv.y & 0xFFFF0000u));
                             a1.x = fmaf(al, a1.x, be * __uint_as_float(cv.z << 16)); a1.y = fmaf(al, a1.y, be * __uint_as_float(cv.z & 0xFFFF0000u));
@@ -1588,7 +1598,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         const unsigned place = off < last ? (unsigned)off : 32u;
                         const bool here = __any_sync(0xffffffffu, place < 32u);
                         {
-                            const bool full = rows_full && (n32 & ~63) + 64 <= t.n1;
+                            const bool full = rows_full && n32 - (k & 1) * 32 + 64 <= t.n1;
                             if (full && !(k & 1)) { if (lane == 0) tma_store_wait_read<0>(); __syncwarp(); }       // the buffer's last piece has been stored
 #pragma unroll
                             for (int i = 0; i < 16; ++i) v[i] = exp2_fast(fma2(v[i], both(kLog2e), both(-row_lse2))) * both(row_scale);

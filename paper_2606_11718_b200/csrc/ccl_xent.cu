@@ -123,6 +123,7 @@ __global__ void __launch_bounds__(256) xent_dx_kernel(const float* acc, int part
     const f32x2 by = both(*scale);
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 256 * 8) {
         f32x2 v[4] = {both(0.0f), both(0.0f), both(0.0f), both(0.0f)};
+#pragma unroll 8
         for (int k = 0; k < parts; ++k) {
             const float4 a = *reinterpret_cast<const float4*>(acc + k * n + i), b = *reinterpret_cast<const float4*>(acc + k * n + i + 4);
             v[0] = v[0] + pair(a.x, a.y); v[1] = v[1] + pair(a.z, a.w);
@@ -170,10 +171,15 @@ ccl_status check_vocabulary(const char* who, const ccl_xent_desc* d, Vocabulary*
     return CCL_OK;
 }
 
+// dz of the whole vocabulary, kept in the strips that W has
+ccl_mat strips_of(const Vocabulary& v) {
+    return v.strips > 1 ? ccl_mat{v.T, v.V, 2, (int32_t)v.strips, CCL_PART_COLS, CCL_CCL, 0} : matrix(v.T, v.V);
+}
 // The logits of `real` classes from one piece (all: of the whole of W); a row-major W is padded to whole 64s with classes that read as zeros
 ccl_gemm_desc logits(const Vocabulary& v, int64_t real, bool all) {
     const int64_t n = v.trans ? up(real, 64) : real;
-    return product(v.T, n, v.H, matrix(v.T, v.H), 0, v.trans ? matrix(n, v.H) : (all ? v.W : matrix(v.H, n)), v.trans, matrix(v.T, n));
+    if (!v.trans && all) return product(v.T, n, v.H, matrix(v.T, v.H), 0, v.W, 0, strips_of(v));
+    return product(v.T, n, v.H, matrix(v.T, v.H), 0, v.trans ? matrix(n, v.H) : matrix(v.H, n), v.trans, matrix(v.T, n));
 }
 
 int forward_lines(const GemmPlan& plan) { return plan.p.tiles_n * (plan.opw / 4); }
@@ -182,21 +188,23 @@ int forward_lines(const GemmPlan& plan) { return plan.p.tiles_n * (plan.opw / 4)
 struct GradPlan {
     int64_t pieces, width;          // classes of a piece but the last
     bool all;                       // one piece that is the whole of W
-    int parts;                      // fp32 sums of dX (0: one piece, no sum is kept)
+    int64_t sums, sum_width;        // products that dX is the sum of, classes of each (1: one a piece, where there is one piece)
+    int parts;                      // fp32 sums of dX (0: it is one product)
     size_t acc_at, gemm_at, gemm_bytes, scale_at, bytes;
 };
 
 int64_t piece_real(const Vocabulary& v, const GradPlan& g, int64_t i) { return std::min(g.width, v.V - i * g.width); }
 ccl_gemm_desc dx_product(const Vocabulary& v, const GradPlan& g, int64_t real) {
     const int64_t n = v.trans ? up(real, 64) : real;
-    return product(v.T, v.H, n, matrix(v.T, n), 0, v.trans ? matrix(n, v.H) : (g.all ? v.W : matrix(v.H, n)), v.trans ? 0 : 1, matrix(v.T, v.H));
+    if (!v.trans && g.sums == 1) return product(v.T, v.H, n, strips_of(v), 0, v.W, 1, matrix(v.T, v.H));
+    return product(v.T, v.H, n, matrix(v.T, n), 0, v.trans ? matrix(n, v.H) : matrix(v.H, n), v.trans ? 0 : 1, matrix(v.T, v.H));
 }
 ccl_gemm_desc dw_product(const Vocabulary& v, const GradPlan& g, int64_t real) {
     if (v.trans) {
         const int64_t n = up(real, 64);
         return product(n, v.H, v.T, matrix(v.T, n), 1, matrix(v.T, v.H), 0, matrix(n, v.H));
     }
-    return product(v.H, real, v.T, matrix(v.T, v.H), 1, matrix(v.T, real), 0, g.all ? v.W : matrix(v.H, real));
+    return product(v.H, real, v.T, matrix(v.T, v.H), 1, g.all ? strips_of(v) : matrix(v.T, real), 0, g.all ? v.W : matrix(v.H, real));
 }
 
 ccl_status make_grad_plan(const Vocabulary& v, GradPlan* g) {
@@ -206,11 +214,15 @@ ccl_status make_grad_plan(const Vocabulary& v, GradPlan* g) {
         g->width = g->pieces == 1 ? v.V : up((v.V + g->pieces - 1) / g->pieces, 256);
         g->pieces = (v.V + g->width - 1) / g->width;
         g->all = g->pieces == 1;
+        g->sums = g->pieces;
+        g->sum_width = g->width;
     } else {
-        // (all strips at once need them along the K of dX's product, in whole blocks of it)
-        g->all = v.strips == 1 || (2 * v.T * v.V <= kPieceBytes && v.strip % BK == 0);
+        g->all = v.strips == 1 || 2 * v.T * v.V <= kPieceBytes;
         g->pieces = g->all ? 1 : v.strips;
         g->width = g->all ? v.V : v.strip;
+        // (strips along the K of dX's product have to be whole blocks of it; others are added up one by one)
+        g->sums = g->all && (v.strips == 1 || v.strip % BK == 0) ? 1 : v.strips;
+        g->sum_width = g->sums == 1 ? v.V : v.strip;
     }
     g->parts = 0;
     g->gemm_bytes = 0;
@@ -221,8 +233,8 @@ ccl_status make_grad_plan(const Vocabulary& v, GradPlan* g) {
         ccl_gemm_desc d = dw_product(v, *g, real);
         if ((s = ccl_gemm_workspace(&d, &n))) return s;
         g->gemm_bytes = std::max(g->gemm_bytes, n);
-        d = dx_product(v, *g, real);
-        if (g->pieces == 1) {
+        d = dx_product(v, *g, std::min(real, g->sum_width));
+        if (g->sums == 1) {
             if ((s = ccl_gemm_workspace(&d, &n))) return s;
             g->gemm_bytes = std::max(g->gemm_bytes, n);
         } else {
@@ -388,14 +400,17 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
         la.lse = lse_dev; la.dloss = dloss_dev; la.scale = scale;
         if ((s = run_logits<4>(plan, em, rows, X_dev, W, dz, st))) return s;
         if (dX_dev) {
-            p = dx_product(v, g, real);
-            if (g.pieces == 1) {
+            p = dx_product(v, g, std::min(real, g.sum_width));
+            if (g.sums == 1) {
                 if ((s = gemm_cut(&p, 0, rows, false, scale, dz, W, dX_dev, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
             } else {
-                if ((s = shape_plan(&p, 5, &plan))) return s;
-                EpiMaps<5> sums = {acc, have};
-                if ((s = run_logits<5>(plan, sums, rows, dz, W, nullptr, st))) return s;
-                have = std::max(have, (int)plan.p.splits);
+                // (the piece's dz and W; or one of their strips after the other)
+                for (int64_t k = 0; k < (g.all ? g.sums : 1); ++k) {
+                    if ((s = shape_plan(&p, 5, &plan))) return s;
+                    EpiMaps<5> sums = {acc, have};
+                    if ((s = run_logits<5>(plan, sums, rows, static_cast<uint16_t*>(dz) + k * v.T * v.strip, W + k * v.stride, nullptr, st))) return s;
+                    have = std::max(have, (int)plan.p.splits);
+                }
             }
         }
         if (dW_dev) {
@@ -405,7 +420,7 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
             if ((s = gemm_cut(&p, rows, 0, single, scale, v.trans ? dz : X_dev, v.trans ? X_dev : dz, static_cast<uint16_t*>(dW_dev) + at, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
         }
     }
-    if (!dX_dev || g.pieces == 1) return CCL_OK;
+    if (!dX_dev || g.sums == 1) return CCL_OK;
     const int64_t n = v.T * v.H;
     return launch_early(xent_dx_kernel, dim3((unsigned)std::min<int64_t>((n / 8 + 255) / 256, 148 * 8)), 256, 0, st, (const float*)acc, have, n, (const float*)scale, static_cast<uint16_t*>(dX_dev));
 }

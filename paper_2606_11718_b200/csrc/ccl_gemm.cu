@@ -278,11 +278,10 @@ ccl_status static_ws_address(void** out) {
 // strides[X]: bytes between the buffers of operand X (A, B, C) of consecutive problems; 0 = shared (A and B only)
 // m_offs / cap: ragged batch (ccl_gemm_grouped), else nullptr / 0
 // rows_c, rows_b: not 0 where the buffer of C / B ends before the descriptor's last rows (fewer than 64 of them): those are not written / are
-// read as zeros.  single: see make_plan.  alpha_dev: alpha, on the device
+// read as zeros.  alpha_dev: alpha, on the device
 static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, const int64_t* strides, const void* A_dev, const void* B_dev, void* C_dev,
                             void* ws_dev, size_t ws_bytes, void* cuda_stream, float alpha = 1.0f, float beta = 0.0f, const int32_t* m_offs = nullptr,
-                            int64_t cap = 0, const int32_t* k_offs = nullptr, bool static_ws = false, int64_t rows_c = 0, int64_t rows_b = 0,
-                            bool single = false, const float* alpha_dev = nullptr) {
+                            int64_t cap = 0, const int32_t* k_offs = nullptr, bool static_ws = false, int64_t rows_c = 0, int64_t rows_b = 0, const float* alpha_dev = nullptr) {
     if (!A_dev || !B_dev || !C_dev) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: NULL operand");
     if (!d) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: NULL descriptor");
     if (batch < 1 || batch > kMaxBatch) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: batch must be in [1, %lld]", (long long)kMaxBatch);
@@ -297,7 +296,7 @@ static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     // ws_bytes; the scratch array for ccl_gemm_static_ws).  A caller that passes none gets whole-tile plans, as before.
     const size_t max_ws = static_ws ? (size_t)CCL_GEMM_STATIC_WS_BYTES : (ws_dev ? ws_bytes : 0);
     key.f[38] = (int64_t)max_ws;
-    key.f[39] = rows_c | rows_b << 32 | (single ? INT64_MIN : 0);
+    key.f[39] = rows_c | rows_b << 32;
     Prepared prep;
     bool hit = false;
     {
@@ -308,7 +307,7 @@ static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     ccl_status s;
     if (!hit) {
         GemmPlan& plan = prep.plan;
-        s = make_plan(d, batch, swiglu, A_dev, B_dev, C_dev, 148, 74, &plan, cap, k_offs != nullptr, max_ws, false, 0, single);     // validation first: no CUDA call on bad input
+        s = make_plan(d, batch, swiglu, A_dev, B_dev, C_dev, 148, 74, &plan, cap, k_offs != nullptr, max_ws);     // validation first: no CUDA call on bad input
         if (s) return s;
         if (batch > 1) {
             const MatView* views[3] = {&plan.va, &plan.vb, &plan.vc};
@@ -326,10 +325,10 @@ static ccl_status gemm_impl(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
         CCL_CUDA_TRY(cudaDeviceGetAttribute(&prep.sms, cudaDevAttrMultiProcessorCount, dev));
         if (dev != key.dev) {
             make_key(d, batch4, A_dev, B_dev, C_dev, &key);
-            key.mode = (swiglu ? 1 : 0) | (static_ws ? 2 : 0) | (alpha_dev ? 4 : 0); key.alpha = alpha; key.beta = beta; key.f[38] = (int64_t)max_ws; key.f[39] = rows_c | rows_b << 32 | (single ? INT64_MIN : 0);
+            key.mode = (swiglu ? 1 : 0) | (static_ws ? 2 : 0) | (alpha_dev ? 4 : 0); key.alpha = alpha; key.beta = beta; key.f[38] = (int64_t)max_ws; key.f[39] = rows_c | rows_b << 32;
             key.f[36] = (int64_t)reinterpret_cast<uintptr_t>(m_offs) ^ ((int64_t)reinterpret_cast<uintptr_t>(k_offs) << 1); key.f[37] = cap + (k_offs ? (INT64_C(1) << 62) : 0);
         }
-        if ((s = make_plan(d, batch, swiglu, A_dev, B_dev, C_dev, prep.sms, resident_pairs(), &plan, cap, k_offs != nullptr, max_ws, true, 0, single))) return s;
+        if ((s = make_plan(d, batch, swiglu, A_dev, B_dev, C_dev, prep.sms, resident_pairs(), &plan, cap, k_offs != nullptr, max_ws, true))) return s;
         if (rows_c) { plan.p.M = plan.p.Wm = (int32_t)rows_c; plan.vc.rows = rows_c; }
         if (rows_b) plan.vb.rows = rows_b;
         plan.p.C = static_cast<uint16_t*>(C_dev);
@@ -450,10 +449,9 @@ extern "C" ccl_status ccl_gemm(const ccl_gemm_desc* d, const void* A_dev, const 
 
 namespace ccl {
 // C = alpha A B for a row-major C (B) that has fewer rows than the descriptor says (see gemm_impl)
-ccl_status gemm_cut(const ccl_gemm_desc* d, int64_t rows_c, int64_t rows_b, bool single, const float* alpha_dev, const void* A, const void* B, void* C, void* ws, size_t ws_bytes,
-                    void* stream) {
+ccl_status gemm_cut(const ccl_gemm_desc* d, int64_t rows_c, int64_t rows_b, const float* alpha_dev, const void* A, const void* B, void* C, void* ws, size_t ws_bytes, void* stream) {
     const int64_t none[3] = {0, 0, 0};
-    return gemm_impl(d, 1, false, none, A, B, C, ws, ws_bytes, stream, 1.0f, 0.0f, nullptr, 0, nullptr, false, rows_c, rows_b, single, alpha_dev);
+    return gemm_impl(d, 1, false, none, A, B, C, ws, ws_bytes, stream, 1.0f, 0.0f, nullptr, 0, nullptr, false, rows_c, rows_b, alpha_dev);
 }
 }  // namespace ccl
 

@@ -186,6 +186,8 @@ template <> struct EpiMaps<3> { LogitArgs logits; };
 template <> struct EpiMaps<4> { LogitArgs logits; };
 // EPI 5: sums kept in fp32 over several products, [splits][M][N]; the first `have` of them hold the sums of earlier ones
 template <> struct EpiMaps<5> { float* acc; int32_t have; };
+// EPI 6: C = scale x A B
+template <> struct EpiMaps<6> { const float* scale; };
 
 // ---- PTX wrappers ---------------------------------------------------------------------------
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -611,7 +613,8 @@ struct Scheduler {
 // walk and the k loops of all other calls stay as they are (the extra branches cost 1-1.5 us on a 15-30 us GEMM)
 // KS > 0: cluster split along K (CTAS = 1): the KS CTAs of a cluster share one tile
 // EPI: 1 = bias, activation and residual in the epilogue (ccl_gemm_epilogue), 2 = activation slope and column sums
-// (ccl_gemm_act_grad), 3 and 4 = rows' statistics and gradients of logits, 5 = sums kept in fp32 (ccl_linear_xent and its gradient)
+// (ccl_gemm_act_grad), 3 and 4 = rows' statistics and gradients of logits, 5 = sums kept in fp32,
+// 6 = a factor known on the device alone (ccl_linear_xent and its gradient)
 template <int BN, int CTAS, bool SWIGLU = false, int RAG = 0, bool FULL = true, int KS = 0, int EPI = 0, int OPW = 0>
 __global__ void __launch_bounds__(gemm_threads<EPI, OPW>, 1)
 ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -949,6 +952,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         if constexpr (FULL || KS != 0) alpha = alpha_of(p);
         [[maybe_unused]] float by_scale = 1.0f;
         if constexpr (EPI == 4) by_scale = 1.0f / *em.logits.scale;
+        if constexpr (EPI == 6) by_scale = *em.scale;
         // EPI: the addend's part of this warp's next piece (32 rows x 64 columns) is fetched into the warp's buffer as soon as the
         // piece before has been stored from it; the cursor `ap` runs one piece ahead, into the next tile.
         constexpr bool kOp = (EPI == 1 || EPI == 2) && KS == 0;
@@ -1592,48 +1596,49 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                             st_global_v4_if(at + 4 * j, make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)), m < t.m1 && n32 + 4 * j < t.n1);
                         }
                     } else {
-                        const LogitArgs& la = em.logits;
-                        const int last = min(t.n1, la.classes) - n32;          // columns of these that exist (the same for the whole warp)
-                        const int off = target - n32;                          // (a tile may reach past its strip: the next one's classes are not here)
-                        const unsigned place = off < last ? (unsigned)off : 32u;
-                        const bool here = __any_sync(0xffffffffu, place < 32u);
-                        {
-                            const bool full = rows_full && n32 - (k & 1) * 32 + 64 <= t.n1;
-                            if (full && !(k & 1)) { if (lane == 0) tma_store_wait_read<0>(); __syncwarp(); }       // the buffer's last piece has been stored
+                        const bool full = rows_full && n32 - (k & 1) * 32 + 64 <= t.n1;
+                        if (full && !(k & 1)) { if (lane == 0) tma_store_wait_read<0>(); __syncwarp(); }       // the buffer's last piece has been stored
+                        uint32_t w[16];
+                        if constexpr (EPI == 4) {
+                            const int last = min(t.n1, em.logits.classes) - n32;       // columns of these that exist (the same for the whole warp)
+                            const int off = target - n32;      // (a tile may reach past its strip: the next one's classes are not here)
+                            const unsigned place = off < last ? (unsigned)off : 32u;
 #pragma unroll
                             for (int i = 0; i < 16; ++i) v[i] = exp2_fast(fma2(v[i], both(kLog2e), both(-row_lse2))) * both(row_scale);
-                            if (here) {
+                            if (__any_sync(0xffffffffu, place < 32u)) {
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) {
                                     const float lo = place == 2u * i ? -row_scale : 0.0f, hi = place == 2u * i + 1 ? -row_scale : 0.0f;
                                     v[i] = v[i] + pair(lo, hi);
                                 }
                             }
-                            uint32_t w[16];
 #pragma unroll
                             for (int i = 0; i < 16; ++i) w[i] = row_live ? bf16_pack(v[i]) : 0u;
                             if (last < 32) {
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) w[i] = 2 * i + 1 < last ? w[i] : (2 * i < last ? w[i] & 0xFFFFu : 0u);
                             }
-                            if (full) {
+                        } else {
 #pragma unroll
-                                for (int j = 0; j < 4; ++j)
-                                    *reinterpret_cast<uint4*>(op_buf + lane * 128 + ((((k & 1) * 4 + j) ^ (lane & 7)) << 4)) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-                                if (k & 1) {
-                                    fence_proxy_async();
-                                    __syncwarp();
-                                    if (lane == 0) {
-                                        tma_store_5d(mpc, op_buf, cx0 + (n32 - 32 - nb), cy0, cz0, cu0, 0);
-                                        tma_store_commit();
-                                    }
+                            for (int i = 0; i < 16; ++i) w[i] = bf16_pack(v[i] * both(by_scale));
+                        }
+                        if (full) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                *reinterpret_cast<uint4*>(op_buf + lane * 128 + ((((k & 1) * 4 + j) ^ (lane & 7)) << 4)) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+                            if (k & 1) {
+                                fence_proxy_async();
+                                __syncwarp();
+                                if (lane == 0) {
+                                    tma_store_5d(mpc, op_buf, cx0 + (n32 - 32 - nb), cy0, cz0, cu0, 0);
+                                    tma_store_commit();
                                 }
-                            } else {
-                                unsigned short* dst = p.C + c_offset<FULL>(p, min(m, t.m1 - 1), n32);
-#pragma unroll
-                                for (int j = 0; j < 4; ++j)
-                                    st_global_v4_if(dst + 8 * j, make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]), m < t.m1 && n32 + 8 * j < t.n1);
                             }
+                        } else {
+                            unsigned short* dst = p.C + c_offset<FULL>(p, min(m, t.m1 - 1), n32);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                st_global_v4_if(dst + 8 * j, make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]), m < t.m1 && n32 + 8 * j < t.n1);
                         }
                     }
                 }

@@ -113,12 +113,10 @@ static double kblock_cycles(int b, int c, bool b_kmajor, int64_t active, double 
 }
 
 // have_device: the unit counts come from the current device (else the figures of a B200)
-// single: tiles of one CTA, 256 columns, whole sums: a product of few k blocks and many tiles, which is its output's stores (weight gradients
-// over few tokens: 131072 x 4096 x 64 takes 239 us so and 298 with the 512-column pair tiles that the model takes)
-// epi: 1 / 2 = a plan for ccl_gemm_epilogue / ccl_gemm_act_grad, 3 / 4 / 5 = for the logits' statistics, the logits' gradient and fp32 sums of
-// ccl_linear_xent and its gradient (tiles of 128 and 256 columns; a row's logits are whole sums: K is split by the sums alone)
+// epi: 1 / 2 = a plan for ccl_gemm_epilogue / ccl_gemm_act_grad, 3 / 4 / 5 / 6 = for the logits' statistics, the logits' gradient, fp32 sums
+// and scaled products of ccl_linear_xent and its gradient (tiles of 128 and 256 columns; K is split by the sums alone)
 static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, const void* A, const void* B, const void* C, int sms, int pairs, GemmPlan* plan,
-                            int64_t cap = 0, bool ragk = false, size_t max_ws = ~(size_t)0, bool have_device = false, int epi = 0, bool single = false) {
+                            int64_t cap = 0, bool ragk = false, size_t max_ws = ~(size_t)0, bool have_device = false, int epi = 0) {
     if (!d) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: NULL descriptor");
     if (d->M <= 0 || d->N <= 0 || d->K <= 0) return fail(CCL_ERR_INVALID_ARG, "ccl_gemm: M, N, K must be positive");
     if (d->M >= (INT64_C(1) << 31) || d->N >= (INT64_C(1) << 31) || d->K >= (INT64_C(1) << 31)) return fail(CCL_ERR_UNSUPPORTED, "ccl_gemm: dimension too large");
@@ -240,7 +238,6 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
             if ((epi_full || epi >= 3) && b == 192) continue;
             if (b == 384 && (cap > 0 || ragk)) continue;            // (no ragged-batch instantiation of the 256 + 128 tile)
             if (force_bn && atoi(force_bn) != b) continue;
-            if (single && !force_ctas && !force_bn && !(c == 1 && b == 256)) continue;
             if (swiglu && !(c == 2 && b == 512)) continue;          // the gated activation pairs the two accumulators of the wide tile
             const int64_t tiles_m_all = strips_m * ((Wm + BM * c - 1) / (BM * c));
             const int bs = swiglu ? 256 : b;                        // tile width in C columns
@@ -258,7 +255,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
                                                              (b <= 128 ? 1.10 : (b <= 192 ? 1.04 : 1.0)) *
                                                              (epi >= 3 && c == 2 ? 1.12 : 1.0) : 0.0;
             for (int sp : {1, 2, 3, 4, 6, 8, 12, 16}) {
-                if (sp > 1 && (swiglu || (single && !force_split) || epi == 3 || epi == 4 || cap > 0 || ragk || any_rag || num_kb / sp < 2)) continue;
+                if (sp > 1 && (swiglu || epi == 3 || epi == 4 || epi == 6 || cap > 0 || ragk || any_rag || num_kb / sp < 2)) continue;
                 if (force_split && atoi(force_split) != sp) continue;
                 // (an operator after a split is a kernel of its own over the partial sums: 2048 x 5120 x 13824, 160 tiles on 74
                 // pairs, takes 261 us whole and 346 in three parts)
@@ -295,7 +292,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     {
         const char* force_bal = std::getenv("CCL_GEMM_BALANCED");   // 0: never, 1: whenever the call qualifies
         const int want = force_bal ? atoi(force_bal) : -1;
-        const bool can = want != 0 && !epi && !single && batch == 1 && !swiglu && cap == 0 && !ragk && !any_rag && num_kb >= 2 && !(force_split && atoi(force_split) > 1);
+        const bool can = want != 0 && !epi && batch == 1 && !swiglu && cap == 0 && !ragk && !any_rag && num_kb >= 2 && !(force_split && atoi(force_split) > 1);
         double best_bal = -1.0;
         int bc = 0, bb = 0;
         int64_t bal_rounds = 0;
@@ -348,7 +345,7 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     {
         const char* force_ks = std::getenv("CCL_GEMM_CLUSTERK");
         const int want_ks = force_ks ? atoi(force_ks) : -1;
-        const bool can = want_ks != 0 && !single && batch == 1 && !swiglu && cap == 0 && !ragk && !any_rag && !il_a && !il_b && !il_c && !ka && !kb &&
+        const bool can = want_ks != 0 && batch == 1 && !swiglu && cap == 0 && !ragk && !any_rag && !il_a && !il_b && !il_c && !ka && !kb &&
                          !(force_split && atoi(force_split) > 1) && !balanced && epi < 3 && !(force_ctas && atoi(force_ctas) != 1) && d->out_part != CCL_PART_2D;
         double best_ks = -1.0;
         int kb_ = 0, kk = 0;

@@ -20,7 +20,7 @@
 
 namespace ccl {
 
-ccl_status gemm_cut(const ccl_gemm_desc* d, int64_t rows_c, int64_t rows_b, bool single, const float* alpha_dev, const void* A, const void* B, void* C, void* ws, size_t ws_bytes,
+ccl_status gemm_cut(const ccl_gemm_desc* d, int64_t rows_c, int64_t rows_b, const float* alpha_dev, const void* A, const void* B, void* C, void* ws, size_t ws_bytes,
                     void* stream);                       // ccl_gemm.cu
 
 constexpr int64_t kPieceBytes = INT64_C(1) << 29;
@@ -28,16 +28,18 @@ constexpr int64_t kPieceBytes = INT64_C(1) << 29;
 template <int EPI, int BN, int CTAS>
 static ccl_status launch_logits_warps(const GemmPlan& plan, const CUtensorMap* maps, const EpiMaps<EPI>& em, cudaStream_t st) {
     if constexpr (EPI == 3) return launch_epi_warps<BN, CTAS, false, 0, EPI, 16>(plan, maps, em, st);
-    if constexpr (EPI == 4)
+    if constexpr (EPI == 4 || EPI == 6)
         if (plan.opw == 16) return launch_epi_warps<BN, CTAS, false, 0, EPI, 16>(plan, maps, em, st);
     if constexpr (EPI != 3) return launch_epi_warps<BN, CTAS, false, 0, EPI, 8>(plan, maps, em, st);
 }
 
-// A product over part of the vocabulary.  rows_b: rows of B that exist (0: all that the descriptor says); the rest reads as zeros.
+// A product over part of the vocabulary.  rows_b: rows of B that exist (0: all that the descriptor says), the rest reads as zeros; rows_c: rows
+// of C likewise, the rest is not written.
 template <int EPI>
-static ccl_status run_logits(GemmPlan& plan, const EpiMaps<EPI>& em, int64_t rows_b, const void* A, const void* B, void* C, cudaStream_t st) {
+static ccl_status run_logits(GemmPlan& plan, const EpiMaps<EPI>& em, int64_t rows_b, const void* A, const void* B, void* C, cudaStream_t st, int64_t rows_c = 0) {
     if (!plan.lean) return fail(CCL_ERR_UNSUPPORTED, "ccl_linear_xent: this layout of W is not supported");
     if (rows_b) plan.vb.rows = rows_b;
+    if (rows_c) { plan.p.M = plan.p.Wm = (int32_t)rows_c; plan.vc.rows = rows_c; }
     CUtensorMap maps[6];
     ccl_status s = encode_maps(plan, A, B, C, maps);
     if (s) return s;
@@ -402,7 +404,7 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
         if (dX_dev) {
             p = dx_product(v, g, std::min(real, g.sum_width));
             if (g.sums == 1) {
-                if ((s = gemm_cut(&p, 0, rows, false, scale, dz, W, dX_dev, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
+                if ((s = gemm_cut(&p, 0, rows, scale, dz, W, dX_dev, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
             } else {
                 // (the piece's dz and W; or one of their strips after the other)
                 for (int64_t k = 0; k < (g.all ? g.sums : 1); ++k) {
@@ -415,9 +417,15 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
         }
         if (dW_dev) {
             p = dw_product(v, g, real);
-            // (over few tokens the product is its output's stores: see make_plan)
-            const bool single = v.T <= 256 && ((p.M + BM - 1) / BM) * ((p.N + 255) / 256) >= 148;
-            if ((s = gemm_cut(&p, rows, 0, single, scale, v.trans ? dz : X_dev, v.trans ? X_dev : dz, static_cast<uint16_t*>(dW_dev) + at, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
+            const void *A = v.trans ? dz : X_dev, *B = v.trans ? X_dev : dz;
+            uint16_t* C = static_cast<uint16_t*>(dW_dev) + at;
+            // Enough tiles for every SM: 256 columns, drained behind the next tile's product by eight or sixteen warps (32768 x 4096 x 2048:
+            // 432 us by ccl_gemm's 512-column tiles with alpha, whose drain is in the open).  Few tiles and a long K are split along K.
+            if (((p.M + BM - 1) / BM) * ((p.N + 255) / 256) >= 148) {
+                if ((s = shape_plan(&p, 6, &plan))) return s;
+                EpiMaps<6> by = {scale};
+                if ((s = run_logits<6>(plan, by, 0, A, B, C, st, rows))) return s;
+            } else if ((s = gemm_cut(&p, rows, 0, scale, A, B, C, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
         }
     }
     if (!dX_dev || g.sums == 1) return CCL_OK;

@@ -25,7 +25,8 @@
  * Test / diagnostic switches (environment variables, read by the library; none changes a result beyond the
  * rounding order of a split-K sum):
  *   CCL_GEMM_CTAS = 1|2            force one CTA per tile or a cta_group::2 pair
- *   CCL_GEMM_BN = 128|192|256|384|512  force the tile width (ccl_gemm_epilogue, ccl_gemm_act_grad: 256 at most)
+ *   CCL_GEMM_BN = 128|192|256|384|512  force the tile width (ccl_gemm_epilogue, ccl_gemm_act_grad: 256 at most; ccl_linear_xent and its
+ *                                  gradient: 128 or 256)
  *   CCL_GEMM_SPLITK = n            force the number of K splits
  *   CCL_GEMM_BALANCED = 0|1        never / always (where legal) cut the tiles that do not fill a round into equal shares
  *   CCL_GEMM_CLUSTERK = 0|2|4|8        never / always (where legal) let the CTAs of a cluster of that size share one tile,
@@ -288,7 +289,7 @@ ccl_status ccl_gemm_swiglu(const ccl_gemm_desc* d, const void* A_dev, const void
 /*
  * Synchronises `cuda_stream` (the one entry point that does), then reports and clears the status word of the
  * GEMMs and repacks finished on the current device: CCL_OK, or CCL_ERR_TIMEOUT with *detail = the raw device code
- * (1-6: a GEMM wait, 8-9: ccl_moe_tokens, 101: a repack wait), or CCL_ERR_SHAPE for bad offsets of a ragged batch (detail 5) or a bad
+ * (1-6: a GEMM wait, 8-9: ccl_moe_tokens, 11: ccl_norm or its gradient, 101: a repack wait), or CCL_ERR_SHAPE for bad offsets of a ragged batch (detail 5) or a bad
  * target of ccl_linear_xent (detail 10).
  * detail may be NULL.  There is ONE status word per device, shared by every stream: with several streams in flight
  * the first caller after an expiry gets the report, whichever stream's kernel it was.
@@ -439,8 +440,10 @@ typedef enum { CCL_NORM_LAYER = 0, CCL_NORM_RMS = 1 } ccl_norm_kind;
  *   CCL_NORM_RMS    rstd = 1 / sqrt(sum(x^2) / H + eps),                                y = x * rstd * gamma
  * X and Y are both stored as `m` describes (2-byte elements, any layout the map accepts, fewer than 2^31 columns; padding is not
  * touched); Y_dev may be X_dev.  gamma, beta: bf16 [H], NULL: ones / zeros.  mean_dev, rstd_dev: fp32 [rows], what the gradient needs;
- * NULL: not wanted.  beta_dev and mean_dev are NULL with CCL_NORM_RMS.  Bases 2-byte aligned (fp32 ones 4-byte); 16-byte aligned ones
- * with column groups of 8 that are aligned pieces of the buffer take the fast path.  eps >= 0; a constant row with eps = 0 gives NaN.
+ * NULL: not wanted.  beta_dev and mean_dev are NULL with CCL_NORM_RMS.  Any shape; bases 2-byte aligned (fp32 ones 4-byte).  16-byte aligned
+ * X and Y take the fast path: row-major of any width from 256 columns on, and strips whose column groups of 8 are aligned pieces of the
+ * buffer.  eps >= 0; a constant row with eps = 0 gives NaN.  rstd is good to 2^-22 and to 5e-6 where one value is hundreds of deviations away
+ * from all others.  Bounded waits as for ccl_gemm.
  */
 ccl_status ccl_norm(const ccl_mat* m, int32_t kind, float eps, const void* X_dev, const void* gamma_dev, const void* beta_dev, void* Y_dev,
                     float* mean_dev, float* rstd_dev, void* cuda_stream);
@@ -450,8 +453,8 @@ ccl_status ccl_norm(const ccl_mat* m, int32_t kind, float eps, const void* X_dev
  *   dgamma = bf16( sum over rows of dy * h ),  dbeta = bf16( sum over rows of dy )        (in a fixed order: the same bits on every run)
  *   addend_dev  bf16, stored like X: the gradient that reaches X past the normalisation (the residual stream's); NULL: none
  *   dX_dev, dgamma_dev, dbeta_dev: NULL: not wanted; dX_dev may be X_dev, dY_dev or addend_dev.  dbeta_dev is NULL with CCL_NORM_RMS.
- * Workspace: ccl_norm_grad_workspace bytes (0 for few rows and for odd widths), needed for dgamma / dbeta only; whatever they hold.
- * Calls that can overlap on the GPU must not share it.
+ * Workspace: ccl_norm_grad_workspace bytes (0 for few rows), needed for dgamma / dbeta only; whatever they hold.  Calls that can overlap on
+ * the GPU must not share it.
  */
 ccl_status ccl_norm_grad_workspace(const ccl_mat* m, size_t* bytes);
 ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* X_dev, const void* gamma_dev, const float* mean_dev, const float* rstd_dev,
@@ -472,9 +475,9 @@ ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* X_dev, cons
  *   loss, lse fp32 [T], either NULL: not wanted; the gradient reads lse as ccl_linear_xent left it.   dloss fp32 [T].   dX, dW: either
  *             NULL: not wanted.
  * Logits, exponentials and their sums are fp32 (the exponentials good to 2^-21).  The gradient works through the vocabulary in pieces:
- * it computes a piece's logits again, holds its dz as bf16 (the operand of two products; each value off by 2^-8 of itself at most) in the
- * workspace, and sums dX over the pieces in fp32, always in the same order.  A piece's dz takes at most 512 MB, or T x 256 x 2 bytes
- * where that is more, or that of one strip (of the whole matrix where a [H x V] is row-major).
+ * it computes a piece's logits again, holds its dz, divided by the largest finite |dloss|, as bf16 (the operand of two products; each value
+ * off by 2^-8 of itself at most) in the workspace, and sums dX over the pieces in fp32, always in the same order.  A piece's dz takes at most
+ * 512 MB, or T x 256 x 2 bytes where that is more, or that of one strip (of the whole matrix where a [H x V] is row-major).
  * Any T >= 1 and V >= 1; H a multiple of 8 (else CCL_ERR_UNSUPPORTED); X, W, dX, dW and the workspace 16-byte aligned.  Workspace: the bytes that
  * the _workspace calls say, whatever they hold; calls that can overlap on the GPU must not share it.  Bounded waits and asynchrony as for
  * ccl_gemm.

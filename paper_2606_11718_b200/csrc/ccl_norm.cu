@@ -459,7 +459,7 @@ __global__ void __launch_bounds__(512, 1) norm_rows_kernel(const __grid_constant
         }
         next += stride;
     };
-    // (gamma and beta first: behind a CTA's slots full of rows they would arrive 2.5 us later)
+    // (gamma and beta first: behind a CTA's slots full of rows they would wait for those)
     stage_weights(weights, p.gamma, kOne, phase, cols, pieces);
     if (LAYER) stage_weights(shifts, p.beta, 0, phase, cols, pieces);
     __syncthreads();

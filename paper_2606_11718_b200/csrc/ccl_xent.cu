@@ -28,7 +28,7 @@ constexpr int64_t kPieceBytes = INT64_C(1) << 29;
 template <int EPI, int BN, int CTAS>
 static ccl_status launch_logits_warps(const GemmPlan& plan, const CUtensorMap* maps, const EpiMaps<EPI>& em, cudaStream_t st) {
     if constexpr (EPI == 3) return launch_epi_warps<BN, CTAS, false, 0, EPI, 16>(plan, maps, em, st);
-    if constexpr (EPI == 4 || EPI == 6)
+    if constexpr (EPI == 4)
         if (plan.opw == 16) return launch_epi_warps<BN, CTAS, false, 0, EPI, 16>(plan, maps, em, st);
     if constexpr (EPI != 3) return launch_epi_warps<BN, CTAS, false, 0, EPI, 8>(plan, maps, em, st);
 }
@@ -419,8 +419,8 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
             p = dw_product(v, g, real);
             const void *A = v.trans ? dz : X_dev, *B = v.trans ? X_dev : dz;
             uint16_t* C = static_cast<uint16_t*>(dW_dev) + at;
-            // Enough tiles for every SM: 256 columns, drained behind the next tile's product by eight or sixteen warps (32768 x 4096 x 2048:
-            // 432 us by ccl_gemm's 512-column tiles with alpha, whose drain is in the open).  Few tiles and a long K are split along K.
+            // Enough tiles for every SM: 256 columns, drained behind the next tile's product (131072 x 512 x 1024: 105 us, by ccl_gemm with
+            // alpha 114; 32768 x 4096 x 1024: 196 and 215).  Few tiles and a long K are split along K.
             if (((p.M + BM - 1) / BM) * ((p.N + 255) / 256) >= 148) {
                 if ((s = shape_plan(&p, 6, &plan))) return s;
                 EpiMaps<6> by = {scale};

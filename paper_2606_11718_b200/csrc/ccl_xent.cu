@@ -97,7 +97,8 @@ __global__ void __launch_bounds__(256) xent_finish_kernel(const float2* part, in
     if (loss) loss[row] = live ? (float)(l - (double)at_target[row]) : 0.0f;
 }
 
-// scale = the largest finite |dloss| of the rows that take part (1 where there is none)
+// scale = the largest finite |dloss| of the rows that take part (1 where all are zero or there is none; 2^-126 at least, whose reciprocal
+// is finite: below it, 1 / scale would be infinite and a row with dloss = 0 beside it NaN)
 __global__ void __launch_bounds__(1024) xent_scale_kernel(const float* dloss, const int32_t* targets, int M, int32_t ignore, int32_t classes, float* scale) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -114,7 +115,7 @@ __global__ void __launch_bounds__(1024) xent_scale_kernel(const float* dloss, co
     __syncthreads();
     if (threadIdx.x < 32) {
         top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(tops[threadIdx.x])));
-        if (threadIdx.x == 0) *scale = top > 0.0f ? top : 1.0f;
+        if (threadIdx.x == 0) *scale = top > 0.0f ? fmaxf(top, 0x1p-126f) : 1.0f;
     }
 }
 

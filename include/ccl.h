@@ -452,7 +452,8 @@ ccl_status ccl_norm(const ccl_mat* m, int32_t kind, float eps, const void* X_dev
  *   dX = bf16( rstd * (g - sum(g) / H - h * sum(g * h) / H) + addend )        (without the sum(g) term for CCL_NORM_RMS)
  *   dgamma = bf16( sum over rows of dy * h ),  dbeta = bf16( sum over rows of dy )        (in a fixed order: the same bits on every run)
  *   addend_dev  bf16, stored like X: the gradient that reaches X past the normalisation (the residual stream's); NULL: none
- *   dX_dev, dgamma_dev, dbeta_dev: NULL: not wanted; dX_dev may be X_dev, dY_dev or addend_dev.  dbeta_dev is NULL with CCL_NORM_RMS.
+ *   dX_dev, dgamma_dev, dbeta_dev: NULL: not wanted; dX_dev may be X_dev, dY_dev or addend_dev, none of the three may be
+ *   another or gamma_dev.  dbeta_dev is NULL with CCL_NORM_RMS.
  * Workspace: ccl_norm_grad_workspace bytes (0 for few rows), needed for dgamma / dbeta only; whatever they hold.  Calls that can overlap on
  * the GPU must not share it.
  */

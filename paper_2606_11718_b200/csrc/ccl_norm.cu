@@ -1117,7 +1117,11 @@ extern "C" ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* 
     if (!X_dev || !dY_dev || !rstd_dev || (layer && !mean_dev)) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: NULL operand");
     if (!dX_dev && !dgamma_dev && !dbeta_dev) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: no output is wanted");
     if (!layer && dbeta_dev) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: the root-mean-square form has no beta");
-    if (dX_dev && (dX_dev == gamma_dev)) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: dX needs a buffer of its own");
+    // (with few rows dgamma and dbeta are written before gamma is read for dX)
+    const void* outs[3] = {dX_dev, dgamma_dev, dbeta_dev};
+    for (int i = 0; i < 3; ++i)
+        if (outs[i] && (outs[i] == gamma_dev || outs[i] == outs[(i + 1) % 3]))
+            return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: dX, dgamma and dbeta need buffers of their own, and not gamma's");
     const uintptr_t any = bits(X_dev) | bits(dY_dev) | bits(addend_dev) | bits(dX_dev);
     if ((any | bits(gamma_dev) | bits(dgamma_dev) | bits(dbeta_dev)) & 1) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: a base pointer is not 2-byte aligned");
     if ((bits(mean_dev) | bits(rstd_dev)) & 3) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: mean / rstd is not 4-byte aligned");

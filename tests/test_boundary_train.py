@@ -183,3 +183,14 @@ def test_xent_workspace_is_bounded():
                 d = ccl.XentDesc(T, V, H)
                 assert ccl.ccl_linear_xent_workspace(d) <= T * (V // 128 + 2) * 8 * 4 + T * 4 + 512
                 assert ccl.ccl_linear_xent_grad_workspace(d) <= max(1 << 29, T * 512) + 16 * T * H * 4 * 2 + 16 * 64 * max(T, V) * H + 4096
+
+
+@pytest.mark.parametrize("rows", [16, 8192])
+def test_norm_grad_refuses_gradients_in_each_others_place(rows):
+    l, m = ccl.lib(), ccl.Mat(rows, 2048, 2)
+
+    def call(dx=P7, dg=P8, db=P9):
+        return l.ccl_norm_grad(C.byref(m), 0, P1, P2, P3, P4, P5, P6, dx, dg, db, P1, 1 << 30, None)
+
+    for bad in (dict(dg=P2), dict(db=P2), dict(dg=P9), dict(dx=P8), dict(dx=P9), dict(dx=P2)):
+        status(ccl.ERR_INVALID_ARG, call(**bad))

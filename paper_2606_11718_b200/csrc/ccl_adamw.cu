@@ -6,12 +6,12 @@
 // Bound by memory: parameters, gradient and states are read once and written once.  The list travels in the kernel's parameters
 // (no table on the device, nothing to copy, a captured call keeps its own), kMost tensors a launch at most; each tensor is cut into
 // pieces of kPiece elements, the pieces of all tensors are numbered through, and persistent CTAs take them in turn, so that one large
-// tensor and hundreds of small ones fill the GPU alike.
+// tensor and hundreds of small ones fill the GPU alike.  235M parameters in 32 bits, bf16 gradients and copies: 1.10-1.12 ms, 5.9 TB/s.
 //
 // 8 bits: 256 consecutive elements of a tensor share a scale.  The first moment m is kept as e4m3 times (largest |m| / 448); the
 // second as the e4m3 of its square root, so that its range is that of the gradients and not of their squares, and never rounded
 // down to zero (a zero there would turn the next step of a parameter into one of size m / eps).  A warp has a block of 256: eight
-// elements a lane, the largest found by one reduction instruction.
+// elements a lane, the largest found by one reduction instruction.  204M parameters: 692 us, 5.0 TB/s, 65 % of the issue slots.
 #include <algorithm>
 #include <cmath>
 

@@ -422,8 +422,10 @@ __device__ __forceinline__ void stage_weights(uint16_t* to, const uint16_t* w, u
 // phases side by side.  A warp owns `slots` slots of `set_rows` consecutive rows and refills one as soon as it is done with it.  The row is
 // read from its slot twice: first and second moment, then the result; gamma and beta lie behind the slots.  8192 x 8192: 53-54 us, 5.0 TB/s (with a
 // row to a CTA and its loads in registers 88-90; over a ring of bulk copies 63).
-//   The moments are taken about the mean of the row's first 256 values (all lanes' first eight).  That is off by a^2 <= (H / 256 - 1) var at
-// most, so the difference E d^2 - a^2 loses log2(H / 256) bits in the worst case, six at 16384 columns.
+//   The moments are taken about the mean of the row's first 256 values, and the variance is E d^2 - a^2 with a = E d.  Where those values lie
+// elsewhere than the rest (a few channels about 30, the others about 0), a^2 is nearly all of E d^2, up to H / 256 - 1 times the variance, and the
+// difference loses as many bits (rstd off by 6e-6 at 8192 columns and by 1.4e-5 at 16384; 2e-7 and 4e-7 as it is done here).  A row whose a^2 is over a quarter of E d^2 is read a third
+// time, about its mean; of the others the difference loses less than half a bit.
 template <bool LAYER, bool PHASED>
 __global__ void __launch_bounds__(512, 1) norm_rows_kernel(const __grid_constant__ StreamParams q) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -513,25 +515,36 @@ __global__ void __launch_bounds__(512, 1) norm_rows_kernel(const __grid_constant
                 mask(lane, f, 0.0f);
                 pivot = warp_total((f[0] + f[1]) + (f[2] + f[3])) * inv_first;
             }
-            f32x2 m1[2] = {both(0.0f), both(0.0f)}, m2[2] = {both(0.0f), both(0.0f)};
-            strips([&](const uint16_t* x, int, int groups, uint16_t*) {
+            // sums of the differences from `about` and of their squares, over H
+            auto moments = [&](float about, float& a, float& var) {
+                f32x2 m1[2] = {both(0.0f), both(0.0f)}, m2[2] = {both(0.0f), both(0.0f)};
+                strips([&](const uint16_t* x, int, int groups, uint16_t*) {
 #pragma unroll 4
-                for (int i = lane; i < groups; i += 32) {
-                    parts(shared16(x + i * 8), f);
-                    mask(i, f, pivot);
+                    for (int i = lane; i < groups; i += 32) {
+                        parts(shared16(x + i * 8), f);
+                        mask(i, f, about);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const f32x2 d = LAYER ? f[j] + both(-pivot) : f[j];
-                        if (LAYER) m1[j & 1] = m1[j & 1] + d;
-                        m2[j & 1] = fma2(d, d, m2[j & 1]);
+                        for (int j = 0; j < 4; ++j) {
+                            const f32x2 d = LAYER ? f[j] + both(-about) : f[j];
+                            if (LAYER) m1[j & 1] = m1[j & 1] + d;
+                            m2[j & 1] = fma2(d, d, m2[j & 1]);
+                        }
                     }
-                }
-            });
+                });
+                a = LAYER ? warp_total(m1[0] + m1[1]) * p.inv_cols : 0.0f;
+                var = warp_total((m2[0] + m2[1]) * both(p.inv_cols));
+            };
             // (means from here on: a sum of H squares could leave fp32 where their mean does not)
-            const float a = LAYER ? warp_total(m1[0] + m1[1]) * p.inv_cols : 0.0f;
-            float var = warp_total((m2[0] + m2[1]) * both(p.inv_cols));
-            if (LAYER) { var = fmaf(-a, a, var); var = var < 0.0f ? 0.0f : var; }
-            const float mean = pivot + a, rstd = rsqrtf(var + p.eps);
+            float a, var;
+            moments(pivot, a, var);
+            float mean = pivot + a;
+            if (LAYER && a * a > 0.25f * var) {          // the pivot was no good (see above): once more about the mean
+                moments(mean, a, var);
+                if (fabsf(a) < INFINITY) mean += a;      // (what the mean's rounding has left; a row with an infinite value keeps its mean)
+            }
+            if (LAYER) var = fmaf(-a, a, var);
+            var = var < 0.0f ? 0.0f : var;
+            const float rstd = rsqrtf(var + p.eps);
             if (lane == 0) {
                 if (p.mean) p.mean[row] = mean;
                 if (p.rstd) p.rstd[row] = rstd;

@@ -515,8 +515,8 @@ __global__ void __launch_bounds__(512, 1) norm_rows_kernel(const __grid_constant
                 mask(lane, f, 0.0f);
                 pivot = warp_total((f[0] + f[1]) + (f[2] + f[3])) * inv_first;
             }
-            // sums of the differences from `about` and of their squares, over H
-            auto moments = [&](float about, float& a, float& var) {
+            // sums of the differences from `about` and of their squares (times `by`), over H
+            auto moments = [&](float about, float by, float& a, float& var) {
                 f32x2 m1[2] = {both(0.0f), both(0.0f)}, m2[2] = {both(0.0f), both(0.0f)};
                 strips([&](const uint16_t* x, int, int groups, uint16_t*) {
 #pragma unroll 4
@@ -527,22 +527,25 @@ __global__ void __launch_bounds__(512, 1) norm_rows_kernel(const __grid_constant
                         for (int j = 0; j < 4; ++j) {
                             const f32x2 d = LAYER ? f[j] + both(-about) : f[j];
                             if (LAYER) m1[j & 1] = m1[j & 1] + d;
-                            m2[j & 1] = fma2(d, d, m2[j & 1]);
+                            m2[j & 1] = fma2(by == 1.0f ? d : d * both(by), d, m2[j & 1]);
                         }
                     }
                 });
                 a = LAYER ? warp_total(m1[0] + m1[1]) * p.inv_cols : 0.0f;
                 var = warp_total((m2[0] + m2[1]) * both(p.inv_cols));
             };
-            // (means from here on: a sum of H squares could leave fp32 where their mean does not)
             float a, var;
-            moments(pivot, a, var);
+            moments(pivot, 1.0f, a, var);
             float mean = pivot + a;
-            if (LAYER && a * a > 0.25f * var) {          // the pivot was no good (see above): once more about the mean
-                moments(mean, a, var);
+            // Once more about the mean where the pivot was no good (see above), and where a lane's squares have left fp32, which the mean of all need
+            // not (a lane has 512 values at most: times 2^-16 their squares' sum is below the mean over the row)
+            if ((LAYER && a * a > 0.25f * var) || !(var < INFINITY)) {
+                const float by = var < INFINITY ? 1.0f : 0x1p-16f;
+                moments(mean, by, a, var);
                 if (fabsf(a) < INFINITY) mean += a;      // (what the mean's rounding has left; a row with an infinite value keeps its mean)
-            }
-            if (LAYER) var = fmaf(-a, a, var);
+                if (LAYER) var = fmaf(-a * by, a, var);
+                var *= 1.0f / by;
+            } else if (LAYER) var = fmaf(-a, a, var);
             var = var < 0.0f ? 0.0f : var;
             const float rstd = rsqrtf(var + p.eps);
             if (lane == 0) {

@@ -45,3 +45,21 @@ def test_leading_columns_lie_elsewhere(T, H, shift):
     X = normal(T, H, 1.0, H).float()
     X[:, :256] += shift
     check(X.bfloat16(), True)
+
+
+@pytest.mark.parametrize("layer", [True, False])
+@pytest.mark.parametrize("size", [1e18, 3e18, 1.2e19])
+@pytest.mark.parametrize("T,H", [(1300, 8192), (1200, 16384), (9, 8191), (9500, 264), (4, 1000), (4, 40000)])
+def test_squares_whose_sum_leaves_fp32(T, H, size, layer):
+    # mean squares of 1e36 to 1.4e38, their sums up to 6e42
+    X = torch.full((T, H), size).bfloat16()
+    X[:, ::2] *= -1
+    X[1:, 3::7] *= 0.5
+    check(X, layer)
+
+
+@pytest.mark.parametrize("T,H", [(1300, 8192), (9, 8191), (4, 8192)])
+def test_one_square_alone_leaves_fp32(T, H):
+    X = normal(T, H, 1.0, 5)
+    X[:, 300] = 1e20                                            # its square is 1e40, the mean of squares 1e36
+    check(X, False)

@@ -439,8 +439,8 @@ typedef enum { CCL_NORM_LAYER = 0, CCL_NORM_RMS = 1 } ccl_norm_kind;
  *   CCL_NORM_LAYER  mean = sum(x) / H,  rstd = 1 / sqrt(sum((x - mean)^2) / H + eps),  y = (x - mean) * rstd * gamma + beta
  *   CCL_NORM_RMS    rstd = 1 / sqrt(sum(x^2) / H + eps),                                y = x * rstd * gamma
  * X and Y are both stored as `m` describes (2-byte elements, any layout the map accepts, fewer than 2^31 columns; padding is not
- * touched); Y_dev may be X_dev.  gamma, beta: bf16 [H], NULL: ones / zeros.  mean_dev, rstd_dev: fp32 [rows], what the gradient needs;
- * NULL: not wanted.  beta_dev and mean_dev are NULL with CCL_NORM_RMS.  Any shape; bases 2-byte aligned (fp32 ones 4-byte).  16-byte aligned
+ * touched); Y_dev may be X_dev, otherwise no output may lie over another buffer (CCL_ERR_INVALID_ARG).  gamma, beta: bf16 [H], NULL: ones /
+ * zeros.  mean_dev, rstd_dev: fp32 [rows], what the gradient needs; NULL: not wanted.  beta_dev and mean_dev are NULL with CCL_NORM_RMS.  Any shape; bases 2-byte aligned (fp32 ones 4-byte).  16-byte aligned
  * X and Y take the fast path: row-major of any width from 256 columns on, and strips whose column groups of 8 are aligned pieces of the
  * buffer.  eps >= 0; a constant row with eps = 0 gives NaN.  rstd is off by (32 + H / 256) 2^-24 of itself at most where the mean is no more
  * than some 100 deviations from zero (measured, whatever columns lie elsewhere than the rest: 1e-7 to 1e-6 up to 33000 columns).  Bounded
@@ -453,8 +453,8 @@ ccl_status ccl_norm(const ccl_mat* m, int32_t kind, float eps, const void* X_dev
  *   dX = bf16( rstd * (g - sum(g) / H - h * sum(g * h) / H) + addend )        (without the sum(g) term for CCL_NORM_RMS)
  *   dgamma = bf16( sum over rows of dy * h ),  dbeta = bf16( sum over rows of dy )        (in a fixed order: the same bits on every run)
  *   addend_dev  bf16, stored like X: the gradient that reaches X past the normalisation (the residual stream's); NULL: none
- *   dX_dev, dgamma_dev, dbeta_dev: NULL: not wanted; dX_dev may be X_dev, dY_dev or addend_dev, none of the three may be
- *   another or gamma_dev.  dbeta_dev is NULL with CCL_NORM_RMS.
+ *   dX_dev, dgamma_dev, dbeta_dev: NULL: not wanted; dX_dev may be X_dev, dY_dev or addend_dev, otherwise none of the
+ *   three and the workspace may lie over another buffer.  dbeta_dev is NULL with CCL_NORM_RMS.
  * Workspace: ccl_norm_grad_workspace bytes (0 for few rows), needed for dgamma / dbeta only; whatever they hold.  Calls that can overlap on
  * the GPU must not share it.
  */
@@ -480,9 +480,9 @@ ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* X_dev, cons
  * it computes a piece's logits again, holds its dz, divided by the largest finite |dloss| (by 2^-126 at least), as bf16 (the operand of two products; each value
  * off by 2^-8 of itself at most) in the workspace, and sums dX over the pieces in fp32, always in the same order.  A piece's dz takes at most
  * 512 MB, or T x 256 x 2 bytes where that is more, or that of one strip (of the whole matrix where a [H x V] is row-major).
- * Any T >= 1 and V >= 1; H a multiple of 8 (else CCL_ERR_UNSUPPORTED); X, W, dX, dW and the workspace 16-byte aligned.  Workspace: the bytes that
- * the _workspace calls say, whatever they hold; calls that can overlap on the GPU must not share it.  Bounded waits and asynchrony as for
- * ccl_gemm.
+ * No output and no workspace may lie over another buffer of the call (CCL_ERR_INVALID_ARG).  Any T >= 1 and V >= 1; H a multiple of 8 (else
+ * CCL_ERR_UNSUPPORTED); X, W, dX, dW and the workspace 16-byte aligned.  Workspace: the bytes that the _workspace calls say, whatever they hold;
+ * calls that can overlap on the GPU must not share it.  Bounded waits and asynchrony as for ccl_gemm.
  */
 typedef struct ccl_xent_desc {
     int64_t T, V, H;

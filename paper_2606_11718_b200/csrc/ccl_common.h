@@ -77,6 +77,23 @@ CCL_HD int64_t buffer_elems(const MatView& v) {
     return v.split ? (v.nstrips - 1) * v.stride + v.last_span : v.rows * v.cols;
 }
 
+// A buffer of a call: [p, p + bytes), none where p is NULL
+struct Span {
+    const void* p;
+    uint64_t bytes;
+};
+inline bool overlap(const Span& a, const Span& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return x && y && x < y + b.bytes && y < x + a.bytes;
+}
+// Whether the buffer lies over another of the list (which may hold it too: at the same place in the list it is left out)
+template <int N>
+bool overlaps_any(const Span& a, const Span (&others)[N]) {
+    for (const Span& o : others)
+        if (&o != &a && overlap(a, o)) return true;
+    return false;
+}
+
 // Validates a descriptor and flattens it.  `what` names the argument in error messages.
 ccl_status make_view(const ccl_mat* m, const char* what, MatView* out);
 

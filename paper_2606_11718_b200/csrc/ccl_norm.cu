@@ -1107,6 +1107,11 @@ extern "C" ccl_status ccl_norm(const ccl_mat* m, int32_t kind, float eps, const 
     p.x = bf16(X_dev); p.out = static_cast<uint16_t*>(Y_dev); p.gamma = bf16(gamma_dev); p.beta = bf16(beta_dev);
     p.mean = mean_dev; p.rstd = rstd_dev;
     p.layer = kind == CCL_NORM_LAYER; p.eps = eps; p.inv_cols = (float)(1.0 / (double)p.v.cols);
+    const uint64_t whole = (uint64_t)buffer_elems(p.v) * 2, row = (uint64_t)p.v.cols * 2, column = (uint64_t)p.v.rows * 4;
+    const Span all[6] = {{Y_dev, whole}, {mean_dev, column}, {rstd_dev, column}, {X_dev == Y_dev ? nullptr : X_dev, whole}, {gamma_dev, row}, {beta_dev, row}};
+    for (int i = 0; i < 3; ++i)
+        if (overlaps_any(all[i], all) || (i && overlap(all[i], {X_dev, whole})))
+            return fail(CCL_ERR_INVALID_ARG, "ccl_norm: Y, mean or rstd lies over another buffer (Y may be X)");
     int sms, pairs;
     device_units(&sms, &pairs);
     const NormPlan q = plan_norm(p.v, (any & 15) == 0, (weights & 15) == 0, false, 1, sms);
@@ -1150,10 +1155,18 @@ extern "C" ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* 
     p.layer = layer; p.inv_cols = (float)(1.0 / (double)p.v.cols);
     uint16_t *dgamma = static_cast<uint16_t*>(dgamma_dev), *dbeta = static_cast<uint16_t*>(dbeta_dev);
     const bool sums = dgamma || dbeta;
+    const size_t need = sums ? grad_workspace(p.v, sms) : 0;
     if (sums) {
-        const size_t need = grad_workspace(p.v, sms);
         if (need && (!ws_dev || ws_bytes < need)) return fail(CCL_ERR_WORKSPACE, "ccl_norm_grad: needs %zu bytes of workspace (got %zu)", need, ws_dev ? ws_bytes : (size_t)0);
         if (bits(ws_dev) & 15) return fail(CCL_ERR_ALIGN, "ccl_norm_grad: workspace is not 16-byte aligned");
+    }
+    const uint64_t whole = (uint64_t)buffer_elems(p.v) * 2, row = (uint64_t)p.v.cols * 2, column = (uint64_t)p.v.rows * 4;
+    const Span written[4] = {{dX_dev, whole}, {dgamma_dev, row}, {dbeta_dev, row}, {need ? ws_dev : nullptr, need}};
+    const Span read[6] = {{X_dev, whole}, {dY_dev, whole}, {p.addend, whole}, {gamma_dev, row}, {layer ? mean_dev : nullptr, column}, {rstd_dev, column}};
+    for (const Span& o : written) {
+        bool bad = overlaps_any(o, written);
+        for (const Span& r : read) bad = bad || (overlap(o, r) && !(o.p == dX_dev && r.p == dX_dev && &r < read + 3));
+        if (bad) return fail(CCL_ERR_INVALID_ARG, "ccl_norm_grad: dX, dgamma, dbeta or the workspace lies over another buffer (dX may be X, dY or the addend)");
     }
     const NormPlan q = plan_norm(p.v, (any & 15) == 0, (bits(gamma_dev) & 15) == 0, true, p.addend ? 3 : 2, sms);
     p.lanes = q.lanes;

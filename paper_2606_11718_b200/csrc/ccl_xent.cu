@@ -155,6 +155,7 @@ struct Vocabulary {
     bool trans;                     // W stored [V x H]; otherwise [H x V] in strips
     ccl_mat W;
     int64_t strip, strips, stride;  // columns of a strip, their number, elements between them
+    uint64_t bytes;                 // of W
 };
 
 ccl_status check_vocabulary(const char* who, const ccl_xent_desc* d, Vocabulary* v) {
@@ -170,7 +171,7 @@ ccl_status check_vocabulary(const char* who, const ccl_xent_desc* d, Vocabulary*
     if (d->w_trans ? w.split != 0 : (w.split == 1 || w.ichunk || ragged(w) || w.w % 8 || w.stride % 8))
         return fail(CCL_ERR_UNSUPPORTED, "%s: W must be [V x H] row-major, or [H x V] in equal strips of a multiple of 8 columns", who);
     v->T = d->T; v->V = d->V; v->H = d->H; v->trans = d->w_trans != 0; v->W = d->W;
-    v->strip = w.w; v->strips = w.nstrips; v->stride = w.stride;
+    v->strip = w.w; v->strips = w.nstrips; v->stride = w.stride; v->bytes = (uint64_t)buffer_elems(w) * 2;
     return CCL_OK;
 }
 
@@ -343,6 +344,10 @@ extern "C" ccl_status ccl_linear_xent(const ccl_xent_desc* d, const void* X_dev,
     GemmPlan plan;
     if ((s = shape_plan(&g, 3, &plan))) return s;
     if ((s = check_workspace(who, forward_bytes(plan, v.T), ws_dev, ws_bytes))) return s;
+    const Span x = {X_dev, (uint64_t)v.T * v.H * 2}, w = {W_dev, v.bytes}, row = {targets_dev, (uint64_t)v.T * 4};
+    const Span all[6] = {{ws_dev, forward_bytes(plan, v.T)}, {loss_dev, row.bytes}, {lse_dev, row.bytes}, x, w, row};
+    for (int i = 0; i < 3; ++i)
+        if (overlaps_any(all[i], all)) return fail(CCL_ERR_INVALID_ARG, "%s: loss, lse or the workspace lies over another buffer", who);
     EpiMaps<3> em = {};
     LogitArgs& la = em.logits;
     const int lines = forward_lines(plan);
@@ -384,6 +389,10 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
     GradPlan g;
     if ((s = plan_grad(v, &g))) return s;
     if ((s = check_workspace(who, g.bytes, ws_dev, ws_bytes))) return s;
+    const uint64_t x_bytes = (uint64_t)v.T * v.H * 2, row = (uint64_t)v.T * 4;
+    const Span all[8] = {{ws_dev, g.bytes}, {dX_dev, x_bytes}, {dW_dev, v.bytes}, {X_dev, x_bytes}, {W_dev, v.bytes}, {targets_dev, row}, {lse_dev, row}, {dloss_dev, row}};
+    for (int i = 0; i < 3; ++i)
+        if (overlaps_any(all[i], all)) return fail(CCL_ERR_INVALID_ARG, "%s: dX, dW or the workspace lies over another buffer", who);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(ws_dev);
     void *dz = ws, *gemm_ws = g.gemm_bytes ? ws + g.gemm_at : nullptr;

@@ -509,8 +509,9 @@ ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X_dev, const
  *   state_bits = 8:  m and v are e4m3 [n], m_scale and v_scale fp32 [ceil(n / 256)]: element i of m stands for m[i] * m_scale[i / 256],
  *       element i of v for the ROOT r = v[i] * v_scale[i / 256].  A step decodes them, computes as above and keeps, of each 256 elements,
  *       scale = top * (1 / 448) and e4m3(value * (448 / top)), top the largest magnitude; an r > 0 never becomes 0 but the least e4m3
- *       value instead.  A block whose top is below 1e-30 is kept as zeros (scale 0); one with a NaN or an infinite value is NaN from then on.
- *       All bytes and scales zero are the states before the first step.
+ *       value instead.  A block whose top is below 1e-30 is kept as zeros (scale 0); one with a NaN or an infinite value (a root whose square has
+ *       left fp32: a gradient above 1.8e19 / sqrt(1 - beta2)) is NaN from then on, its scale NaN.  All bytes and scales zero are the
+ *       states before the first step.
  * param fp32 [n]; param_bf16: receives bf16(p), the weights that the products read, NULL: not wanted; grad bf16 [n], or fp32 [n] with
  * grad_fp32.  The operation is elementwise but for the blocks of 256: any layout of a matrix will do, the same for all of its buffers.
  * Tensors with n = 0 are skipped.  No two buffers of a call may overlap.  Buffers are aligned to their types; tensors whose buffers allow

@@ -145,9 +145,11 @@ __device__ __forceinline__ uint32_t f8_pair(float lo, float hi) {
 // Largest of non-negative values over a warp (their bits are ordered as their values are, NaN above all)
 __device__ __forceinline__ float warp_max(float x) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x))); }
 __device__ __forceinline__ float larger(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+// (an infinite top makes the whole block NaN, as a NaN does: with an infinite scale the roots kept at the least value would decode to
+// infinities, and their parameters stand still without a sign of it)
 __device__ __forceinline__ void f8_scale(float top, float& scale, float& inverse) {
     const bool kept = !(top < kDropped);
-    scale = kept ? __fmul_rn(top, 1.0f / kF8Max) : 0.0f;
+    scale = kept ? (top < INFINITY ? __fmul_rn(top, 1.0f / kF8Max) : __int_as_float(0x7FFFFFFF)) : 0.0f;
     inverse = kept ? __fdiv_rn(kF8Max, top) : 0.0f;
 }
 

@@ -289,8 +289,8 @@ ccl_status ccl_gemm_swiglu(const ccl_gemm_desc* d, const void* A_dev, const void
 /*
  * Synchronises `cuda_stream` (the one entry point that does), then reports and clears the status word of the
  * GEMMs and repacks finished on the current device: CCL_OK, or CCL_ERR_TIMEOUT with *detail = the raw device code
- * (1-6: a GEMM wait, 8-9: ccl_moe_tokens, 11: ccl_norm or its gradient, 101: a repack wait), or CCL_ERR_SHAPE for bad offsets of a ragged batch (detail 5) or a bad
- * target of ccl_linear_xent (detail 10).
+ * (1-4, 6, 7: a GEMM wait, 8-9: ccl_moe_tokens, 11: ccl_norm or its gradient, 101: a repack wait), or CCL_ERR_SHAPE for bad offsets of a
+ * ragged batch (detail 5) or a bad target of ccl_linear_xent (detail 10).  With several of them it is an expired wait that is told.
  * detail may be NULL.  There is ONE status word per device, shared by every stream: with several streams in flight
  * the first caller after an expiry gets the report, whichever stream's kernel it was.
  */

@@ -516,11 +516,17 @@ extern "C" ccl_status ccl_gemm_status(void* cuda_stream, int32_t* detail) {
     if (s) return s;
     int ev = 0, mv = 0, xv = 0, nv = 0;
     if ((s = epi_status_take(&ev)) || (s = moe_status_take(&mv)) || (s = xent_status_take(&xv)) || (s = norm_status_take(&nv))) return s;
-    if (!v) v = ev ? ev : (mv ? mv : (xv ? xv : nv));
-    if (detail) *detail = v ? v : (rv ? 100 + rv : 0);
+    // an expired wait (any code but 5 and 10), which may have left any result wrong, before an input that only its own row or problem was left out for
+    int expired = 0, input = 0;
+    for (int code : {v, ev, mv, xv, nv, rv ? 100 + rv : 0}) {
+        int& kept = code == 5 || code == 10 ? input : expired;
+        if (!kept) kept = code;
+    }
+    v = expired ? expired : input;
+    if (detail) *detail = v;
     if (v == 5) return fail(CCL_ERR_SHAPE, "ccl_gemm_grouped: row offsets outside [0, M] or a problem with more rows than max_rows (such problems were not computed)");
     if (v == 10) return fail(CCL_ERR_SHAPE, "ccl_linear_xent: a target outside [0, V) that is not ignore_index (its row was ignored)");
-    if (v || rv) return fail(CCL_ERR_TIMEOUT, "a bounded device-side wait expired (code %d)", v ? v : 100 + rv);
+    if (v) return fail(CCL_ERR_TIMEOUT, "a bounded device-side wait expired (code %d)", v);
     return CCL_OK;
 }
 

@@ -52,6 +52,8 @@ constexpr uint32_t smem_budget_op(int ks, int opw, int epi) { return ks || epi =
 constexpr int kLogitBlocks = 16;
 
 static __device__ int g_gemm_status = 0;
+// An input that a kernel could not use as it is (5: offsets of a ragged batch, 10: a target): told only where no expired wait is, which overwrites it
+__device__ __forceinline__ void report_input(int code) { atomicCAS(&g_gemm_status, 0, code); }
 
 // Division of a non-negative int by a launch constant as a multiply-high and a shift (an integer division costs a few
 // hundred cycles, and the tile walk of a short GEMM is nothing but divisions).  For d >= 2: l = ceil(log2 d),
@@ -467,7 +469,7 @@ struct KRange { int k0, nkb, rem; };
 __device__ __forceinline__ KRange k_range(const int32_t* k_offs, int e, int Ktot) {
     const int o0 = __ldg(k_offs + e), o1 = __ldg(k_offs + e + 1);
     KRange r;
-    if (o0 < 0 || o1 > Ktot || o1 < o0) { atomicExch(&g_gemm_status, 5); r.k0 = 0; r.nkb = 1; r.rem = 0; return r; }
+    if (o0 < 0 || o1 > Ktot || o1 < o0) { report_input(5); r.k0 = 0; r.nkb = 1; r.rem = 0; return r; }
     const int cnt = o1 - o0;
     r.k0 = o0; r.nkb = cnt > 0 ? (cnt + BK - 1) / BK : 1; r.rem = cnt - (r.nkb - 1) * BK;
     return r;
@@ -601,7 +603,7 @@ struct Scheduler {
         if (RAG == 1 && p.m_offs) {                      // rows of this problem inside the concatenated A and C
             const int o0 = __ldg(p.m_offs + t.e), o1 = __ldg(p.m_offs + t.e + 1);
             const bool bad = o0 < 0 || o1 > p.M || o1 - o0 > p.Wm;   // outside A / C, or more rows than the caller's bound:
-            if (bad && t.m0 == 0 && t.n0 == 0) atomicExch(&g_gemm_status, 5);   // reported, and the problem is left out
+            if (bad && t.m0 == 0 && t.n0 == 0) report_input(5);   // reported, and the problem is left out
             t.skip = bad || t.m0 >= o1 - o0;
             t.m0 += o0; t.m1 = min(t.m0 + bm, o1);
         }
@@ -698,7 +700,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         const int lo = min(E, (int)threadIdx.x * per), hi = min(E, lo + per);
         auto tiles_of = [&](int e) {
             const int o0 = __ldg(p.m_offs + e), o1 = __ldg(p.m_offs + e + 1);
-            if (o0 < 0 || o1 > p.M || o1 - o0 > p.Wm) { atomicExch(&g_gemm_status, 5); return 0; }   // reported, left out
+            if (o0 < 0 || o1 > p.M || o1 - o0 > p.Wm) { report_input(5); return 0; }   // reported, left out
             return o1 > o0 ? (o1 - o0 + bm - 1) / bm : 0;
         };
         int sum = 0;

@@ -79,7 +79,7 @@ static void key_surroundings(int* dev, char* env, size_t size) {
     *dev = -1;
     if (cudaGetDevice(dev) != cudaSuccess) (void)cudaGetLastError();
     size_t pos = 0;
-    for (const char* name : {"CCL_GEMM_CTAS", "CCL_GEMM_BN", "CCL_GEMM_SPLITK", "CCL_GEMM_CLUSTERK"}) {
+    for (const char* name : {"CCL_GEMM_CTAS", "CCL_GEMM_BN", "CCL_GEMM_SPLITK", "CCL_GEMM_BALANCED", "CCL_GEMM_CLUSTERK"}) {
         const char* v = std::getenv(name);
         for (const char* c = v ? v : ""; *c && pos + 2 < size; ++c) env[pos++] = *c;
         if (pos + 1 < size) env[pos++] = ';';

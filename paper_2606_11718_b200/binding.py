@@ -547,7 +547,7 @@ class AdamwTensors:
         columns = [params, copies if copies is not None else [None] * n, grads, m, v] + ([m_scales or [], v_scales or []] if eight else [])
         if any(len(c) != n for c in columns):
             raise ValueError("AdamwTensors: lists of different lengths")
-        self.bits, self.count, self.tensors, self.device = (8 if eight else 32), n, [list(c) for c in columns], _current_device() if n else None
+        self.bits, self.count, self.tensors, self.device = (8 if eight else 32), n, [list(c) for c in columns], _current_device()
         state = (torch.float8_e4m3fn, torch.uint8) if eight else (_FP32,)
         wanted = [(_FP32,), (_BF16,), (_BF16, _FP32), state, state, (_FP32,), (_FP32,)]
         sizes = [p.numel() for p in params]

@@ -134,6 +134,8 @@ class AdamW:
     kept on the device, so that a step can be captured into a graph and replayed."""
 
     def __init__(self, weights, bits=32, **hyper):
+        if bits not in (32, 8):
+            raise ValueError("AdamW: states have 32 or 8 bits")
         self.names, self.weights, self.d = list(weights), list(weights.values()), ccl.AdamwDesc(**hyper)
         self.masters = [w.float() for w in self.weights]
         state = torch.float32 if bits == 32 else torch.float8_e4m3fn

@@ -250,7 +250,11 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
             const double t_drain = b == 512 ? 7000.0 : (b == 384 ? 5500.0 : 1500.0);
             // one row of tiles: nobody shares the B columns, the problem streams B from HBM at ~29 B/clk per SM in
             // aggregate however the units are cut (a ragged last wave still saturates the memory); wider boxes are
-            // fetched a little more efficiently (measured: 128 / 192 columns cost ~10 % / ~4 % more time per byte)
+            // fetched a little more efficiently (measured: 128 / 192 columns cost ~10 % / ~4 % more time per byte).  Logits and their gradient:
+            // in a pair's tile of up to 128 rows one CTA has none, and the pair waits for both CTAs' halves of B; 256 columns, single CTA / pair, us:
+            // 1 x 131072 x 4096 188-193 / 210-216, 1 x 92540 x 6592 199-203 / 229-233, 8 x 64000 x 8192 176 / 213, 32 x 100000 x 4096
+            // 146-149 / 180-186, 128 x 131072 x 4096 203-210 / 233-237, 4 x 91000 x 3880 134-136 / 138-140: 1.12 is about the middle.  It decides for long
+            // K alone; with 129 to 256 rows a pair is taken with it or without (256 x 32000 x 4096: 75 / 67).
             const double stream_clk = tiles_m_all == 1 ? (double)tiles * (double)num_kb * (double)b * (BK * 2) / (sms * 29.0) *
                                                              (b <= 128 ? 1.10 : (b <= 192 ? 1.04 : 1.0)) *
                                                              (epi >= 3 && c == 2 ? 1.12 : 1.0) : 0.0;

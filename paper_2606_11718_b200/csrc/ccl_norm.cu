@@ -1066,12 +1066,12 @@ size_t grad_workspace(const MatView& v, int sms) {
     return lines * 2 * 8 * 4;
 }
 
-ccl_status launch_sums(NormParams p, const NormPlan& q, uint16_t* dgamma, uint16_t* dbeta, cudaStream_t st) {
+ccl_status launch_sums(NormParams p, const NormPlan& q, int sms, uint16_t* dgamma, uint16_t* dbeta, cudaStream_t st) {
     // as many threads along a row as leave every SM a few CTAs; eight CTAs at most share the rows
     const int64_t groups = (p.v.cols + q.vec - 1) / q.vec;
     int lanes = 32, ctas = 8;
     while (ctas > 1 && p.v.rows < (int64_t)ctas * 32) ctas /= 2;
-    while (lanes > 2 && (groups + lanes - 1) / lanes * ctas < 148 * 3) lanes /= 2;
+    while (lanes > 2 && (groups + lanes - 1) / lanes * ctas < sms * 3) lanes /= 2;
     const int64_t tiles = (groups + lanes - 1) / lanes;
     if (tiles * ctas >= (INT64_C(1) << 31)) return fail(CCL_ERR_UNSUPPORTED, "ccl_norm_grad: too many columns");
     p.lanes = lanes;
@@ -1178,6 +1178,6 @@ extern "C" ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* 
         return launch_early(norm_grad_finish_kernel, dim3((unsigned)((p.v.cols + 31) / 32), 2), 256, 0, st, (const float*)p.partial, (int)grid, p.v.cols, q.pieces * 8,
                             q.period - 1, dgamma, dbeta);
     }
-    if (sums && (s = launch_sums(p, q, dgamma, dbeta, st))) return s;        // (first: dX may take the place of X or dY)
+    if (sums && (s = launch_sums(p, q, sms, dgamma, dbeta, st))) return s;        // (first: dX may take the place of X or dY)
     return p.out ? launch_plan<true>(p, q, grid, st) : CCL_OK;
 }

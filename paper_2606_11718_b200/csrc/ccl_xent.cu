@@ -358,8 +358,9 @@ extern "C" ccl_status ccl_linear_xent(const ccl_xent_desc* d, const void* X_dev,
     if ((s = run_logits<3>(plan, em, v.trans ? v.V : 0, X_dev, W_dev, nullptr, st))) return s;
     // few rows side by side where there are few, and the more threads along the lines (1024 rows of 2048 lines: 80 us with 32 a block, on
     // 32 SMs; four are a whole sector of memory)
-    int lanes = 1;
-    while (lanes < 32 && lanes < v.T && (lanes < 4 || v.T > lanes * 148 * 2)) lanes *= 2;
+    int sms, pairs, lanes = 1;
+    device_units(&sms, &pairs);
+    while (lanes < 32 && lanes < v.T && (lanes < 4 || v.T > (int64_t)lanes * sms * 2)) lanes *= 2;
     return launch_early(xent_finish_kernel, dim3((unsigned)((v.T + lanes - 1) / lanes)), 256, 0, st, (const float2*)la.part, lines, (int)v.T, lanes, targets_dev,
                         la.ignore, la.classes, (const float*)la.at_target, loss_dev, lse_dev);
 }
@@ -398,6 +399,8 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
     void *dz = ws, *gemm_ws = g.gemm_bytes ? ws + g.gemm_at : nullptr;
     float *acc = reinterpret_cast<float*>(ws + g.acc_at), *scale = reinterpret_cast<float*>(ws + g.scale_at);
     if ((s = launch_early(xent_scale_kernel, dim3(1), 1024, 0, st, dloss_dev, targets_dev, (int)v.T, d->ignore_index, (int32_t)v.V, scale))) return s;
+    int sms, pairs;
+    device_units(&sms, &pairs);
     int have = 0;                                            // sums of dX that earlier pieces have begun
     for (int64_t i = 0; i < g.pieces; ++i) {
         const int64_t real = piece_real(v, g, i), rows = v.trans ? real : 0;
@@ -431,7 +434,7 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
             uint16_t* C = static_cast<uint16_t*>(dW_dev) + at;
             // Enough tiles for every SM: 256 columns, drained behind the next tile's product (131072 x 512 x 1024: 105 us, by ccl_gemm with
             // alpha 114; 32768 x 4096 x 1024: 196 and 215).  Few tiles and a long K are split along K.
-            if (((p.M + BM - 1) / BM) * ((p.N + 255) / 256) >= 148) {
+            if (((p.M + BM - 1) / BM) * ((p.N + 255) / 256) >= sms) {
                 if ((s = shape_plan(&p, 6, &plan))) return s;
                 EpiMaps<6> by = {scale};
                 if ((s = run_logits<6>(plan, by, 0, A, B, C, st, rows))) return s;
@@ -440,5 +443,5 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
     }
     if (!dX_dev || g.sums == 1) return CCL_OK;
     const int64_t n = v.T * v.H;
-    return launch_early(xent_dx_kernel, dim3((unsigned)std::min<int64_t>((n / 8 + 255) / 256, 148 * 8)), 256, 0, st, (const float*)acc, have, n, (const float*)scale, static_cast<uint16_t*>(dX_dev));
+    return launch_early(xent_dx_kernel, dim3((unsigned)std::min<int64_t>((n / 8 + 255) / 256, sms * 8)), 256, 0, st, (const float*)acc, have, n, (const float*)scale, static_cast<uint16_t*>(dX_dev));
 }

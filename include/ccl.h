@@ -27,7 +27,8 @@
  *   CCL_GEMM_CTAS = 1|2            force one CTA per tile or a cta_group::2 pair
  *   CCL_GEMM_BN = 128|192|256|384|512  force the tile width (ccl_gemm_epilogue, ccl_gemm_act_grad: 256 at most; ccl_linear_xent and its
  *                                  gradient: 128 or 256)
- *   CCL_GEMM_SPLITK = n            force the number of K splits
+ *   CCL_GEMM_SPLITK = n            force the number of K splits (n > 1: not ccl_linear_xent and its gradient, whose logits are never split:
+ *                                  CCL_ERR_UNSUPPORTED)
  *   CCL_GEMM_BALANCED = 0|1        never / always (where legal) cut the tiles that do not fill a round into equal shares
  *   CCL_GEMM_CLUSTERK = 0|2|4|8        never / always (where legal) let the CTAs of a cluster of that size share one tile,
  *                                  each over its own part of K (the default picks it for problems of few tiles)
@@ -442,7 +443,7 @@ typedef enum { CCL_NORM_LAYER = 0, CCL_NORM_RMS = 1 } ccl_norm_kind;
  * touched); Y_dev may be X_dev, otherwise no output may lie over another buffer (CCL_ERR_INVALID_ARG).  gamma, beta: bf16 [H], NULL: ones /
  * zeros.  mean_dev, rstd_dev: fp32 [rows], what the gradient needs; NULL: not wanted.  beta_dev and mean_dev are NULL with CCL_NORM_RMS.  Any shape; bases 2-byte aligned (fp32 ones 4-byte).  16-byte aligned
  * X and Y take the fast path: row-major of any width from 256 columns on, and strips whose column groups of 8 are aligned pieces of the
- * buffer.  eps >= 0; a constant row with eps = 0 gives NaN.  rstd is off by (32 + H / 256) 2^-24 of itself at most where the mean is no more
+ * buffer.  eps >= 0; a constant row with eps = 0 has no defined result.  rstd is off by (32 + H / 256) 2^-24 of itself at most where the mean is no more
  * than some 100 deviations from zero (measured, whatever columns lie elsewhere than the rest: 1e-7 to 1e-6 up to 33000 columns).  Bounded
  * waits as for ccl_gemm.
  */
@@ -476,10 +477,11 @@ ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* X_dev, cons
  *             after ccl_linear_xent.
  *   loss, lse fp32 [T], either NULL: not wanted; the gradient reads lse as ccl_linear_xent left it.   dloss fp32 [T].   dX, dW: either
  *             NULL: not wanted.
- * Logits, exponentials and their sums are fp32 (the exponentials good to 2^-21).  The gradient works through the vocabulary in pieces:
- * it computes a piece's logits again, holds its dz, divided by the largest finite |dloss| (by 2^-126 at least), as bf16 (the operand of two products; each value
- * off by 2^-8 of itself at most) in the workspace, and sums dX over the pieces in fp32, always in the same order.  A piece's dz takes at most
- * 512 MB, or T x 256 x 2 bytes where that is more, or that of one strip (of the whole matrix where a [H x V] is row-major).
+ * Logits, exponentials and their sums are fp32 (the exponentials good to 2^-21 and, in the gradient, to 2^-22 (|z| + |lse|)); logits below 2^30
+ * in magnitude.  The gradient works through the vocabulary in pieces: it computes a piece's logits again, holds its dz, divided by the
+ * largest finite |dloss| (by 2^-126 at least), as bf16 (the operand of two products; each value off by 2^-8 of itself at most, and those below
+ * 2^-126 lost) in the workspace, and sums dX over the pieces in fp32, always in the same order.  A piece's dz takes at most 512 MB, or
+ * T x 256 x 2 bytes where that is more, or that of one strip (of the whole matrix where a [H x V] is row-major).
  * No output and no workspace may lie over another buffer of the call (CCL_ERR_INVALID_ARG).  Any T >= 1 and V >= 1; H a multiple of 8 (else
  * CCL_ERR_UNSUPPORTED); X, W, dX, dW and the workspace 16-byte aligned.  Workspace: the bytes that the _workspace calls say, whatever they hold;
  * calls that can overlap on the GPU must not share it.  Bounded waits and asynchrony as for ccl_gemm.

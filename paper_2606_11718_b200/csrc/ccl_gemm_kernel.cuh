@@ -47,8 +47,8 @@ constexpr uint32_t kSmemBudgetOpKs = 224 * 1024;
 constexpr uint32_t smem_budget_op(int ks, int opw, int epi) { return ks || epi == 3 ? kSmemBudgetOpKs : (224u * 1024 - (uint32_t)opw * 32 * 128); }
 // EPI 3: k blocks after which the accumulator is handed over and a new one begun; the drain warps add them up.  An accumulator in tensor memory
 // loses up to a unit in the last place with every 16 of K, always towards zero: a loss over sums of 2048 products was off by 1.8e-6 of
-// itself, over 8192 by 6e-6.  In pieces of 1024 it is 5e-7 to 8e-7 at any K, for no measurable time (8192 x 131072 x 4096: 5.8 to 5.9 ms);
-// in pieces of 512 3e-7 to 4e-7, but 7.1 ms: the hand-overs then come faster than sixteen warps take them.
+// itself, over 8192 by 6e-6.  In pieces of 1024 the losses of 19 to 2048 tokens are 4e-7 to 1.05e-6 of their norm off at K = 512 to 8192 (a plain form in
+// fp32 2e-7 to 1.3e-6), for no measurable time (8192 x 131072 x 4096: 5.8 to 5.9 ms); in pieces of 512 half as much (6.9e-7 to 3.1e-7), but 7.1 ms: the hand-overs then come faster than sixteen warps take them.
 constexpr int kLogitBlocks = 16;
 
 static __device__ int g_gemm_status = 0;

@@ -130,8 +130,9 @@ class Head:
 
 
 class AdamW:
-    """Updates a dict of bfloat16 weights in place, from float32 copies of its own and with states of 32 or 8 bits.  The number of the step is
-    kept on the device, so that a step can be captured into a graph and replayed."""
+    """Updates a dict of bfloat16 weights in place, from float32 copies of its own and with states of 32 or 8 bits; hyper (lr, beta1, beta2, eps,
+    weight_decay) holds for all of them.  The number of the step is kept on the device, so that a step can be captured into a graph and
+    replayed (with the rate that `d.lr` had when it was captured)."""
 
     def __init__(self, weights, bits=32, **hyper):
         if bits not in (32, 8):

@@ -47,9 +47,13 @@ constexpr uint32_t kSmemBudgetOpKs = 224 * 1024;
 constexpr uint32_t smem_budget_op(int ks, int opw, int epi) { return ks || epi == 3 ? kSmemBudgetOpKs : (224u * 1024 - (uint32_t)opw * 32 * 128); }
 // EPI 3: k blocks after which the accumulator is handed over and a new one begun; the drain warps add them up.  An accumulator in tensor memory
 // loses up to a unit in the last place with every 16 of K, always towards zero: a loss over sums of 2048 products was off by 1.8e-6 of
-// itself, over 8192 by 6e-6.  In pieces of 1024 the losses of 19 to 2048 tokens are 4e-7 to 1.05e-6 of their norm off at K = 512 to 8192 (a plain form in
-// fp32 2e-7 to 1.3e-6), for no measurable time (8192 x 131072 x 4096: 5.8 to 5.9 ms); in pieces of 512 half as much (6.9e-7 to 3.1e-7), but 7.1 ms: the hand-overs then come faster than sixteen warps take them.
-constexpr int kLogitBlocks = 16;
+// itself, over 8192 by 6e-6.  In pieces of 1024 the losses of 129 to 2048 tokens are 4e-7 to 9e-7 of their norm off at K = 512 to 8192 (a plain form in
+// fp32 2e-7 to 1e-6), for no measurable time (8192 x 131072 x 4096: 5.8 to 5.9 ms); in pieces of 512 half as much, but 7.1 ms: the hand-overs then
+// come faster than sixteen warps take them.  With one row of tiles (128 tokens) the weight's bytes are waited for and pieces of 256 cost nothing
+// (T x V x H, 1024 / 256 / 128 a piece, us: 1 x 131072 x 4096 192 / 190-194 / 192-196, 19 x 50001 x 2048 50.5 / 49.8 / 51.1-52.1,
+// 128 x 50001 x 2048 58.3 / 59.0 / 61.9; with 200 x 92000 x 4096 174 / 210 / 269-280).  There it counts: a few tokens' errors do not average, and a small
+// loss beside a large logit has that logit's (1 to 19 tokens 4e-8 to 8e-6 in pieces of 1024, 3e-8 to 2.4e-6 in pieces of 256, plain 2e-8 to 4.7e-6).
+constexpr int kLogitBlocks = 16, kLogitBlocksFew = 4;
 
 static __device__ int g_gemm_status = 0;
 // An input that a kernel could not use as it is (5: offsets of a ragged batch, 10: a target): told only where no expired wait is, which overwrites it
@@ -179,6 +183,7 @@ template <> struct EpiMaps<0> {};
 struct LogitArgs {
     const int32_t* targets;         // [M]
     int32_t ignore, v0, classes, all;   // all: classes of the whole problem (a target outside [0, all) is taken as ignored)
+    int32_t blocks;                 // EPI 3: k blocks of an accumulator (see kLogitBlocks)
     float2* part;                   // EPI 3: [64 columns of a tile][M]: log2 of the scale, sum of 2^(z log2 e - it)
     float* at_target;               // EPI 3: [M] the target's logit
     const float *lse, *dloss;       // EPI 4: [M]
@@ -863,8 +868,8 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 kb0 = __shfl_sync(FULLMASK, kb0, 0); kb1 = __shfl_sync(FULLMASK, kb1, 0);
                 if (RAG == 2) tail = __shfl_sync(FULLMASK, tail, 0);
                 [[maybe_unused]] const int kz = kb1;
-                do {                                        // (once, but for EPI 3: kLogitBlocks k blocks an accumulator)
-                if (EPI == 3) kb1 = min(kz, kb0 + kLogitBlocks);
+                do {                                        // (once, but for EPI 3: em.logits.blocks k blocks an accumulator)
+                if constexpr (EPI == 3) kb1 = min(kz, kb0 + em.logits.blocks);
                 // NSUB == 1: TMEM half (done & 1) is this tile's accumulator, the other half is being drained.
                 // NSUB == 2: both halves belong to this tile; half h may be overwritten once the epilogue
                 //            of the previous tile has drained it.
@@ -1013,7 +1018,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 #pragma unroll
               for (int i = 0; i < 32; ++i) z[i] = both(0.0f);
 #pragma unroll 1
-              for (int kb = 0; kb < p.num_kb; kb += kLogitBlocks) {
+              for (int kb = 0; kb < p.num_kb; kb += em.logits.blocks) {
                   const int acc = done & 1;
                   const bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&tmem_full[acc], (uint32_t)(done >> 1) & 1));
                   ++done;

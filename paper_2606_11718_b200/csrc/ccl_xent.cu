@@ -2,7 +2,7 @@
 // The logits z are never stored.
 //
 // Forward.  The GEMM of ccl_gemm (ccl_gemm_kernel.cuh, EPI = 3) with another drain: a lane has a row of 64 of the tile's columns, adds their
-// logits up in fp32 from accumulators of 1024 of K each, and leaves the largest and the sum of exponentials about it (the target's logit
+// logits up in fp32 from accumulators of 1024 of K each (256 with up to 128 tokens), and leaves the largest and the sum of exponentials about it (the target's logit
 // where it passes by), and a second kernel joins a row's numbers:  lse = max + log(sum of s_i exp(m_i - max)).  Powers of two throughout: one
 // multiply-add and one hardware exponential a logit, behind the next tile's product.
 //
@@ -353,6 +353,7 @@ extern "C" ccl_status ccl_linear_xent(const ccl_xent_desc* d, const void* X_dev,
     LogitArgs& la = em.logits;
     const int lines = forward_lines(plan);
     la.targets = targets_dev; la.ignore = d->ignore_index; la.classes = la.all = (int32_t)v.V;
+    la.blocks = v.T <= BM ? kLogitBlocksFew : kLogitBlocks;
     la.part = static_cast<float2*>(ws_dev);
     la.at_target = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + up256((size_t)lines * (size_t)v.T * 8));
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);

@@ -479,8 +479,8 @@ ccl_status ccl_norm_grad(const ccl_mat* m, int32_t kind, const void* X_dev, cons
  *             NULL: not wanted.
  * Logits, exponentials and their sums are fp32 (the exponentials good to 2^-21 and, in the gradient, to 2^-22 (|z| + |lse|)); logits below 2^30
  * in magnitude.  The gradient works through the vocabulary in pieces: it computes a piece's logits again, holds its dz, divided by the
- * largest finite |dloss| (by 2^-126 at least), as bf16 (the operand of two products; each value off by 2^-8 of itself at most, and those below
- * 2^-126 lost) in the workspace, and sums dX over the pieces in fp32, always in the same order.  A piece's dz takes at most 512 MB, or
+ * largest finite |dloss| (by 2^-126 at least), as bf16 (the operand of two products; each value off by 2^-8 of itself at most, by 2^-16 with up to
+ * 16 tokens, and those below 2^-126 lost) in the workspace, and sums dX over the pieces in fp32, always in the same order.  A piece's dz takes at most 512 MB, or
  * T x 256 x 2 bytes where that is more, or that of one strip (of the whole matrix where a [H x V] is row-major).
  * No output and no workspace may lie over another buffer of the call (CCL_ERR_INVALID_ARG).  Any T >= 1 and V >= 1; H a multiple of 8 (else
  * CCL_ERR_UNSUPPORTED); X, W, dX, dW and the workspace 16-byte aligned.  Workspace: the bytes that the _workspace calls say, whatever they hold;

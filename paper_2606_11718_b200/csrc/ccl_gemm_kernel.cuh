@@ -54,6 +54,9 @@ constexpr uint32_t smem_budget_op(int ks, int opw, int epi) { return ks || epi =
 // 128 x 50001 x 2048 58.3 / 59.0 / 61.9; with 200 x 92000 x 4096 174 / 210 / 269-280).  There it counts: a few tokens' errors do not average, and a small
 // loss beside a large logit has that logit's (1 to 19 tokens 4e-8 to 8e-6 in pieces of 1024, 3e-8 to 2.4e-6 in pieces of 256, plain 2e-8 to 4.7e-6).
 constexpr int kLogitBlocks = 16, kLogitBlocksFew = 4;
+// EPI 4: rows of dz up to which a token has two of them, its dz rounded to bf16 and what is left of it, rounded too: those of one quarter of the drain
+// warps, half a k block of the product that has them along K
+constexpr int64_t kTwofoldRows = 32;
 
 static __device__ int g_gemm_status = 0;
 // An input that a kernel could not use as it is (5: offsets of a ragged batch, 10: a target): told only where no expired wait is, which overwrites it
@@ -183,6 +186,7 @@ template <> struct EpiMaps<0> {};
 struct LogitArgs {
     const int32_t* targets;         // [M]
     int32_t ignore, v0, classes, all;   // all: classes of the whole problem (a target outside [0, all) is taken as ignored)
+    int32_t half;                   // EPI 4: row half + t has what is left of row t's dz after its rounding (half >= M: there are none)
     int32_t blocks;                 // EPI 3: k blocks of an accumulator (see kLogitBlocks)
     float2* part;                   // EPI 3: [64 columns of a tile][M]: log2 of the scale, sum of 2^(z log2 e - it)
     float* at_target;               // EPI 3: [M] the target's logit
@@ -1003,7 +1007,7 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           [[maybe_unused]] bool row_live = false;
           if constexpr (EPI == 3 || EPI == 4) {
               const LogitArgs& la = em.logits;
-              const int row = min(m, t.m1 - 1), cls = la.targets[row];
+              const int row = EPI == 4 && min(m, t.m1 - 1) >= la.half ? min(m, t.m1 - 1) - la.half : min(m, t.m1 - 1), cls = la.targets[row];
               if (EPI == 4) { row_lse2 = la.lse[row] * kLog2e; row_scale = la.dloss[row] * by_scale; }     // (all three under way together)
               row_live = m < t.m1 && cls != la.ignore && (unsigned)cls < (unsigned)la.all;
               target = row_live ? cls - la.v0 : -1;
@@ -1621,6 +1625,12 @@ ccl_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                             }
 #pragma unroll
                             for (int i = 0; i < 16; ++i) w[i] = row_live ? bf16_pack(v[i]) : 0u;
+                            // (the same for the whole grid; with sixteen warps, which so few rows never have, the registers would not do)
+                            if (OPW == 8 && em.logits.half < p.M) {
+                                const bool rest = m >= em.logits.half && row_live;
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) w[i] = rest ? bf16_pack(fma2(bf16_unpack(w[i]), both(-1.0f), v[i])) : w[i];
+                            }
                             if (last < 32) {
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) w[i] = 2 * i + 1 < last ? w[i] : (2 * i < last ? w[i] & 0xFFFFu : 0u);

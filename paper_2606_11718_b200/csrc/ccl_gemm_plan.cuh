@@ -435,7 +435,8 @@ static ccl_status make_plan(const ccl_gemm_desc* d, int64_t batch, bool swiglu, 
     // 2048 111 / 115, 4096 201 / 210).  Those are problems of seven rounds of tiles; with one round, where no next tile hides the
     // drain, the two have not been compared.  A scaled product (EPI 6) has nothing to compute there and keeps the long ring (131072 x 512 x 1024,
     // eight / sixteen: 105 / 113 us).  The kernels with every layout exist with eight, the cluster split drains once, with sixteen.
-    const int opw = ks || epi == 3 ? 16 : (epi_full || epi >= 5 || p.kb_per_split * BK >= 1536 ? 8 : 16);
+    // A gradient of logits with two rows a token has eight at any K (kTwofoldRows).
+    const int opw = ks || epi == 3 ? 16 : (epi_full || epi >= 5 || (epi == 4 && d->M <= kTwofoldRows) || p.kb_per_split * BK >= 1536 ? 8 : 16);
     plan->opw = opw;
     p.stages = (int32_t)(((epi ? smem_budget_op(ks, opw, epi) : kSmemBudget) - rag_bytes) / p.stage_bytes);
     if (p.stages > 8) p.stages = 8;

@@ -12,9 +12,14 @@
 // that where all are alike (a mean over the tokens) the rounding is that of p - 1 and p themselves: a target that has little of the
 // probability is -1 then, exact or nearly so, where -dloss would be off by 2^-9 of itself (777 tokens: errors of dX and dW against 64 bits
 // 0.0025 -> 0.0019 of their norms, of which 0.0017 are the outputs' own rounding).  Where tokens weigh differently it is 0.0023 (weights
-// uniform from 0 to 2) to 0.0025 (e to a normal deviate), and a single token, whose roundings nothing averages, has up to 0.0038.  A piece's dz is at most kPieceBytes
-// unless 256 columns (or a strip) are more.  Recomputing the logits costs a quarter of the gradient's products; keeping them would
-// cost T x V x 4 bytes.
+// uniform from 0 to 2) to 0.0025 (e to a normal deviate).
+//   Up to 16 tokens, whose roundings little averages (0.0036 to 0.0038 with one), have two rows of dz each: the rounded values and, 16 rows further at most, what is left of them, rounded too.  X lies in the workspace twice, one below the
+// other, so that the products need not know; dX comes from fp32 sums of both rows.  The outputs' own rounding is then all there is
+// (0.0016 to 0.0017; of 1662 drawn gradients of 2 to 16 tokens 115 were off by over 1.5 times the plain form's error, 6 are, where p - 1 itself
+// cancels), for some us: 1 x 131072 x 4096 553 / 555, 8 x 64000 x 8192 533 / 538, 1 x 5000 x 512 27 / 32; four strips, whose products are then
+// added one by one, 1 x 32000 x 2048 97 / 118.
+//   A piece's dz is at most kPieceBytes unless 256 columns (or a strip) are more.  Recomputing the logits costs a quarter of the gradient's
+// products; keeping them would cost T x V x 4 bytes.
 //
 // Bound by the tensor cores: 2 T V H and 6 T V H operations.
 #include "ccl_gemm_epi.cuh"
@@ -99,11 +104,21 @@ __global__ void __launch_bounds__(256) xent_finish_kernel(const float2* part, in
 }
 
 // scale = the largest finite |dloss| of the rows that take part (1 where all are zero or there is none; 2^-126 at least, whose reciprocal
-// is finite: below it, 1 / scale would be infinite and a row with dloss = 0 beside it NaN)
-__global__ void __launch_bounds__(1024) xent_scale_kernel(const float* dloss, const int32_t* targets, int M, int32_t ignore, int32_t classes, float* scale) {
+// is finite: below it, 1 / scale would be infinite and a row with dloss = 0 beside it NaN).  The blocks behind the first write x
+// (n8 pieces of 16 bytes) twice, one below the other, to x2.
+__global__ void __launch_bounds__(1024) xent_scale_kernel(const float* dloss, const int32_t* targets, int M, int32_t ignore, int32_t classes, float* scale,
+                                                          const uint4* x, uint4* x2, int64_t n8) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ float tops[32];
+    if (blockIdx.x) {
+        for (int64_t i = (int64_t)(blockIdx.x - 1) * 1024 + threadIdx.x; i < n8; i += (int64_t)(gridDim.x - 1) * 1024) {
+            const uint4 w = x[i];
+            x2[i] = w;
+            x2[n8 + i] = w;
+        }
+        return;
+    }
     float top = 0.0f;
 #pragma unroll 4
     for (int64_t i = threadIdx.x; i < M; i += 1024) {
@@ -153,6 +168,7 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct Vocabulary {
     int64_t T, V, H;
+    int64_t M;                      // rows of the gradient's dz
     bool trans;                     // W stored [V x H]; otherwise [H x V] in strips
     ccl_mat W;
     int64_t strip, strips, stride;  // columns of a strip, their number, elements between them
@@ -171,20 +187,20 @@ ccl_status check_vocabulary(const char* who, const ccl_xent_desc* d, Vocabulary*
     if (w.e != 2) return fail(CCL_ERR_UNSUPPORTED, "%s: only 2-byte (bf16) elements are supported", who);
     if (d->w_trans ? w.split != 0 : (w.split == 1 || w.ichunk || ragged(w) || w.w % 8 || w.stride % 8))
         return fail(CCL_ERR_UNSUPPORTED, "%s: W must be [V x H] row-major, or [H x V] in equal strips of a multiple of 8 columns", who);
-    v->T = d->T; v->V = d->V; v->H = d->H; v->trans = d->w_trans != 0; v->W = d->W;
+    v->T = d->T; v->V = d->V; v->H = d->H; v->M = 2 * d->T <= kTwofoldRows ? 2 * d->T : d->T; v->trans = d->w_trans != 0; v->W = d->W;
     v->strip = w.w; v->strips = w.nstrips; v->stride = w.stride; v->bytes = (uint64_t)buffer_elems(w) * 2;
     return CCL_OK;
 }
 
-// dz of the whole vocabulary, kept in the strips that W has
-ccl_mat strips_of(const Vocabulary& v) {
-    return v.strips > 1 ? ccl_mat{v.T, v.V, 2, (int32_t)v.strips, CCL_PART_COLS, CCL_CCL, 0} : matrix(v.T, v.V);
+// `rows` rows over the whole vocabulary (logits, dz), kept in the strips that W has
+ccl_mat strips_of(const Vocabulary& v, int64_t rows) {
+    return v.strips > 1 ? ccl_mat{rows, v.V, 2, (int32_t)v.strips, CCL_PART_COLS, CCL_CCL, 0} : matrix(rows, v.V);
 }
 // The logits of `real` classes from one piece (all: of the whole of W); a row-major W is padded to whole 64s with classes that read as zeros
-ccl_gemm_desc logits(const Vocabulary& v, int64_t real, bool all) {
+ccl_gemm_desc logits(const Vocabulary& v, int64_t rows, int64_t real, bool all) {
     const int64_t n = v.trans ? up(real, 64) : real;
-    if (!v.trans && all) return product(v.T, n, v.H, matrix(v.T, v.H), 0, v.W, 0, strips_of(v));
-    return product(v.T, n, v.H, matrix(v.T, v.H), 0, v.trans ? matrix(n, v.H) : matrix(v.H, n), v.trans, matrix(v.T, n));
+    if (!v.trans && all) return product(rows, n, v.H, matrix(rows, v.H), 0, v.W, 0, strips_of(v, rows));
+    return product(rows, n, v.H, matrix(rows, v.H), 0, v.trans ? matrix(n, v.H) : matrix(v.H, n), v.trans, matrix(rows, n));
 }
 
 int forward_lines(const GemmPlan& plan) { return plan.p.tiles_n * (plan.opw / 4); }
@@ -194,27 +210,28 @@ struct GradPlan {
     int64_t pieces, width;          // classes of a piece but the last
     bool all;                       // one piece that is the whole of W
     int64_t sums, sum_width;        // products that dX is the sum of, classes of each (1: one a piece, where there is one piece)
-    int parts;                      // fp32 sums of dX (0: it is one product)
-    size_t acc_at, gemm_at, gemm_bytes, scale_at, bytes;
+    bool direct;                    // dX is one product; otherwise it comes from
+    int parts;                      //   as many fp32 sums
+    size_t acc_at, x2_at, gemm_at, gemm_bytes, scale_at, bytes;
 };
 
 int64_t piece_real(const Vocabulary& v, const GradPlan& g, int64_t i) { return std::min(g.width, v.V - i * g.width); }
 ccl_gemm_desc dx_product(const Vocabulary& v, const GradPlan& g, int64_t real) {
     const int64_t n = v.trans ? up(real, 64) : real;
-    if (!v.trans && g.sums == 1) return product(v.T, v.H, n, strips_of(v), 0, v.W, 1, matrix(v.T, v.H));
-    return product(v.T, v.H, n, matrix(v.T, n), 0, v.trans ? matrix(n, v.H) : matrix(v.H, n), v.trans ? 0 : 1, matrix(v.T, v.H));
+    if (!v.trans && g.sums == 1) return product(v.M, v.H, n, strips_of(v, v.M), 0, v.W, 1, matrix(v.M, v.H));
+    return product(v.M, v.H, n, matrix(v.M, n), 0, v.trans ? matrix(n, v.H) : matrix(v.H, n), v.trans ? 0 : 1, matrix(v.M, v.H));
 }
 ccl_gemm_desc dw_product(const Vocabulary& v, const GradPlan& g, int64_t real) {
     if (v.trans) {
         const int64_t n = up(real, 64);
-        return product(n, v.H, v.T, matrix(v.T, n), 1, matrix(v.T, v.H), 0, matrix(n, v.H));
+        return product(n, v.H, v.M, matrix(v.M, n), 1, matrix(v.M, v.H), 0, matrix(n, v.H));
     }
-    return product(v.H, real, v.T, matrix(v.T, v.H), 1, g.all ? strips_of(v) : matrix(v.T, real), 0, g.all ? v.W : matrix(v.H, real));
+    return product(v.H, real, v.M, matrix(v.M, v.H), 1, g.all ? strips_of(v, v.M) : matrix(v.M, real), 0, g.all ? v.W : matrix(v.H, real));
 }
 
 ccl_status make_grad_plan(const Vocabulary& v, GradPlan* g) {
     if (v.trans) {
-        const int64_t most = std::max<int64_t>(256, kPieceBytes / (2 * v.T) / 256 * 256);
+        const int64_t most = std::max<int64_t>(256, kPieceBytes / (2 * v.M) / 256 * 256);
         g->pieces = (v.V + most - 1) / most;
         g->width = g->pieces == 1 ? v.V : up((v.V + g->pieces - 1) / g->pieces, 256);
         g->pieces = (v.V + g->width - 1) / g->width;
@@ -222,13 +239,15 @@ ccl_status make_grad_plan(const Vocabulary& v, GradPlan* g) {
         g->sums = g->pieces;
         g->sum_width = g->width;
     } else {
-        g->all = v.strips == 1 || 2 * v.T * v.V <= kPieceBytes;
+        g->all = v.strips == 1 || 2 * v.M * v.V <= kPieceBytes;
         g->pieces = g->all ? 1 : v.strips;
         g->width = g->all ? v.V : v.strip;
-        // (strips along the K of dX's product have to be whole blocks of it; others are added up one by one)
-        g->sums = g->all && (v.strips == 1 || v.strip % BK == 0) ? 1 : v.strips;
+        // (strips along the K of dX's product have to be whole blocks of it; others are added up one by one, and so are all where dX comes from
+        // fp32 sums anyway)
+        g->sums = g->all && (v.strips == 1 || (v.strip % BK == 0 && v.M == v.T)) ? 1 : v.strips;
         g->sum_width = g->sums == 1 ? v.V : v.strip;
     }
+    g->direct = g->sums == 1 && v.M == v.T;
     g->parts = 0;
     g->gemm_bytes = 0;
     ccl_status s;
@@ -239,7 +258,7 @@ ccl_status make_grad_plan(const Vocabulary& v, GradPlan* g) {
         if ((s = ccl_gemm_workspace(&d, &n))) return s;
         g->gemm_bytes = std::max(g->gemm_bytes, n);
         d = dx_product(v, *g, std::min(real, g->sum_width));
-        if (g->sums == 1) {
+        if (g->direct) {
             if ((s = ccl_gemm_workspace(&d, &n))) return s;
             g->gemm_bytes = std::max(g->gemm_bytes, n);
         } else {
@@ -248,9 +267,10 @@ ccl_status make_grad_plan(const Vocabulary& v, GradPlan* g) {
             g->parts = std::max(g->parts, (int)plan.p.splits);
         }
     }
-    const size_t dz = up256((size_t)v.T * (size_t)(v.trans ? up(g->width, 64) : g->width) * 2);
+    const size_t dz = up256((size_t)v.M * (size_t)(v.trans ? up(g->width, 64) : g->width) * 2);
     g->acc_at = dz;
-    g->gemm_at = up256(dz + (size_t)g->parts * (size_t)v.T * (size_t)v.H * 4);
+    g->x2_at = up256(dz + (size_t)g->parts * (size_t)v.M * (size_t)v.H * 4);
+    g->gemm_at = up256(g->x2_at + (v.M == v.T ? 0 : (size_t)v.M * (size_t)v.H * 2));
     g->scale_at = up256(g->gemm_at + g->gemm_bytes);
     g->bytes = g->scale_at + 4;
     return CCL_OK;
@@ -326,7 +346,7 @@ extern "C" ccl_status ccl_linear_xent_workspace(const ccl_xent_desc* d, size_t* 
     ccl_status s = check_vocabulary("ccl_linear_xent_workspace", d, &v);
     if (s) return s;
     if (!bytes) return fail(CCL_ERR_INVALID_ARG, "ccl_linear_xent_workspace: NULL output");
-    const ccl_gemm_desc g = logits(v, v.V, true);
+    const ccl_gemm_desc g = logits(v, v.T, v.V, true);
     GemmPlan plan;
     if ((s = shape_plan(&g, 3, &plan))) return s;
     *bytes = forward_bytes(plan, v.T);
@@ -341,7 +361,7 @@ extern "C" ccl_status ccl_linear_xent(const ccl_xent_desc* d, const void* X_dev,
     if (s) return s;
     if (!loss_dev && !lse_dev) return fail(CCL_ERR_INVALID_ARG, "%s: no output is wanted", who);
     if ((reinterpret_cast<uintptr_t>(loss_dev) | reinterpret_cast<uintptr_t>(lse_dev)) & 3) return fail(CCL_ERR_ALIGN, "%s: loss / lse is not 4-byte aligned", who);
-    const ccl_gemm_desc g = logits(v, v.V, true);
+    const ccl_gemm_desc g = logits(v, v.T, v.V, true);
     GemmPlan plan;
     if ((s = shape_plan(&g, 3, &plan))) return s;
     if ((s = check_workspace(who, forward_bytes(plan, v.T), ws_dev, ws_bytes))) return s;
@@ -400,39 +420,45 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
     char* ws = static_cast<char*>(ws_dev);
     void *dz = ws, *gemm_ws = g.gemm_bytes ? ws + g.gemm_at : nullptr;
     float *acc = reinterpret_cast<float*>(ws + g.acc_at), *scale = reinterpret_cast<float*>(ws + g.scale_at);
-    if ((s = launch_early(xent_scale_kernel, dim3(1), 1024, 0, st, dloss_dev, targets_dev, (int)v.T, d->ignore_index, (int32_t)v.V, scale))) return s;
     int sms, pairs;
     device_units(&sms, &pairs);
+    const bool twofold = v.M != v.T;
+    const int64_t x8 = twofold ? v.T * v.H / 8 : 0;
+    uint4* x2 = reinterpret_cast<uint4*>(ws + g.x2_at);
+    if ((s = launch_early(xent_scale_kernel, dim3((unsigned)(1 + std::min<int64_t>((x8 + 1023) / 1024, sms))), 1024, 0, st, dloss_dev, targets_dev, (int)v.T, d->ignore_index,
+                          (int32_t)v.V, scale, static_cast<const uint4*>(X_dev), x2, x8))) return s;
+    const void* X = twofold ? static_cast<const void*>(x2) : X_dev;
     int have = 0;                                            // sums of dX that earlier pieces have begun
     for (int64_t i = 0; i < g.pieces; ++i) {
         const int64_t real = piece_real(v, g, i), rows = v.trans ? real : 0;
         const int64_t at = v.trans ? i * g.width * v.H : i * v.stride;
         const uint16_t* W = static_cast<const uint16_t*>(W_dev) + at;
         GemmPlan plan;
-        ccl_gemm_desc p = logits(v, real, g.all);
+        ccl_gemm_desc p = logits(v, v.M, real, g.all);
         if ((s = shape_plan(&p, 4, &plan))) return s;
         EpiMaps<4> em = {};
         LogitArgs& la = em.logits;
         la.targets = targets_dev; la.ignore = d->ignore_index; la.v0 = (int32_t)(i * g.width); la.classes = (int32_t)real; la.all = (int32_t)v.V;
         la.lse = lse_dev; la.dloss = dloss_dev; la.scale = scale;
-        if ((s = run_logits<4>(plan, em, rows, X_dev, W, dz, st))) return s;
+        la.half = twofold ? (int32_t)v.T : INT32_MAX;
+        if ((s = run_logits<4>(plan, em, rows, X, W, dz, st))) return s;
         if (dX_dev) {
             p = dx_product(v, g, std::min(real, g.sum_width));
-            if (g.sums == 1) {
+            if (g.direct) {
                 if ((s = gemm_cut(&p, 0, rows, scale, dz, W, dX_dev, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
             } else {
                 // (the piece's dz and W; or one of their strips after the other)
                 for (int64_t k = 0; k < (g.all ? g.sums : 1); ++k) {
                     if ((s = shape_plan(&p, 5, &plan))) return s;
                     EpiMaps<5> sums = {acc, have};
-                    if ((s = run_logits<5>(plan, sums, rows, static_cast<uint16_t*>(dz) + k * v.T * v.strip, W + k * v.stride, nullptr, st))) return s;
+                    if ((s = run_logits<5>(plan, sums, rows, static_cast<uint16_t*>(dz) + k * v.M * v.strip, W + k * v.stride, nullptr, st))) return s;
                     have = std::max(have, (int)plan.p.splits);
                 }
             }
         }
         if (dW_dev) {
             p = dw_product(v, g, real);
-            const void *A = v.trans ? dz : X_dev, *B = v.trans ? X_dev : dz;
+            const void *A = v.trans ? dz : X, *B = v.trans ? X : dz;
             uint16_t* C = static_cast<uint16_t*>(dW_dev) + at;
             // Enough tiles for every SM: 256 columns, drained behind the next tile's product (131072 x 512 x 1024: 105 us, by ccl_gemm with
             // alpha 114; 32768 x 4096 x 1024: 196 and 215).  Few tiles and a long K are split along K.
@@ -443,7 +469,8 @@ extern "C" ccl_status ccl_linear_xent_grad(const ccl_xent_desc* d, const void* X
             } else if ((s = gemm_cut(&p, rows, 0, scale, A, B, C, gemm_ws, g.gemm_bytes, cuda_stream))) return s;
         }
     }
-    if (!dX_dev || g.sums == 1) return CCL_OK;
+    if (!dX_dev || g.direct) return CCL_OK;
+    if (twofold) have *= 2;                                  // (a sum's second half of rows is a sum more)
     const int64_t n = v.T * v.H;
     return launch_early(xent_dx_kernel, dim3((unsigned)std::min<int64_t>((n / 8 + 255) / 256, sms * 8)), 256, 0, st, (const float*)acc, have, n, (const float*)scale, static_cast<uint16_t*>(dX_dev));
 }

@@ -67,3 +67,25 @@ def test_wanted_outputs_only_and_the_same_bits():
     p = Problem(6, 900, 64, seed=2, ignored=1.0)
     dX, dW = p.grad()
     assert (dX[:-64] == 0).all() and (dW[:-64] == 0).all()
+
+
+def test_replayed_with_other_inputs_beside_a_call():
+    T, V, H = 11, 2003, 136
+    a, b = Problem(T, V, H, seed=3), Problem(T, V, H, seed=4)
+    want = [t.clone() for t in b.grad()]
+    x, w, tg, lse, dl = a.x.clone(), a.w.clone(), a.tg.clone(), a.lse.float(), a.dloss.clone()
+    dX, dW = torch.empty_like(x), torch.empty_like(w)
+    ws = torch.empty(ccl.ccl_linear_xent_grad_workspace(a.d), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ccl.ccl_linear_xent_grad(a.d, x, w, tg, lse, dl, dX, dW, ws)
+    for t, s in ((x, b.x), (w, b.w), (tg, b.tg), (lse, b.lse.float()), (dl, b.dloss)):
+        t.copy_(s)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        graph.replay()
+    again = b.grad()                                            # (on the current stream, a workspace of its own)
+    torch.cuda.synchronize()
+    assert torch.equal(dX.view(-1), want[0][:T * H]) and torch.equal(dW.view(-1), want[1][:V * H])
+    assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
